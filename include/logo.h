@@ -17,6 +17,9 @@
  *                                logo_select, and its backward
  *   logo_branch_transform / _bwd Eq. 5 LP / SO transforms U^L -> U^G (Q on the
  *                                selected rows only)
+ *   logo_decode_prefix_attn, logo_cache_evict, logo_verify_draft
+ *                                serving: drafted tokens of a batch over a shared
+ *                                prefix and bounded caches
  *
  * Conventions shared by every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller.  The
@@ -195,6 +198,101 @@ LOGO_API int logo_decode_local_attn(const logo_bf16* q, const logo_bf16* k_ring,
 LOGO_API int logo_decode_global_sparse_attn(const logo_bf16* q, const logo_bf16* k_cache, const logo_bf16* v_cache,
                 const int32_t* seq_len, const int32_t* cu_q, const int32_t* n_sel_total, logo_bf16* o_c,
                 logo_dims dims, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* logo_decode_prefix_attn -- one serving step of the global branch (Eq. 8) for a
+ *   batch whose sequences start with the same long text: the keys and values
+ *   of that prefix are held, and read, once for all sequences.  Each sequence
+ *   brings n_new >= 1 new tokens (one in plain decoding; the last accepted
+ *   token and the drafts after it when drafts are to be verified).
+ *   The new tokens' queries are q [B, n_new, Hq, D].  Packed row r of the
+ *   selection (logo_select on dims (B, T = n_new)) is token pos[r] of its
+ *   sequence b.  It attends
+ *     - all prefix_len rows of k_prefix, v_prefix [prefix_len, Hkv, D] (both
+ *       may be NULL when prefix_len is 0), and
+ *     - the rows s < min(len, max(0, len - n_new + pos[r] + 1)) of its own
+ *       caches k_cache, v_cache [B, L, Hkv, D], L = dims.T, where len =
+ *       seq_len[b] clamped to [0, L] counts the tokens after the prefix, the
+ *       n_new new ones included and last: the drafts are causal among
+ *       themselves.  Rows s >= len may hold anything.  The order of the other
+ *       rows does not matter (logo_cache_evict changes it).
+ *   A row that sees no key gets o = 0 and lse = -infinity.
+ * Out: o_c [B*n_new, Hq, D] bf16 packed and lse_c [Hq, B*n_new] float32 packed
+ *      (may be NULL): rows >= n_sel_total are left untouched.
+ *      mass_out [B, Hkv, L] float32 (NULL: not wanted; then mass_in is not
+ *      read): the attention weight every own cache row has received,
+ *        mass_out[b,h,s] = m + sum over the selected rows r of b and the query
+ *                          heads g of KV head h of exp(scale q_rg.k_s - lse_rg)
+ *      for s < len, m = mass_in[b,h,s] for s < len - n_new and 0 for the new
+ *      tokens; entries s >= len are left untouched.  mass_out may be mass_in.
+ *      Sequences without a selected row keep m.
+ *   dims: B, T = L, Hq, Hkv, D in {64, 128}; scale as elsewhere.
+ *   Products in bf16 with fp32 accumulation, softmax and weights in fp32.
+ *   Results do not depend on the order in which the GPU runs the blocks.
+ *   Workspace: logo_decode_prefix_workspace_size(...) bytes, one per call in
+ *   flight (with_mass: whether mass_out will be given).
+ *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer or a size out of range;
+ *   LOGO_ERR_UNSUPPORTED for D, Hq % Hkv, 16-byte alignment of a bf16 pointer,
+ *   or B * n_new > 2^24; LOGO_ERR_WORKSPACE. */
+LOGO_API size_t logo_decode_prefix_workspace_size(logo_dims dims, int n_new, int prefix_len, int with_mass);
+LOGO_API int logo_decode_prefix_attn(const logo_bf16* q, const logo_bf16* k_prefix, const logo_bf16* v_prefix,
+                const logo_bf16* k_cache, const logo_bf16* v_cache, const int32_t* seq_len, const int32_t* pos,
+                const int32_t* cu_q, const int32_t* n_sel_total, logo_bf16* o_c, float* lse_c, const float* mass_in,
+                float* mass_out, logo_dims dims, int n_new, int prefix_len, float scale, void* workspace,
+                size_t workspace_bytes, void* stream);
+
+/* logo_cache_evict -- cuts every sequence's cache back to `budget` rows per KV
+ *   head, keeping the rows that have received the most attention
+ *   (logo_decode_prefix_attn's mass) and the most recent ones.
+ *   slot_pos [B, Hkv, L] int32 holds the token position of every cache row.
+ *   For each (b, h), with len = seq_len[b] clamped to [0, L] and end =
+ *   min(len, budget): the rows with slot_pos >= n_seen[b] - recent come first,
+ *   the others by falling mass; equal rows go to the lower row (-0.0 equals
+ *   +0.0, a NaN mass comes last of all).  The first `end` rows of that order
+ *   stay.  Rows that stay and lie below `end` are not touched; the i-th row at
+ *   or above `end` that stays moves into the i-th row below `end` that does
+ *   not.  So the order of the rows is not kept: attention over a cache does
+ *   not depend on it, and slot_pos goes along.
+ *   k_cache, v_cache [B, L, Hkv, D] bf16: changed in place, rows >= end left as
+ *   they are.  mass, slot_pos are read; mass_out, slot_pos_out [B, Hkv, L]
+ *   receive entries < end (the others untouched) and may be mass / slot_pos.
+ *   new_len [B] int32 = end (not seq_len itself: it is read throughout the
+ *   call).  budget in [1, L], recent in [0, budget].
+ *   dims: B, T = L, Hkv, D in {64, 128} (Hq is not read).
+ *   Results are exact and deterministic.  Workspace:
+ *   logo_cache_evict_workspace_size(dims) bytes.
+ *   Errors: LOGO_ERR_INVALID_ARG, LOGO_ERR_UNSUPPORTED (D, B * T > 2^30,
+ *   B * Hkv > 2^24, 16-byte alignment of a cache or the workspace),
+ *   LOGO_ERR_WORKSPACE. */
+LOGO_API size_t logo_cache_evict_workspace_size(logo_dims dims);
+LOGO_API int logo_cache_evict(logo_bf16* k_cache, logo_bf16* v_cache, const float* mass, const int32_t* slot_pos,
+                const int32_t* seq_len, const int32_t* n_seen, float* mass_out, int32_t* slot_pos_out,
+                int32_t* new_len, logo_dims dims, int budget, int recent, void* workspace, size_t workspace_bytes,
+                void* stream);
+
+/* logo_verify_draft -- accepts or rejects the drafted tokens of each sequence
+ *   and samples the token after the last accepted one, so that the tokens are
+ *   distributed as if drawn from the target alone.
+ *   draft [B, m] int32; q_draft [B, m, V] and p_target [B, m+1, V] float32:
+ *   the probabilities that drafts were drawn from and the target's;
+ *   u [B, m] float32 uniform on [0, 1); noise [B, V] float32, exponentially
+ *   distributed with mean 1; draft_len [B] int32: drafts of each sequence,
+ *   clamped to [0, m] (NULL: m for all).
+ *   Draft i is accepted while p = p_target[b,i,draft[b,i]] > 0 and
+ *   u[b,i] * q_draft[b,i,draft[b,i]] <= p (one fp32 product); a token outside
+ *   [0, V) is rejected.  a = number accepted before the first rejection.
+ *   r_v = max(p_target[b,a,v] - q_draft[b,a,v], 0) if a draft was rejected, or
+ *   p_target[b,a,v] if none was, or if no such r_v is positive.  The sampled
+ *   token is the v with the largest r_v / noise[b,v] among r_v > 0 (fp32
+ *   difference and quotient, ties to the lowest v; 0 if there is none): the
+ *   race of exponential clocks draws v with probability r_v / sum r.
+ * Out: tokens [B, m+1] int32: the a accepted drafts, the sampled token, then
+ *      -1; n_accept [B] int32 = a.
+ *   B * (m + 1) <= 2^24, V >= 1.  Results are exact and deterministic.
+ *   Workspace: logo_verify_draft_workspace_size(B, m, V) bytes. */
+LOGO_API size_t logo_verify_draft_workspace_size(int B, int m, int V);
+LOGO_API int logo_verify_draft(const int32_t* draft, const float* q_draft, const float* p_target, const float* u,
+                const float* noise, const int32_t* draft_len, int32_t* tokens, int32_t* n_accept, int B, int m, int V,
+                void* workspace, size_t workspace_bytes, void* stream);
 
 /* logo_select_noalloc -- logo_select for callers that cannot allocate.
  *   No counterpart in the paper: this is a deployment variant of logo_select.

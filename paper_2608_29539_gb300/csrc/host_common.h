@@ -43,5 +43,6 @@ int decode_tu_status(int clear);
 int transform_tu_status(int clear);
 int gate_tu_status(int clear);
 int selftest_tu_status(int clear);
+int prefix_attn_tu_status(int clear);
 
 }  // namespace logo

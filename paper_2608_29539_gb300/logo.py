@@ -74,6 +74,15 @@ _SIGS = {
     "logo_decode_local_attn": (_c_int, [_vp, _vp, _vp, _vp, _vp, Dims, _c_int, _c_float, _vp, _c_size, _vp]),
     "logo_decode_global_sparse_attn": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, Dims, _c_float, _vp, _c_size,
                                                 _vp]),
+    "logo_decode_prefix_workspace_size": (_c_size, [Dims, _c_int, _c_int, _c_int]),
+    "logo_decode_prefix_attn": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, Dims, _c_int,
+                                         _c_int, _c_float, _vp, _c_size, _vp]),
+    "logo_cache_evict_workspace_size": (_c_size, [Dims]),
+    "logo_cache_evict": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, Dims, _c_int, _c_int, _vp, _c_size,
+                                  _vp]),
+    "logo_verify_draft_workspace_size": (_c_size, [_c_int, _c_int, _c_int]),
+    "logo_verify_draft": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _vp, _c_size,
+                                   _vp]),
     "logo_local_attn_fwd": (_c_int, [_vp, _vp, _vp, _vp, _vp, Dims, _c_int, _c_float, _vp]),
     "logo_local_attn_bwd_workspace_size": (_c_size, [Dims]),
     "logo_local_attn_bwd": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, Dims, _c_int, _c_float, _vp,
@@ -363,6 +372,157 @@ def logo_decode_global_sparse_attn(q, k_cache, v_cache, seq_len, cu_q, n_sel_tot
     _call("logo_decode_global_sparse_attn", _p(q), _p(k_cache), _p(v_cache), _p(seq_len), _p(cu_q),
           _p(n_sel_total), _p(o_c), dims, float(scale), _p(ws), nbytes, _stream())
     return o_c
+
+
+def logo_decode_prefix_workspace(q, k_prefix, k_cache, with_mass: bool = False):
+    """A workspace for logo_decode_prefix_attn calls of these shapes (one per
+    call in flight)."""
+    B, n_new, Hq, D = q.shape
+    dims = Dims(B, k_cache.shape[1], Hq, k_cache.shape[2], D)
+    P = 0 if k_prefix is None else k_prefix.shape[0]
+    return _workspace(int(lib().logo_decode_prefix_workspace_size(dims, n_new, P, int(bool(with_mass)))), q.device)
+
+
+def logo_decode_prefix_attn(q, k_prefix, v_prefix, k_cache, v_cache, seq_len, pos, cu_q, n_sel_total,
+                            scale: float = 0.0, mass_in=None, mass_out=None, o_c=None, lse_c=None, workspace=None):
+    """One serving step of the global branch (Eq. 8) over a prefix that all
+    sequences share and each sequence's own cache.
+
+    q [B, n_new, Hq, D]; k_prefix / v_prefix [P, Hkv, D] (None: no prefix);
+    k_cache / v_cache [B, L, Hkv, D]; seq_len [B] int32 (own tokens, the n_new
+    new ones included and last); pos, cu_q, n_sel_total from logo_select on
+    (B, n_new) gates.  With mass_in [B, Hkv, L] float32 the attention weight
+    each own cache row receives is added into mass_out (None: mass_in itself).
+    Returns (o_c [B*n_new, Hq, D], lse_c [Hq, B*n_new], mass_out or None);
+    packed rows >= n_sel_total are untouched."""
+    _need(q, torch.bfloat16, "q")
+    if q.dim() != 4:
+        raise ValueError("q must be [B, n_new, Hq, D]")
+    B, n_new, Hq, D = q.shape
+    _need(k_cache, torch.bfloat16, "k_cache")
+    if k_cache.dim() != 4 or k_cache.shape[0] != B or k_cache.shape[3] != D:
+        raise ValueError(f"k_cache has shape {tuple(k_cache.shape)}, expected ({B}, L, Hkv, {D})")
+    _, Lc, Hkv, _ = k_cache.shape
+    _need(v_cache, torch.bfloat16, "v_cache", k_cache.shape)
+    if (k_prefix is None) != (v_prefix is None):
+        raise ValueError("k_prefix and v_prefix come together")
+    P = 0
+    if k_prefix is not None:
+        P = k_prefix.shape[0]
+        _need(k_prefix, torch.bfloat16, "k_prefix", (P, Hkv, D))
+        _need(v_prefix, torch.bfloat16, "v_prefix", (P, Hkv, D))
+    cap = B * n_new
+    _need(seq_len, torch.int32, "seq_len", (B,))
+    _need(pos, torch.int32, "pos", (cap,))
+    _need(cu_q, torch.int32, "cu_q", (B + 1,))
+    _need(n_sel_total, torch.int32, "n_sel_total", (1,))
+    if mass_in is None:
+        if mass_out is not None:
+            raise ValueError("mass_out needs mass_in")
+    else:
+        _need(mass_in, torch.float32, "mass_in", (B, Hkv, Lc))
+        if mass_out is None:
+            mass_out = mass_in
+        else:
+            _need(mass_out, torch.float32, "mass_out", (B, Hkv, Lc))
+    if o_c is None:
+        o_c = torch.empty((cap, Hq, D), dtype=torch.bfloat16, device=q.device)
+    else:
+        _need(o_c, torch.bfloat16, "o_c", (cap, Hq, D))
+    if lse_c is None:
+        lse_c = torch.empty((Hq, cap), dtype=torch.float32, device=q.device)
+    else:
+        _need(lse_c, torch.float32, "lse_c", (Hq, cap))
+    dims = Dims(B, Lc, Hq, Hkv, D)
+    if workspace is None:
+        workspace = logo_decode_prefix_workspace(q, k_prefix, k_cache, mass_in is not None)
+    _call("logo_decode_prefix_attn", q.data_ptr(), k_prefix.data_ptr() if P else None,
+          v_prefix.data_ptr() if P else None, k_cache.data_ptr(), v_cache.data_ptr(), seq_len.data_ptr(),
+          pos.data_ptr(), cu_q.data_ptr(), n_sel_total.data_ptr(), o_c.data_ptr(), lse_c.data_ptr(),
+          None if mass_in is None else mass_in.data_ptr(), None if mass_out is None else mass_out.data_ptr(), dims,
+          n_new, P, float(scale), workspace.data_ptr(), workspace.nbytes, _stream())
+    return o_c, lse_c, mass_out
+
+
+def logo_cache_evict_workspace(k_cache):
+    """A workspace for logo_cache_evict calls on caches of this shape."""
+    B, Lc, Hkv, D = k_cache.shape
+    return _workspace(int(lib().logo_cache_evict_workspace_size(Dims(B, Lc, Hkv, Hkv, D))), k_cache.device)
+
+
+def logo_cache_evict(k_cache, v_cache, mass, slot_pos, seq_len, n_seen, budget: int, recent: int, mass_out=None,
+                     slot_pos_out=None, new_len=None, workspace=None):
+    """Cut every (sequence, KV head) back to `budget` cache rows: those whose
+    slot_pos >= n_seen - recent, then the largest mass, ties to the lower row.
+
+    k_cache / v_cache [B, L, Hkv, D] bf16 change in place (rows that stay move
+    into the places of rows that go; the order is not kept); mass [B, Hkv, L]
+    float32 and slot_pos [B, Hkv, L] int32 (token position of each row) go
+    along, into mass_out / slot_pos_out (None: in place); seq_len, n_seen [B]
+    int32.  Returns (mass_out, slot_pos_out, new_len [B] int32)."""
+    _need(k_cache, torch.bfloat16, "k_cache")
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must be [B, L, Hkv, D]")
+    B, Lc, Hkv, D = k_cache.shape
+    _need(v_cache, torch.bfloat16, "v_cache", k_cache.shape)
+    _need(mass, torch.float32, "mass", (B, Hkv, Lc))
+    _need(slot_pos, torch.int32, "slot_pos", (B, Hkv, Lc))
+    _need(seq_len, torch.int32, "seq_len", (B,))
+    _need(n_seen, torch.int32, "n_seen", (B,))
+    mass_out = mass if mass_out is None else _need(mass_out, torch.float32, "mass_out", (B, Hkv, Lc))
+    slot_pos_out = (slot_pos if slot_pos_out is None
+                    else _need(slot_pos_out, torch.int32, "slot_pos_out", (B, Hkv, Lc)))
+    if new_len is None:
+        new_len = torch.empty((B,), dtype=torch.int32, device=k_cache.device)
+    else:
+        _need(new_len, torch.int32, "new_len", (B,))
+    if workspace is None:
+        workspace = logo_cache_evict_workspace(k_cache)
+    _call("logo_cache_evict", k_cache.data_ptr(), v_cache.data_ptr(), mass.data_ptr(), slot_pos.data_ptr(),
+          seq_len.data_ptr(), n_seen.data_ptr(), mass_out.data_ptr(), slot_pos_out.data_ptr(), new_len.data_ptr(),
+          Dims(B, Lc, Hkv, Hkv, D), int(budget), int(recent), workspace.data_ptr(), workspace.nbytes, _stream())
+    return mass_out, slot_pos_out, new_len
+
+
+def logo_verify_draft_workspace(p_target):
+    """A workspace for logo_verify_draft calls on probabilities of this shape."""
+    B, m1, V = p_target.shape
+    return _workspace(int(lib().logo_verify_draft_workspace_size(B, m1 - 1, V)), p_target.device)
+
+
+def logo_verify_draft(draft, q_draft, p_target, u, noise, draft_len=None, tokens=None, n_accept=None, workspace=None):
+    """Speculative sampling: accept the drafts draft [B, m] int32 (drawn from
+    q_draft [B, m, V] float32) against p_target [B, m+1, V] float32 with the
+    uniforms u [B, m], and draw the next token with the exponentials noise
+    [B, V].  draft_len [B] int32: drafts of each sequence (None: m).  Returns
+    (tokens [B, m+1] int32: accepted drafts, the drawn token, -1 ...;
+    n_accept [B] int32)."""
+    _need(p_target, torch.float32, "p_target")
+    if p_target.dim() != 3 or p_target.shape[1] < 1:
+        raise ValueError("p_target must be [B, m + 1, V]")
+    B, m1, V = p_target.shape
+    m = m1 - 1
+    _need(draft, torch.int32, "draft", (B, m))
+    _need(q_draft, torch.float32, "q_draft", (B, m, V))
+    _need(u, torch.float32, "u", (B, m))
+    _need(noise, torch.float32, "noise", (B, V))
+    if draft_len is not None:
+        _need(draft_len, torch.int32, "draft_len", (B,))
+    if tokens is None:
+        tokens = torch.empty((B, m1), dtype=torch.int32, device=p_target.device)
+    else:
+        _need(tokens, torch.int32, "tokens", (B, m1))
+    if n_accept is None:
+        n_accept = torch.empty((B,), dtype=torch.int32, device=p_target.device)
+    else:
+        _need(n_accept, torch.int32, "n_accept", (B,))
+    if workspace is None:
+        workspace = logo_verify_draft_workspace(p_target)
+    _call("logo_verify_draft", draft.data_ptr() if m else None, q_draft.data_ptr() if m else None,
+          p_target.data_ptr(), u.data_ptr() if m else None, noise.data_ptr(),
+          None if draft_len is None else draft_len.data_ptr(), tokens.data_ptr(), n_accept.data_ptr(), B, m, V,
+          workspace.data_ptr(), workspace.nbytes, _stream())
+    return tokens, n_accept
 
 
 def logo_select_noalloc(gate_p, mode: int, b_th: float = 0.5, ratio: float = 0.0, z=None, pos=None, cu_q=None,
