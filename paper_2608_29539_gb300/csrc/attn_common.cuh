@@ -3,6 +3,7 @@
 // query-sparse global (Eq. 8) branches, and the row/key visibility rule.
 #pragma once
 #include <cuda.h>
+#include <cuda_runtime.h>
 
 #include <cstdint>
 
@@ -34,6 +35,25 @@ struct GlobalTile {
     int cost;     // KV blocks visited (the ordering key)
     int pad0, pad1, pad2;
 };
+
+// The global forward kernel on rows and tiles that its caller laid out: q
+// [1, q_rows, Hkv, D] against k, v [1, T, Hkv, D], one query row per (packed
+// row, KV head); every tile's entry has a slot (its result is a share: O
+// transposed [slot * Hkv + h][D][128], row maxima in log2 units and row sums
+// [slot * Hkv + h][128]).  tiles, n_tiles and next_item (zero) are written by
+// an earlier launch; n_items bounds n_tiles * Hkv.
+struct TileShares {
+    const logo_bf16 *q, *k, *v;
+    const int32_t* pos;  // position of each row: it sees the keys 0 .. pos
+    const GlobalTile* tiles;
+    const int32_t* n_tiles;
+    int32_t* next_item;
+    float *o_part, *m_part, *l_part;
+    int64_t q_rows;
+    int T, Hkv, n_items;
+    float scale_log2;
+};
+int launch_tile_shares(const TileShares& t, int D, cudaStream_t st);
 
 // A tile whose KV range is split: the merge kernel combines slots
 // slot0 .. slot0 + nsplit - 1 into its output rows.

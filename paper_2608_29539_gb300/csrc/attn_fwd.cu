@@ -972,6 +972,29 @@ int check_attn_ptrs(const void* q, const void* k, const void* v)
 
 }  // namespace
 
+int launch_tile_shares(const TileShares& t, int D, cudaStream_t st)
+{
+    FwdParams prm{};
+    if (!encode_bf16_4d(&prm.tm_q, t.q, D, t.Hkv, t.q_rows, 1, 64, kBM) ||
+        !encode_bf16_4d(&prm.tm_k, t.k, D, t.Hkv, t.T, 1, 64, kBN) ||
+        !encode_bf16_4d(&prm.tm_v, t.v, D, t.Hkv, t.T, 1, 64, kBN))
+        return LOGO_ERR_CUDA;
+    prm.pos = t.pos;
+    prm.tiles = t.tiles;
+    prm.n_tiles = t.n_tiles;
+    prm.next_item = t.next_item;
+    prm.o_part = t.o_part;
+    prm.m_part = t.m_part;
+    prm.l_part = t.l_part;
+    prm.B = 1;
+    prm.T = t.T;
+    prm.Hq = t.Hkv;
+    prm.Hkv = t.Hkv;
+    prm.window = kNoWindow;
+    prm.scale_log2 = t.scale_log2;
+    return D == 128 ? launch_fwd<128, true>(prm, t.n_items, st) : launch_fwd<64, true>(prm, t.n_items, st);
+}
+
 int attn_fwd_tu_status(int clear) { return read_tu_status(clear); }
 
 }  // namespace logo

@@ -2,9 +2,10 @@
 sequence's length hold NaN; output rows past the selected count hold
 sentinels.
 
-Error bounds, from the formats alone (A = sum w |v|; E = 2^-24 D max scale
-sum |q k|, the fp32 accumulation error of a logit):
-  o    2^-9 |o| (its rounding to bf16) + 2^-9 A (weights rounded to bf16)
+Error bounds, from the formats alone (bf16 has 8 significant bits: rounding x
+moves it by at most 2^-8 |x|; A = sum w |v|; E = 2^-24 D max scale sum |q k|,
+the fp32 accumulation error of a logit):
+  o    2^-8 |o| (its rounding to bf16) + 2^-8 A (weights rounded to bf16)
        + (2 E + 2^-16) A (logits, fp32 sums)
   lse  E + 2^-20 + 2^-22 |lse|
   mass (2 E + 2^-18) of what was added + 2^-22 of the whole
@@ -41,7 +42,7 @@ def _check(got_o, got_lse, got_mass, ref, rows, D, lens):
     N = len(rows)
     E = 2.0 ** -24 * D * ref["big"]
     o = got_o[:N].float().cpu().numpy().astype(np.float64)
-    bound = 2.0 ** -9 * (np.abs(ref["o"]) + ref["absv"]) + (2 * E + 2.0 ** -16) * ref["absv"]
+    bound = 2.0 ** -8 * (np.abs(ref["o"]) + ref["absv"]) + (2 * E + 2.0 ** -16) * ref["absv"]
     assert np.isfinite(o).all()
     assert (np.abs(o - ref["o"]) <= bound).all(), float((np.abs(o - ref["o"]) - bound).max())
     lse = got_lse[:, :N].cpu().numpy().astype(np.float64)
@@ -176,6 +177,7 @@ def test_matches_the_decode_call_when_there_is_no_prefix():
     a = Lg.logo_decode_global_sparse_attn(q.view(B, Hq, D), kc, vc, lens, cu, ns)
     b, lse, mass = Lg.logo_decode_prefix_attn(q, None, None, kc, vc, lens, pos, cu, ns)
     torch.cuda.synchronize()
+    assert Lg.logo_get_device_status() == 0
     assert mass is None
     n = int(ns)
     assert n == 3
@@ -213,7 +215,7 @@ def test_cache_offsets_beyond_32_bits():
     ref = w @ tail_v.double()
     absv = w @ tail_v.double().abs()
     got = o[1, 63].double().cpu()
-    assert ((got - ref).abs() <= 2.0 ** -9 * (ref.abs() + absv) + (2 * E + 2.0 ** -16) * absv).all()
+    assert ((got - ref).abs() <= 2.0 ** -8 * (ref.abs() + absv) + (2 * E + 2.0 ** -16) * absv).all()
     assert ((m[1, 63, L - 300:].double().cpu() - w).abs() <= (2 * E + 2.0 ** -18) * w).all()
     assert bool((o[0] == 0).all()) and float((m[0, :, :5] - 0.2).abs().max()) <= 2.0 ** -18
 

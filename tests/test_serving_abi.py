@@ -26,8 +26,8 @@ def logo():
 def test_prefix_attn_host_checks(logo):
     L = logo.lib()
     d = logo.Dims(4, 256, 8, 2, 128)
-    ws = L.logo_decode_prefix_workspace_size(d, 2, 100, 1)
-    assert ws > 0
+    ws = L.logo_decode_prefix_workspace_size(d, 2, 100, 0)
+    assert 0 < ws <= L.logo_decode_prefix_workspace_size(d, 2, 100, 1)
     for bad, n, P in ((logo.Dims(4, 256, 8, 2, 96), 1, 0), (logo.Dims(4, 256, 8, 3, 128), 1, 0),
                       (logo.Dims(0, 256, 8, 2, 128), 1, 0), (d, 0, 0), (d, 1, -1),
                       (logo.Dims(1 << 14, 4, 8, 2, 128), 1 << 11, 0)):
