@@ -39,7 +39,7 @@ struct GlobalTile {
 // The global forward kernel on rows and tiles that its caller laid out: q
 // [1, q_rows, Hkv, D] against k, v [1, T, Hkv, D], one query row per (packed
 // row, KV head); every tile's entry has a slot (its result is a share: O
-// transposed [slot * Hkv + h][D][128], row maxima in log2 units and row sums
+// [slot * Hkv + h][128][D], row maxima in log2 units and row sums
 // [slot * Hkv + h][128]).  tiles, n_tiles and next_item (zero) are written by
 // an earlier launch; n_items bounds n_tiles * Hkv.
 struct TileShares {

@@ -87,6 +87,7 @@ struct FwdParams {
     float* o_part;                 // global split entries: unnormalised O [slot * Hq + h][D][128]
     float* m_part;                 // ... their running max (log2 units) [slot * Hq + h][128]
     float* l_part;                 // ... and their row sums
+    int part_rows;                 // o_part as [slot * Hq + h][128][D] instead
     int B, T, Hq, Hkv, window, cap;
     int q_tiles;                   // local: query tiles per sequence
     float scale_log2;              // softmax scale * log2(e)
@@ -628,6 +629,18 @@ __global__ void __launch_bounds__(384, 1) attn_fwd_kernel(const __grid_constant_
                 // one share of a split KV range: unnormalised O, stored transposed
                 // ([d][row]) so that the warp's 32 rows of a column are one line
                 const int64_t unit = static_cast<int64_t>(it.slot) * p.Hq + it.h;
+                if (p.part_rows) {  // the caller joins whole rows: a row as it lies here
+                    if (!row_valid) continue;
+                    float* prow = p.o_part + (unit * kBM + r) * D;
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            *reinterpret_cast<uint4*>(prow + c * 32 + i) =
+                                make_uint4(ov[c][i], ov[c][i + 1], ov[c][i + 2], ov[c][i + 3]);
+                    p.l_part[unit * kBM + r] = lv;
+                    continue;
+                }
                 float* pcol = p.o_part + unit * kBM * D + r;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c)
@@ -986,6 +999,7 @@ int launch_tile_shares(const TileShares& t, int D, cudaStream_t st)
     prm.o_part = t.o_part;
     prm.m_part = t.m_part;
     prm.l_part = t.l_part;
+    prm.part_rows = 1;
     prm.B = 1;
     prm.T = t.T;
     prm.Hq = t.Hkv;
