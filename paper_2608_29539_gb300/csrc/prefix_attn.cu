@@ -65,10 +65,7 @@ struct PaCfg {
     static constexpr int kQBytes = kPaRows * D * 2;
     static constexpr int kOffRing = 2 * kQBytes;  // after two Q tiles
     static constexpr int kOffMerge = kOffRing + kStages * kTileBytes;
-    // the warps' O, a block of columns at a time: rows x columns = 1024 floats a
-    // warp, rows 8 floats apart from a multiple of 32 so that a fragment's rows
-    // fall on different banks
-    static constexpr int kMergeBytes = kPaWarps * (1024 + 8 * kPaRows) * 4;
+    static constexpr int kMergeBytes = kPaWarps * 16 * (64 + 8) * 4;  // the warps' 16 rows of O, 64 columns at a time
     static constexpr int kSmemBytes = kOffMerge + kMergeBytes + 1024;
 };
 
@@ -118,13 +115,16 @@ struct PaParams {
     float *wo_part, *wm_part, *wl_part;
     float* logits;  // [B, Hkv, L, R] log2 units, R = n_new * G
     int B, L, Hq, Hkv, G, n_new, P, cap, R, rt_own_max, w_pre, w_own, nCta;
-    int wpr;  // join: warps per (row, head)
     int n_sm;
     float scale_log2;
 };
 
 // Own cache rows that token i of a sequence with len tokens sees.
 __device__ __forceinline__ int own_visible(int len, int n_new, int i) { return min(len, max(0, len - n_new + i + 1)); }
+
+// Token of packed row r among its sequence's new ones (no load on the way to
+// the keys when there is one only).
+__device__ __forceinline__ int token_of(const PaParams& p, int r) { return p.n_new == 1 ? 0 : __ldg(p.pos + r); }
 
 struct OwnSeq {
     int row0, n, len, tiles, rts;  // first packed row, rows, tokens, key tiles, row tiles
@@ -139,7 +139,7 @@ __device__ __forceinline__ OwnSeq own_seq(const PaParams& p, int b)
     o.len = max(0, min(__ldg(p.seq_len + b), p.L));
     o.tiles = o.rts = 0;
     if (o.n > 0) {
-        o.tiles = (own_visible(o.len, p.n_new, __ldg(p.pos + row1 - 1)) + kPaTile - 1) / kPaTile;
+        o.tiles = (own_visible(o.len, p.n_new, token_of(p, row1 - 1)) + kPaTile - 1) / kPaTile;
         o.rts = (o.n * p.G + kPaRows - 1) / kPaRows;
     }
     return o;
@@ -240,8 +240,8 @@ struct PaIter {
 struct PaWarp {
     uint32_t sQ, sRing, kv_full, kv_empty;  // kv_*: the first barrier, the others 8 bytes on
     volatile int* abort_flag;
-    float* merge;     // [warp][rows][columns + 8]
-    float2* sh_ml;    // [warp][kPaRows]
+    float* merge;     // [warp][16][64 + 8]
+    float2* sh_ml;    // [warp][16]
     const int* vis;   // [kPaRows] keys that each row of the piece sees
     int warp, lane, n;  // n: tiles consumed, K and V counted
 };
@@ -263,33 +263,35 @@ __device__ __forceinline__ bool products_sync_and(bool ok)
 
 __device__ __forceinline__ void products_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
 
-// One piece, by the eight warps: MT blocks of 16 rows against the warp's 16 keys
-// of every tile, then the warps' results joined in shared memory.  Returns
-// false, to all of them, if a wait of any gave up.
-template <int D, int MT>
+// One piece, by the eight warps.  Up to 16 rows: each warp takes 16 keys of
+// every tile (STEPS = 1).  Up to 32: four warps take rows 0 .. 15, four the
+// others, each on 32 keys (STEPS = 2).  Fragments are fetched a batch ahead of
+// the products that use them (two warps a scheduler hide little).  Then the
+// warps' results are joined in shared memory.  Returns false, to all warps, if
+// a wait of any gave up.
+template <int D, int STEPS>
 __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, PaWarp& w, bool ok)
 {
     using C = PaCfg<D>;
-    constexpr int NT = D / 8;
+    constexpr int NT = D / 8, KS = D / 16;
+    constexpr int kGroup = kPaWarps / STEPS;  // warps that share the rows' keys
     const int lane = w.lane, gid = lane >> 2, tig = lane & 3, mi = lane >> 3, rr = lane & 7;
     const bool with_logits = it.own && p.mass_out != nullptr;
-    const int k0 = w.warp * 16;  // this warp's first key of a tile
-    // this lane's rows: 16 mt + 8 i + gid
-    int vis[MT][2];
-    float m_run[MT][2], l_run[MT][2], oc[MT][NT][4];
+    const int rg = w.warp / kGroup, k0 = w.warp % kGroup * 16 * STEPS;  // row group, first key of a tile
+    // this lane's rows: 16 rg + 8 i + gid
+    int vis[2];
+    float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f}, oc[NT][4];
+    uint32_t qa[KS][4];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    for (int i = 0; i < 2; ++i) vis[i] = ok ? w.vis[16 * rg + 8 * i + gid] : 0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            vis[mt][i] = ok ? w.vis[16 * mt + 8 * i + gid] : 0;
-            m_run[mt][i] = -INFINITY;
-            l_run[mt][i] = 0.f;
-        }
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int i = 0; i < 4; ++i) oc[nt][i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) oc[mt][nt][i] = 0.f;
-    }
+    for (int ks = 0; ks < KS; ++ks)
+        ldsm_x4(w.sQ + (ks / 4) * C::kQHalf + sw128_offset(16 * rg + (mi & 1) * 8 + rr, (ks % 4) * 2 + (mi >> 1)), qa[ks][0],
+                qa[ks][1], qa[ks][2], qa[ks][3]);
 
     for (int t = it.t0; t < it.t1 && ok; ++t) {
         const int stK = w.n % C::kStages, fK = w.n / C::kStages;
@@ -298,189 +300,214 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
         const uint32_t sK = w.sRing + stK * C::kTileBytes, sV = w.sRing + stV * C::kTileBytes;
         ok = mbar_wait(w.kv_full + 8 * stK, fK & 1, w.abort_flag);
         if (!(ok = __all_sync(0xffffffffu, ok))) break;  // the warp leaves together
-        // ---- S = Q K^T over the warp's 16 keys (two 8-key blocks)
-        float sc[MT][2][4];
+        // ---- S = Q K^T over the warp's keys, in blocks of 16 (two 8-key halves);
+        //      even and odd steps of the head dimension add up apart
+        float sc[STEPS][2][4];
+        {
+            float sa[STEPS][2][2][4];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+            for (int st = 0; st < STEPS; ++st)
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+                for (int h = 0; h < 4; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[mt][nt][i] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-            const int half = ks / 4, ch0 = (ks % 4) * 2;
-            uint32_t b0, b1, b2, b3;
-            ldsm_x4(sK + half * C::kHalfBytes + sw128_offset(k0 + (mi >> 1) * 8 + rr, ch0 + (mi & 1)), b0, b1, b2, b3);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                uint32_t a[4];
-                ldsm_x4(w.sQ + half * C::kQHalf + sw128_offset(16 * mt + (mi & 1) * 8 + rr, ch0 + (mi >> 1)), a[0], a[1],
-                        a[2], a[3]);
-                mma_bf16_16816(sc[mt][0], a, b0, b1);
-                mma_bf16_16816(sc[mt][1], a, b2, b3);
-            }
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(w.kv_empty + 8 * stK);
-        // ---- online softmax; keys at and past `vis` are not seen (their K may be
-        //      anything, NaN included)
-        const int key0 = t * kPaTile + k0 + 2 * tig;
-        bool grow = false;
-        float mx[MT][2];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            mx[mt][0] = mx[mt][1] = -INFINITY;
-#pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+                    for (int i = 0; i < 4; ++i) sa[st][h >> 1][h & 1][i] = 0.f;
+            constexpr int kBatches = KS * STEPS / 4;
+            uint32_t f[2][4][4];
+            auto fetch = [&](int bt) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = sc[mt][nt][i] * p.scale_log2;
-                    sc[mt][nt][i] = key0 + nt * 8 + (i & 1) < vis[mt][i >> 1] ? x : -INFINITY;
-                    mx[mt][i >> 1] = fmaxf(mx[mt][i >> 1], sc[mt][nt][i]);
+                    const int ks = (bt * 4 + i) / STEPS, st = (bt * 4 + i) % STEPS;
+                    uint32_t(&x)[4] = f[bt & 1][i];
+                    ldsm_x4(sK + (ks / 4) * C::kHalfBytes +
+                                sw128_offset(k0 + st * 16 + (mi >> 1) * 8 + rr, (ks % 4) * 2 + (mi & 1)),
+                            x[0], x[1], x[2], x[3]);
                 }
-            if (with_logits) {
-                float* lg = p.logits + ((static_cast<int64_t>(it.b) * p.Hkv + it.kvh) * p.L + key0) * p.R + it.row0 +
-                            16 * mt + gid;
+            };
+            fetch(0);
+#pragma unroll
+            for (int bt = 0; bt < kBatches; ++bt) {
+                if (bt + 1 < kBatches) fetch(bt + 1);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int ks = (bt * 4 + i) / STEPS, st = (bt * 4 + i) % STEPS;
+                    const uint32_t(&x)[4] = f[bt & 1][i];
+                    mma_bf16_16816(sa[st][ks & 1][0], qa[ks], x[0], x[1]);
+                    mma_bf16_16816(sa[st][ks & 1][1], qa[ks], x[2], x[3]);
+                }
+            }
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st)
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (16 * mt + 8 * (i >> 1) + gid < it.nrows && key0 + nt * 8 + (i & 1) < it.len)
-                            lg[static_cast<int64_t>(nt * 8 + (i & 1)) * p.R + 8 * (i >> 1)] = sc[mt][nt][i];
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                mx[mt][i] = fmaxf(mx[mt][i], __shfl_xor_sync(0xffffffffu, mx[mt][i], 1));
-                mx[mt][i] = fmaxf(mx[mt][i], __shfl_xor_sync(0xffffffffu, mx[mt][i], 2));
-                // O is rescaled only when the maximum has grown by more than 2^8:
-                // until then l and O hold values up to 2^8 times larger, which fp32
-                // takes without loss (and bf16's P: its precision is relative)
-                grow |= mx[mt][i] > m_run[mt][i] + 8.0f;
-            }
+                    for (int i = 0; i < 4; ++i) sc[st][nt][i] = sa[st][0][nt][i] + sa[st][1][nt][i];
         }
-        if (__any_sync(0xffffffffu, grow)) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                float alpha[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    alpha[i] = 1.f;
-                    if (mx[mt][i] > m_run[mt][i] + 8.0f) {
-                        alpha[i] = ex2_approx(m_run[mt][i] - mx[mt][i]);  // 0 while nothing was seen
-                        m_run[mt][i] = mx[mt][i];
-                        l_run[mt][i] *= alpha[i];
-                    }
-                }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    oc[mt][nt][0] *= alpha[0];
-                    oc[mt][nt][1] *= alpha[0];
-                    oc[mt][nt][2] *= alpha[1];
-                    oc[mt][nt][3] *= alpha[1];
-                }
-            }
-        }
-        uint32_t pa[MT][4];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const float m0 = m_run[mt][0] == -INFINITY ? 0.f : m_run[mt][0];
-            const float m1 = m_run[mt][1] == -INFINITY ? 0.f : m_run[mt][1];
-#pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    sc[mt][nt][i] = ex2_approx(sc[mt][nt][i] - (i < 2 ? m0 : m1));
-                    l_run[mt][i >> 1] += sc[mt][nt][i];  // this lane's keys; the quad's are added at the end
-                }
-            // P as the A fragment: rows = rows, k = the 16 keys
-            pa[mt][0] = pack_bf16x2(sc[mt][0][0], sc[mt][0][1]);
-            pa[mt][1] = pack_bf16x2(sc[mt][0][2], sc[mt][0][3]);
-            pa[mt][2] = pack_bf16x2(sc[mt][1][0], sc[mt][1][1]);
-            pa[mt][3] = pack_bf16x2(sc[mt][1][2], sc[mt][1][3]);
-        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(w.kv_empty + 8 * stK);
         ok = mbar_wait(w.kv_full + 8 * stV, fV & 1, w.abort_flag);
         if (!(ok = __all_sync(0xffffffffu, ok))) break;
         const int end = it.len - t * kPaTile;  // rows of the tile that hold a token
-        if (it.own && end < k0 + 16) {
+        if (it.own && end < k0 + 16 * STEPS) {
             // a cache row past the length may hold anything: zero its V, so that P = 0
             // keeps it out of the product
-            for (int i = lane; i < 16 * (D / 8); i += 32) {
+            for (int i = lane; i < 16 * STEPS * (D / 8); i += 32) {
                 const int row = k0 + i / (D / 8), ch = i % (D / 8);
                 if (row >= end) st_shared_v4(sV + (ch >> 3) * C::kHalfBytes + sw128_offset(row, ch & 7), 0u, 0u, 0u, 0u);
             }
             fence_proxy_async_smem();  // ordered before the stage's next TMA write
             __syncwarp();
         }
-        // ---- O += P V over the 16 keys
+        // the first of V's fragments, in flight during the softmax
+        constexpr int kBatchesV = NT / 2 * STEPS / 4;
+        uint32_t f[2][4][4];
+        auto fetch = [&](int bt) {
 #pragma unroll
-        for (int np = 0; np < NT / 2; ++np) {
-            const int col = np * 16 + (mi >> 1) * 8;
-            uint32_t b0, b1, b2, b3;
-            ldsm_x4_trans(sV + (col / 64) * C::kHalfBytes + sw128_offset(k0 + (mi & 1) * 8 + rr, (col % 64) / 8), b0, b1,
-                          b2, b3);
+            for (int i = 0; i < 4; ++i) {
+                const int np = (bt * 4 + i) / STEPS, st = (bt * 4 + i) % STEPS, col = np * 16 + (mi >> 1) * 8;
+                uint32_t(&x)[4] = f[bt & 1][i];
+                ldsm_x4_trans(sV + (col / 64) * C::kHalfBytes +
+                                  sw128_offset(k0 + st * 16 + (mi & 1) * 8 + rr, (col % 64) / 8),
+                              x[0], x[1], x[2], x[3]);
+            }
+        };
+        fetch(0);
+        // ---- online softmax; keys at and past `vis` are not seen (their K may be
+        //      anything, NaN included)
+        const int key0 = t * kPaTile + k0 + 2 * tig;
+        float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                mma_bf16_16816(oc[mt][2 * np], pa[mt], b0, b1);
-                mma_bf16_16816(oc[mt][2 * np + 1], pa[mt], b2, b3);
+        for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = sc[st][nt][i] * p.scale_log2;
+                    sc[st][nt][i] = key0 + st * 16 + nt * 8 + (i & 1) < vis[i >> 1] ? x : -INFINITY;
+                    mx[i >> 1] = fmaxf(mx[i >> 1], sc[st][nt][i]);
+                }
+        if (with_logits) {
+            float* lg = p.logits + ((static_cast<int64_t>(it.b) * p.Hkv + it.kvh) * p.L + key0) * p.R + it.row0 + 16 * rg +
+                        gid;
+            const bool r0 = 16 * rg + gid < it.nrows, r1 = 16 * rg + 8 + gid < it.nrows;
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {  // key0 + off
+                    const int off = st * 16 + (k >> 1) * 8 + (k & 1);
+                    float* at = lg + static_cast<int64_t>(off) * p.R;
+                    if (key0 + off < it.len) {
+                        if (r0) at[0] = sc[st][k >> 1][k & 1];
+                        if (r1) at[8] = sc[st][k >> 1][2 + (k & 1)];
+                    }
+                }
+        }
+        bool grow = false;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
+            mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
+            // O is rescaled only when the maximum has grown by more than 2^8: until
+            // then l and O hold values up to 2^8 times larger, which fp32 takes without
+            // loss (and bf16's P: its precision is relative)
+            grow |= mx[i] > m_run[i] + 8.0f;
+        }
+        if (__any_sync(0xffffffffu, grow)) {
+            float alpha[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                alpha[i] = 1.f;
+                if (mx[i] > m_run[i] + 8.0f) {
+                    alpha[i] = ex2_approx(m_run[i] - mx[i]);  // 0 while nothing was seen
+                    m_run[i] = mx[i];
+                    l_run[i] *= alpha[i];
+                }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                oc[nt][0] *= alpha[0];
+                oc[nt][1] *= alpha[0];
+                oc[nt][2] *= alpha[1];
+                oc[nt][3] *= alpha[1];
+            }
+        }
+        uint32_t pa[STEPS][4];
+        const float m0 = m_run[0] == -INFINITY ? 0.f : m_run[0], m1 = m_run[1] == -INFINITY ? 0.f : m_run[1];
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sc[st][nt][i] = ex2_approx(sc[st][nt][i] - (i < 2 ? m0 : m1));
+                    l_run[i >> 1] += sc[st][nt][i];  // this lane's keys; the quad's are added at the end
+                }
+            // P as the A fragment: rows = rows, k = the 16 keys
+            pa[st][0] = pack_bf16x2(sc[st][0][0], sc[st][0][1]);
+            pa[st][1] = pack_bf16x2(sc[st][0][2], sc[st][0][3]);
+            pa[st][2] = pack_bf16x2(sc[st][1][0], sc[st][1][1]);
+            pa[st][3] = pack_bf16x2(sc[st][1][2], sc[st][1][3]);
+        }
+        // ---- O += P V
+#pragma unroll
+        for (int bt = 0; bt < kBatchesV; ++bt) {
+            if (bt + 1 < kBatchesV) fetch(bt + 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int np = (bt * 4 + i) / STEPS, st = (bt * 4 + i) % STEPS;
+                const uint32_t(&x)[4] = f[bt & 1][i];
+                mma_bf16_16816(oc[2 * np], pa[st], x[0], x[1]);
+                mma_bf16_16816(oc[2 * np + 1], pa[st], x[2], x[3]);
             }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(w.kv_empty + 8 * stV);
     }
 
-    // ---- the eight warps' (m, l, O) joined
+    // ---- the warps' (m, l, O) joined
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            float l = l_run[mt][i];
-            l += __shfl_xor_sync(0xffffffffu, l, 1);
-            l += __shfl_xor_sync(0xffffffffu, l, 2);
-            if (tig == 0) w.sh_ml[w.warp * kPaRows + 16 * mt + 8 * i + gid] = make_float2(m_run[mt][i], l);
-        }
+    for (int i = 0; i < 2; ++i) {
+        float l = l_run[i];
+        l += __shfl_xor_sync(0xffffffffu, l, 1);
+        l += __shfl_xor_sync(0xffffffffu, l, 2);
+        if (tig == 0) w.sh_ml[w.warp * 16 + 8 * i + gid] = make_float2(m_run[i], l);
+    }
     if (!products_sync_and(ok)) return false;
     const int64_t at = static_cast<int64_t>(it.slot) * (it.own ? p.w_own : p.w_pre);
-    float f[MT][2];  // 2^(m of this warp - M) of this lane's rows
+    float f[2];  // 2^(m of this warp - M) of this lane's rows
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int i = 0; i < 2; ++i) {
+        const float2* ml = w.sh_ml + rg * kGroup * 16 + 8 * i + gid;  // [warp of the group][16]
+        float M = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = 16 * mt + 8 * i + gid;
-            float M = -INFINITY, l = 0.f;
+        for (int k = 0; k < kGroup; ++k) M = fmaxf(M, ml[k * 16].x);
+        const float Mu = M == -INFINITY ? 0.f : M;
 #pragma unroll
-            for (int k = 0; k < kPaWarps; ++k) M = fmaxf(M, w.sh_ml[k * kPaRows + row].x);
-            const float Mu = M == -INFINITY ? 0.f : M;
-#pragma unroll
-            for (int k = 0; k < kPaWarps; ++k) {
-                const float2 v = w.sh_ml[k * kPaRows + row];
-                l += ex2_approx(v.x - Mu) * v.y;
-            }
-            f[mt][i] = ex2_approx(m_run[mt][i] - Mu);
-            if (w.warp == 0 && tig == 0 && row < it.nrows)
-                reinterpret_cast<float2*>(it.own ? p.ml_own : p.ml_pre)[at + row] = make_float2(M, l);
-        }
-    constexpr int kR = 16 * MT, kCols = 1024 / kR < D ? 1024 / kR : D, kStride = kCols + 8;
+        for (int k = 0; k < kGroup; ++k) l += ex2_approx(ml[k * 16].x - Mu) * ml[k * 16].y;
+        f[i] = ex2_approx(m_run[i] - Mu);
+        const int row = 16 * rg + 8 * i + gid;
+        if (w.warp % kGroup == 0 && tig == 0 && row < it.nrows)
+            reinterpret_cast<float2*>(it.own ? p.ml_own : p.ml_pre)[at + row] = make_float2(M, l);
+    }
+    constexpr int kCols = 64, kStride = kCols + 8;  // rows 8 floats off a multiple of 32: no bank conflicts
     float* o_part = (it.own ? p.o_own : p.o_pre) + at * D;
     const int tid = w.warp * 32 + lane;
 #pragma unroll
     for (int c0 = 0; c0 < D; c0 += kCols) {
-        float* mine = w.merge + w.warp * kR * kStride;
+        float* mine = w.merge + w.warp * 16 * kStride;
 #pragma unroll
         for (int nt = 0; nt < kCols / 8; ++nt)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    *reinterpret_cast<float2*>(mine + (16 * mt + 8 * i + gid) * kStride + nt * 8 + 2 * tig) =
-                        make_float2(oc[mt][c0 / 8 + nt][2 * i] * f[mt][i], oc[mt][c0 / 8 + nt][2 * i + 1] * f[mt][i]);
+            for (int i = 0; i < 2; ++i)
+                *reinterpret_cast<float2*>(mine + (8 * i + gid) * kStride + nt * 8 + 2 * tig) =
+                    make_float2(oc[c0 / 8 + nt][2 * i] * f[i], oc[c0 / 8 + nt][2 * i + 1] * f[i]);
         products_sync();
-        for (int i = tid; i < kR * kCols / 4; i += kPaWarps * 32) {
+        for (int i = tid; i < it.nrows * (kCols / 4); i += kPaWarps * 32) {
             const int row = i / (kCols / 4), c = i % (kCols / 4) * 4;
-            if (row >= it.nrows) continue;
+            const float* src = w.merge + ((row >> 4) * kGroup * 16 + (row & 15)) * kStride + c;
             float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int k = 0; k < kPaWarps; ++k) {
-                const float4 v = *reinterpret_cast<const float4*>(w.merge + (k * kR + row) * kStride + c);
+            for (int k = 0; k < kGroup; ++k) {
+                const float4 v = *reinterpret_cast<const float4*>(src + k * 16 * kStride);
                 a.x += v.x, a.y += v.y, a.z += v.z, a.w += v.w;
             }
             *reinterpret_cast<float4*>(o_part + static_cast<int64_t>(row) * D + c0 + c) = a;
@@ -557,7 +584,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ __align__(8) uint64_t bar_q_full[2], bar_q_empty[2], bar_kv_full[C::kStages], bar_kv_empty[C::kStages];
-    __shared__ float2 sh_ml[kPaWarps * kPaRows];
+    __shared__ float2 sh_ml[kPaWarps * 16];
     __shared__ int sh_vis[2][kPaRows], sh_scan[kPaThreads / 32], sh_base, sh_b0;
     __shared__ PaPiece sh_piece[2];
     __shared__ volatile int abort_flag;
@@ -689,7 +716,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
                 if (lane < it.nrows) {
                     const int m = it.row0 + lane, r = it.seg_row0 + m / p.G, g = m % p.G;
                     const int b = it.own ? it.b : seq_of_row(p.cu_q, p.B, r);
-                    const int i = __ldg(p.pos + r);
+                    const int i = token_of(p, r);
                     vis = it.own ? own_visible(it.len, p.n_new, i) : it.len;
                     at = ((static_cast<int64_t>(b) * p.n_new + i) * p.Hq + it.kvh * p.G + g) * D;
                 }
@@ -776,35 +803,30 @@ struct PaParts {
     int n;
 };
 
-// p.wpr warps join the parts of one (row, head).
-template <int D>
+// WPR warps join the parts of one (row, head), CH parts at a time: their
+// statistics and O are loaded together and added up with a running maximum,
+// which saves a round trip to memory.
+template <int D, int WPR, int CH>
 __global__ void __launch_bounds__(256) pa_join_kernel(const __grid_constant__ PaParams p)
 {
     constexpr int E = D / 32, kWarps = 8;
     __shared__ float sh_o[kWarps][D];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % p.wpr;
-    const int task = blockIdx.x * (kWarps / p.wpr) + warp / p.wpr;
-    const int r = task / p.Hq, h = task % p.Hq, kvh = h / p.G, g = h % p.G;
+    __shared__ float2 sh_ml[kWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % WPR;
+    const int task = blockIdx.x * (kWarps / WPR) + warp / WPR;
+    const int r = min(task / p.Hq, p.cap - 1), h = task % p.Hq, kvh = h / p.G, g = h % p.G;
+    // loads that depend on nothing, together
+    const PaSched s = *p.sched;
+    const int2 row = p.rows[r];
+    const PaRun pre = p.P > 0 ? p.run_pre[kvh] : PaRun{0, 0};
+    const int ns = p.wq ? p.wcount[2] : 0, nrt = p.wq ? p.wcount[3] : 0;
+    const bool active = task / p.Hq < s.N;
     float acc[E], M = -INFINITY, Ls = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) acc[i] = 0.f;
-    const PaSched s = *p.sched;
-    const bool active = r < s.N;
     if (active) {
-        const int2 row = p.rows[r];  // (read beside the schedule)
-        PaParts x[2];                // prefix, own cache
+        PaParts x[2];  // prefix, own cache
         x[0] = x[1] = PaParts{nullptr, nullptr, nullptr, 0, 0, 0};
-        if (s.wide) {
-            const int m = r * p.G + g;
-            const int64_t step = static_cast<int64_t>(p.wcount[3]) * p.Hkv * 128;
-            const int64_t at = (static_cast<int64_t>(m / 128) * p.Hkv + kvh) * 128 + m % 128;
-            x[0] = PaParts{p.wm_part + at, p.wl_part + at, p.wo_part + at * D, step, step * D, p.wcount[2]};
-        } else if (s.K > 0) {
-            const PaRun run = p.run_pre[kvh];
-            const int64_t at = static_cast<int64_t>(kvh + run.c0) * p.w_pre + r * p.G + g;
-            x[0] = PaParts{p.ml_pre + 2 * at, p.ml_pre + 2 * at + 1, p.o_pre + at * D, 2 * p.w_pre,
-                           static_cast<int64_t>(p.w_pre) * D, run.n};
-        }
         if (row.y >= 0) {
             const int m = (r - row.y) * p.G + g, id = (row.x * p.Hkv + kvh) * p.rt_own_max + m / kPaRows;
             const PaRun run = p.run_own[id];
@@ -812,53 +834,79 @@ __global__ void __launch_bounds__(256) pa_join_kernel(const __grid_constant__ Pa
             x[1] = PaParts{p.ml_own + 2 * at, p.ml_own + 2 * at + 1, p.o_own + at * D, 2 * p.w_own,
                            static_cast<int64_t>(p.w_own) * D, run.n};
         }
-        // (m, l) of up to 32 parts of each segment a lane; more in further rounds
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            for (int e = lane; e < x[k].n; e += 32) {
-                const float vm = __ldg(x[k].m + e * x[k].s_ml), vl = __ldg(x[k].l + e * x[k].s_ml);
-                if (vm == -INFINITY) continue;
-                const float m = fmaxf(M, vm);
-                Ls = Ls * ex2_approx(M - m) + vl * ex2_approx(vm - m);
-                M = m;
-            }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            const float m2 = __shfl_xor_sync(0xffffffffu, M, o), l2 = __shfl_xor_sync(0xffffffffu, Ls, o);
-            const float m = fmaxf(M, m2);
-            if (m != -INFINITY) Ls = Ls * ex2_approx(M - m) + l2 * ex2_approx(m2 - m);
-            M = m;
+        if (s.wide) {
+            const int m = r * p.G + g;
+            const int64_t step = static_cast<int64_t>(nrt) * p.Hkv * 128;
+            const int64_t at = (static_cast<int64_t>(m / 128) * p.Hkv + kvh) * 128 + m % 128;
+            x[0] = PaParts{p.wm_part + at, p.wl_part + at, p.wo_part + at * D, step, step * D, ns};
+        } else if (s.K > 0) {
+            const int64_t at = static_cast<int64_t>(kvh + pre.c0) * p.w_pre + r * p.G + g;
+            x[0] = PaParts{p.ml_pre + 2 * at, p.ml_pre + 2 * at + 1, p.o_pre + at * D, 2 * p.w_pre,
+                           static_cast<int64_t>(p.w_pre) * D, pre.n};
         }
-        if (M != -INFINITY) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-#pragma unroll 8
-                for (int e = sub; e < x[k].n; e += p.wpr) {
-                    // a part whose keys the row does not see has weight 0 and an O of zeros
-                    const float w = ex2_approx(__ldg(x[k].m + e * x[k].s_ml) - M);
-                    const float* src = x[k].o + e * x[k].s_o + lane * E;
-                    float v[E];
+        for (int k = 0; k < 2; ++k) {
+            for (int e0 = sub * CH; e0 < x[k].n; e0 += WPR * CH) {
+                float vm[CH], vl[CH], v[CH][E], top = M;
+#pragma unroll
+                for (int e = 0; e < CH; ++e) {
+                    const int at = min(e0 + e, x[k].n - 1);
+                    vm[e] = __ldg(x[k].m + at * x[k].s_ml);
+                    vl[e] = __ldg(x[k].l + at * x[k].s_ml);
+                    const float* src = x[k].o + at * x[k].s_o + lane * E;
                     if constexpr (E == 4) {
                         const float4 t = __ldg(reinterpret_cast<const float4*>(src));
-                        v[0] = t.x, v[1] = t.y, v[2] = t.z, v[3] = t.w;
+                        v[e][0] = t.x, v[e][1] = t.y, v[e][2] = t.z, v[e][3] = t.w;
                     } else {
                         const float2 t = __ldg(reinterpret_cast<const float2*>(src));
-                        v[0] = t.x, v[1] = t.y;
+                        v[e][0] = t.x, v[e][1] = t.y;
                     }
-#pragma unroll
-                    for (int i = 0; i < E; ++i) acc[i] += w * v[i];
                 }
+#pragma unroll
+                for (int e = 0; e < CH; ++e) {
+                    if (e0 + e >= x[k].n) vm[e] = -INFINITY;
+                    top = fmaxf(top, vm[e]);
+                }
+                if (top == -INFINITY) continue;
+                const float a = ex2_approx(M - top);
+                Ls *= a;
+#pragma unroll
+                for (int i = 0; i < E; ++i) acc[i] *= a;
+#pragma unroll
+                for (int e = 0; e < CH; ++e) {
+                    // a part whose keys the row does not see has weight 0 and an O of zeros
+                    const float w = ex2_approx(vm[e] - top);
+                    Ls += w * vl[e];
+#pragma unroll
+                    for (int i = 0; i < E; ++i) acc[i] += w * v[e][i];
+                }
+                M = top;
             }
         }
     }
-    if (p.wpr > 1) {
+    if constexpr (WPR > 1) {
 #pragma unroll
         for (int i = 0; i < E; ++i) sh_o[warp][lane * E + i] = acc[i];
+        if (lane == 0) sh_ml[warp] = make_float2(M, Ls);
         __syncthreads();
-        if (sub == 0)
-            for (int w = 1; w < p.wpr; ++w)
+        if (sub == 0) {
+            float top = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < E; ++i) acc[i] += sh_o[warp + w][lane * E + i];
+            for (int w = 0; w < WPR; ++w) top = fmaxf(top, sh_ml[warp + w].x);
+            Ls = 0.f;
+#pragma unroll
+            for (int i = 0; i < E; ++i) acc[i] = 0.f;
+            if (top != -INFINITY) {
+#pragma unroll
+                for (int w = 0; w < WPR; ++w) {
+                    const float f = ex2_approx(sh_ml[warp + w].x - top);
+                    Ls += f * sh_ml[warp + w].y;
+#pragma unroll
+                    for (int i = 0; i < E; ++i) acc[i] += f * sh_o[warp + w][lane * E + i];
+                }
+            }
+            M = top;
+        }
     }
     if (active && sub == 0) {
         const float inv = Ls > 0.f ? 1.0f / Ls : 0.f;
@@ -876,53 +924,52 @@ __global__ void __launch_bounds__(256) pa_join_kernel(const __grid_constant__ Pa
 }
 
 // ------------------------------------------------------------------ weights
-// A block: `keys` cache rows of one (sequence, KV head).  `lpk` lanes (a power
-// of two) share a cache row's R logits, which lie together, as do those of
-// neighbouring rows: every load of a warp is one stretch.  Four rows at a time,
-// so that four loads are in flight.
-__global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_constant__ PaParams p, int lpk, int keys)
+// A block: 4 * 256 / lpk cache rows of one (sequence, KV head), four a thread, so
+// that four loads are in flight.  `lpk` lanes (a power of two) share a cache
+// row's R logits, which lie together, as do those of neighbouring rows: every
+// load of a warp is one stretch.
+__global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_constant__ PaParams p, int lpk)
 {
     extern __shared__ float sh_lse2[];
     constexpr int kAt = 4;
-    const int chunks = (p.L + keys - 1) / keys;
+    const int keys_at = kPaMassThreads / lpk, keys = kAt * keys_at, chunks = (p.L + keys - 1) / keys;
     const int bh = blockIdx.x / chunks, first = blockIdx.x % chunks * keys;
     const int b = bh / p.Hkv, kvh = bh % p.Hkv, tid = threadIdx.x;
     const PaSeq q = p.seqs[b];
     if (first >= q.len) return;
     const int nm = q.tiles > 0 ? q.n * p.G : 0;
-    const int keys_at = kPaMassThreads / lpk, sub = tid % lpk;
-    const int last = min(q.len, first + keys);
+    const int sub = tid % lpk, last = min(q.len, first + keys);
     const int n_keys = min(q.len, q.tiles * kPaTile);  // cache rows with logits
     const int64_t base = static_cast<int64_t>(bh) * p.L;
-    auto load = [&](float (&x)[kAt], int k, int m) {
+    float x[kAt], old[kAt];
+    auto load = [&](int m) {
 #pragma unroll
         for (int i = 0; i < kAt; ++i) {
-            const int key = k + i * keys_at + tid / lpk;
+            const int key = first + i * keys_at + tid / lpk;
             x[i] = key < n_keys && m < nm ? __ldg(p.logits + (base + key) * p.R + m) : -INFINITY;
         }
     };
-    float x[kAt];
-    load(x, first, sub);  // in flight beside the rows' statistics
+    load(sub);  // in flight beside the old weights and the rows' statistics
+#pragma unroll
+    for (int i = 0; i < kAt; ++i) {
+        const int key = first + i * keys_at + tid / lpk;
+        old[i] = sub == 0 && key < min(last, q.len - p.n_new) ? p.mass_in[base + key] : 0.f;
+    }
     const float* l2 = p.lse2 + (static_cast<int64_t>(kvh) * p.cap + q.row0) * p.G;
     for (int m = tid; m < nm; m += kPaMassThreads) sh_lse2[m] = l2[m];
     __syncthreads();
-    // (the trip count is the same for all threads: the sums below are the warp's)
-    for (int k = first; k < last; k += kAt * keys_at) {
-        float add[kAt] = {0.f, 0.f, 0.f, 0.f};
-        if (k > first) load(x, k, sub);
-        for (int m = sub; m < nm; m += lpk) {
-            if (m > sub) load(x, k, m);
-            const float l = sh_lse2[m];
+    float add[kAt] = {0.f, 0.f, 0.f, 0.f};
+    for (int m = sub; m < nm; m += lpk) {
+        if (m > sub) load(m);
+        const float l = sh_lse2[m];
 #pragma unroll
-            for (int i = 0; i < kAt; ++i) add[i] += exp2f(x[i] - l);  // exp2f: no weight is flushed to zero
-        }
+        for (int i = 0; i < kAt; ++i) add[i] += exp2f(x[i] - l);  // exp2f: no weight is flushed to zero
+    }
 #pragma unroll
-        for (int i = 0; i < kAt; ++i) {
-            for (int o = lpk / 2; o; o >>= 1) add[i] += __shfl_xor_sync(0xffffffffu, add[i], o);
-            const int key = k + i * keys_at + tid / lpk;
-            if (sub == 0 && key < last)
-                p.mass_out[base + key] = (key < q.len - p.n_new ? p.mass_in[base + key] : 0.f) + add[i];
-        }
+    for (int i = 0; i < kAt; ++i) {
+        for (int o = lpk / 2; o; o >>= 1) add[i] += __shfl_xor_sync(0xffffffffu, add[i], o);
+        const int key = first + i * keys_at + tid / lpk;
+        if (sub == 0 && key < last) p.mass_out[base + key] = old[i] + add[i];
     }
 }
 
@@ -1049,18 +1096,15 @@ int launch_prefix(PaParams& p, cudaStream_t st)
     }
     // few (row, head) pairs have many parts each: eight warps a pair then
     const long long pairs = static_cast<long long>(p.cap) * p.Hq;
-    p.wpr = pairs < 2048 ? 8 : 1;
-    const long long blocks = (pairs * p.wpr + 7) / 8;
-    if (blocks > 0x7fffffffll) return LOGO_ERR_UNSUPPORTED;
-    pa_join_kernel<D><<<static_cast<unsigned>(blocks), 256, 0, st>>>(p);
+    if (pairs < 2048) pa_join_kernel<D, 8, 4><<<static_cast<unsigned>(pairs), 256, 0, st>>>(p);
+    else pa_join_kernel<D, 1, 8><<<static_cast<unsigned>((pairs + 7) / 8), 256, 0, st>>>(p);
     if (p.mass_out) {
         int lpk = 1;
         while (lpk < 32 && 2 * lpk <= p.R) lpk *= 2;
-        // two rounds of four cache rows a thread, to many blocks
-        const int keys = std::min(1024, 8 * kPaMassThreads / lpk);
+        const int keys = 4 * kPaMassThreads / lpk;
         const long long n = static_cast<long long>(p.B) * p.Hkv * ((p.L + keys - 1) / keys);
         if (n > 0x7fffffffll) return LOGO_ERR_UNSUPPORTED;
-        pa_mass_kernel<<<static_cast<unsigned>(n), kPaMassThreads, p.R * sizeof(float), st>>>(p, lpk, keys);
+        pa_mass_kernel<<<static_cast<unsigned>(n), kPaMassThreads, p.R * sizeof(float), st>>>(p, lpk);
     }
     return cudaGetLastError() == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }
