@@ -45,7 +45,7 @@ namespace {
 constexpr int kPaWarps = 8;      // warps that do the products; then the TMA warp, then the planners
 constexpr int kPaPlanners = 2;
 constexpr int kPaThreads = 384;  // three warpgroups, for the register split
-constexpr uint32_t kPaRegsRows = 200, kPaRegsLoad = 104;
+constexpr uint32_t kPaRegsRows = 184, kPaRegsLoad = 136;
 static_assert(128 * (2 * kPaRegsRows + kPaRegsLoad) <= kPaThreads * 168, "register split exceeds the launch allocation");
 constexpr int kPaTile = 128;         // keys per tile
 constexpr int kPaRows = 32;          // rows of a piece at most
@@ -264,20 +264,21 @@ __device__ __forceinline__ bool products_sync_and(bool ok)
 __device__ __forceinline__ void products_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
 
 // One piece, by the eight warps.  Up to 16 rows: each warp takes 16 keys of
-// every tile (STEPS = 1).  Up to 32: four warps take rows 0 .. 15, four the
-// others, each on 32 keys (STEPS = 2).  Fragments are fetched a batch ahead of
-// the products that use them (two warps a scheduler hide little).  Then the
-// warps' results are joined in shared memory.  Returns false, to all warps, if
-// a wait of any gave up.
-template <int D, int STEPS>
+// every tile.  Up to 32: four warps take rows 0 .. 15, four the others, each on
+// 32 keys in two steps (one code path for both: a second one, met by a few SMs
+// only, cost them 8 us of instruction fetches).  Fragments are fetched a batch
+// ahead of the products that use them (two warps a scheduler hide little).  Then
+// the warps' results are joined in shared memory.  Returns false, to all warps,
+// if a wait of any gave up.
+template <int D>
 __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, PaWarp& w, bool ok)
 {
     using C = PaCfg<D>;
     constexpr int NT = D / 8, KS = D / 16;
-    constexpr int kGroup = kPaWarps / STEPS;  // warps that share the rows' keys
     const int lane = w.lane, gid = lane >> 2, tig = lane & 3, mi = lane >> 3, rr = lane & 7;
     const bool with_logits = it.own && p.mass_out != nullptr;
-    const int rg = w.warp / kGroup, k0 = w.warp % kGroup * 16 * STEPS;  // row group, first key of a tile
+    const int steps = it.nrows <= 16 ? 1 : 2, group = kPaWarps / steps;  // warps that share the rows' keys
+    const int rg = w.warp / group, k0 = w.warp % group * 16 * steps;     // row group, first key of a tile
     // this lane's rows: 16 rg + 8 i + gid
     int vis[2];
     float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f}, oc[NT][4];
@@ -300,165 +301,159 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
         const uint32_t sK = w.sRing + stK * C::kTileBytes, sV = w.sRing + stV * C::kTileBytes;
         ok = mbar_wait(w.kv_full + 8 * stK, fK & 1, w.abort_flag);
         if (!(ok = __all_sync(0xffffffffu, ok))) break;  // the warp leaves together
-        // ---- S = Q K^T over the warp's keys, in blocks of 16 (two 8-key halves);
-        //      even and odd steps of the head dimension add up apart
-        float sc[STEPS][2][4];
-        {
-            float sa[STEPS][2][2][4];
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st)
+#pragma unroll 1
+        for (int st = 0; st < steps; ++st) {
+            const int k1 = k0 + 16 * st;  // this step's first key of the tile
+            // ---- S = Q K^T over 16 keys (two 8-key halves); even and odd steps of
+            //      the head dimension add up apart
+            float sc[2][4];
+            {
+                float sa[2][2][4];
 #pragma unroll
                 for (int h = 0; h < 4; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sa[st][h >> 1][h & 1][i] = 0.f;
-            constexpr int kBatches = KS * STEPS / 4;
+                    for (int i = 0; i < 4; ++i) sa[h >> 1][h & 1][i] = 0.f;
+                uint32_t f[2][4][4];
+                auto fetch = [&](int bt) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int ks = bt * 4 + i;
+                        uint32_t(&x)[4] = f[bt & 1][i];
+                        ldsm_x4(sK + (ks / 4) * C::kHalfBytes +
+                                    sw128_offset(k1 + (mi >> 1) * 8 + rr, (ks % 4) * 2 + (mi & 1)),
+                                x[0], x[1], x[2], x[3]);
+                    }
+                };
+                fetch(0);
+#pragma unroll
+                for (int bt = 0; bt < KS / 4; ++bt) {
+                    if (bt + 1 < KS / 4) fetch(bt + 1);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int ks = bt * 4 + i;
+                        const uint32_t(&x)[4] = f[bt & 1][i];
+                        mma_bf16_16816(sa[ks & 1][0], qa[ks], x[0], x[1]);
+                        mma_bf16_16816(sa[ks & 1][1], qa[ks], x[2], x[3]);
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sc[nt][i] = sa[0][nt][i] + sa[1][nt][i];
+            }
+            if (st == steps - 1) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(w.kv_empty + 8 * stK);
+            }
+            if (st == 0) {
+                ok = mbar_wait(w.kv_full + 8 * stV, fV & 1, w.abort_flag);
+                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                const int end = it.len - t * kPaTile;  // rows of the tile that hold a token
+                if (it.own && end < k0 + 16 * steps) {
+                    // a cache row past the length may hold anything: zero its V, so
+                    // that P = 0 keeps it out of the product
+                    for (int i = lane; i < 16 * steps * (D / 8); i += 32) {
+                        const int row = k0 + i / (D / 8), ch = i % (D / 8);
+                        if (row >= end)
+                            st_shared_v4(sV + (ch >> 3) * C::kHalfBytes + sw128_offset(row, ch & 7), 0u, 0u, 0u, 0u);
+                    }
+                    fence_proxy_async_smem();  // ordered before the stage's next TMA write
+                    __syncwarp();
+                }
+            }
+            // the first of V's fragments, in flight during the softmax
             uint32_t f[2][4][4];
             auto fetch = [&](int bt) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int ks = (bt * 4 + i) / STEPS, st = (bt * 4 + i) % STEPS;
+                    const int col = (bt * 4 + i) * 16 + (mi >> 1) * 8;
                     uint32_t(&x)[4] = f[bt & 1][i];
-                    ldsm_x4(sK + (ks / 4) * C::kHalfBytes +
-                                sw128_offset(k0 + st * 16 + (mi >> 1) * 8 + rr, (ks % 4) * 2 + (mi & 1)),
-                            x[0], x[1], x[2], x[3]);
+                    ldsm_x4_trans(sV + (col / 64) * C::kHalfBytes +
+                                      sw128_offset(k1 + (mi & 1) * 8 + rr, (col % 64) / 8),
+                                  x[0], x[1], x[2], x[3]);
                 }
             };
             fetch(0);
-#pragma unroll
-            for (int bt = 0; bt < kBatches; ++bt) {
-                if (bt + 1 < kBatches) fetch(bt + 1);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int ks = (bt * 4 + i) / STEPS, st = (bt * 4 + i) % STEPS;
-                    const uint32_t(&x)[4] = f[bt & 1][i];
-                    mma_bf16_16816(sa[st][ks & 1][0], qa[ks], x[0], x[1]);
-                    mma_bf16_16816(sa[st][ks & 1][1], qa[ks], x[2], x[3]);
-                }
-            }
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st)
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sc[st][nt][i] = sa[st][0][nt][i] + sa[st][1][nt][i];
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(w.kv_empty + 8 * stK);
-        ok = mbar_wait(w.kv_full + 8 * stV, fV & 1, w.abort_flag);
-        if (!(ok = __all_sync(0xffffffffu, ok))) break;
-        const int end = it.len - t * kPaTile;  // rows of the tile that hold a token
-        if (it.own && end < k0 + 16 * STEPS) {
-            // a cache row past the length may hold anything: zero its V, so that P = 0
-            // keeps it out of the product
-            for (int i = lane; i < 16 * STEPS * (D / 8); i += 32) {
-                const int row = k0 + i / (D / 8), ch = i % (D / 8);
-                if (row >= end) st_shared_v4(sV + (ch >> 3) * C::kHalfBytes + sw128_offset(row, ch & 7), 0u, 0u, 0u, 0u);
-            }
-            fence_proxy_async_smem();  // ordered before the stage's next TMA write
-            __syncwarp();
-        }
-        // the first of V's fragments, in flight during the softmax
-        constexpr int kBatchesV = NT / 2 * STEPS / 4;
-        uint32_t f[2][4][4];
-        auto fetch = [&](int bt) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int np = (bt * 4 + i) / STEPS, st = (bt * 4 + i) % STEPS, col = np * 16 + (mi >> 1) * 8;
-                uint32_t(&x)[4] = f[bt & 1][i];
-                ldsm_x4_trans(sV + (col / 64) * C::kHalfBytes +
-                                  sw128_offset(k0 + st * 16 + (mi & 1) * 8 + rr, (col % 64) / 8),
-                              x[0], x[1], x[2], x[3]);
-            }
-        };
-        fetch(0);
-        // ---- online softmax; keys at and past `vis` are not seen (their K may be
-        //      anything, NaN included)
-        const int key0 = t * kPaTile + k0 + 2 * tig;
-        float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st)
+            // ---- online softmax; keys at and past `vis` are not seen (their K may be
+            //      anything, NaN included)
+            const int key0 = t * kPaTile + k1 + 2 * tig;
+            float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = sc[st][nt][i] * p.scale_log2;
-                    sc[st][nt][i] = key0 + st * 16 + nt * 8 + (i & 1) < vis[i >> 1] ? x : -INFINITY;
-                    mx[i >> 1] = fmaxf(mx[i >> 1], sc[st][nt][i]);
+                    const float x = sc[nt][i] * p.scale_log2;
+                    sc[nt][i] = key0 + nt * 8 + (i & 1) < vis[i >> 1] ? x : -INFINITY;
+                    mx[i >> 1] = fmaxf(mx[i >> 1], sc[nt][i]);
                 }
-        if (with_logits) {
-            float* lg = p.logits + ((static_cast<int64_t>(it.b) * p.Hkv + it.kvh) * p.L + key0) * p.R + it.row0 + 16 * rg +
-                        gid;
-            const bool r0 = 16 * rg + gid < it.nrows, r1 = 16 * rg + 8 + gid < it.nrows;
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st)
+            if (with_logits) {
+                float* lg = p.logits + ((static_cast<int64_t>(it.b) * p.Hkv + it.kvh) * p.L + key0) * p.R + it.row0 +
+                            16 * rg + gid;
+                const bool r0 = 16 * rg + gid < it.nrows, r1 = 16 * rg + 8 + gid < it.nrows;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {  // key0 + off
-                    const int off = st * 16 + (k >> 1) * 8 + (k & 1);
+                    const int off = (k >> 1) * 8 + (k & 1);
                     float* at = lg + static_cast<int64_t>(off) * p.R;
                     if (key0 + off < it.len) {
-                        if (r0) at[0] = sc[st][k >> 1][k & 1];
-                        if (r1) at[8] = sc[st][k >> 1][2 + (k & 1)];
+                        if (r0) at[0] = sc[k >> 1][k & 1];
+                        if (r1) at[8] = sc[k >> 1][2 + (k & 1)];
                     }
                 }
-        }
-        bool grow = false;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-            mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
-            // O is rescaled only when the maximum has grown by more than 2^8: until
-            // then l and O hold values up to 2^8 times larger, which fp32 takes without
-            // loss (and bf16's P: its precision is relative)
-            grow |= mx[i] > m_run[i] + 8.0f;
-        }
-        if (__any_sync(0xffffffffu, grow)) {
-            float alpha[2];
+            }
+            bool grow = false;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                alpha[i] = 1.f;
-                if (mx[i] > m_run[i] + 8.0f) {
-                    alpha[i] = ex2_approx(m_run[i] - mx[i]);  // 0 while nothing was seen
-                    m_run[i] = mx[i];
-                    l_run[i] *= alpha[i];
+                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
+                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
+                // O is rescaled only when the maximum has grown by more than 2^8: until
+                // then l and O hold values up to 2^8 times larger, which fp32 takes
+                // without loss (and bf16's P: its precision is relative)
+                grow |= mx[i] > m_run[i] + 8.0f;
+            }
+            if (__any_sync(0xffffffffu, grow)) {
+                float alpha[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    alpha[i] = 1.f;
+                    if (mx[i] > m_run[i] + 8.0f) {
+                        alpha[i] = ex2_approx(m_run[i] - mx[i]);  // 0 while nothing was seen
+                        m_run[i] = mx[i];
+                        l_run[i] *= alpha[i];
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    oc[nt][0] *= alpha[0];
+                    oc[nt][1] *= alpha[0];
+                    oc[nt][2] *= alpha[1];
+                    oc[nt][3] *= alpha[1];
                 }
             }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                oc[nt][0] *= alpha[0];
-                oc[nt][1] *= alpha[0];
-                oc[nt][2] *= alpha[1];
-                oc[nt][3] *= alpha[1];
-            }
-        }
-        uint32_t pa[STEPS][4];
-        const float m0 = m_run[0] == -INFINITY ? 0.f : m_run[0], m1 = m_run[1] == -INFINITY ? 0.f : m_run[1];
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
+            const float m0 = m_run[0] == -INFINITY ? 0.f : m_run[0], m1 = m_run[1] == -INFINITY ? 0.f : m_run[1];
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    sc[st][nt][i] = ex2_approx(sc[st][nt][i] - (i < 2 ? m0 : m1));
-                    l_run[i >> 1] += sc[st][nt][i];  // this lane's keys; the quad's are added at the end
+                    sc[nt][i] = ex2_approx(sc[nt][i] - (i < 2 ? m0 : m1));
+                    l_run[i >> 1] += sc[nt][i];  // this lane's keys; the quad's are added at the end
                 }
             // P as the A fragment: rows = rows, k = the 16 keys
-            pa[st][0] = pack_bf16x2(sc[st][0][0], sc[st][0][1]);
-            pa[st][1] = pack_bf16x2(sc[st][0][2], sc[st][0][3]);
-            pa[st][2] = pack_bf16x2(sc[st][1][0], sc[st][1][1]);
-            pa[st][3] = pack_bf16x2(sc[st][1][2], sc[st][1][3]);
-        }
-        // ---- O += P V
+            const uint32_t pa[4] = {pack_bf16x2(sc[0][0], sc[0][1]), pack_bf16x2(sc[0][2], sc[0][3]),
+                                    pack_bf16x2(sc[1][0], sc[1][1]), pack_bf16x2(sc[1][2], sc[1][3])};
+            // ---- O += P V
 #pragma unroll
-        for (int bt = 0; bt < kBatchesV; ++bt) {
-            if (bt + 1 < kBatchesV) fetch(bt + 1);
+            for (int bt = 0; bt < NT / 8; ++bt) {
+                if (bt + 1 < NT / 8) fetch(bt + 1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int np = (bt * 4 + i) / STEPS, st = (bt * 4 + i) % STEPS;
-                const uint32_t(&x)[4] = f[bt & 1][i];
-                mma_bf16_16816(oc[2 * np], pa[st], x[0], x[1]);
-                mma_bf16_16816(oc[2 * np + 1], pa[st], x[2], x[3]);
+                for (int i = 0; i < 4; ++i) {
+                    const int np = bt * 4 + i;
+                    const uint32_t(&x)[4] = f[bt & 1][i];
+                    mma_bf16_16816(oc[2 * np], pa, x[0], x[1]);
+                    mma_bf16_16816(oc[2 * np + 1], pa, x[2], x[3]);
+                }
             }
         }
+        if (!ok) break;
         __syncwarp();
         if (lane == 0) mbar_arrive(w.kv_empty + 8 * stV);
     }
@@ -476,16 +471,14 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
     float f[2];  // 2^(m of this warp - M) of this lane's rows
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const float2* ml = w.sh_ml + rg * kGroup * 16 + 8 * i + gid;  // [warp of the group][16]
+        const float2* ml = w.sh_ml + rg * group * 16 + 8 * i + gid;  // [warp of the group][16]
         float M = -INFINITY, l = 0.f;
-#pragma unroll
-        for (int k = 0; k < kGroup; ++k) M = fmaxf(M, ml[k * 16].x);
+        for (int k = 0; k < group; ++k) M = fmaxf(M, ml[k * 16].x);
         const float Mu = M == -INFINITY ? 0.f : M;
-#pragma unroll
-        for (int k = 0; k < kGroup; ++k) l += ex2_approx(ml[k * 16].x - Mu) * ml[k * 16].y;
+        for (int k = 0; k < group; ++k) l += ex2_approx(ml[k * 16].x - Mu) * ml[k * 16].y;
         f[i] = ex2_approx(m_run[i] - Mu);
         const int row = 16 * rg + 8 * i + gid;
-        if (w.warp % kGroup == 0 && tig == 0 && row < it.nrows)
+        if (w.warp % group == 0 && tig == 0 && row < it.nrows)
             reinterpret_cast<float2*>(it.own ? p.ml_own : p.ml_pre)[at + row] = make_float2(M, l);
     }
     constexpr int kCols = 64, kStride = kCols + 8;  // rows 8 floats off a multiple of 32: no bank conflicts
@@ -503,10 +496,10 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
         products_sync();
         for (int i = tid; i < it.nrows * (kCols / 4); i += kPaWarps * 32) {
             const int row = i / (kCols / 4), c = i % (kCols / 4) * 4;
-            const float* src = w.merge + ((row >> 4) * kGroup * 16 + (row & 15)) * kStride + c;
+            const float* src = w.merge + ((row >> 4) * group * 16 + (row & 15)) * kStride + c;
             float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < kGroup; ++k) {
+#pragma unroll 4
+            for (int k = 0; k < group; ++k) {
                 const float4 v = *reinterpret_cast<const float4*>(src + k * 16 * kStride);
                 a.x += v.x, a.y += v.y, a.z += v.z, a.w += v.w;
             }
@@ -517,52 +510,19 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
     return true;
 }
 
-// Rows, positions and tiles of the wide prefix, by the whole launch.  The last
-// CTA picks the number of shares that each row tile's key range is cut into:
-// the least time of the busiest SM, an item (row tile, share, KV head) counted
-// with 6 key blocks for its start and its join.  Items lie share by share, so
-// that the SMs work on the same keys at the same time.
+// Rows, positions and tiles of the wide prefix, by one warp of every CTA beside
+// the other roles.  The last CTA's picks the number of shares that each row
+// tile's key range is cut into: the least time of the busiest SM, an item (row
+// tile, share, KV head) counted with 6 key blocks for its start and its join.
+// Items lie share by share, so that the SMs work on the same keys at the same
+// time.
 template <int D>
-__device__ __forceinline__ void wide_prep(const PaParams& p, const PaSched& s)
+__device__ __forceinline__ void wide_prep(const PaParams& p, const PaSched& s, int lane)
 {
-    __shared__ unsigned int sh_best;
-    const int rows = s.wide ? s.N * p.G : 0, tid = threadIdx.x, nRT = (rows + 127) / 128;
-    if (blockIdx.x == gridDim.x - 1) {
-        const int blocks = (p.P + 127) / 128;
-        const int most = rows > 0 ? max(1, min(min(blocks, kPaWideUnits / (nRT * p.Hkv)), 255)) : 0;
-        if (tid == 0) sh_best = ~0u;
-        __syncthreads();
-        if (tid < most) {
-            const int n = tid + 1;
-            const long long items = static_cast<long long>(nRT) * p.Hkv * n;
-            const long long cost = (items + p.n_sm - 1) / p.n_sm * ((blocks + n - 1) / n + 6);
-            atomicMin(&sh_best, static_cast<unsigned int>(min(cost, 0xfffffell) << 8) | static_cast<unsigned int>(n));
-        }
-        __syncthreads();
-        const int ns = rows > 0 ? sh_best & 255 : 0;
-        for (int e = tid; e < nRT * ns; e += kPaThreads) {
-            const int sh = e / nRT, rt = e % nRT;
-            GlobalTile g{};
-            g.row0 = rt * 128;
-            g.nrows = min(128, rows - g.row0);
-            g.b = 0;
-            g.min_pos = g.max_pos = p.P - 1;
-            g.blk_lo = static_cast<int>(static_cast<long long>(blocks) * sh / ns);
-            g.blk_hi = static_cast<int>(static_cast<long long>(blocks) * (sh + 1) / ns) - 1;
-            g.slot = e;
-            g.cost = g.blk_hi - g.blk_lo + 1;
-            p.wtiles[e] = g;
-        }
-        if (tid == 0) {
-            p.wcount[0] = nRT * ns;
-            p.wcount[1] = 0;
-            p.wcount[2] = ns;
-            p.wcount[3] = nRT;
-        }
-    }
-    // a warp takes a row: [KV head][g][D] of q -> [KV head][D] for each g
-    const int vecs = p.Hkv * (D / 8), lane = tid & 31;
-    for (int M = blockIdx.x * (kPaThreads / 32) + (tid >> 5); M < nRT * 128; M += gridDim.x * (kPaThreads / 32)) {
+    const int rows = s.wide ? s.N * p.G : 0, nRT = (rows + 127) / 128;
+    // a row: [KV head][g][D] of q -> [KV head][D] for each g
+    const int vecs = p.Hkv * (D / 8);
+    for (int M = blockIdx.x; M < nRT * 128; M += gridDim.x) {
         uint4* dst = reinterpret_cast<uint4*>(p.wq + static_cast<int64_t>(M) * p.Hkv * D);
         if (M >= rows) {  // the last tile's idle rows: finite
             for (int v = lane; v < vecs; v += 32) dst[v] = make_uint4(0u, 0u, 0u, 0u);
@@ -570,10 +530,40 @@ __device__ __forceinline__ void wide_prep(const PaParams& p, const PaSched& s)
         }
         const int r = M / p.G, g = M % p.G, b = seq_of_row(p.cu_q, p.B, r);
         const uint4* src =
-            reinterpret_cast<const uint4*>(p.q + (static_cast<int64_t>(b) * p.n_new + __ldg(p.pos + r)) * p.Hq * D);
+            reinterpret_cast<const uint4*>(p.q + (static_cast<int64_t>(b) * p.n_new + token_of(p, r)) * p.Hq * D);
 #pragma unroll 4
         for (int v = lane; v < vecs; v += 32) dst[v] = src[(v / (D / 8) * p.G + g) * (D / 8) + v % (D / 8)];
         if (lane == 0) p.wpos[M] = p.P - 1;
+    }
+    if (blockIdx.x != gridDim.x - 1) return;
+    const int blocks = (p.P + 127) / 128;
+    const int most = rows > 0 ? max(1, min(min(blocks, kPaWideUnits / (nRT * p.Hkv)), 255)) : 0;
+    unsigned int best = ~0u;
+    for (int n = lane + 1; n <= most; n += 32) {
+        const long long items = static_cast<long long>(nRT) * p.Hkv * n;
+        const long long cost = (items + p.n_sm - 1) / p.n_sm * ((blocks + n - 1) / n + 6);
+        best = min(best, static_cast<unsigned int>(min(cost, 0xfffffell) << 8) | static_cast<unsigned int>(n));
+    }
+    best = __reduce_min_sync(0xffffffffu, best);
+    const int ns = rows > 0 ? best & 255 : 0;
+    for (int e = lane; e < nRT * ns; e += 32) {
+        const int sh = e / nRT, rt = e % nRT;
+        GlobalTile g{};
+        g.row0 = rt * 128;
+        g.nrows = min(128, rows - g.row0);
+        g.b = 0;
+        g.min_pos = g.max_pos = p.P - 1;
+        g.blk_lo = static_cast<int>(static_cast<long long>(blocks) * sh / ns);
+        g.blk_hi = static_cast<int>(static_cast<long long>(blocks) * (sh + 1) / ns) - 1;
+        g.slot = e;
+        g.cost = g.blk_hi - g.blk_lo + 1;
+        p.wtiles[e] = g;
+    }
+    if (lane == 0) {
+        p.wcount[0] = nRT * ns;
+        p.wcount[1] = 0;
+        p.wcount[2] = ns;
+        p.wcount[3] = nRT;
     }
 }
 
@@ -584,6 +574,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ __align__(8) uint64_t bar_q_full[2], bar_q_empty[2], bar_kv_full[C::kStages], bar_kv_empty[C::kStages];
+    __shared__ __align__(8) uint64_t bar_go;  // the first piece's loads of Q are on their way
     __shared__ float2 sh_ml[kPaWarps * 16];
     __shared__ int sh_vis[2][kPaRows], sh_scan[kPaThreads / 32], sh_base, sh_b0;
     __shared__ PaPiece sh_piece[2];
@@ -594,6 +585,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     if (tid == 0) {
         abort_flag = 0;
         sh_b0 = 0;
+        mbar_init(smem_u32(&bar_go), 1);
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(smem_u32(&bar_kv_full[s]), 1);
             mbar_init(smem_u32(&bar_kv_empty[s]), kPaWarps);
@@ -662,7 +654,6 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
             for (int r = o.row0; r < o.row0 + o.n; ++r) p.rows[r] = make_int2(b, o.tiles > 0 ? o.row0 : -1);
         }
     }
-    if (p.wq) wide_prep<D>(p, s);
     __syncwarp();  // whole warps from here on (setmaxnreg wants them)
     __syncthreads();
     __syncwarp();
@@ -678,6 +669,9 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
             int n = 0;
             bool ok = true;
             while (ok && iter.template next<C::kRunCost>(p, s, &it)) {
+                // when all SMs fill their rings, their first tiles are 24 MB, and a load
+                // behind them takes 4 us
+                if (n == 0 && it.t1 - it.t0 > 1 && !(ok = mbar_wait(smem_u32(&bar_go), 0, &abort_flag))) break;
                 const CUtensorMap* tk = it.own ? &p.tm_kc : &p.tm_kp;
                 const CUtensorMap* tv = it.own ? &p.tm_vc : &p.tm_vp;
                 for (int t = it.t0; t < it.t1 && ok; ++t) {
@@ -722,31 +716,25 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
                 }
                 __syncwarp();
                 constexpr int kChunks = D / 8;       // 16-byte chunks of a row
-                constexpr int kAt = kChunks * 16 / 32;  // chunks of 16 rows a lane
                 const uint32_t qbase = sQ + qb * C::kQBytes;
-                bool ok = true;
-                for (int r0 = 0; r0 == 0 || r0 < it.nrows; r0 += 16) {
-                    uint4 v[kAt];
+                uint4 v[kChunks];  // 32 rows: row k * 32 / kChunks + lane / kChunks
 #pragma unroll
-                    for (int k = 0; k < kAt; ++k) {
-                        const int i = k * 32 + lane, row = r0 + i / kChunks;
-                        const int64_t src = __shfl_sync(0xffffffffu, at, row & 31);
-                        v[k] = make_uint4(0u, 0u, 0u, 0u);
-                        if (row < it.nrows) v[k] = __ldg(reinterpret_cast<const uint4*>(p.q + src) + i % kChunks);
-                    }
-                    if (r0 == 0) {
-                        ok = mbar_wait(smem_u32(&bar_q_empty[qb]), ((piece >> 1) & 1) ^ 1, &abort_flag);
-                        if (!(ok = __all_sync(0xffffffffu, ok))) break;
-                    }
-#pragma unroll
-                    for (int k = 0; k < kAt; ++k) {
-                        const int i = k * 32 + lane, row = r0 + i / kChunks, ch = i % kChunks;
-                        if (row < it.nrows)
-                            st_shared_v4(qbase + (ch >> 3) * C::kQHalf + sw128_offset(row, ch & 7), v[k].x, v[k].y,
-                                         v[k].z, v[k].w);
-                    }
+                for (int k = 0; k < kChunks; ++k) {
+                    const int row = (k * 32 + lane) / kChunks;
+                    const int64_t src = __shfl_sync(0xffffffffu, at, row);
+                    v[k] = make_uint4(0u, 0u, 0u, 0u);
+                    if (row < it.nrows) v[k] = __ldg(reinterpret_cast<const uint4*>(p.q + src) + lane % kChunks);
                 }
-                if (!ok) break;
+                if (piece == 0 && lane == 0) mbar_arrive(smem_u32(&bar_go));
+                bool ok = mbar_wait(smem_u32(&bar_q_empty[qb]), ((piece >> 1) & 1) ^ 1, &abort_flag);
+                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+#pragma unroll
+                for (int k = 0; k < kChunks; ++k) {
+                    const int row = (k * 32 + lane) / kChunks, ch = lane % kChunks;
+                    if (row < it.nrows)
+                        st_shared_v4(qbase + (ch >> 3) * C::kQHalf + sw128_offset(row, ch & 7), v[k].x, v[k].y, v[k].z,
+                                     v[k].w);
+                }
                 sh_vis[qb][lane] = vis;
                 if (lane == 0) sh_piece[qb] = it;
                 __syncwarp();
@@ -756,6 +744,8 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
                 }
                 if (!more) break;
             }
+        } else if (warp == kPaWarps + 1 + kPaPlanners && p.wq) {
+            wide_prep<D>(p, s, lane);
         }
         return;
     }
@@ -786,9 +776,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
             products_sync_and(true);
             break;
         }
-        if (it.nrows <= 16) ok = pa_piece<D, 1>(p, it, w, ok);
-        else ok = pa_piece<D, 2>(p, it, w, ok);
-        if (!ok) break;
+        if (!pa_piece<D>(p, it, w, ok)) break;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bar_q_empty[qb]));
     }
@@ -924,15 +912,15 @@ __global__ void __launch_bounds__(256) pa_join_kernel(const __grid_constant__ Pa
 }
 
 // ------------------------------------------------------------------ weights
-// A block: 4 * 256 / lpk cache rows of one (sequence, KV head), four a thread, so
-// that four loads are in flight.  `lpk` lanes (a power of two) share a cache
-// row's R logits, which lie together, as do those of neighbouring rows: every
-// load of a warp is one stretch.
+// A block: AT * 256 / lpk cache rows of one (sequence, KV head), AT a thread (or
+// `lpk` threads, a power of two, each of which takes a share of the R logits of
+// a cache row, four floats at a time where R allows).  A cache row's logits lie
+// together, as do those of neighbouring rows.
+template <int AT, int VEC>
 __global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_constant__ PaParams p, int lpk)
 {
     extern __shared__ float sh_lse2[];
-    constexpr int kAt = 4;
-    const int keys_at = kPaMassThreads / lpk, keys = kAt * keys_at, chunks = (p.L + keys - 1) / keys;
+    const int keys_at = kPaMassThreads / lpk, keys = AT * keys_at, chunks = (p.L + keys - 1) / keys;
     const int bh = blockIdx.x / chunks, first = blockIdx.x % chunks * keys;
     const int b = bh / p.Hkv, kvh = bh % p.Hkv, tid = threadIdx.x;
     const PaSeq q = p.seqs[b];
@@ -941,36 +929,66 @@ __global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_co
     const int sub = tid % lpk, last = min(q.len, first + keys);
     const int n_keys = min(q.len, q.tiles * kPaTile);  // cache rows with logits
     const int64_t base = static_cast<int64_t>(bh) * p.L;
-    float x[kAt], old[kAt];
+    float x[AT][VEC], old[AT];
     auto load = [&](int m) {
 #pragma unroll
-        for (int i = 0; i < kAt; ++i) {
+        for (int i = 0; i < AT; ++i) {
             const int key = first + i * keys_at + tid / lpk;
-            x[i] = key < n_keys && m < nm ? __ldg(p.logits + (base + key) * p.R + m) : -INFINITY;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[i][e] = -INFINITY;
+            if (key < n_keys && m < nm) {
+                const float* src = p.logits + (base + key) * p.R + m;
+                if constexpr (VEC == 4) {
+                    const float4 v = __ldg(reinterpret_cast<const float4*>(src));
+                    x[i][0] = v.x, x[i][1] = v.y, x[i][2] = v.z, x[i][3] = v.w;
+                } else {
+                    x[i][0] = __ldg(src);
+                }
+            }
         }
     };
-    load(sub);  // in flight beside the old weights and the rows' statistics
+    load(sub * VEC);  // in flight beside the old weights and the rows' statistics
 #pragma unroll
-    for (int i = 0; i < kAt; ++i) {
+    for (int i = 0; i < AT; ++i) {
         const int key = first + i * keys_at + tid / lpk;
         old[i] = sub == 0 && key < min(last, q.len - p.n_new) ? p.mass_in[base + key] : 0.f;
     }
     const float* l2 = p.lse2 + (static_cast<int64_t>(kvh) * p.cap + q.row0) * p.G;
-    for (int m = tid; m < nm; m += kPaMassThreads) sh_lse2[m] = l2[m];
+    // past nm: rows that were not selected, whose logits are not written (VEC rows
+    // at a time reach them)
+    for (int m = tid; m < nm + VEC - 1; m += kPaMassThreads) sh_lse2[m] = m < nm ? l2[m] : INFINITY;
     __syncthreads();
-    float add[kAt] = {0.f, 0.f, 0.f, 0.f};
-    for (int m = sub; m < nm; m += lpk) {
-        if (m > sub) load(m);
-        const float l = sh_lse2[m];
+    float add[AT];
 #pragma unroll
-        for (int i = 0; i < kAt; ++i) add[i] += exp2f(x[i] - l);  // exp2f: no weight is flushed to zero
+    for (int i = 0; i < AT; ++i) add[i] = 0.f;
+    for (int m = sub * VEC; m < nm; m += lpk * VEC) {
+        if (m > sub * VEC) load(m);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float l = sh_lse2[m + e];
+            // exp2f: no weight is flushed to zero
+#pragma unroll
+            for (int i = 0; i < AT; ++i) add[i] += m + e < nm ? exp2f(x[i][e] - l) : 0.f;
+        }
     }
 #pragma unroll
-    for (int i = 0; i < kAt; ++i) {
+    for (int i = 0; i < AT; ++i) {
         for (int o = lpk / 2; o; o >>= 1) add[i] += __shfl_xor_sync(0xffffffffu, add[i], o);
         const int key = first + i * keys_at + tid / lpk;
         if (sub == 0 && key < last) p.mass_out[base + key] = old[i] + add[i];
     }
+}
+
+template <int AT, int VEC>
+int launch_mass(const PaParams& p, cudaStream_t st)
+{
+    int lpk = 1;  // four loads a thread at least, up to a warp for a cache row
+    while (lpk < 32 && 2 * lpk * VEC * 4 <= p.R) lpk *= 2;
+    const int keys = AT * kPaMassThreads / lpk;
+    const long long n = static_cast<long long>(p.B) * p.Hkv * ((p.L + keys - 1) / keys);
+    if (n > 0x7fffffffll) return LOGO_ERR_UNSUPPORTED;
+    pa_mass_kernel<AT, VEC><<<static_cast<unsigned>(n), kPaMassThreads, (p.R + VEC) * sizeof(float), st>>>(p, lpk);
+    return LOGO_OK;
 }
 
 // ---------------------------------------------------------------------- host
@@ -1097,14 +1115,11 @@ int launch_prefix(PaParams& p, cudaStream_t st)
     // few (row, head) pairs have many parts each: eight warps a pair then
     const long long pairs = static_cast<long long>(p.cap) * p.Hq;
     if (pairs < 2048) pa_join_kernel<D, 8, 4><<<static_cast<unsigned>(pairs), 256, 0, st>>>(p);
-    else pa_join_kernel<D, 1, 8><<<static_cast<unsigned>((pairs + 7) / 8), 256, 0, st>>>(p);
+    else pa_join_kernel<D, 1, 4><<<static_cast<unsigned>((pairs + 7) / 8), 256, 0, st>>>(p);
     if (p.mass_out) {
-        int lpk = 1;
-        while (lpk < 32 && 2 * lpk <= p.R) lpk *= 2;
-        const int keys = 4 * kPaMassThreads / lpk;
-        const long long n = static_cast<long long>(p.B) * p.Hkv * ((p.L + keys - 1) / keys);
-        if (n > 0x7fffffffll) return LOGO_ERR_UNSUPPORTED;
-        pa_mass_kernel<<<static_cast<unsigned>(n), kPaMassThreads, p.R * sizeof(float), st>>>(p, lpk);
+        const int rc = p.R % 4 == 0 ? (p.R <= 4 ? launch_mass<4, 4>(p, st) : launch_mass<2, 4>(p, st))
+                                    : launch_mass<4, 1>(p, st);
+        if (rc != LOGO_OK) return rc;
     }
     return cudaGetLastError() == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }
