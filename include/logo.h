@@ -287,8 +287,9 @@ LOGO_API int logo_cache_evict(logo_bf16* k_cache, logo_bf16* v_cache, const floa
  *   race of exponential clocks draws v with probability r_v / sum r.
  * Out: tokens [B, m+1] int32: the a accepted drafts, the sampled token, then
  *      -1; n_accept [B] int32 = a.
- *   B * (m + 1) <= 2^24, V >= 1.  Results are exact and deterministic.
- *   Workspace: logo_verify_draft_workspace_size(B, m, V) bytes. */
+ *   B * (m + 1) <= 2^24, 1 <= V <= 2^30.  Results are exact and deterministic.
+ *   Workspace: logo_verify_draft_workspace_size(B, m, V) bytes (a small fixed
+ *   room that the call does not need at present). */
 LOGO_API size_t logo_verify_draft_workspace_size(int B, int m, int V);
 LOGO_API int logo_verify_draft(const int32_t* draft, const float* q_draft, const float* p_target, const float* u,
                 const float* noise, const int32_t* draft_len, int32_t* tokens, int32_t* n_accept, int B, int m, int V,

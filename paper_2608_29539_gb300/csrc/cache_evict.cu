@@ -1,24 +1,36 @@
 // cache_evict.cu -- cuts a sequence's cache back to its budget by accumulated
 // attention weight.
 //
-// One block per (sequence, KV head).  Every cache row has a 33-bit rank key:
-// rows inside the recent window above all others, then the order-preserving
-// image of the fp32 weight; equal keys go to the lower row.  A radix select
-// finds the key of the last row that stays; one ordered pass then lists the
-// holes (rows below `end` that go) and the movers (rows at or above `end` that
-// stay) in rising order, and mover i is copied into hole i.  No mover's source
-// is any mover's destination, so the copies need no order.
+// Every cache row of a (sequence, KV head) has a rank key: rows inside the
+// recent window above all others, then the order-preserving image of the fp32
+// weight; equal keys go to the lower row.  A radix select (8 bits a pass) finds
+// the key of the last row that stays and how many of the rows with that key do;
+// one ordered pass lists the holes (rows below `end` that go) and the movers
+// (rows at or above `end` that stay) in rising order, and mover i is copied into
+// hole i.  No mover's row is any mover's destination, so the copies need no
+// order, and no fewer rows could be moved.
+//
+// A thread-block cluster takes a (sequence, KV head), each CTA an equal stretch
+// of its rows: keys are formed once and stay in shared memory, the passes'
+// histograms meet in distributed shared memory, and the same CTAs then move the
+// rows (HBM-bound: 4 D bytes a moved row of K and V, read and written), so that
+// the cut of a whole batch is one launch.
 #include <cuda_bf16.h>
 
 #include <cstdint>
 
+#include "cluster.cuh"
 #include "host_common.h"
 #include "logo_status.cuh"
 
 namespace logo {
 namespace {
 
-constexpr int kEvThreads = 1024;
+constexpr int kEvThreads = 512;
+constexpr int kEvWarps = kEvThreads / 32;
+constexpr int kEvMaxCluster = 8;          // portable cluster size
+constexpr int kEvSmemKeys = 48 * 1024;    // keys of a CTA's stretch in shared memory; longer ones are formed anew each pass
+constexpr int kEvMovesAt = 4;             // moves in flight per warp
 
 struct EvParams {
     logo_bf16 *k, *v;
@@ -27,7 +39,7 @@ struct EvParams {
     float* mass_out;
     int32_t *pos_out, *new_len;
     int32_t* lists;  // [B * Hkv][L]: holes from the front, movers from the back
-    int B, L, Hkv, D, budget, recent;
+    int B, L, Hkv, D, budget, recent, smem_keys;
 };
 
 // Larger key: stays longer.  0xffffffff: inside the recent window; a float's
@@ -40,116 +52,214 @@ __device__ __forceinline__ uint32_t evict_key(float mass, int pos, int first_rec
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Exclusive sums over the block's 1024 threads of two counts below 2^16 each, packed.
-__device__ __forceinline__ uint32_t block_excl_scan(uint32_t v, uint32_t* total, uint32_t* sh)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint32_t x = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-    }
-    if (lane == 31) sh[warp] = x;
-    __syncthreads();
-    if (warp == 0) {
-        const uint32_t w0 = sh[lane];
-        uint32_t w = w0;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t y = __shfl_up_sync(0xffffffffu, w, o);
-            if (lane >= o) w += y;
-        }
-        sh[lane] = w - w0;
-        if (lane == 31) sh[32] = w;
-    }
-    __syncthreads();
-    const uint32_t r = sh[warp] + x - v;
-    *total = sh[32];
-    __syncthreads();
-    return r;
-}
-
 __global__ void __launch_bounds__(kEvThreads) evict_kernel(EvParams p)
 {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t sh_scan[33];
+    extern __shared__ uint32_t sh_keys[];
+    __shared__ int hist[2][256];                    // this CTA's, two passes' worth (read by the cluster)
+    __shared__ int sh_count[3];                     // ties, holes, movers of this CTA (read by the cluster)
+    __shared__ int sh_warp[3][kEvWarps];            // ... of each warp
+    __shared__ int sh_lane[256];                    // the cluster's histogram
     __shared__ uint32_t sh_prefix;
-    __shared__ int sh_need;
-    const int bh = blockIdx.x, b = bh / p.Hkv, h = bh % p.Hkv;
-    const int tid = threadIdx.x;
-    const int len = max(0, min(p.seq_len[b], p.L));
-    const int end = min(len, p.budget);
+    __shared__ int sh_need, sh_ties;
+    const uint32_t cs = cluster_size(), rank = cluster_rank();
+    const int bh = blockIdx.x / cs, b = bh / p.Hkv, h = bh % p.Hkv;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int len = max(0, min(p.seq_len[b], p.L)), end = min(len, p.budget);
     const int64_t base = static_cast<int64_t>(bh) * p.L;
     const float* mass = p.mass + base;
     const int32_t* pos = p.slot_pos + base;
-    if (h == 0 && tid == 0) p.new_len[b] = end;
-    if (len <= p.budget) {
-        for (int s = tid; s < len; s += kEvThreads) {
-            const float m = mass[s];
-            const int q = pos[s];
-            p.mass_out[base + s] = m;
-            p.pos_out[base + s] = q;
+    if (h == 0 && rank == 0 && tid == 0) p.new_len[b] = end;
+    // this CTA's rows [s0, s0 + cnt)
+    const int per = (len + cs - 1) / cs, s0 = min(len, per * static_cast<int>(rank)), cnt = min(len - s0, per);
+    if (len <= p.budget) {  // (all CTAs of the cluster)
+        for (int i = tid; i < cnt; i += kEvThreads) {
+            const float m = mass[s0 + i];
+            const int q = pos[s0 + i];
+            p.mass_out[base + s0 + i] = m;
+            p.pos_out[base + s0 + i] = q;
         }
         return;
     }
     const int first_recent = p.n_seen[b] - p.recent;
-    // radix select: the key of the end-th largest, and how many rows with it stay
+    const bool in_smem = per <= p.smem_keys;
+    for (int i = tid; i < 512; i += kEvThreads) hist[i >> 8][i & 255] = 0;
+    if (in_smem) {
+#pragma unroll 4
+        for (int i = tid; i < cnt; i += kEvThreads) sh_keys[i] = evict_key(mass[s0 + i], pos[s0 + i], first_recent);
+    }
+    __syncthreads();
+    auto key_at = [&](int i) { return in_smem ? sh_keys[i] : evict_key(mass[s0 + i], pos[s0 + i], first_recent); };
+
+    // ---- the key of the end-th largest, and how many rows with it stay
     uint32_t prefix = 0;
-    int need = end;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
-        for (int s = tid; s < len; s += kEvThreads) {
-            const uint32_t k = evict_key(mass[s], pos[s], first_recent);
-            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+    int need = end, ties = 0;
+    for (int pass = 0; pass < 4; ++pass) {
+        const int shift = 24 - 8 * pass, buf = pass & 1;
+        for (int i0 = warp * 32; i0 < cnt; i0 += kEvThreads) {
+            const int i = i0 + lane;
+            const uint32_t k = i < cnt ? key_at(i) : 0u;
+            const bool in = i < cnt && (pass == 0 || (k ^ prefix) >> (shift + 8) == 0);
+            const int digit = (k >> shift) & 255u;
+            // lanes with the same digit count once
+            const uint32_t peers = __match_any_sync(0xffffffffu, in ? digit : 256);
+            if (in && lane == __ffs(peers) - 1) atomicAdd(&hist[buf][digit], __popc(peers));
+        }
+        cluster_sync();  // every CTA's histogram of this pass is complete
+        if (tid < 256) {
+            int sum = 0;
+            for (uint32_t r = 0; r < cs; ++r) sum += cluster_read(&hist[buf][tid], r);
+            sh_lane[tid] = sum;
+            hist[buf ^ 1][tid] = 0;  // the last pass's, read by all before the barrier
         }
         __syncthreads();
-        if (tid == 0) {
-            int d = 255, n = need;
-            while (d > 0 && static_cast<int>(hist[d]) < n) n -= hist[d--];
-            sh_prefix = prefix | (static_cast<uint32_t>(d) << shift);
-            sh_need = n;
+        if (warp == 0) {  // lane l: digits 255 - 8 l down to 248 - 8 l
+            int own[8], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += own[i] = sh_lane[255 - 8 * lane - i];
+            int incl = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += y;
+            }
+            int before = incl - sum;  // rows with a larger digit
+            if (before < need && need <= incl) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (before < need && need <= before + own[i]) {
+                        sh_prefix = prefix | static_cast<uint32_t>(255 - 8 * lane - i) << shift;
+                        sh_need = need - before;
+                        sh_ties = own[i];
+                    }
+                    before += own[i];
+                }
+            }
         }
         __syncthreads();
         prefix = sh_prefix;
         need = sh_need;
+        ties = sh_ties;
     }
-    // ordered pass: ties, then holes and movers
+
+    // ---- ordered: a warp takes a stretch of 32-row groups
+    const int seg = (cnt + 32 * kEvWarps - 1) / (32 * kEvWarps) * 32;
+    const int w0 = min(cnt, warp * seg), w1 = min(cnt, w0 + seg);
+    const uint32_t below = (1u << lane) - 1;
+    // (this CTA's count i of every warp, in sh_warp) -> first number of this warp
+    // over the cluster; all threads
+    auto first_of = [&](int i) {
+        int mine = 0, total = 0;
+        for (int k = 0; k < kEvWarps; ++k) {
+            mine += k < warp ? sh_warp[i][k] : 0;
+            total += sh_warp[i][k];
+        }
+        if (tid == 0) sh_count[i] = total;
+        return mine;
+    };
+    auto over_cluster = [&](int i, int* all) {  // counts of the CTAs before this one; of all
+        int mine = 0, sum = 0;
+        for (uint32_t r = 0; r < cs; ++r) {
+            const int c = cluster_read(&sh_count[i], r);
+            mine += r < rank ? c : 0;
+            sum += c;
+        }
+        *all = sum;
+        return mine;
+    };
+    int all, tie0 = 0;
+    const bool all_ties = need == ties;  // the usual case: no equal keys to tell apart
+    if (!all_ties) {
+        int n = 0;
+        for (int i0 = w0; i0 < w1; i0 += 32)
+            n += __popc(__ballot_sync(0xffffffffu, i0 + lane < w1 && key_at(i0 + lane) == prefix));
+        if (lane == 0) sh_warp[0][warp] = n;
+        __syncthreads();
+        tie0 = first_of(0);
+        cluster_sync();
+        tie0 += over_cluster(0, &all);
+    }
+    // does row i stay?  `t`: ties before this group, moved on
+    auto keeps = [&](int i, int& t) {
+        const uint32_t k = i < w1 ? key_at(i) : 0u;
+        if (all_ties) return i < w1 && k >= prefix;
+        const uint32_t eq = __ballot_sync(0xffffffffu, i < w1 && k == prefix);
+        const bool keep = i < w1 && (k > prefix || (k == prefix && t + __popc(eq & below) < need));
+        t += __popc(eq);
+        return keep;
+    };
+    int n_hole = 0, n_move = 0, t = tie0;
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+        const int i = i0 + lane;
+        const bool keep = keeps(i, t);
+        n_hole += __popc(__ballot_sync(0xffffffffu, i < w1 && s0 + i < end && !keep));
+        n_move += __popc(__ballot_sync(0xffffffffu, keep && s0 + i >= end));
+    }
+    if (lane == 0) {
+        sh_warp[1][warp] = n_hole;
+        sh_warp[2][warp] = n_move;
+    }
+    __syncthreads();
+    int hole = first_of(1), move = first_of(2);
+    cluster_sync();
+    int holes;
+    hole += over_cluster(1, &holes);
+    move += over_cluster(2, &all);
     int32_t* lists = p.lists + base;
-    uint32_t ties = 0, n_hole = 0, n_move = 0;
-    for (int s0 = 0; s0 < len; s0 += kEvThreads) {
-        const int s = s0 + tid;
-        const uint32_t k = s < len ? evict_key(mass[s], pos[s], first_recent) : 0u;
-        const bool tie = s < len && k == prefix;
-        uint32_t total;
-        const uint32_t tie_rank = ties + block_excl_scan(tie ? 1u : 0u, &total, sh_scan);
-        ties += total;
-        const bool keep = s < len && (k > prefix || (tie && tie_rank < static_cast<uint32_t>(need)));
-        const bool hole = s < end && !keep, mover = s >= end && keep;
-        const uint32_t r = block_excl_scan((hole ? 1u : 0u) | (mover ? 0x10000u : 0u), &total, sh_scan);
-        if (hole) lists[n_hole + (r & 0xffffu)] = s;
-        if (mover) lists[p.L - 1 - (n_move + (r >> 16))] = s;
-        n_hole += total & 0xffffu;
-        n_move += total >> 16;
-        if (s < end && keep) {
+    const bool copies = p.mass_out != p.mass || p.pos_out != p.slot_pos;
+    t = tie0;
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+        const int i = i0 + lane, s = s0 + i;
+        const bool keep = keeps(i, t);
+        const bool is_hole = i < w1 && s < end && !keep, is_move = keep && s >= end;
+        const uint32_t bh_ = __ballot_sync(0xffffffffu, is_hole), bm = __ballot_sync(0xffffffffu, is_move);
+        if (is_hole) lists[hole + __popc(bh_ & below)] = s;
+        if (is_move) lists[p.L - 1 - (move + __popc(bm & below))] = s;
+        if (copies && keep && s < end) {
             p.mass_out[base + s] = mass[s];
             p.pos_out[base + s] = pos[s];
         }
+        hole += __popc(bh_);
+        move += __popc(bm);
     }
-    __syncthreads();  // the lists are written
-    const int warp = tid >> 5, lane = tid & 31, vecs = p.D / 8;
-    for (uint32_t i = warp; i < n_hole; i += kEvThreads / 32) {
-        const int dst = lists[i], src = lists[p.L - 1 - i];
-        if (lane < vecs) {
-            const int64_t sr = ((static_cast<int64_t>(b) * p.L + src) * p.Hkv + h) * vecs + lane;
-            const int64_t dr = ((static_cast<int64_t>(b) * p.L + dst) * p.Hkv + h) * vecs + lane;
-            reinterpret_cast<uint4*>(p.k)[dr] = reinterpret_cast<const uint4*>(p.k)[sr];
-            reinterpret_cast<uint4*>(p.v)[dr] = reinterpret_cast<const uint4*>(p.v)[sr];
+    cluster_sync();  // the lists are written (and no CTA leaves while another reads its counts)
+
+    // ---- the moves: half a warp takes K, half V, a 16-byte chunk a lane (D = 64:
+    //      two moves at once)
+    const int chunks = p.D / 8, per_warp = 16 / chunks;  // moves side by side
+    const int half = lane / 16, sub = lane % 16 / chunks, ch = lane % chunks;
+    uint4* rows = reinterpret_cast<uint4*>(half ? p.v : p.k);
+    const int64_t row0 = (static_cast<int64_t>(b) * p.L * p.Hkv + h) * chunks + ch;
+    const int64_t step = static_cast<int64_t>(p.Hkv) * chunks;
+    const int n_warps = static_cast<int>(cs) * kEvWarps;
+    for (int i0 = (static_cast<int>(rank) * kEvWarps + warp) * per_warp; i0 < holes;
+         i0 += n_warps * per_warp * kEvMovesAt) {
+        int dst[kEvMovesAt], src[kEvMovesAt];
+        uint4 v[kEvMovesAt];
+        float m[kEvMovesAt];
+        int q[kEvMovesAt];
+#pragma unroll
+        for (int j = 0; j < kEvMovesAt; ++j) {
+            const int i = i0 + j * n_warps * per_warp + sub;
+            dst[j] = i < holes ? lists[i] : -1;
+            src[j] = i < holes ? lists[p.L - 1 - i] : 0;
         }
-        if (lane == 0) {
-            p.mass_out[base + dst] = mass[src];
-            p.pos_out[base + dst] = pos[src];
+#pragma unroll
+        for (int j = 0; j < kEvMovesAt; ++j) {
+            if (dst[j] < 0) continue;
+            v[j] = rows[row0 + src[j] * step];
+            if (half == 0 && ch == 0) {
+                m[j] = mass[src[j]];
+                q[j] = pos[src[j]];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kEvMovesAt; ++j) {
+            if (dst[j] < 0) continue;
+            rows[row0 + dst[j] * step] = v[j];
+            if (half == 0 && ch == 0) {
+                p.mass_out[base + dst[j]] = m[j];
+                p.pos_out[base + dst[j]] = q[j];
+            }
         }
     }
 }
@@ -209,6 +319,20 @@ extern "C" int logo_cache_evict(logo_bf16* k_cache, logo_bf16* v_cache, const fl
     p.D = dims.D;
     p.budget = budget;
     p.recent = recent;
-    evict_kernel<<<dims.B * dims.Hkv, kEvThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
-    return cudaGetLastError() == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
+    static bool attr_done = false;  // benign race: setting the attribute twice is harmless
+    if (!attr_done) {
+        if (set_smem_limit(evict_kernel, kEvSmemKeys * 4) != cudaSuccess) return LOGO_ERR_CUDA;
+        attr_done = true;
+    }
+    // CTAs per (sequence, KV head): up to four per SM in all, stretches of a row a
+    // thread at least
+    const int64_t pairs = static_cast<int64_t>(dims.B) * dims.Hkv;
+    int cs = 1;
+    while (cs < kEvMaxCluster && pairs * cs * 2 <= 4ll * device_sm_count() && dims.T / (cs * 2) >= kEvThreads) cs *= 2;
+    const int per = (dims.T + cs - 1) / cs;
+    p.smem_keys = per <= kEvSmemKeys ? per : 0;
+    cudaLaunchAttribute attr{};
+    const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(pairs) * cs, kEvThreads, cs, p.smem_keys * 4,
+                                                  static_cast<cudaStream_t>(stream), &attr);
+    return cudaLaunchKernelEx(&cfg, evict_kernel, p) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }

@@ -6,15 +6,25 @@
 // v wins (largest r_v / e_v) with probability r_v / sum r.  So r need not be
 // normalised, one pass over the row suffices, and the result is a maximum:
 // exact, and the same whatever order the row is read in.
+//
+// Bound by HBM: three rows of V floats a sequence (p, q and the clocks).  A
+// thread-block cluster takes a sequence, each of its CTAs an equal stretch of
+// the row (as many CTAs as the batch leaves SMs for), and the CTAs' maxima meet
+// in distributed shared memory: one launch, no scratch, no counters.
+#include <cuda_runtime.h>
+
 #include <cstdint>
 
+#include "cluster.cuh"
 #include "host_common.h"
 #include "logo_status.cuh"
 
 namespace logo {
 namespace {
 
-constexpr int kVdThreads = 1024;
+constexpr int kVdThreads = 512;
+constexpr int kVdAt = 4;           // loads of each row in flight per thread
+constexpr int kVdMaxCluster = 8;   // portable cluster size
 
 struct VdParams {
     const int32_t* draft;
@@ -24,77 +34,118 @@ struct VdParams {
     int B, m, V;
 };
 
-// A candidate as one comparable word: the score's bits (a non-negative float
-// orders as its bits), then the lower index first.  0: no candidate.
-__device__ __forceinline__ unsigned long long race_key(float r, float e, int v)
+__device__ __forceinline__ unsigned long long max64(unsigned long long a, unsigned long long b) { return a > b ? a : b; }
+
+// A candidate (r > 0) against the best so far, as one comparable word: the
+// score's bits (a non-negative float orders as its bits), then the lower index
+// first.  0: no candidate.  The exact quotient is formed only where the fast one
+// (off by 2 units in the last place; 0 for e above 2^126, and flushed where it is
+// not a normal number) does not rule it out.
+__device__ __forceinline__ void race(float r, float e, int v, unsigned long long& best)
 {
-    if (!(r > 0.f)) return 0ull;
+    if (!(r > 0.f)) return;
+    const float top = __uint_as_float(static_cast<uint32_t>(best >> 32));
+    if (top > 1.0e-30f && __fdividef(r, e) * 1.000002f < top && e < 8.0e37f) return;
     float s = __fdiv_rn(r, e);
     if (!(s > 0.f)) s = 0.f;  // underflowed, or not a clock: behind all others
-    return (static_cast<unsigned long long>(__float_as_uint(s)) << 32) | (0xffffffffu - static_cast<uint32_t>(v));
+    best = max64(best, (static_cast<unsigned long long>(__float_as_uint(s)) << 32) |
+                           (0xffffffffu - static_cast<uint32_t>(v)));
+}
+
+// The best candidate of the row p (or p - q) over the whole cluster, in every CTA.
+template <bool RESIDUAL>
+__device__ __forceinline__ unsigned long long race_row(const float* __restrict__ p, const float* __restrict__ q,
+                                                       const float* __restrict__ e, int v0, int v1,
+                                                       unsigned long long* sh, unsigned long long* sh_best)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    unsigned long long best = 0;
+    for (int v = v0 + tid; v < v1; v += kVdAt * kVdThreads) {
+        float pv[kVdAt], qv[kVdAt], ev[kVdAt];
+#pragma unroll
+        for (int k = 0; k < kVdAt; ++k) {
+            const int i = v + k * kVdThreads;
+            const bool in = i < v1;
+            pv[k] = in ? __ldcs(p + i) : 0.f;
+            qv[k] = RESIDUAL && in ? __ldcs(q + i) : 0.f;
+            ev[k] = in ? __ldcs(e + i) : 1.f;
+        }
+#pragma unroll
+        for (int k = 0; k < kVdAt; ++k)
+            race(RESIDUAL ? __fsub_rn(pv[k], qv[k]) : pv[k], ev[k], v + k * kVdThreads, best);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) best = max64(best, __shfl_xor_sync(0xffffffffu, best, o));
+    if (lane == 0) sh[warp] = best;
+    __syncthreads();
+    if (warp == 0) {
+        best = lane < kVdThreads / 32 ? sh[lane] : 0;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) best = max64(best, __shfl_xor_sync(0xffffffffu, best, o));
+        if (lane == 0) *sh_best = best;
+    }
+    cluster_sync();
+    best = 0;
+    const uint32_t n = cluster_size();
+    for (uint32_t c = 0; c < n; ++c) best = max64(best, cluster_read(sh_best, c));
+    return best;
 }
 
 __global__ void __launch_bounds__(kVdThreads) verify_kernel(VdParams p)
 {
-    __shared__ unsigned long long sh_best[2][32];
+    __shared__ unsigned long long sh[kVdThreads / 32], sh_best[2];
     __shared__ int sh_a;
-    const int b = blockIdx.x, tid = threadIdx.x;
+    const uint32_t cs = cluster_size(), rank = cluster_rank();
+    const int b = blockIdx.x / cs, tid = threadIdx.x;
     const int m = p.draft_len ? max(0, min(p.draft_len[b], p.m)) : p.m;
-    if (tid == 0) {
+    if (tid < 32) {  // drafts accepted before the first rejection, 32 at a time
         int a = 0;
-        for (; a < m; ++a) {
-            const int64_t row = static_cast<int64_t>(b) * p.m + a;
-            const int d = p.draft[row];
-            if (d < 0 || d >= p.V) break;
-            const float pd = p.p[(static_cast<int64_t>(b) * (p.m + 1) + a) * p.V + d];
-            const float qd = p.q[row * p.V + d];
-            if (!(pd > 0.f && __fmul_rn(p.u[row], qd) <= pd)) break;
+        for (int i0 = 0; i0 < m; i0 += 32) {
+            bool ok = false;
+            const int i = i0 + tid;
+            if (i < m) {
+                const int64_t row = static_cast<int64_t>(b) * p.m + i;
+                const int d = p.draft[row];
+                if (d >= 0 && d < p.V) {
+                    const float pd = p.p[(static_cast<int64_t>(b) * (p.m + 1) + i) * p.V + d];
+                    const float qd = p.q[row * p.V + d];
+                    ok = pd > 0.f && __fmul_rn(p.u[row], qd) <= pd;
+                }
+            }
+            const uint32_t bad = ~__ballot_sync(0xffffffffu, ok);
+            const int n = bad ? __ffs(bad) - 1 : 32;
+            a += n;
+            if (n < 32) break;
         }
-        sh_a = a;
+        if (tid == 0) sh_a = a;
     }
     __syncthreads();
     const int a = sh_a;
     const float* pr = p.p + (static_cast<int64_t>(b) * (p.m + 1) + a) * p.V;
-    const float* qr = a < m ? p.q + (static_cast<int64_t>(b) * p.m + a) * p.V : nullptr;
     const float* e = p.noise + static_cast<int64_t>(b) * p.V;
-    unsigned long long best = 0, best_p = 0;  // of the residual, and of p itself should the residual be empty
-    for (int v = tid; v < p.V; v += kVdThreads) {
-        const float pv = pr[v], ev = e[v];
-        const unsigned long long kp = race_key(pv, ev, v);
-        best_p = kp > best_p ? kp : best_p;
-        if (qr) {
-            const unsigned long long kr = race_key(__fsub_rn(pv, qr[v]), ev, v);
-            best = kr > best ? kr : best;
-        }
+    const int v0 = static_cast<int>(static_cast<int64_t>(p.V) * rank / cs);
+    const int v1 = static_cast<int>(static_cast<int64_t>(p.V) * (rank + 1) / cs);
+    unsigned long long best = 0;
+    if (a < m) best = race_row<true>(pr, p.q + (static_cast<int64_t>(b) * p.m + a) * p.V, e, v0, v1, sh, sh_best);
+    // no draft rejected, or (the same in every CTA) nothing left of p - q
+    if (best == 0) {
+        __syncthreads();
+        best = race_row<false>(pr, nullptr, e, v0, v1, sh, sh_best + 1);
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const unsigned long long x = __shfl_xor_sync(0xffffffffu, best, o), y = __shfl_xor_sync(0xffffffffu, best_p, o);
-        best = x > best ? x : best;
-        best_p = y > best_p ? y : best_p;
-    }
-    if ((tid & 31) == 0) {
-        sh_best[0][tid >> 5] = best;
-        sh_best[1][tid >> 5] = best_p;
-    }
-    __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < kVdThreads / 32; ++w) {
-            best = sh_best[0][w] > best ? sh_best[0][w] : best;
-            best_p = sh_best[1][w] > best_p ? sh_best[1][w] : best_p;
-        }
-        const unsigned long long k = best ? best : best_p;
-        p.n_accept[b] = a;
+    if (rank == 0) {
         int32_t* out = p.tokens + static_cast<int64_t>(b) * (p.m + 1);
-        for (int i = 0; i < a; ++i) out[i] = p.draft[static_cast<int64_t>(b) * p.m + i];
-        out[a] = k ? static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(k)) : 0;
-        for (int i = a + 1; i <= p.m; ++i) out[i] = -1;
+        for (int i = tid; i <= p.m; i += kVdThreads) {
+            const int32_t drawn = best ? static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(best)) : 0;
+            out[i] = i < a ? p.draft[static_cast<int64_t>(b) * p.m + i] : i == a ? drawn : -1;
+        }
+        if (tid == 0) p.n_accept[b] = a;
     }
+    cluster_sync();  // no CTA leaves while another may read its maximum
 }
 
 bool verify_sizes_ok(int B, int m, int V)
 {
-    return B >= 1 && m >= 0 && V >= 1 && static_cast<int64_t>(B) * (static_cast<int64_t>(m) + 1) <= (1ll << 24);
+    return B >= 1 && m >= 0 && V >= 1 && V <= (1 << 30) && static_cast<int64_t>(B) * (static_cast<int64_t>(m) + 1) <= (1ll << 24);
 }
 
 }  // namespace
@@ -114,6 +165,13 @@ extern "C" int logo_verify_draft(const int32_t* draft, const float* q_draft, con
     if (!workspace || workspace_bytes < logo_verify_draft_workspace_size(B, m, V) || !aligned16(workspace))
         return LOGO_ERR_WORKSPACE;
     VdParams p{draft, q_draft, p_target, u, noise, draft_len, tokens, n_accept, B, m, V};
-    verify_kernel<<<B, kVdThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
-    return cudaGetLastError() == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
+    // CTAs per sequence: up to four per SM in all, stretches of a few loads a thread at least
+    int cs = 1;
+    while (cs < kVdMaxCluster && static_cast<int64_t>(B) * cs * 2 <= 4ll * device_sm_count() &&
+           V / (cs * 2) >= 2 * kVdThreads)
+        cs *= 2;
+    cudaLaunchAttribute attr{};
+    const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(B) * cs, kVdThreads, cs, 0,
+                                                  static_cast<cudaStream_t>(stream), &attr);
+    return cudaLaunchKernelEx(&cfg, verify_kernel, p) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }
