@@ -3,9 +3,10 @@
 //
 // Every cache row of a (sequence, KV head) has a rank key: rows inside the
 // recent window above all others, then the order-preserving image of the fp32
-// weight; equal keys go to the lower row.  A radix select (8 bits a pass) finds
-// the key of the last row that stays and how many of the rows with that key do;
-// one ordered pass lists the holes (rows below `end` that go) and the movers
+// weight; equal keys go to the lower row.  A radix select (11, 11 and 10 bits a
+// pass; it ends as soon as all rows of a digit stay, which is after two passes
+// unless weights are equal or nearly so) finds the key of the last row that
+// stays and how many of the rows with that key do; one ordered pass lists the holes (rows below `end` that go) and the movers
 // (rows at or above `end` that stay) in rising order, and mover i is copied into
 // hole i.  No mover's row is any mover's destination, so the copies need no
 // order, and no fewer rows could be moved.
@@ -14,7 +15,9 @@
 // of its rows: keys are formed once and stay in shared memory, the passes'
 // histograms meet in distributed shared memory, and the same CTAs then move the
 // rows (HBM-bound: 4 D bytes a moved row of K and V, read and written), so that
-// the cut of a whole batch is one launch.
+// the cut of a whole batch is one launch.  The plan is bound by latency (barriers
+// and round trips), so a batch that fills the SMs with one CTA a (sequence, KV
+// head) does without clusters.
 #include <cuda_bf16.h>
 
 #include <cstdint>
@@ -31,6 +34,8 @@ constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvMaxCluster = 8;          // portable cluster size
 constexpr int kEvSmemKeys = 48 * 1024;    // keys of a CTA's stretch in shared memory; longer ones are formed anew each pass
 constexpr int kEvMovesAt = 4;             // moves in flight per warp
+constexpr int kEvBins = 2048;
+static_assert(kEvBins == 4 * kEvThreads, "a thread scans four digits");
 
 struct EvParams {
     logo_bf16 *k, *v;
@@ -52,16 +57,23 @@ __device__ __forceinline__ uint32_t evict_key(float mass, int pos, int first_rec
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(kEvThreads) evict_kernel(EvParams p)
+template <bool CLUSTER>
+__device__ __forceinline__ void evict_sync()
+{
+    if constexpr (CLUSTER) cluster_sync();
+    else __syncthreads();
+}
+
+template <bool IN_SMEM, bool CLUSTER>
+__global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(EvParams p)
 {
     extern __shared__ uint32_t sh_keys[];
-    __shared__ int hist[2][256];                    // this CTA's, two passes' worth (read by the cluster)
+    __shared__ __align__(16) int hist[2][kEvBins];  // this CTA's, two passes' worth (read by the cluster)
     __shared__ int sh_count[3];                     // ties, holes, movers of this CTA (read by the cluster)
     __shared__ int sh_warp[3][kEvWarps];            // ... of each warp
-    __shared__ int sh_lane[256];                    // the cluster's histogram
     __shared__ uint32_t sh_prefix;
     __shared__ int sh_need, sh_ties;
-    const uint32_t cs = cluster_size(), rank = cluster_rank();
+    const uint32_t cs = CLUSTER ? cluster_size() : 1, rank = CLUSTER ? cluster_rank() : 0;
     const int bh = blockIdx.x / cs, b = bh / p.Hkv, h = bh % p.Hkv;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int len = max(0, min(p.seq_len[b], p.L)), end = min(len, p.budget);
@@ -81,64 +93,80 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(EvParams p)
         return;
     }
     const int first_recent = p.n_seen[b] - p.recent;
-    const bool in_smem = per <= p.smem_keys;
-    for (int i = tid; i < 512; i += kEvThreads) hist[i >> 8][i & 255] = 0;
-    if (in_smem) {
-#pragma unroll 4
+#pragma unroll
+    for (int k = 0; k < 2; ++k) reinterpret_cast<int4*>(hist[k])[tid] = make_int4(0, 0, 0, 0);
+    if constexpr (IN_SMEM) {
+#pragma unroll 8
         for (int i = tid; i < cnt; i += kEvThreads) sh_keys[i] = evict_key(mass[s0 + i], pos[s0 + i], first_recent);
     }
     __syncthreads();
-    auto key_at = [&](int i) { return in_smem ? sh_keys[i] : evict_key(mass[s0 + i], pos[s0 + i], first_recent); };
+    auto key_at = [&](int i) { return IN_SMEM ? sh_keys[i] : evict_key(mass[s0 + i], pos[s0 + i], first_recent); };
 
     // ---- the key of the end-th largest, and how many rows with it stay
     uint32_t prefix = 0;
     int need = end, ties = 0;
-    for (int pass = 0; pass < 4; ++pass) {
-        const int shift = 24 - 8 * pass, buf = pass & 1;
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, buf = pass & 1;
+        const uint32_t mask = pass < 2 ? 2047u : 1023u;
+        const int above = pass == 0 ? 31 : pass == 1 ? 21 : 10;  // bits decided before (pass 0: none, and no key differs)
         for (int i0 = warp * 32; i0 < cnt; i0 += kEvThreads) {
             const int i = i0 + lane;
             const uint32_t k = i < cnt ? key_at(i) : 0u;
-            const bool in = i < cnt && (pass == 0 || (k ^ prefix) >> (shift + 8) == 0);
-            const int digit = (k >> shift) & 255u;
-            // lanes with the same digit count once
-            const uint32_t peers = __match_any_sync(0xffffffffu, in ? digit : 256);
-            if (in && lane == __ffs(peers) - 1) atomicAdd(&hist[buf][digit], __popc(peers));
-        }
-        cluster_sync();  // every CTA's histogram of this pass is complete
-        if (tid < 256) {
-            int sum = 0;
-            for (uint32_t r = 0; r < cs; ++r) sum += cluster_read(&hist[buf][tid], r);
-            sh_lane[tid] = sum;
-            hist[buf ^ 1][tid] = 0;  // the last pass's, read by all before the barrier
-        }
-        __syncthreads();
-        if (warp == 0) {  // lane l: digits 255 - 8 l down to 248 - 8 l
-            int own[8], sum = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += own[i] = sh_lane[255 - 8 * lane - i];
-            int incl = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += y;
+            const bool in = i < cnt && (pass == 0 || (k ^ prefix) >> above == 0);
+            const int digit = (k >> shift) & mask;
+            int same;
+            const uint32_t who = __match_all_sync(0xffffffffu, in ? digit : -1, &same);
+            if (same) {  // equal weights: count once
+                if (in && lane == 0) atomicAdd(&hist[buf][digit], __popc(who));
+            } else if (in) {
+                atomicAdd(&hist[buf][digit], 1);
             }
-            int before = incl - sum;  // rows with a larger digit
-            if (before < need && need <= incl) {
+        }
+        evict_sync<CLUSTER>();  // every CTA's histogram of this pass is complete
+        // thread t: digits 2047 - 4 t down to 2044 - 4 t
+        int own[4] = {0, 0, 0, 0};
+        const int at = kEvThreads - 1 - tid;
+        if constexpr (CLUSTER) {
+            int4 v[kEvMaxCluster];  // all reads in flight
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (before < need && need <= before + own[i]) {
-                        sh_prefix = prefix | static_cast<uint32_t>(255 - 8 * lane - i) << shift;
-                        sh_need = need - before;
-                        sh_ties = own[i];
-                    }
-                    before += own[i];
+            for (uint32_t r = 0; r < kEvMaxCluster; ++r)
+                v[r] = r < cs ? cluster_read4(&hist[buf][4 * at], r) : make_int4(0, 0, 0, 0);
+#pragma unroll
+            for (uint32_t r = 0; r < kEvMaxCluster; ++r)
+                own[0] += v[r].w, own[1] += v[r].z, own[2] += v[r].y, own[3] += v[r].x;
+        } else {
+            const int4 v = reinterpret_cast<const int4*>(hist[buf])[at];
+            own[0] = v.w, own[1] = v.z, own[2] = v.y, own[3] = v.x;
+        }
+        reinterpret_cast<int4*>(hist[buf ^ 1])[tid] = make_int4(0, 0, 0, 0);  // the last pass's, read by all by now
+        const int sum = own[0] + own[1] + own[2] + own[3];
+        int incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        if (lane == 31) sh_warp[0][warp] = incl;
+        __syncthreads();
+        int before = incl - sum;  // rows with a larger digit
+#pragma unroll
+        for (int k = 0; k < kEvWarps; ++k) before += k < warp ? sh_warp[0][k] : 0;
+        if (before < need && need <= before + sum) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (before < need && need <= before + own[i]) {
+                    sh_prefix = prefix | static_cast<uint32_t>(4 * at + 3 - i) << shift;
+                    sh_need = need - before;
+                    sh_ties = own[i];
                 }
+                before += own[i];
             }
         }
         __syncthreads();
         prefix = sh_prefix;
         need = sh_need;
         ties = sh_ties;
+        if (need == ties) break;  // all rows with this digit stay
     }
 
     // ---- ordered: a warp takes a stretch of 32-row groups
@@ -149,6 +177,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(EvParams p)
     // over the cluster; all threads
     auto first_of = [&](int i) {
         int mine = 0, total = 0;
+#pragma unroll
         for (int k = 0; k < kEvWarps; ++k) {
             mine += k < warp ? sh_warp[i][k] : 0;
             total += sh_warp[i][k];
@@ -157,11 +186,17 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(EvParams p)
         return mine;
     };
     auto over_cluster = [&](int i, int* all) {  // counts of the CTAs before this one; of all
-        int mine = 0, sum = 0;
-        for (uint32_t r = 0; r < cs; ++r) {
-            const int c = cluster_read(&sh_count[i], r);
-            mine += r < rank ? c : 0;
-            sum += c;
+        if constexpr (!CLUSTER) {
+            *all = sh_count[i];
+            return 0;
+        }
+        int c[kEvMaxCluster], mine = 0, sum = 0;
+#pragma unroll
+        for (uint32_t r = 0; r < kEvMaxCluster; ++r) c[r] = r < cs ? cluster_read(&sh_count[i], r) : 0;
+#pragma unroll
+        for (uint32_t r = 0; r < kEvMaxCluster; ++r) {
+            mine += r < rank ? c[r] : 0;
+            sum += c[r];
         }
         *all = sum;
         return mine;
@@ -175,13 +210,13 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(EvParams p)
         if (lane == 0) sh_warp[0][warp] = n;
         __syncthreads();
         tie0 = first_of(0);
-        cluster_sync();
+        evict_sync<CLUSTER>();
         tie0 += over_cluster(0, &all);
     }
     // does row i stay?  `t`: ties before this group, moved on
     auto keeps = [&](int i, int& t) {
         const uint32_t k = i < w1 ? key_at(i) : 0u;
-        if (all_ties) return i < w1 && k >= prefix;
+        if (all_ties) return i < w1 && k >= prefix;  // (prefix: the least key that stays, or a bound below it)
         const uint32_t eq = __ballot_sync(0xffffffffu, i < w1 && k == prefix);
         const bool keep = i < w1 && (k > prefix || (k == prefix && t + __popc(eq & below) < need));
         t += __popc(eq);
@@ -200,7 +235,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(EvParams p)
     }
     __syncthreads();
     int hole = first_of(1), move = first_of(2);
-    cluster_sync();
+    evict_sync<CLUSTER>();
     int holes;
     hole += over_cluster(1, &holes);
     move += over_cluster(2, &all);
@@ -221,7 +256,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(EvParams p)
         hole += __popc(bh_);
         move += __popc(bm);
     }
-    cluster_sync();  // the lists are written (and no CTA leaves while another reads its counts)
+    evict_sync<CLUSTER>();  // the lists are written (and no CTA leaves while another reads its counts)
 
     // ---- the moves: half a warp takes K, half V, a 16-byte chunk a lane (D = 64:
     //      two moves at once)
@@ -319,20 +354,19 @@ extern "C" int logo_cache_evict(logo_bf16* k_cache, logo_bf16* v_cache, const fl
     p.D = dims.D;
     p.budget = budget;
     p.recent = recent;
-    static bool attr_done = false;  // benign race: setting the attribute twice is harmless
-    if (!attr_done) {
-        if (set_smem_limit(evict_kernel, kEvSmemKeys * 4) != cudaSuccess) return LOGO_ERR_CUDA;
-        attr_done = true;
-    }
-    // CTAs per (sequence, KV head): up to four per SM in all, stretches of a row a
-    // thread at least
+    // CTAs per (sequence, KV head): up to two per SM in all (as many as are resident
+    // at once), stretches of a row a thread at least
     const int64_t pairs = static_cast<int64_t>(dims.B) * dims.Hkv;
     int cs = 1;
-    while (cs < kEvMaxCluster && pairs * cs * 2 <= 4ll * device_sm_count() && dims.T / (cs * 2) >= kEvThreads) cs *= 2;
+    while (cs < kEvMaxCluster && pairs * cs * 2 <= 2ll * device_sm_count() && dims.T / (cs * 2) >= kEvThreads) cs *= 2;
     const int per = (dims.T + cs - 1) / cs;
     p.smem_keys = per <= kEvSmemKeys ? per : 0;
+    auto kernel = p.smem_keys == 0 ? evict_kernel<false, true> : cs > 1 ? evict_kernel<true, true> : evict_kernel<true, false>;
+    if (p.smem_keys > 8000) {  // more than the default limit of dynamic shared memory allows
+        if (set_smem_limit(kernel, kEvSmemKeys * 4) != cudaSuccess) return LOGO_ERR_CUDA;
+    }
     cudaLaunchAttribute attr{};
     const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(pairs) * cs, kEvThreads, cs, p.smem_keys * 4,
                                                   static_cast<cudaStream_t>(stream), &attr);
-    return cudaLaunchKernelEx(&cfg, evict_kernel, p) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }

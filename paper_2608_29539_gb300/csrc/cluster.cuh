@@ -49,6 +49,16 @@ __device__ __forceinline__ int cluster_read(const int* p, uint32_t rank)
     return v;
 }
 
+__device__ __forceinline__ int4 cluster_read4(const int* p, uint32_t rank)
+{
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "r"(cluster_addr(p, rank))
+                 : "memory");
+    return v;
+}
+
 // Launch configuration of `blocks` CTAs in clusters of cs (attr: storage for the
 // attribute, which the configuration points to).
 inline cudaLaunchConfig_t cluster_config(unsigned blocks, unsigned threads, unsigned cs, size_t smem, cudaStream_t st,
@@ -63,7 +73,7 @@ inline cudaLaunchConfig_t cluster_config(unsigned blocks, unsigned threads, unsi
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cs > 1 ? 1 : 0;  // (a launch without attributes is cheaper for the host)
     return cfg;
 }
 

@@ -23,7 +23,7 @@ namespace logo {
 namespace {
 
 constexpr int kVdThreads = 512;
-constexpr int kVdAt = 4;           // loads of each row in flight per thread
+constexpr int kVdAt = 8;           // loads of each row in flight per thread
 constexpr int kVdMaxCluster = 8;   // portable cluster size
 
 struct VdParams {
@@ -85,13 +85,17 @@ __device__ __forceinline__ unsigned long long race_row(const float* __restrict__
         if (lane == 0) *sh_best = best;
     }
     cluster_sync();
-    best = 0;
     const uint32_t n = cluster_size();
-    for (uint32_t c = 0; c < n; ++c) best = max64(best, cluster_read(sh_best, c));
+    unsigned long long of[kVdMaxCluster];
+#pragma unroll
+    for (uint32_t c = 0; c < kVdMaxCluster; ++c) of[c] = c < n ? cluster_read(sh_best, c) : 0;
+    best = 0;
+#pragma unroll
+    for (uint32_t c = 0; c < kVdMaxCluster; ++c) best = max64(best, of[c]);
     return best;
 }
 
-__global__ void __launch_bounds__(kVdThreads) verify_kernel(VdParams p)
+__global__ void __launch_bounds__(kVdThreads, 2) verify_kernel(VdParams p)
 {
     __shared__ unsigned long long sh[kVdThreads / 32], sh_best[2];
     __shared__ int sh_a;
@@ -165,9 +169,10 @@ extern "C" int logo_verify_draft(const int32_t* draft, const float* q_draft, con
     if (!workspace || workspace_bytes < logo_verify_draft_workspace_size(B, m, V) || !aligned16(workspace))
         return LOGO_ERR_WORKSPACE;
     VdParams p{draft, q_draft, p_target, u, noise, draft_len, tokens, n_accept, B, m, V};
-    // CTAs per sequence: up to four per SM in all, stretches of a few loads a thread at least
+    // CTAs per sequence: up to two per SM in all (as many as are resident at once),
+    // stretches of a few loads a thread at least
     int cs = 1;
-    while (cs < kVdMaxCluster && static_cast<int64_t>(B) * cs * 2 <= 4ll * device_sm_count() &&
+    while (cs < kVdMaxCluster && static_cast<int64_t>(B) * cs * 2 <= 2ll * device_sm_count() &&
            V / (cs * 2) >= 2 * kVdThreads)
         cs *= 2;
     cudaLaunchAttribute attr{};

@@ -126,7 +126,8 @@ def _p(t):
 
 
 def _stream():
-    return _vp(torch.cuda.current_stream().cuda_stream)
+    # the raw handle of torch.cuda.current_stream() (0.1 us; the object costs 3)
+    return _vp(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
 def _call(name, *args):
@@ -142,7 +143,7 @@ def _need(t, dtype, name, shape=None):
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     return t
 
