@@ -24,8 +24,8 @@
 //   to the tcgen05 kernel of the prefill's global branch instead, in tiles of
 //   128 rows and shares of the prefix (pa_rows_kernel lays them out first, on
 //   the device as the count of rows is known only there).
-// pa_join_kernel: joins each (row, head)'s pieces.
-// pa_mass_kernel: adds up the weights exp(x - lse) of every own cache row from
+// pa_finish_kernel (or pa_join_kernel, then pa_mass_kernel): joins each (row,
+//   head)'s pieces, and adds up the weights exp(x - lse) of every own cache row from
 //   the logits that pa_rows_kernel wrote down (4 bytes a row and key, against
 //   4 D bytes of K and V a key for all rows; reading K again would cost half of
 //   the cache traffic).
@@ -791,47 +791,70 @@ struct PaParts {
     int n;
 };
 
+// What the parts are found by that does not depend on the row.
+struct PaPre {
+    PaRun run;    // of the prefix and KV head
+    int ns, nrt;  // wide prefix: shares, row tiles
+};
+
+__device__ __forceinline__ PaPre pa_pre(const PaParams& p, int kvh)
+{
+    return PaPre{p.P > 0 ? p.run_pre[kvh] : PaRun{0, 0}, p.wq ? p.wcount[2] : 0, p.wq ? p.wcount[3] : 0};
+}
+
+// Parts of packed row r, head g of KV head kvh: x[0] of the prefix, x[1] of the
+// cache of sequence b, whose first packed row is row0 (-1: no own key is seen).
+template <int D>
+__device__ __forceinline__ void pa_parts(const PaParams& p, const PaSched& s, const PaPre& pre, int r, int b, int row0,
+                                         int kvh, int g, PaParts (&x)[2])
+{
+    x[0] = x[1] = PaParts{nullptr, nullptr, nullptr, 0, 0, 0};
+    if (row0 >= 0) {
+        const int m = (r - row0) * p.G + g, id = (b * p.Hkv + kvh) * p.rt_own_max + m / kPaRows;
+        const PaRun run = p.run_own[id];
+        const int64_t at = static_cast<int64_t>(id + run.c0) * p.w_own + m % kPaRows;
+        x[1] = PaParts{p.ml_own + 2 * at, p.ml_own + 2 * at + 1, p.o_own + at * D, 2 * p.w_own,
+                       static_cast<int64_t>(p.w_own) * D, run.n};
+    }
+    if (s.wide) {
+        const int m = r * p.G + g;
+        const int64_t step = static_cast<int64_t>(pre.nrt) * p.Hkv * 128;
+        const int64_t at = (static_cast<int64_t>(m / 128) * p.Hkv + kvh) * 128 + m % 128;
+        x[0] = PaParts{p.wm_part + at, p.wl_part + at, p.wo_part + at * D, step, step * D, pre.ns};
+    } else if (s.K > 0) {
+        const int64_t at = static_cast<int64_t>(kvh + pre.run.c0) * p.w_pre + r * p.G + g;
+        x[0] = PaParts{p.ml_pre + 2 * at, p.ml_pre + 2 * at + 1, p.o_pre + at * D, 2 * p.w_pre,
+                       static_cast<int64_t>(p.w_pre) * D, pre.run.n};
+    }
+}
+
+// lse of a row in log2 units for the weights exp2(x - lse2): x = -inf where the
+// row sees nothing, and a row that sees no key at all gets weights 0.
+__device__ __forceinline__ float weight_lse2(float M, float Ls) { return M == -INFINITY ? INFINITY : M + log2f(Ls); }
+
 // WPR warps join the parts of one (row, head), CH parts at a time: their
 // statistics and O are loaded together and added up with a running maximum,
 // which saves a round trip to memory.
 template <int D, int WPR, int CH>
-__global__ void __launch_bounds__(256) pa_join_kernel(const __grid_constant__ PaParams p)
+__device__ __forceinline__ void pa_join(const PaParams& p, int block)
 {
     constexpr int E = D / 32, kWarps = 8;
-    __shared__ float sh_o[kWarps][D];
+    __shared__ float sh_o[WPR > 1 ? kWarps : 1][D];
     __shared__ float2 sh_ml[kWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % WPR;
-    const int task = blockIdx.x * (kWarps / WPR) + warp / WPR;
+    const int task = block * (kWarps / WPR) + warp / WPR;
     const int r = min(task / p.Hq, p.cap - 1), h = task % p.Hq, kvh = h / p.G, g = h % p.G;
     // loads that depend on nothing, together
     const PaSched s = *p.sched;
     const int2 row = p.rows[r];
-    const PaRun pre = p.P > 0 ? p.run_pre[kvh] : PaRun{0, 0};
-    const int ns = p.wq ? p.wcount[2] : 0, nrt = p.wq ? p.wcount[3] : 0;
+    const PaPre pre = pa_pre(p, kvh);
     const bool active = task / p.Hq < s.N;
     float acc[E], M = -INFINITY, Ls = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) acc[i] = 0.f;
     if (active) {
-        PaParts x[2];  // prefix, own cache
-        x[0] = x[1] = PaParts{nullptr, nullptr, nullptr, 0, 0, 0};
-        if (row.y >= 0) {
-            const int m = (r - row.y) * p.G + g, id = (row.x * p.Hkv + kvh) * p.rt_own_max + m / kPaRows;
-            const PaRun run = p.run_own[id];
-            const int64_t at = static_cast<int64_t>(id + run.c0) * p.w_own + m % kPaRows;
-            x[1] = PaParts{p.ml_own + 2 * at, p.ml_own + 2 * at + 1, p.o_own + at * D, 2 * p.w_own,
-                           static_cast<int64_t>(p.w_own) * D, run.n};
-        }
-        if (s.wide) {
-            const int m = r * p.G + g;
-            const int64_t step = static_cast<int64_t>(nrt) * p.Hkv * 128;
-            const int64_t at = (static_cast<int64_t>(m / 128) * p.Hkv + kvh) * 128 + m % 128;
-            x[0] = PaParts{p.wm_part + at, p.wl_part + at, p.wo_part + at * D, step, step * D, ns};
-        } else if (s.K > 0) {
-            const int64_t at = static_cast<int64_t>(kvh + pre.c0) * p.w_pre + r * p.G + g;
-            x[0] = PaParts{p.ml_pre + 2 * at, p.ml_pre + 2 * at + 1, p.o_pre + at * D, 2 * p.w_pre,
-                           static_cast<int64_t>(p.w_pre) * D, pre.n};
-        }
+        PaParts x[2];
+        pa_parts<D>(p, s, pre, r, row.x, row.y, kvh, g, x);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             for (int e0 = sub * CH; e0 < x[k].n; e0 += WPR * CH) {
@@ -902,28 +925,34 @@ __global__ void __launch_bounds__(256) pa_join_kernel(const __grid_constant__ Pa
 #pragma unroll
         for (int i = 0; i < E; i += 2) dst[i / 2] = cvt_bf16x2(acc[i] * inv, acc[i + 1] * inv);
         if (lane == 0) {
-            const float lse2 = M + log2f(Ls);  // -inf for a row without a key
-            if (p.lse) p.lse[static_cast<int64_t>(h) * p.cap + r] = lse2 * kLn2;
-            // the weights take exp2(x - lse2) with x = -inf where a row sees nothing
-            if (p.mass_out)
-                p.lse2[(static_cast<int64_t>(kvh) * p.cap + r) * p.G + g] = M == -INFINITY ? INFINITY : lse2;
+            if (p.lse) p.lse[static_cast<int64_t>(h) * p.cap + r] = (M + log2f(Ls)) * kLn2;  // -inf without a key
+            if (p.lse2) p.lse2[(static_cast<int64_t>(kvh) * p.cap + r) * p.G + g] = weight_lse2(M, Ls);
         }
     }
 }
 
 // ------------------------------------------------------------------ weights
-// A block: AT * 256 / lpk cache rows of one (sequence, KV head), AT a thread (or
+constexpr int kPaMassAt = 2;  // cache rows per thread
+
+// A block: 2 * 256 / lpk cache rows of one (sequence, KV head), two a thread (or
 // `lpk` threads, a power of two, each of which takes a share of the R logits of
 // a cache row, four floats at a time where R allows).  A cache row's logits lie
-// together, as do those of neighbouring rows.
-template <int AT, int VEC>
-__global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_constant__ PaParams p, int lpk)
+// together, as do those of neighbouring rows.  FUSED: the block forms the rows'
+// lse from their parts itself; else it reads what the join has left.
+template <int D, int VEC, bool FUSED>
+__device__ __forceinline__ void pa_mass(const PaParams& p, int block, int lpk, float* sh_lse2)
 {
-    extern __shared__ float sh_lse2[];
+    constexpr int AT = kPaMassAt;
     const int keys_at = kPaMassThreads / lpk, keys = AT * keys_at, chunks = (p.L + keys - 1) / keys;
-    const int bh = blockIdx.x / chunks, first = blockIdx.x % chunks * keys;
+    const int bh = block / chunks, first = block % chunks * keys;
     const int b = bh / p.Hkv, kvh = bh % p.Hkv, tid = threadIdx.x;
     const PaSeq q = p.seqs[b];
+    PaSched s{};
+    PaPre pre{};
+    if constexpr (FUSED) {
+        s = *p.sched;
+        pre = pa_pre(p, kvh);
+    }
     if (first >= q.len) return;
     const int nm = q.tiles > 0 ? q.n * p.G : 0;
     const int sub = tid % lpk, last = min(q.len, first + keys);
@@ -953,10 +982,34 @@ __global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_co
         const int key = first + i * keys_at + tid / lpk;
         old[i] = sub == 0 && key < min(last, q.len - p.n_new) ? p.mass_in[base + key] : 0.f;
     }
-    const float* l2 = p.lse2 + (static_cast<int64_t>(kvh) * p.cap + q.row0) * p.G;
-    // past nm: rows that were not selected, whose logits are not written (VEC rows
-    // at a time reach them)
-    for (int m = tid; m < nm + VEC - 1; m += kPaMassThreads) sh_lse2[m] = m < nm ? l2[m] : INFINITY;
+    if constexpr (FUSED) {
+        const int lane = tid & 31;
+        for (int m = tid >> 5; m < nm; m += kPaMassThreads / 32) {
+            PaParts part[2];
+            pa_parts<D>(p, s, pre, q.row0 + m / p.G, b, q.row0, kvh, m % p.G, part);
+            float M = -INFINITY, Ls = 0.f;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                for (int e = lane; e < part[k].n; e += 32) {
+                    const float vm = __ldg(part[k].m + e * part[k].s_ml), vl = __ldg(part[k].l + e * part[k].s_ml);
+                    if (vm == -INFINITY) continue;
+                    const float top = fmaxf(M, vm);
+                    Ls = Ls * ex2_approx(M - top) + vl * ex2_approx(vm - top);
+                    M = top;
+                }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) {
+                const float m2 = __shfl_xor_sync(0xffffffffu, M, o), l2 = __shfl_xor_sync(0xffffffffu, Ls, o);
+                const float top = fmaxf(M, m2);
+                if (top != -INFINITY) Ls = Ls * ex2_approx(M - top) + l2 * ex2_approx(m2 - top);
+                M = top;
+            }
+            if (lane == 0) sh_lse2[m] = weight_lse2(M, Ls);
+        }
+    } else {
+        const float* l2 = p.lse2 + (static_cast<int64_t>(kvh) * p.cap + q.row0) * p.G;
+        for (int m = tid; m < nm; m += kPaMassThreads) sh_lse2[m] = l2[m];
+    }
     __syncthreads();
     float add[AT];
 #pragma unroll
@@ -965,10 +1018,11 @@ __global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_co
         if (m > sub * VEC) load(m);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
+            if (m + e >= nm) break;  // rows that were not selected: no logits
             const float l = sh_lse2[m + e];
             // exp2f: no weight is flushed to zero
 #pragma unroll
-            for (int i = 0; i < AT; ++i) add[i] += m + e < nm ? exp2f(x[i][e] - l) : 0.f;
+            for (int i = 0; i < AT; ++i) add[i] += exp2f(x[i][e] - l);
         }
     }
 #pragma unroll
@@ -979,15 +1033,60 @@ __global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_co
     }
 }
 
-template <int AT, int VEC>
-int launch_mass(const PaParams& p, cudaStream_t st)
+// Up to kPaFusedR rows a (sequence, KV head), join and weights share a launch: a
+// block of the weights then forms its rows' lse from their parts itself, which
+// saves the launch between the two (57 us a call against 59 at 32 sequences, one
+// new token; 89 against 91 with 20 rows).  That work is done by every block, a
+// warp a row: with more than four rows a warp it takes longer than the launch.
+constexpr int kPaFusedR = 32;
+
+template <int D, int WPR, int CH, int VEC>
+__global__ void __launch_bounds__(256) pa_finish_kernel(const __grid_constant__ PaParams p, int join_blocks, int lpk)
 {
+    __shared__ float sh_lse2[kPaFusedR];
+    if (blockIdx.x < join_blocks) pa_join<D, WPR, CH>(p, blockIdx.x);
+    else pa_mass<D, VEC, true>(p, blockIdx.x - join_blocks, lpk, sh_lse2);
+}
+
+template <int D, int WPR, int CH>
+__global__ void __launch_bounds__(256) pa_join_kernel(const __grid_constant__ PaParams p)
+{
+    pa_join<D, WPR, CH>(p, blockIdx.x);
+}
+
+template <int VEC>
+__global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_constant__ PaParams p, int lpk)
+{
+    extern __shared__ float sh_dyn[];
+    pa_mass<128, VEC, false>(p, blockIdx.x, lpk, sh_dyn);  // (D does not enter without the parts)
+}
+
+// Join and weights.
+template <int D, int WPR, int CH>
+int launch_finish(PaParams& p, cudaStream_t st)
+{
+    const long long pairs = static_cast<long long>(p.cap) * p.Hq;
+    const int join = static_cast<int>((pairs + 8 / WPR - 1) / (8 / WPR));
+    if (!p.mass_out) {
+        p.lse2 = nullptr;
+        pa_join_kernel<D, WPR, CH><<<join, 256, 0, st>>>(p);
+        return LOGO_OK;
+    }
+    const int vec = p.R % 4 == 0 ? 4 : 1;
     int lpk = 1;  // four loads a thread at least, up to a warp for a cache row
-    while (lpk < 32 && 2 * lpk * VEC * 4 <= p.R) lpk *= 2;
-    const int keys = AT * kPaMassThreads / lpk;
-    const long long n = static_cast<long long>(p.B) * p.Hkv * ((p.L + keys - 1) / keys);
-    if (n > 0x7fffffffll) return LOGO_ERR_UNSUPPORTED;
-    pa_mass_kernel<AT, VEC><<<static_cast<unsigned>(n), kPaMassThreads, (p.R + VEC) * sizeof(float), st>>>(p, lpk);
+    while (lpk < 32 && 2 * lpk * vec * 4 <= p.R) lpk *= 2;
+    const int keys = kPaMassAt * kPaMassThreads / lpk;
+    const long long mass = static_cast<long long>(p.B) * p.Hkv * ((p.L + keys - 1) / keys);
+    if (join + mass > 0x7fffffffll) return LOGO_ERR_UNSUPPORTED;
+    if (p.R <= kPaFusedR) {
+        p.lse2 = nullptr;
+        auto kernel = vec == 4 ? pa_finish_kernel<D, WPR, CH, 4> : pa_finish_kernel<D, WPR, CH, 1>;
+        kernel<<<static_cast<unsigned>(join + mass), 256, 0, st>>>(p, join, lpk);
+    } else {
+        pa_join_kernel<D, WPR, CH><<<join, 256, 0, st>>>(p);
+        auto kernel = vec == 4 ? pa_mass_kernel<4> : pa_mass_kernel<1>;
+        kernel<<<static_cast<unsigned>(mass), kPaMassThreads, p.R * sizeof(float), st>>>(p, lpk);
+    }
     return LOGO_OK;
 }
 
@@ -1112,15 +1211,10 @@ int launch_prefix(PaParams& p, cudaStream_t st)
         const int rc = launch_tile_shares(t, D, st);
         if (rc != LOGO_OK) return rc;
     }
-    // few (row, head) pairs have many parts each: eight warps a pair then
-    const long long pairs = static_cast<long long>(p.cap) * p.Hq;
-    if (pairs < 2048) pa_join_kernel<D, 8, 4><<<static_cast<unsigned>(pairs), 256, 0, st>>>(p);
-    else pa_join_kernel<D, 1, 4><<<static_cast<unsigned>((pairs + 7) / 8), 256, 0, st>>>(p);
-    if (p.mass_out) {
-        const int rc = p.R % 4 == 0 ? (p.R <= 4 ? launch_mass<4, 4>(p, st) : launch_mass<2, 4>(p, st))
-                                    : launch_mass<4, 1>(p, st);
-        if (rc != LOGO_OK) return rc;
-    }
+    // few (row, head) pairs have many parts each: four warps a pair then (2048 pairs:
+    // 53.3 us a call against 55.3 with one; 5120: 94.3 against 88.9)
+    const int rc = static_cast<long long>(p.cap) * p.Hq <= 4096 ? launch_finish<D, 4, 4>(p, st) : launch_finish<D, 1, 4>(p, st);
+    if (rc != LOGO_OK) return rc;
     return cudaGetLastError() == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }
 
