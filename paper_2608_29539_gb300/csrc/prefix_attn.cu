@@ -18,8 +18,8 @@
 //   of Q, and eight do the products with warp-level MMA: decoding has a group's
 //   few heads per sequence as rows, mostly padding for a tcgen05 tile, and HBM
 //   bounds it (a tile's 64 KB take 2790 clocks at an SM's share of it).  Each
-//   warp takes its own 16 keys of every tile with its own running maximum and
-//   sum, so that none waits for another inside a piece.
+//   warp takes its own keys with its own running maximum and sum, so that none
+//   waits for another inside a piece.
 // More than 32 rows of the prefix per KV head are bound by the products and go
 //   to the tcgen05 kernel of the prefill's global branch instead, in tiles of
 //   128 rows and shares of the prefix (pa_rows_kernel lays them out first, on
@@ -113,8 +113,8 @@ struct PaParams {
     GlobalTile* wtiles;
     int32_t* wcount;  // tiles, next item, shares, row tiles
     float *wo_part, *wm_part, *wl_part;
-    float* logits;  // [B, Hkv, L, R] log2 units, R = n_new * G
-    int B, L, Hq, Hkv, G, n_new, P, cap, R, rt_own_max, w_pre, w_own, nCta;
+    float* logits;  // [B, Hkv, R, Lp] log2 units, R = n_new * G, Lp = L up to a multiple of 4
+    int B, L, Lp, Hq, Hkv, G, n_new, P, cap, R, rt_own_max, w_pre, w_own, nCta;
     int n_sm;
     float scale_log2;
 };
@@ -263,13 +263,16 @@ __device__ __forceinline__ bool products_sync_and(bool ok)
 
 __device__ __forceinline__ void products_sync() { asm volatile("barrier.cta.sync 1, 256;" ::: "memory"); }
 
-// One piece, by the eight warps.  Up to 16 rows: each warp takes 16 keys of
-// every tile.  Up to 32: four warps take rows 0 .. 15, four the others, each on
-// 32 keys in two steps (one code path for both: a second one, met by a few SMs
-// only, cost them 8 us of instruction fetches).  Fragments are fetched a batch
-// ahead of the products that use them (two warps a scheduler hide little).  Then
-// the warps' results are joined in shared memory.  Returns false, to all warps,
-// if a wait of any gave up.
+// One piece, by the eight warps in two groups of four, a warp taking 32 keys of a
+// tile.  More than 16 rows: each group takes 16 rows, of every tile.  Up to 16:
+// the groups take the tiles in turn.  Either way a warp has two independent
+// blocks of 16 keys in flight, and fetches fragments a batch ahead of the
+// products that use them, as two warps a scheduler hide little of each other's
+// latency; and there is one code path (a second one, met by a few SMs only, cost
+// them 8 us of instruction fetches).  16 sequences of up to 8192 keys, 8 KV heads,
+// 32 rows: 54.2 us a call, 271 MB at 74% of the measured HBM rate (56.1 with 16
+// keys after 16 keys).  Then the warps' results are joined in shared memory.
+// Returns false, to all warps, if a wait of any gave up.
 template <int D>
 __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, PaWarp& w, bool ok)
 {
@@ -277,8 +280,9 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
     constexpr int NT = D / 8, KS = D / 16;
     const int lane = w.lane, gid = lane >> 2, tig = lane & 3, mi = lane >> 3, rr = lane & 7;
     const bool with_logits = it.own && p.mass_out != nullptr;
-    const int steps = it.nrows <= 16 ? 1 : 2, group = kPaWarps / steps;  // warps that share the rows' keys
-    const int rg = w.warp / group, k0 = w.warp % group * 16 * steps;     // row group, first key of a tile
+    const bool split_rows = it.nrows > 16;
+    const int group = split_rows ? 4 : 8;  // warps that share the rows' keys
+    const int rg = split_rows ? w.warp >> 2 : 0, k0 = (w.warp & 3) * 32;  // row group, first key of a tile
     // this lane's rows: 16 rg + 8 i + gid
     int vis[2];
     float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f}, oc[NT][4];
@@ -301,159 +305,166 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
         const uint32_t sK = w.sRing + stK * C::kTileBytes, sV = w.sRing + stV * C::kTileBytes;
         ok = mbar_wait(w.kv_full + 8 * stK, fK & 1, w.abort_flag);
         if (!(ok = __all_sync(0xffffffffu, ok))) break;  // the warp leaves together
-#pragma unroll 1
-        for (int st = 0; st < steps; ++st) {
-            const int k1 = k0 + 16 * st;  // this step's first key of the tile
-            // ---- S = Q K^T over 16 keys (two 8-key halves); even and odd steps of
-            //      the head dimension add up apart
-            float sc[2][4];
-            {
-                float sa[2][2][4];
+        if (!split_rows && ((t - it.t0) & 1) != w.warp >> 2) {
+            // the other group's tile: released once it has landed (earlier, the
+            // release could fall into the stage's previous phase)
+            if (lane == 0) mbar_arrive(w.kv_empty + 8 * stK);
+            ok = mbar_wait(w.kv_full + 8 * stV, fV & 1, w.abort_flag);
+            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+            if (lane == 0) mbar_arrive(w.kv_empty + 8 * stV);
+            continue;
+        }
+        // ---- S = Q K^T over 2 x 16 keys (two 8-key halves each)
+        float sc[2][2][4];
 #pragma unroll
-                for (int h = 0; h < 4; ++h)
+        for (int st = 0; st < 2; ++st)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sa[h >> 1][h & 1][i] = 0.f;
-                uint32_t f[2][4][4];
-                auto fetch = [&](int bt) {
+            for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int ks = bt * 4 + i;
-                        uint32_t(&x)[4] = f[bt & 1][i];
-                        ldsm_x4(sK + (ks / 4) * C::kHalfBytes +
-                                    sw128_offset(k1 + (mi >> 1) * 8 + rr, (ks % 4) * 2 + (mi & 1)),
-                                x[0], x[1], x[2], x[3]);
-                    }
-                };
-                fetch(0);
-#pragma unroll
-                for (int bt = 0; bt < KS / 4; ++bt) {
-                    if (bt + 1 < KS / 4) fetch(bt + 1);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int ks = bt * 4 + i;
-                        const uint32_t(&x)[4] = f[bt & 1][i];
-                        mma_bf16_16816(sa[ks & 1][0], qa[ks], x[0], x[1]);
-                        mma_bf16_16816(sa[ks & 1][1], qa[ks], x[2], x[3]);
-                    }
-                }
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sc[nt][i] = sa[0][nt][i] + sa[1][nt][i];
-            }
-            if (st == steps - 1) {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(w.kv_empty + 8 * stK);
-            }
-            if (st == 0) {
-                ok = mbar_wait(w.kv_full + 8 * stV, fV & 1, w.abort_flag);
-                if (!(ok = __all_sync(0xffffffffu, ok))) break;
-                const int end = it.len - t * kPaTile;  // rows of the tile that hold a token
-                if (it.own && end < k0 + 16 * steps) {
-                    // a cache row past the length may hold anything: zero its V, so
-                    // that P = 0 keeps it out of the product
-                    for (int i = lane; i < 16 * steps * (D / 8); i += 32) {
-                        const int row = k0 + i / (D / 8), ch = i % (D / 8);
-                        if (row >= end)
-                            st_shared_v4(sV + (ch >> 3) * C::kHalfBytes + sw128_offset(row, ch & 7), 0u, 0u, 0u, 0u);
-                    }
-                    fence_proxy_async_smem();  // ordered before the stage's next TMA write
-                    __syncwarp();
-                }
-            }
-            // the first of V's fragments, in flight during the softmax
-            uint32_t f[2][4][4];
+                for (int i = 0; i < 4; ++i) sc[st][nt][i] = 0.f;
+        {
+            uint32_t f[2][4][4];  // a batch: two steps of the head dimension x two blocks of keys
             auto fetch = [&](int bt) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int col = (bt * 4 + i) * 16 + (mi >> 1) * 8;
+                    const int ks = bt * 2 + i / 2, st = i % 2;
                     uint32_t(&x)[4] = f[bt & 1][i];
-                    ldsm_x4_trans(sV + (col / 64) * C::kHalfBytes +
-                                      sw128_offset(k1 + (mi & 1) * 8 + rr, (col % 64) / 8),
-                                  x[0], x[1], x[2], x[3]);
+                    ldsm_x4(sK + (ks / 4) * C::kHalfBytes +
+                                sw128_offset(k0 + st * 16 + (mi >> 1) * 8 + rr, (ks % 4) * 2 + (mi & 1)),
+                            x[0], x[1], x[2], x[3]);
                 }
             };
             fetch(0);
-            // ---- online softmax; keys at and past `vis` are not seen (their K may be
-            //      anything, NaN included)
-            const int key0 = t * kPaTile + k1 + 2 * tig;
-            float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+            for (int bt = 0; bt < KS / 2; ++bt) {
+                if (bt + 1 < KS / 2) fetch(bt + 1);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = sc[nt][i] * p.scale_log2;
-                    sc[nt][i] = key0 + nt * 8 + (i & 1) < vis[i >> 1] ? x : -INFINITY;
-                    mx[i >> 1] = fmaxf(mx[i >> 1], sc[nt][i]);
-                }
-            if (with_logits) {
-                float* lg = p.logits + ((static_cast<int64_t>(it.b) * p.Hkv + it.kvh) * p.L + key0) * p.R + it.row0 +
-                            16 * rg + gid;
-                const bool r0 = 16 * rg + gid < it.nrows, r1 = 16 * rg + 8 + gid < it.nrows;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {  // key0 + off
-                    const int off = (k >> 1) * 8 + (k & 1);
-                    float* at = lg + static_cast<int64_t>(off) * p.R;
-                    if (key0 + off < it.len) {
-                        if (r0) at[0] = sc[k >> 1][k & 1];
-                        if (r1) at[8] = sc[k >> 1][2 + (k & 1)];
-                    }
-                }
-            }
-            bool grow = false;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
-                // O is rescaled only when the maximum has grown by more than 2^8: until
-                // then l and O hold values up to 2^8 times larger, which fp32 takes
-                // without loss (and bf16's P: its precision is relative)
-                grow |= mx[i] > m_run[i] + 8.0f;
-            }
-            if (__any_sync(0xffffffffu, grow)) {
-                float alpha[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    alpha[i] = 1.f;
-                    if (mx[i] > m_run[i] + 8.0f) {
-                        alpha[i] = ex2_approx(m_run[i] - mx[i]);  // 0 while nothing was seen
-                        m_run[i] = mx[i];
-                        l_run[i] *= alpha[i];
-                    }
-                }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    oc[nt][0] *= alpha[0];
-                    oc[nt][1] *= alpha[0];
-                    oc[nt][2] *= alpha[1];
-                    oc[nt][3] *= alpha[1];
-                }
-            }
-            const float m0 = m_run[0] == -INFINITY ? 0.f : m_run[0], m1 = m_run[1] == -INFINITY ? 0.f : m_run[1];
-#pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    sc[nt][i] = ex2_approx(sc[nt][i] - (i < 2 ? m0 : m1));
-                    l_run[i >> 1] += sc[nt][i];  // this lane's keys; the quad's are added at the end
-                }
-            // P as the A fragment: rows = rows, k = the 16 keys
-            const uint32_t pa[4] = {pack_bf16x2(sc[0][0], sc[0][1]), pack_bf16x2(sc[0][2], sc[0][3]),
-                                    pack_bf16x2(sc[1][0], sc[1][1]), pack_bf16x2(sc[1][2], sc[1][3])};
-            // ---- O += P V
-#pragma unroll
-            for (int bt = 0; bt < NT / 8; ++bt) {
-                if (bt + 1 < NT / 8) fetch(bt + 1);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int np = bt * 4 + i;
+                    const int ks = bt * 2 + i / 2, st = i % 2;
                     const uint32_t(&x)[4] = f[bt & 1][i];
-                    mma_bf16_16816(oc[2 * np], pa, x[0], x[1]);
-                    mma_bf16_16816(oc[2 * np + 1], pa, x[2], x[3]);
+                    mma_bf16_16816(sc[st][0], qa[ks], x[0], x[1]);
+                    mma_bf16_16816(sc[st][1], qa[ks], x[2], x[3]);
                 }
             }
         }
-        if (!ok) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(w.kv_empty + 8 * stK);
+        ok = mbar_wait(w.kv_full + 8 * stV, fV & 1, w.abort_flag);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        const int end = it.len - t * kPaTile;  // rows of the tile that hold a token
+        if (it.own && end < k0 + 32) {
+            // a cache row past the length may hold anything: zero its V, so that P = 0
+            // keeps it out of the product
+            for (int i = lane; i < 32 * (D / 8); i += 32) {
+                const int row = k0 + i / (D / 8), ch = i % (D / 8);
+                if (row >= end) st_shared_v4(sV + (ch >> 3) * C::kHalfBytes + sw128_offset(row, ch & 7), 0u, 0u, 0u, 0u);
+            }
+            fence_proxy_async_smem();  // ordered before the stage's next TMA write
+            __syncwarp();
+        }
+        // the first of V's fragments, in flight during the softmax
+        uint32_t f[2][4][4];  // a batch: two 16-column steps x two blocks of keys
+        auto fetch = [&](int bt) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int col = (bt * 2 + i / 2) * 16 + (mi >> 1) * 8, st = i % 2;
+                uint32_t(&x)[4] = f[bt & 1][i];
+                ldsm_x4_trans(sV + (col / 64) * C::kHalfBytes +
+                                  sw128_offset(k0 + st * 16 + (mi & 1) * 8 + rr, (col % 64) / 8),
+                              x[0], x[1], x[2], x[3]);
+            }
+        };
+        fetch(0);
+        // ---- online softmax; keys at and past `vis` are not seen (their K may be
+        //      anything, NaN included)
+        const int key0 = t * kPaTile + k0 + 2 * tig;
+        float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = sc[st][nt][i] * p.scale_log2;
+                    sc[st][nt][i] = key0 + st * 16 + nt * 8 + (i & 1) < vis[i >> 1] ? x : -INFINITY;
+                    mx[i >> 1] = fmaxf(mx[i >> 1], sc[st][nt][i]);
+                }
+        if (with_logits) {
+            // (a pair of keys at a time; the second may be the first past the length)
+            const int row = it.row0 + 16 * rg + gid;
+            float* lg = p.logits + ((static_cast<int64_t>(it.b) * p.Hkv + it.kvh) * p.R + row) * p.Lp + key0;
+            const bool r0 = 16 * rg + gid < it.nrows, r1 = 16 * rg + 8 + gid < it.nrows;
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) {
+                    const int off = st * 16 + nt * 8;
+                    if (key0 + off < it.len) {
+                        if (r0) *reinterpret_cast<float2*>(lg + off) = make_float2(sc[st][nt][0], sc[st][nt][1]);
+                        if (r1)
+                            *reinterpret_cast<float2*>(lg + 8 * static_cast<int64_t>(p.Lp) + off) =
+                                make_float2(sc[st][nt][2], sc[st][nt][3]);
+                    }
+                }
+        }
+        bool grow = false;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
+            mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
+            // O is rescaled only when the maximum has grown by more than 2^8: until
+            // then l and O hold values up to 2^8 times larger, which fp32 takes without
+            // loss (and bf16's P: its precision is relative)
+            grow |= mx[i] > m_run[i] + 8.0f;
+        }
+        if (__any_sync(0xffffffffu, grow)) {
+            float alpha[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                alpha[i] = 1.f;
+                if (mx[i] > m_run[i] + 8.0f) {
+                    alpha[i] = ex2_approx(m_run[i] - mx[i]);  // 0 while nothing was seen
+                    m_run[i] = mx[i];
+                    l_run[i] *= alpha[i];
+                }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                oc[nt][0] *= alpha[0];
+                oc[nt][1] *= alpha[0];
+                oc[nt][2] *= alpha[1];
+                oc[nt][3] *= alpha[1];
+            }
+        }
+        uint32_t pa[2][4];
+        const float m0 = m_run[0] == -INFINITY ? 0.f : m_run[0], m1 = m_run[1] == -INFINITY ? 0.f : m_run[1];
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sc[st][nt][i] = ex2_approx(sc[st][nt][i] - (i < 2 ? m0 : m1));
+                    l_run[i >> 1] += sc[st][nt][i];  // this lane's keys; the quad's are added at the end
+                }
+            // P as the A fragment: rows = rows, k = the 16 keys
+            pa[st][0] = pack_bf16x2(sc[st][0][0], sc[st][0][1]);
+            pa[st][1] = pack_bf16x2(sc[st][0][2], sc[st][0][3]);
+            pa[st][2] = pack_bf16x2(sc[st][1][0], sc[st][1][1]);
+            pa[st][3] = pack_bf16x2(sc[st][1][2], sc[st][1][3]);
+        }
+        // ---- O += P V
+#pragma unroll
+        for (int bt = 0; bt < NT / 4; ++bt) {
+            if (bt + 1 < NT / 4) fetch(bt + 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int np = bt * 2 + i / 2, st = i % 2;
+                const uint32_t(&x)[4] = f[bt & 1][i];
+                mma_bf16_16816(oc[2 * np], pa[st], x[0], x[1]);
+                mma_bf16_16816(oc[2 * np + 1], pa[st], x[2], x[3]);
+            }
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(w.kv_empty + 8 * stV);
     }
@@ -932,20 +943,21 @@ __device__ __forceinline__ void pa_join(const PaParams& p, int block)
 }
 
 // ------------------------------------------------------------------ weights
-constexpr int kPaMassAt = 2;  // cache rows per thread
-
-// A block: 2 * 256 / lpk cache rows of one (sequence, KV head), two a thread (or
-// `lpk` threads, a power of two, each of which takes a share of the R logits of
-// a cache row, four floats at a time where R allows).  A cache row's logits lie
-// together, as do those of neighbouring rows.  FUSED: the block forms the rows'
-// lse from their parts itself; else it reads what the join has left.
-template <int D, int VEC, bool FUSED>
-__device__ __forceinline__ void pa_mass(const PaParams& p, int block, int lpk, float* sh_lse2)
+// A block: one of the `chunks` equal shares of the cache rows of one (sequence,
+// KV head), 1024 / rs of them at a time: four a thread (a row's logits of
+// neighbouring keys lie together), by rs threads (a power of two), each of which
+// takes every rs-th of the R rows.  The logits come mostly from L2 and their
+// latency bounds the pass, so a thread has four 16-byte loads in flight, the
+// first of them during the statistics.  FUSED: the block forms the rows' lse from
+// their parts itself; else it reads what the join has left.
+template <int D, bool FUSED>
+__device__ __forceinline__ void pa_mass(const PaParams& p, int block, int chunks, int rs, float* sh_lse2)
 {
-    constexpr int AT = kPaMassAt;
-    const int keys_at = kPaMassThreads / lpk, keys = AT * keys_at, chunks = (p.L + keys - 1) / keys;
-    const int bh = block / chunks, first = block % chunks * keys;
-    const int b = bh / p.Hkv, kvh = bh % p.Hkv, tid = threadIdx.x;
+    constexpr int U = 4;  // rows in flight
+    __shared__ float4 sh_add[kPaMassThreads];
+    const int at = kPaMassThreads / rs, keys = 4 * at;
+    const int bh = block / chunks, ch = block % chunks;
+    const int b = bh / p.Hkv, kvh = bh % p.Hkv, tid = threadIdx.x, sub = tid / at;
     const PaSeq q = p.seqs[b];
     PaSched s{};
     PaPre pre{};
@@ -953,99 +965,113 @@ __device__ __forceinline__ void pa_mass(const PaParams& p, int block, int lpk, f
         s = *p.sched;
         pre = pa_pre(p, kvh);
     }
-    if (first >= q.len) return;
+    const int steps = (q.len + keys - 1) / keys;
+    const int k0 = static_cast<int>(static_cast<int64_t>(steps) * ch / chunks) * keys;
+    const int k1 = static_cast<int>(static_cast<int64_t>(steps) * (ch + 1) / chunks) * keys;
+    if (k0 >= k1) return;
     const int nm = q.tiles > 0 ? q.n * p.G : 0;
-    const int sub = tid % lpk, last = min(q.len, first + keys);
     const int n_keys = min(q.len, q.tiles * kPaTile);  // cache rows with logits
     const int64_t base = static_cast<int64_t>(bh) * p.L;
-    float x[AT][VEC], old[AT];
-    auto load = [&](int m) {
+    const float* lg = p.logits + static_cast<int64_t>(bh) * p.R * p.Lp;
+    float4 x[U];
+    auto load = [&](int key, int m0) {
 #pragma unroll
-        for (int i = 0; i < AT; ++i) {
-            const int key = first + i * keys_at + tid / lpk;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) x[i][e] = -INFINITY;
-            if (key < n_keys && m < nm) {
-                const float* src = p.logits + (base + key) * p.R + m;
-                if constexpr (VEC == 4) {
-                    const float4 v = __ldg(reinterpret_cast<const float4*>(src));
-                    x[i][0] = v.x, x[i][1] = v.y, x[i][2] = v.z, x[i][3] = v.w;
-                } else {
-                    x[i][0] = __ldg(src);
-                }
-            }
+        for (int u = 0; u < U; ++u) {
+            const int m = m0 + u * rs;
+            x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (key < n_keys && m < nm)
+                x[u] = __ldg(reinterpret_cast<const float4*>(lg + static_cast<int64_t>(m) * p.Lp + key));
         }
     };
-    load(sub * VEC);  // in flight beside the old weights and the rows' statistics
-#pragma unroll
-    for (int i = 0; i < AT; ++i) {
-        const int key = first + i * keys_at + tid / lpk;
-        old[i] = sub == 0 && key < min(last, q.len - p.n_new) ? p.mass_in[base + key] : 0.f;
-    }
+    int key = k0 + tid % at * 4;
+    load(key, sub);
     if constexpr (FUSED) {
-        const int lane = tid & 31;
-        for (int m = tid >> 5; m < nm; m += kPaMassThreads / 32) {
-            PaParts part[2];
-            pa_parts<D>(p, s, pre, q.row0 + m / p.G, b, q.row0, kvh, m % p.G, part);
+        // eight lanes a row
+        const int l8 = tid & 7;
+        for (int m0 = 0; m0 < nm; m0 += kPaMassThreads / 8) {
+            const int m = m0 + (tid >> 3);
             float M = -INFINITY, Ls = 0.f;
+            if (m < nm) {
+                PaParts part[2];
+                pa_parts<D>(p, s, pre, q.row0 + m / p.G, b, q.row0, kvh, m % p.G, part);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-                for (int e = lane; e < part[k].n; e += 32) {
-                    const float vm = __ldg(part[k].m + e * part[k].s_ml), vl = __ldg(part[k].l + e * part[k].s_ml);
-                    if (vm == -INFINITY) continue;
-                    const float top = fmaxf(M, vm);
-                    Ls = Ls * ex2_approx(M - top) + vl * ex2_approx(vm - top);
-                    M = top;
-                }
+                for (int k = 0; k < 2; ++k)
+                    for (int e = l8; e < part[k].n; e += 8) {
+                        const float vm = __ldg(part[k].m + e * part[k].s_ml), vl = __ldg(part[k].l + e * part[k].s_ml);
+                        if (vm == -INFINITY) continue;
+                        const float top = fmaxf(M, vm);
+                        Ls = Ls * ex2_approx(M - top) + vl * ex2_approx(vm - top);
+                        M = top;
+                    }
+            }
 #pragma unroll
-            for (int o = 16; o; o >>= 1) {
+            for (int o = 4; o; o >>= 1) {
                 const float m2 = __shfl_xor_sync(0xffffffffu, M, o), l2 = __shfl_xor_sync(0xffffffffu, Ls, o);
                 const float top = fmaxf(M, m2);
                 if (top != -INFINITY) Ls = Ls * ex2_approx(M - top) + l2 * ex2_approx(m2 - top);
                 M = top;
             }
-            if (lane == 0) sh_lse2[m] = weight_lse2(M, Ls);
+            if (m < nm && l8 == 0) sh_lse2[m] = weight_lse2(M, Ls);
         }
     } else {
         const float* l2 = p.lse2 + (static_cast<int64_t>(kvh) * p.cap + q.row0) * p.G;
         for (int m = tid; m < nm; m += kPaMassThreads) sh_lse2[m] = l2[m];
     }
     __syncthreads();
-    float add[AT];
+    for (int kb = k0;; key += keys) {
+        float old[4], add[4] = {0.f, 0.f, 0.f, 0.f};
+        if (sub == 0)
 #pragma unroll
-    for (int i = 0; i < AT; ++i) add[i] = 0.f;
-    for (int m = sub * VEC; m < nm; m += lpk * VEC) {
-        if (m > sub * VEC) load(m);
+            for (int e = 0; e < 4; ++e) old[e] = key + e < q.len - p.n_new ? p.mass_in[base + key + e] : 0.f;
+        for (int m0 = sub; m0 < nm; m0 += U * rs) {
+            if (m0 > sub) load(key, m0);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            if (m + e >= nm) break;  // rows that were not selected: no logits
-            const float l = sh_lse2[m + e];
-            // exp2f: no weight is flushed to zero
-#pragma unroll
-            for (int i = 0; i < AT; ++i) add[i] += exp2f(x[i][e] - l);
+            for (int u = 0; u < U; ++u) {
+                if (m0 + u * rs >= nm) break;
+                const float l = sh_lse2[m0 + u * rs];
+                // exp2f: no weight is flushed to zero
+                add[0] += exp2f(x[u].x - l);
+                add[1] += exp2f(x[u].y - l);
+                add[2] += exp2f(x[u].z - l);
+                add[3] += exp2f(x[u].w - l);
+            }
         }
-    }
+        kb += keys;
+        if (kb < k1) load(key + keys, sub);
+        if (rs > 1) {
+            sh_add[tid] = make_float4(add[0], add[1], add[2], add[3]);
+            __syncthreads();
+            if (sub == 0)
+                for (int k = 1; k < rs; ++k) {
+                    const float4 v = sh_add[k * at + tid];
+                    add[0] += v.x, add[1] += v.y, add[2] += v.z, add[3] += v.w;
+                }
+        }
+        if (sub == 0)
 #pragma unroll
-    for (int i = 0; i < AT; ++i) {
-        for (int o = lpk / 2; o; o >>= 1) add[i] += __shfl_xor_sync(0xffffffffu, add[i], o);
-        const int key = first + i * keys_at + tid / lpk;
-        if (sub == 0 && key < last) p.mass_out[base + key] = old[i] + add[i];
+            for (int e = 0; e < 4; ++e)
+                if (key + e < q.len) p.mass_out[base + key + e] = old[e] + (key + e < n_keys ? add[e] : 0.f);
+        if (kb >= k1) break;
+        if (rs > 1) __syncthreads();
     }
 }
 
 // Up to kPaFusedR rows a (sequence, KV head), join and weights share a launch: a
-// block of the weights then forms its rows' lse from their parts itself, which
-// saves the launch between the two (57 us a call against 59 at 32 sequences, one
-// new token; 89 against 91 with 20 rows).  That work is done by every block, a
-// warp a row: with more than four rows a warp it takes longer than the launch.
-constexpr int kPaFusedR = 32;
+// block of the weights then forms its rows' lse from their parts itself, eight
+// lanes a row, which saves the launch between the two (call times, fused against
+// not: 44.4 us against 50.8 at 40 rows, 4 sequences; 90.6 against 98.0 at 64 rows,
+// 16 sequences of 4096; 111.8 against 117.7 at 256 rows, 16 sequences of 2048).
+// Every block does that work: at 512 rows it costs more (96.4 us against 94.1).
+constexpr int kPaFusedR = 256;
 
-template <int D, int WPR, int CH, int VEC>
-__global__ void __launch_bounds__(256) pa_finish_kernel(const __grid_constant__ PaParams p, int join_blocks, int lpk)
+template <int D, int WPR, int CH>
+__global__ void __launch_bounds__(256, 4)
+    pa_finish_kernel(const __grid_constant__ PaParams p, int join_blocks, int chunks, int rs)
 {
     __shared__ float sh_lse2[kPaFusedR];
-    if (blockIdx.x < join_blocks) pa_join<D, WPR, CH>(p, blockIdx.x);
-    else pa_mass<D, VEC, true>(p, blockIdx.x - join_blocks, lpk, sh_lse2);
+    const int mass = gridDim.x - join_blocks;  // first, as they take longer
+    if (blockIdx.x >= mass) pa_join<D, WPR, CH>(p, blockIdx.x - mass);
+    else pa_mass<D, true>(p, blockIdx.x, chunks, rs, sh_lse2);
 }
 
 template <int D, int WPR, int CH>
@@ -1054,11 +1080,10 @@ __global__ void __launch_bounds__(256) pa_join_kernel(const __grid_constant__ Pa
     pa_join<D, WPR, CH>(p, blockIdx.x);
 }
 
-template <int VEC>
-__global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_constant__ PaParams p, int lpk)
+__global__ void __launch_bounds__(kPaMassThreads) pa_mass_kernel(const __grid_constant__ PaParams p, int chunks, int rs)
 {
     extern __shared__ float sh_dyn[];
-    pa_mass<128, VEC, false>(p, blockIdx.x, lpk, sh_dyn);  // (D does not enter without the parts)
+    pa_mass<128, false>(p, blockIdx.x, chunks, rs, sh_dyn);  // (D does not enter without the parts)
 }
 
 // Join and weights.
@@ -1072,20 +1097,20 @@ int launch_finish(PaParams& p, cudaStream_t st)
         pa_join_kernel<D, WPR, CH><<<join, 256, 0, st>>>(p);
         return LOGO_OK;
     }
-    const int vec = p.R % 4 == 0 ? 4 : 1;
-    int lpk = 1;  // four loads a thread at least, up to a warp for a cache row
-    while (lpk < 32 && 2 * lpk * vec * 4 <= p.R) lpk *= 2;
-    const int keys = kPaMassAt * kPaMassThreads / lpk;
-    const long long mass = static_cast<long long>(p.B) * p.Hkv * ((p.L + keys - 1) / keys);
+    int rs = 1;  // four rows a thread, while four threads suffice for that
+    while (rs < 4 && rs * 4 < p.R) rs *= 2;
+    const int keys = 4 * kPaMassThreads / rs;
+    const long long bh = static_cast<long long>(p.B) * p.Hkv;
+    // one wave of blocks, as their start and the statistics cost as much as a few steps
+    const int chunks = static_cast<int>(std::min<long long>((p.L + keys - 1) / keys, std::max(1ll, 4ll * p.n_sm / bh)));
+    const long long mass = bh * chunks;
     if (join + mass > 0x7fffffffll) return LOGO_ERR_UNSUPPORTED;
     if (p.R <= kPaFusedR) {
         p.lse2 = nullptr;
-        auto kernel = vec == 4 ? pa_finish_kernel<D, WPR, CH, 4> : pa_finish_kernel<D, WPR, CH, 1>;
-        kernel<<<static_cast<unsigned>(join + mass), 256, 0, st>>>(p, join, lpk);
+        pa_finish_kernel<D, WPR, CH><<<static_cast<unsigned>(join + mass), 256, 0, st>>>(p, join, chunks, rs);
     } else {
         pa_join_kernel<D, WPR, CH><<<join, 256, 0, st>>>(p);
-        auto kernel = vec == 4 ? pa_mass_kernel<4> : pa_mass_kernel<1>;
-        kernel<<<static_cast<unsigned>(mass), kPaMassThreads, p.R * sizeof(float), st>>>(p, lpk);
+        pa_mass_kernel<<<static_cast<unsigned>(mass), kPaMassThreads, p.R * sizeof(float), st>>>(p, chunks, rs);
     }
     return LOGO_OK;
 }
@@ -1114,7 +1139,7 @@ size_t prefix_layout(const logo_dims& d, int n_new, int P, bool with_mass, char*
     const int64_t tiles = d.Hkv * ((P + kPaTile - 1ll) / kPaTile) + d.B * d.Hkv * rt_own * ((d.T + kPaTile - 1) / kPaTile);
     const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>(tiles, device_sm_count()));
     const int64_t w_pre = std::min<int64_t>(kPaRows, cap * G), w_own = std::min<int64_t>(kPaRows, R);
-    const int64_t runs_own = d.B * d.Hkv * rt_own;
+    const int64_t runs_own = d.B * d.Hkv * rt_own, Lp = round_up(d.T, 4);
     const int64_t slots_pre = P > 0 ? d.Hkv + ctas : 0, slots_own = runs_own + ctas;
     const bool wide = P > 0 && cap * G > kPaRows;
     const int64_t w_rows = wide ? cap * G : 0, w_rt = (w_rows + 127) / 128;
@@ -1142,7 +1167,7 @@ size_t prefix_layout(const logo_dims& d, int n_new, int P, bool with_mass, char*
     char* wo_part = take(w_units * 128 * d.D * 4);
     char* wm_part = take(w_units * 128 * 4);
     char* wl_part = take(w_units * 128 * 4);
-    char* logits = take(with_mass ? static_cast<size_t>(d.B) * d.Hkv * d.T * R * 4 : 0);
+    char* logits = take(with_mass ? static_cast<size_t>(d.B) * d.Hkv * R * Lp * 4 : 0);
     if (p) {
         p->sched = reinterpret_cast<PaSched*>(sched);
         p->seqs = reinterpret_cast<PaSeq*>(seqs);
@@ -1164,6 +1189,7 @@ size_t prefix_layout(const logo_dims& d, int n_new, int P, bool with_mass, char*
         p->logits = reinterpret_cast<float*>(logits);
         p->B = d.B;
         p->L = d.T;
+        p->Lp = static_cast<int>(Lp);
         p->Hq = d.Hq;
         p->Hkv = d.Hkv;
         p->G = static_cast<int>(G);
