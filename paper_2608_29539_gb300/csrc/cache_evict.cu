@@ -6,20 +6,23 @@
 // weight; equal keys go to the lower row.  A radix select (11, 11 and 10 bits a
 // pass; it ends as soon as all rows of a digit stay, which is after two passes
 // unless weights are equal or nearly so) finds the key of the last row that
-// stays and how many of the rows with that key do; one ordered pass lists the holes (rows below `end` that go) and the movers
-// (rows at or above `end` that stay) in rising order, and mover i is copied into
-// hole i.  No mover's row is any mover's destination, so the copies need no
-// order, and no fewer rows could be moved.
+// stays and how many of the rows with that key do; one ordered pass lists the
+// holes (rows below `end` that go) and the movers (rows at or above `end` that
+// stay) in rising order, and mover i is copied into hole i.  No mover's row is any
+// mover's destination, so the copies need no order, and no fewer rows could be
+// moved.
 //
-// A thread-block cluster takes a (sequence, KV head), each CTA an equal stretch
-// of its rows: keys are formed once and stay in shared memory, the passes'
+// A CTA or a thread-block cluster takes a (sequence, KV head), each CTA an equal
+// stretch of its rows: keys are formed once and stay in shared memory, the passes'
 // histograms meet in distributed shared memory, and the same CTAs then move the
-// rows (HBM-bound: 4 D bytes a moved row of K and V, read and written), so that
-// the cut of a whole batch is one launch.  The plan is bound by latency (barriers
-// and round trips), so a batch that fills the SMs with one CTA a (sequence, KV
-// head) does without clusters.
+// rows (4 D bytes a moved row of K and V, read and written), so that the cut of a
+// whole batch is one launch.  The plan is bound by latency (barriers and round
+// trips): 64 pairs of 16384 rows cut to 2048 plan for 20 us, in which HBM idles,
+// and move 102 MB in 17, at 6.2 TB/s; 256 pairs of 2056 rows cut to 2048 plan for
+// 11 us and hardly move.
 #include <cuda_bf16.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "cluster.cuh"
@@ -33,7 +36,7 @@ constexpr int kEvThreads = 512;
 constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvMaxCluster = 8;          // portable cluster size
 constexpr int kEvSmemKeys = 48 * 1024;    // keys of a CTA's stretch in shared memory; longer ones are formed anew each pass
-constexpr int kEvMovesAt = 4;             // moves in flight per warp
+constexpr int kEvMovesAt = 3;             // moves in flight per warp
 constexpr int kEvBins = 2048;
 static_assert(kEvBins == 4 * kEvThreads, "a thread scans four digits");
 
@@ -109,6 +112,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(EvParams p)
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, buf = pass & 1;
         const uint32_t mask = pass < 2 ? 2047u : 1023u;
         const int above = pass == 0 ? 31 : pass == 1 ? 21 : 10;  // bits decided before (pass 0: none, and no key differs)
+#pragma unroll 4
         for (int i0 = warp * 32; i0 < cnt; i0 += kEvThreads) {
             const int i = i0 + lane;
             const uint32_t k = i < cnt ? key_at(i) : 0u;
@@ -223,6 +227,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(EvParams p)
         return keep;
     };
     int n_hole = 0, n_move = 0, t = tie0;
+#pragma unroll 4
     for (int i0 = w0; i0 < w1; i0 += 32) {
         const int i = i0 + lane;
         const bool keep = keeps(i, t);
@@ -242,6 +247,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(EvParams p)
     int32_t* lists = p.lists + base;
     const bool copies = p.mass_out != p.mass || p.pos_out != p.slot_pos;
     t = tie0;
+#pragma unroll 4
     for (int i0 = w0; i0 < w1; i0 += 32) {
         const int i = i0 + lane, s = s0 + i;
         const bool keep = keeps(i, t);
@@ -265,36 +271,36 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(EvParams p)
     uint4* rows = reinterpret_cast<uint4*>(half ? p.v : p.k);
     const int64_t row0 = (static_cast<int64_t>(b) * p.L * p.Hkv + h) * chunks + ch;
     const int64_t step = static_cast<int64_t>(p.Hkv) * chunks;
-    const int n_warps = static_cast<int>(cs) * kEvWarps;
-    for (int i0 = (static_cast<int>(rank) * kEvWarps + warp) * per_warp; i0 < holes;
-         i0 += n_warps * per_warp * kEvMovesAt) {
-        int dst[kEvMovesAt], src[kEvMovesAt];
-        uint4 v[kEvMovesAt];
-        float m[kEvMovesAt];
-        int q[kEvMovesAt];
-#pragma unroll
-        for (int j = 0; j < kEvMovesAt; ++j) {
-            const int i = i0 + j * n_warps * per_warp + sub;
-            dst[j] = i < holes ? lists[i] : -1;
-            src[j] = i < holes ? lists[p.L - 1 - i] : 0;
+    // an equal stretch of the lists a warp, 32 moves at a time: a lane looks one up
+    // and moves its weight and position, then all lanes move the rows
+    const int n_warps = static_cast<int>(cs) * kEvWarps, w_all = static_cast<int>(rank) * kEvWarps + warp;
+    const int m0 = static_cast<int>(static_cast<int64_t>(holes) * w_all / n_warps);
+    const int m1 = static_cast<int>(static_cast<int64_t>(holes) * (w_all + 1) / n_warps);
+    for (int c0 = m0; c0 < m1; c0 += 32) {
+        const int n = min(32, m1 - c0);
+        const int to = lane < n ? lists[c0 + lane] : 0, from = lane < n ? lists[p.L - 1 - (c0 + lane)] : 0;
+        float m = 0.f;
+        int q = 0;
+        if (lane < n) {
+            m = mass[from];
+            q = pos[from];
         }
+        for (int r = 0; r < n; r += kEvMovesAt * per_warp) {
+            uint4 v[kEvMovesAt];
 #pragma unroll
-        for (int j = 0; j < kEvMovesAt; ++j) {
-            if (dst[j] < 0) continue;
-            v[j] = rows[row0 + src[j] * step];
-            if (half == 0 && ch == 0) {
-                m[j] = mass[src[j]];
-                q[j] = pos[src[j]];
+            for (int j = 0; j < kEvMovesAt; ++j) {
+                const int i = r + j * per_warp + sub, src = __shfl_sync(0xffffffffu, from, i & 31);
+                if (i < n) v[j] = rows[row0 + src * step];
+            }
+#pragma unroll
+            for (int j = 0; j < kEvMovesAt; ++j) {
+                const int i = r + j * per_warp + sub, dst = __shfl_sync(0xffffffffu, to, i & 31);
+                if (i < n) rows[row0 + dst * step] = v[j];
             }
         }
-#pragma unroll
-        for (int j = 0; j < kEvMovesAt; ++j) {
-            if (dst[j] < 0) continue;
-            rows[row0 + dst[j] * step] = v[j];
-            if (half == 0 && ch == 0) {
-                p.mass_out[base + dst[j]] = m[j];
-                p.pos_out[base + dst[j]] = q[j];
-            }
+        if (lane < n) {
+            p.mass_out[base + to] = m;
+            p.pos_out[base + to] = q;
         }
     }
 }
@@ -306,6 +312,33 @@ int check_evict(const logo_dims& d)
     if (static_cast<int64_t>(d.B) * d.T > (1ll << 30)) return LOGO_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(d.B) * d.Hkv > (1ll << 24)) return LOGO_ERR_UNSUPPORTED;
     return LOGO_OK;
+}
+
+// CTAs per (sequence, KV head), up to nearly two per SM in all (as many as are
+// resident at once): the least of what the barriers and exchanges of a cluster cost, more where
+// SMs hold two CTAs, plus a CTA's share of the rows to rank and to move, in units
+// of a row to rank (1.2 ns; moving one of D = 128 takes as long as ranking four).
+// Measured with 1 / 2 / 4 / 8 CTAs a pair (us): 16 pairs of 2100 rows, 2000 stay
+// 8.7 / 11.0 / 10.4 / 11.9; of 3000, 1500 stay 16.9 / 14.6 / 12.5 / 13.0; 4 pairs of
+// 16384, 12000 stay 65 / 38 / 24 / 19; 40 pairs of 6000, 5800 stay 14.7 / 14.8 / 16.1
+// / 32; 64 pairs of 16384, 2048 stay 82 / 52 / 42 / 66.
+int evict_ctas(int64_t pairs, const logo_dims& d, int budget)
+{
+    constexpr int64_t kCost[] = {0, 3500, 2600, 4400}, kCrowd[] = {0, 1500, 3300, 2200};
+    const int64_t sms = device_sm_count();
+    const int64_t work = d.T + d.D / 32ll * std::max(0, std::min(budget, d.T - budget));
+    int best = 1;
+    int64_t least = work;
+    // (clusters do not fill the last places of a group of SMs: 76 of four CTAs take 38 us
+    // where 72 take 26)
+    for (int k = 1; 1 << k <= kEvMaxCluster && (pairs << k) * 20 <= 2 * sms * 19; ++k) {
+        const int64_t cost = kCost[k] + (pairs << k > sms ? kCrowd[k] : 0) + (work >> k);
+        if (cost < least) {
+            least = cost;
+            best = 1 << k;
+        }
+    }
+    return best;
 }
 
 size_t evict_ws_bytes(const logo_dims& d)
@@ -354,11 +387,8 @@ extern "C" int logo_cache_evict(logo_bf16* k_cache, logo_bf16* v_cache, const fl
     p.D = dims.D;
     p.budget = budget;
     p.recent = recent;
-    // CTAs per (sequence, KV head): up to two per SM in all (as many as are resident
-    // at once), stretches of a row a thread at least
     const int64_t pairs = static_cast<int64_t>(dims.B) * dims.Hkv;
-    int cs = 1;
-    while (cs < kEvMaxCluster && pairs * cs * 2 <= 2ll * device_sm_count() && dims.T / (cs * 2) >= kEvThreads) cs *= 2;
+    const int cs = evict_ctas(pairs, dims, budget);
     const int per = (dims.T + cs - 1) / cs;
     p.smem_keys = per <= kEvSmemKeys ? per : 0;
     auto kernel = p.smem_keys == 0 ? evict_kernel<false, true> : cs > 1 ? evict_kernel<true, true> : evict_kernel<true, false>;

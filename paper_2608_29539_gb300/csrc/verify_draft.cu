@@ -171,10 +171,9 @@ extern "C" int logo_verify_draft(const int32_t* draft, const float* q_draft, con
     VdParams p{draft, q_draft, p_target, u, noise, draft_len, tokens, n_accept, B, m, V};
     // CTAs per sequence: up to two per SM in all (as many as are resident at once),
     // stretches of a few loads a thread at least
+    const int64_t resident = 2ll * device_sm_count();
     int cs = 1;
-    while (cs < kVdMaxCluster && static_cast<int64_t>(B) * cs * 2 <= 2ll * device_sm_count() &&
-           V / (cs * 2) >= 2 * kVdThreads)
-        cs *= 2;
+    while (cs < kVdMaxCluster && static_cast<int64_t>(B) * cs * 2 <= resident && V / (cs * 2) >= 2 * kVdThreads) cs *= 2;
     cudaLaunchAttribute attr{};
     const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(B) * cs, kVdThreads, cs, 0,
                                                   static_cast<cudaStream_t>(stream), &attr);

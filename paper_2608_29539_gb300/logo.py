@@ -51,6 +51,7 @@ class Dims(ctypes.Structure):
 
 
 _lib = None
+_fns = {}  # name -> its function in the loaded library
 
 _SIGS = {
     "logo_get_device_status": (_c_int, [ctypes.POINTER(_c_int)]),
@@ -117,6 +118,7 @@ def lib():
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args
+            _fns[name] = fn
         _lib = L
     return _lib
 
@@ -127,23 +129,29 @@ def _p(t):
 
 def _stream():
     # the raw handle of torch.cuda.current_stream() (0.1 us; the object costs 3)
-    return _vp(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _call(name, *args):
-    rc = getattr(lib(), name)(*args)
+    fn = _fns.get(name)
+    rc = fn(*args) if fn is not None else getattr(lib(), name)(*args)
     if rc != LOGO_OK:
         raise LogoError(name, rc)
 
 
 def _need(t, dtype, name, shape=None):
+    try:  # one pass over what has to hold; what does not is named below
+        if t.dtype is dtype and t.is_cuda and t.is_contiguous() and (shape is None or t.shape == shape):
+            return t
+    except AttributeError:
+        pass
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if shape is not None and t.shape != shape and tuple(t.shape) != tuple(shape):
+    if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     return t
 

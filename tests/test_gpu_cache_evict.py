@@ -70,6 +70,17 @@ def test_long_caches(B, H, L, budget):
     _run(B, H, 64, L, [L] * B, budget, 200, mass, slot_pos, n_seen)
 
 
+# one CTA, clusters of two, four and eight per (sequence, KV head); the first sequences shorter than one CTA's stretch
+@pytest.mark.parametrize("B,H,L,budget", [(40, 2, 1500, 700), (40, 2, 6000, 3000), (5, 2, 6000, 3000),
+                                          (5, 1, 20000, 9000)])
+def test_few_different_weights_in_many_ctas(B, H, L, budget):
+    g = torch.Generator().manual_seed(B + L)
+    lens = ([budget + 1, 0, budget + 40, L - 1] + [L] * B)[:B]
+    slot_pos, n_seen = _positions(B, H, L, lens, g, False)
+    mass = torch.randint(0, 5, (B, H, L), generator=g).float()
+    _run(B, H, 64, L, lens, budget, 100, mass, slot_pos, n_seen)
+
+
 def test_equal_weights_go_to_the_lower_row():
     B, H, L, budget = 2, 2, 3000, 1111
     g = torch.Generator().manual_seed(2)
