@@ -20,10 +20,10 @@
 //   bounds it (a tile's 64 KB take 2790 clocks at an SM's share of it).  Each
 //   warp takes its own keys with its own running maximum and sum, so that none
 //   waits for another inside a piece.
-// More than 32 rows of the prefix per KV head are bound by the products and go
-//   to the tcgen05 kernel of the prefill's global branch instead, in tiles of
-//   128 rows and shares of the prefix (pa_rows_kernel lays them out first, on
-//   the device as the count of rows is known only there).
+// Many rows of a long prefix per KV head are bound by the products and go to the
+//   tcgen05 kernel of the prefill's global branch instead ("wide" below), in tiles
+//   of 128 rows and shares of the prefix (pa_rows_kernel lays them out first, on the
+//   device as the count of rows is known only there).
 // pa_finish_kernel (or pa_join_kernel, then pa_mass_kernel): joins each (row,
 //   head)'s pieces, and adds up the weights exp(x - lse) of every own cache row from
 //   the logits that pa_rows_kernel wrote down (4 bytes a row and key, against
@@ -48,9 +48,17 @@ constexpr int kPaThreads = 384;  // three warpgroups, for the register split
 constexpr uint32_t kPaRegsRows = 184, kPaRegsLoad = 136;
 static_assert(128 * (2 * kPaRegsRows + kPaRegsLoad) <= kPaThreads * 168, "register split exceeds the launch allocation");
 constexpr int kPaTile = 128;         // keys per tile
+constexpr int kPaBox = 32;           // rows of an own cache that a copy brings: a warp's keys of a tile
 constexpr int kPaRows = 32;          // rows of a piece at most
 constexpr int kPaWideUnits = 1216;   // (row tile, share, KV head) units that the wide prefix is cut into, or one share
 constexpr int kPaMassThreads = 256;
+// A prefix is read again for each 32 rows by pa_rows_kernel up to this many units
+// (see PaSched) an SM, as counted at run time, and the tcgen05 kernel is not
+// launched where no selection can pass the second number.  Call times, read again
+// against tcgen05: 22 row tiles, 4 KV heads, 2 keys 41.6 us, 56.9; 16 and 16 and 500
+// keys (8 units) 50.3, 63.7; 6 row tiles, 6307 keys (2 units of at most 9) 21.8, 33.3;
+// 6 row tiles, 4 KV heads, 8000 keys (10 units of at most 17) 33.1, 31.0.
+constexpr int kPaNarrow = 8, kPaNarrowCap = 12;
 constexpr int kPaMaxR = 8192;        // n_new * (Hq / Hkv) at most (the weights' row statistics in shared memory)
 
 template <int D>
@@ -76,7 +84,7 @@ struct PaCfg {
 struct PaSched {
     int K;      // length of the prefix part; 0 if there is none, or if it is wide
     int total;  // length of the line
-    int N, PT, n, wide;
+    int N, PT, n, wide, rt_pre;  // rt_pre: row tiles of a prefix that is not wide
 };
 
 // What the join and the weights need to know of a sequence.
@@ -103,7 +111,7 @@ struct PaParams {
     PaSched* sched;
     PaSeq* seqs;               // [B]
     int2* rows;                // [cap]: sequence of each packed row, first packed row of that sequence (-1: none of its keys are seen)
-    PaRun *run_pre, *run_own;  // [Hkv], [B][Hkv][rt_own_max]
+    PaRun *run_pre, *run_own;  // [Hkv][rt_pre], [B][Hkv][rt_own_max]
     float *o_pre, *ml_pre;     // prefix pieces: [slot][w_pre][D], [slot][w_pre][2]
     float *o_own, *ml_own;
     float* lse2;               // [Hkv][cap * G] log2 units; +infinity for a row without a key
@@ -115,7 +123,7 @@ struct PaParams {
     float *wo_part, *wm_part, *wl_part;
     float* logits;  // [B, Hkv, R, Lp] log2 units, R = n_new * G, Lp = L up to a multiple of 4
     int B, L, Lp, Hq, Hkv, G, n_new, P, cap, R, rt_own_max, w_pre, w_own, nCta;
-    int n_sm;
+    int n_sm, rt_narrow;  // rt_narrow: row tiles of the prefix up to which it is not wide
     float scale_log2;
 };
 
@@ -190,9 +198,9 @@ struct PaIter {
                 first = k * (COST + tiles);
                 it->own = 0;
                 it->b = 0;
-                it->kvh = k;
-                it->row0 = 0;
-                it->nrows = s.N * p.G;
+                it->kvh = k / s.rt_pre;
+                it->row0 = k % s.rt_pre * kPaRows;
+                it->nrows = min(kPaRows, s.N * p.G - it->row0);
                 it->seg_row0 = 0;
                 it->len = p.P;
                 it->slot = k + c;
@@ -305,9 +313,10 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
         const uint32_t sK = w.sRing + stK * C::kTileBytes, sV = w.sRing + stV * C::kTileBytes;
         ok = mbar_wait(w.kv_full + 8 * stK, fK & 1, w.abort_flag);
         if (!(ok = __all_sync(0xffffffffu, ok))) break;  // the warp leaves together
-        if (!split_rows && ((t - it.t0) & 1) != w.warp >> 2) {
-            // the other group's tile: released once it has landed (earlier, the
-            // release could fall into the stage's previous phase)
+        const int end = it.len - t * kPaTile;  // rows of the tile that hold a token
+        if ((!split_rows && ((t - it.t0) & 1) != w.warp >> 2) || end <= k0) {
+            // the other group's tile, or no keys for this warp: released once it has
+            // landed (earlier, the release could fall into the stage's previous phase)
             if (lane == 0) mbar_arrive(w.kv_empty + 8 * stK);
             ok = mbar_wait(w.kv_full + 8 * stV, fV & 1, w.abort_flag);
             if (!(ok = __all_sync(0xffffffffu, ok))) break;
@@ -351,7 +360,6 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
         if (lane == 0) mbar_arrive(w.kv_empty + 8 * stK);
         ok = mbar_wait(w.kv_full + 8 * stV, fV & 1, w.abort_flag);
         if (!(ok = __all_sync(0xffffffffu, ok))) break;
-        const int end = it.len - t * kPaTile;  // rows of the tile that hold a token
         if (it.own && end < k0 + 32) {
             // a cache row past the length may hold anything: zero its V, so that P = 0
             // keeps it out of the product
@@ -629,8 +637,9 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     PaSched s;
     s.N = N;
     s.PT = (p.P + kPaTile - 1) / kPaTile;
-    s.wide = p.P > 0 && N * p.G > kPaRows;
-    s.K = N > 0 && p.P > 0 && !s.wide ? p.Hkv * (C::kRunCost + s.PT) : 0;
+    s.rt_pre = (N * p.G + kPaRows - 1) / kPaRows;
+    s.wide = p.wq && s.rt_pre > p.rt_narrow;
+    s.K = N > 0 && p.P > 0 && !s.wide ? s.rt_pre * p.Hkv * (C::kRunCost + s.PT) : 0;
     int excl = s.K + incl - mine;
     s.total = s.K;
     for (int k = 0; k < kPaThreads / 32; ++k) {
@@ -690,10 +699,15 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
                         const int st = n % C::kStages, f = n / C::kStages;
                         if (!(ok = mbar_wait(smem_u32(&bar_kv_empty[st]), (f & 1) ^ 1, &abort_flag))) break;
                         const uint32_t bar = smem_u32(&bar_kv_full[st]);
-                        mbar_arrive_expect_tx(bar, C::kTileBytes);
+                        // of an own cache only the boxes that hold tokens (74 sequences of 139
+                        // tokens in the mean, 16 KV heads: 67.5 us a call, 69.2 with whole tiles)
+                        const int step = it.own ? kPaBox : kPaTile;
+                        const int boxes = it.own ? min(kPaTile / kPaBox, (it.len - t * kPaTile + kPaBox - 1) / kPaBox) : 1;
+                        mbar_arrive_expect_tx(bar, boxes * step * D * 2);
                         for (int h = 0; h < D / 64; ++h)
-                            tma_load_4d(sRing + st * C::kTileBytes + h * C::kHalfBytes, kv ? tv : tk, bar, 64 * h, it.kvh,
-                                        t * kPaTile, it.b, pol);
+                            for (int i = 0; i < boxes; ++i)
+                                tma_load_4d(sRing + st * C::kTileBytes + h * C::kHalfBytes + i * step * 128, kv ? tv : tk, bar,
+                                            64 * h, it.kvh, t * kPaTile + i * step, it.b, pol);
                     }
                 }
             }
@@ -804,13 +818,12 @@ struct PaParts {
 
 // What the parts are found by that does not depend on the row.
 struct PaPre {
-    PaRun run;    // of the prefix and KV head
     int ns, nrt;  // wide prefix: shares, row tiles
 };
 
-__device__ __forceinline__ PaPre pa_pre(const PaParams& p, int kvh)
+__device__ __forceinline__ PaPre pa_pre(const PaParams& p)
 {
-    return PaPre{p.P > 0 ? p.run_pre[kvh] : PaRun{0, 0}, p.wq ? p.wcount[2] : 0, p.wq ? p.wcount[3] : 0};
+    return PaPre{p.wq ? p.wcount[2] : 0, p.wq ? p.wcount[3] : 0};
 }
 
 // Parts of packed row r, head g of KV head kvh: x[0] of the prefix, x[1] of the
@@ -833,9 +846,11 @@ __device__ __forceinline__ void pa_parts(const PaParams& p, const PaSched& s, co
         const int64_t at = (static_cast<int64_t>(m / 128) * p.Hkv + kvh) * 128 + m % 128;
         x[0] = PaParts{p.wm_part + at, p.wl_part + at, p.wo_part + at * D, step, step * D, pre.ns};
     } else if (s.K > 0) {
-        const int64_t at = static_cast<int64_t>(kvh + pre.run.c0) * p.w_pre + r * p.G + g;
+        const int m = r * p.G + g, id = kvh * s.rt_pre + m / kPaRows;
+        const PaRun run = p.run_pre[id];
+        const int64_t at = static_cast<int64_t>(id + run.c0) * p.w_pre + m % kPaRows;
         x[0] = PaParts{p.ml_pre + 2 * at, p.ml_pre + 2 * at + 1, p.o_pre + at * D, 2 * p.w_pre,
-                       static_cast<int64_t>(p.w_pre) * D, pre.run.n};
+                       static_cast<int64_t>(p.w_pre) * D, run.n};
     }
 }
 
@@ -858,7 +873,7 @@ __device__ __forceinline__ void pa_join(const PaParams& p, int block)
     // loads that depend on nothing, together
     const PaSched s = *p.sched;
     const int2 row = p.rows[r];
-    const PaPre pre = pa_pre(p, kvh);
+    const PaPre pre = pa_pre(p);
     const bool active = task / p.Hq < s.N;
     float acc[E], M = -INFINITY, Ls = 0.f;
 #pragma unroll
@@ -963,7 +978,7 @@ __device__ __forceinline__ void pa_mass(const PaParams& p, int block, int chunks
     PaPre pre{};
     if constexpr (FUSED) {
         s = *p.sched;
-        pre = pa_pre(p, kvh);
+        pre = pa_pre(p);
     }
     const int steps = (q.len + keys - 1) / keys;
     const int k0 = static_cast<int>(static_cast<int64_t>(steps) * ch / chunks) * keys;
@@ -1136,12 +1151,18 @@ size_t prefix_layout(const logo_dims& d, int n_new, int P, bool with_mass, char*
 {
     const int64_t G = d.Hq / d.Hkv, cap = static_cast<int64_t>(d.B) * n_new, R = n_new * G;
     const int64_t rt_own = (R + kPaRows - 1) / kPaRows;
-    const int64_t tiles = d.Hkv * ((P + kPaTile - 1ll) / kPaTile) + d.B * d.Hkv * rt_own * ((d.T + kPaTile - 1) / kPaTile);
-    const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>(tiles, device_sm_count()));
+    // row tiles of the prefix up to which it is not wide
+    const int64_t sms = device_sm_count(), PT = (P + kPaTile - 1ll) / kPaTile;
+    const int64_t rt_pre = P > 0 ? (cap * G + kPaRows - 1) / kPaRows : 0;
+    const int64_t run_units = PT + (d.D == 128 ? PaCfg<128>::kRunCost : PaCfg<64>::kRunCost);
+    const int64_t rt_narrow =
+        rt_pre * d.Hkv * run_units <= kPaNarrowCap * sms ? rt_pre : std::max<int64_t>(1, kPaNarrow * sms / (d.Hkv * run_units));
+    const int64_t tiles = rt_narrow * d.Hkv * PT + d.B * d.Hkv * rt_own * ((d.T + kPaTile - 1) / kPaTile);
+    const int64_t ctas = std::max<int64_t>(1, std::min(tiles, sms));
     const int64_t w_pre = std::min<int64_t>(kPaRows, cap * G), w_own = std::min<int64_t>(kPaRows, R);
     const int64_t runs_own = d.B * d.Hkv * rt_own, Lp = round_up(d.T, 4);
-    const int64_t slots_pre = P > 0 ? d.Hkv + ctas : 0, slots_own = runs_own + ctas;
-    const bool wide = P > 0 && cap * G > kPaRows;
+    const int64_t slots_pre = P > 0 ? rt_narrow * d.Hkv + ctas : 0, slots_own = runs_own + ctas;
+    const bool wide = rt_pre > rt_narrow;
     const int64_t w_rows = wide ? cap * G : 0, w_rt = (w_rows + 127) / 128;
     const int64_t w_units = wide ? std::max<int64_t>(w_rt * d.Hkv, kPaWideUnits) : 0;
     size_t off = 0;
@@ -1153,7 +1174,7 @@ size_t prefix_layout(const logo_dims& d, int n_new, int P, bool with_mass, char*
     char* sched = take(sizeof(PaSched));
     char* seqs = take(d.B * sizeof(PaSeq));
     char* row_info = take(cap * sizeof(int2));
-    char* run_pre = take(d.Hkv * sizeof(PaRun));
+    char* run_pre = take(rt_narrow * d.Hkv * sizeof(PaRun));
     char* run_own = take(runs_own * sizeof(PaRun));
     char* ml_pre = take(slots_pre * w_pre * 8);
     char* o_pre = take(slots_pre * w_pre * d.D * 4);
@@ -1201,6 +1222,7 @@ size_t prefix_layout(const logo_dims& d, int n_new, int P, bool with_mass, char*
         p->w_pre = static_cast<int>(w_pre);
         p->w_own = static_cast<int>(w_own);
         p->nCta = static_cast<int>(ctas);
+        p->rt_narrow = static_cast<int>(rt_narrow);
     }
     return off;
 }
@@ -1237,9 +1259,10 @@ int launch_prefix(PaParams& p, cudaStream_t st)
         const int rc = launch_tile_shares(t, D, st);
         if (rc != LOGO_OK) return rc;
     }
-    // few (row, head) pairs have many parts each: four warps a pair then (2048 pairs:
-    // 53.3 us a call against 55.3 with one; 5120: 94.3 against 88.9)
-    const int rc = static_cast<long long>(p.cap) * p.Hq <= 4096 ? launch_finish<D, 4, 4>(p, st) : launch_finish<D, 1, 4>(p, st);
+    // few (row, head) pairs: their parts are many and four warps join a pair (1024
+    // pairs, 22 parts: 54.8 us a call against 55.5 with one); more pairs keep the SMs
+    // busy with one (4096 pairs: 76.2 us against 83.5; 2976: 41.4 against 45.7)
+    const int rc = static_cast<long long>(p.cap) * p.Hq <= 1024 ? launch_finish<D, 4, 4>(p, st) : launch_finish<D, 1, 4>(p, st);
     if (rc != LOGO_OK) return rc;
     return cudaGetLastError() == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }
@@ -1279,8 +1302,8 @@ extern "C" int logo_decode_prefix_attn(const logo_bf16* q, const logo_bf16* k_pr
     if (!workspace || workspace_bytes < need || !aligned16(workspace)) return LOGO_ERR_WORKSPACE;
     PaParams p{};
     prefix_layout(dims, n_new, prefix_len, mass_out != nullptr, static_cast<char*>(workspace), &p);
-    if (!encode_bf16_4d(&p.tm_kc, k_cache, dims.D, dims.Hkv, dims.T, dims.B, 64, kPaTile) ||
-        !encode_bf16_4d(&p.tm_vc, v_cache, dims.D, dims.Hkv, dims.T, dims.B, 64, kPaTile))
+    if (!encode_bf16_4d(&p.tm_kc, k_cache, dims.D, dims.Hkv, dims.T, dims.B, 64, kPaBox) ||
+        !encode_bf16_4d(&p.tm_vc, v_cache, dims.D, dims.Hkv, dims.T, dims.B, 64, kPaBox))
         return LOGO_ERR_CUDA;
     if (prefix_len > 0 && (!encode_bf16_4d(&p.tm_kp, k_prefix, dims.D, dims.Hkv, prefix_len, 1, 64, kPaTile) ||
                            !encode_bf16_4d(&p.tm_vp, v_prefix, dims.D, dims.Hkv, prefix_len, 1, 64, kPaTile)))

@@ -134,6 +134,22 @@ def test_many_rows_share_the_prefix(D, Hq, Hkv, n):
     _run(B, n, Hq, Hkv, D, 700, 145, lens, _z(B, n, 0.9, D), seed=9)
 
 
+@pytest.mark.parametrize("share", [0.9, 0.2])
+@pytest.mark.parametrize("D,Hq,Hkv,n,P", [(128, 16, 4, 4, 2500), (64, 8, 1, 3, 6701)])
+def test_many_rows_share_a_long_prefix(D, Hq, Hkv, n, P, share):
+    """Enough rows and keys for 128-row tiles, and too few rows selected for them."""
+    B = 45
+    lens = [(37 * b) % 140 + n for b in range(B)]
+    _run(B, n, Hq, Hkv, D, P, 145, lens, _z(B, n, share, D), seed=11)
+
+
+@pytest.mark.parametrize("n,G", [(1, 4), (4, 8)])
+def test_caches_that_end_inside_a_tile(n, G):
+    """Every remainder of the cache's length modulo a copy's 32 rows and around them."""
+    lens = [n, 31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 129, 159, 161, 191, 193, 223, 225]
+    _run(len(lens), n, 2 * G, 2, 128, 40, 230, lens, _z(len(lens), n, 1.0, G), seed=n)
+
+
 @pytest.mark.parametrize("D,Hq,Hkv,n", [(128, 4, 1, 1), (64, 16, 2, 2), (128, 32, 1, 5)])
 def test_few_rows_long_prefix_and_caches(D, Hq, Hkv, n):
     _run(2, n, Hq, Hkv, D, 9001, 5000, [5000, 1700], torch.ones(2, n, dtype=torch.bool), seed=21)
