@@ -232,7 +232,10 @@ LOGO_API int logo_decode_global_sparse_attn(const logo_bf16* q, const logo_bf16*
  *   flight (with_mass: whether mass_out will be given).
  *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer or a size out of range;
  *   LOGO_ERR_UNSUPPORTED for D, Hq % Hkv, 16-byte alignment of a bf16 pointer,
- *   or B * n_new > 2^24; LOGO_ERR_WORKSPACE. */
+ *   or a size past what the kernels count in: with G = Hq / Hkv, B * n_new <=
+ *   2^24, B * n_new * G <= 2^28, n_new * G <= 8192, prefix_len <= 2^30, Hkv <=
+ *   2^16, at most 2^28 tiles of 128 keys by 32 rows and 2^23 of 128 rows;
+ *   LOGO_ERR_WORKSPACE. */
 LOGO_API size_t logo_decode_prefix_workspace_size(logo_dims dims, int n_new, int prefix_len, int with_mass);
 LOGO_API int logo_decode_prefix_attn(const logo_bf16* q, const logo_bf16* k_prefix, const logo_bf16* v_prefix,
                 const logo_bf16* k_cache, const logo_bf16* v_cache, const int32_t* seq_len, const int32_t* pos,
