@@ -57,9 +57,16 @@ constexpr int kPaMassThreads = 256;
 // (see PaSched) an SM, as counted at run time, and the tcgen05 kernel is not
 // launched where no selection can pass the second number.  Call times, read again
 // against tcgen05: 22 row tiles, 4 KV heads, 2 keys 41.6 us, 56.9; 16 and 16 and 500
-// keys (8 units) 50.3, 63.7; 6 row tiles, 6307 keys (2 units of at most 9) 21.8, 33.3;
-// 6 row tiles, 4 KV heads, 8000 keys (10 units of at most 17) 33.1, 31.0.
-constexpr int kPaNarrow = 8, kPaNarrowCap = 12;
+// keys (8 units) 50.3, 63.7.  With a launch saved (at most 15 units, all or half of
+// the rows selected; 16 row tiles, 8 KV heads, 2000 keys): 43.8 and 33.1,
+// against 41.4 and 39.3; 10 row tiles, 4 KV heads, 8000 keys 41.2 and 31.5, against
+// 40.7 and 36.8.
+constexpr int kPaNarrow = 8, kPaNarrowCap = 18;
+// A run's start and end (its Q, the join of the warps) are counted as this many
+// tiles when the shares are cut (with 1, D = 128: 16 sequences of 8192 tokens, 32
+// rows 51.1 us a call against 49.9; with 3, D = 64: 128 sequences of up to 400
+// tokens, two rows 29.1 against 27.9).
+constexpr int kRunCost = 2;
 constexpr int kPaMaxR = 8192;        // n_new * (Hq / Hkv) at most (the weights' row statistics in shared memory)
 
 template <int D>
@@ -67,9 +74,6 @@ struct PaCfg {
     static constexpr int kTileBytes = kPaTile * D * 2;  // one K or V tile
     static constexpr int kHalfBytes = kPaTile * 128;    // its 64-column half (128-byte rows)
     static constexpr int kStages = D == 128 ? 5 : 10;   // K and V tiles in turn: 160 KB
-    // a run's start and end (its Q, the join of the warps) cost about as much as
-    // 96 KB of tiles: counted as tiles when the shares are cut
-    static constexpr int kRunCost = D == 128 ? 2 : 3;
     static constexpr int kQHalf = kPaRows * 128;
     static constexpr int kQBytes = kPaRows * D * 2;
     static constexpr int kOffRing = 2 * kQBytes;  // after two Q tiles
@@ -155,10 +159,9 @@ __device__ __forceinline__ OwnSeq own_seq(const PaParams& p, int b)
 }
 
 // Units of a sequence on the line.
-template <int COST>
 __device__ __forceinline__ int own_units(const PaParams& p, const OwnSeq& o)
 {
-    return o.tiles > 0 ? (COST + o.tiles) * o.rts * p.Hkv : 0;
+    return o.tiles > 0 ? (kRunCost + o.tiles) * o.rts * p.Hkv : 0;
 }
 
 __device__ __forceinline__ int share_start(const PaSched& s, int c)
@@ -187,7 +190,6 @@ struct PaIter {
     PaRun* run;             // of the last piece: where its run is noted,
     int run_end;            // ... and the run's last unit
 
-    template <int COST>
     __device__ __forceinline__ bool next(const PaParams& p, const PaSched& s, PaPiece* it)
     {
         for (;;) {
@@ -195,8 +197,8 @@ struct PaIter {
             int tiles, first;  // of the run: tiles, first unit
             if (u < s.K) {
                 tiles = s.PT;
-                const int k = u / (COST + tiles);
-                first = k * (COST + tiles);
+                const int k = u / (kRunCost + tiles);
+                first = k * (kRunCost + tiles);
                 it->own = 0;
                 it->b = 0;
                 it->kvh = k / s.rt_pre;
@@ -208,16 +210,16 @@ struct PaIter {
                 run = p.run_pre + k;
             } else {
                 OwnSeq o = own_seq(p, b);
-                int units = own_units<COST>(p, o);
+                int units = own_units(p, o);
                 while (u - base >= units) {  // ends: u < u1 <= the line's length
                     base += units;
                     ++b;
                     o = own_seq(p, b);
-                    units = own_units<COST>(p, o);
+                    units = own_units(p, o);
                 }
                 tiles = o.tiles;
-                const int k = (u - base) / (COST + tiles);
-                first = base + k * (COST + tiles);
+                const int k = (u - base) / (kRunCost + tiles);
+                first = base + k * (kRunCost + tiles);
                 it->own = 1;
                 it->b = b;
                 it->kvh = k / o.rts;
@@ -230,10 +232,10 @@ struct PaIter {
                 it->slot = id + c;
                 run = p.run_own + id;
             }
-            it->t0 = max(0, u - first - COST);
-            u = min(u1, first + COST + tiles);
-            it->t1 = max(0, u - first - COST);
-            run_end = first + COST + tiles - 1;
+            it->t0 = max(0, u - first - kRunCost);
+            u = min(u1, first + kRunCost + tiles);
+            it->t1 = max(0, u - first - kRunCost);
+            run_end = first + kRunCost + tiles - 1;
             if (it->t1 > it->t0) return true;  // else the share ends in the run's overhead
         }
     }
@@ -478,54 +480,68 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
         if (lane == 0) mbar_arrive(w.kv_empty + 8 * stV);
     }
 
-    // ---- the warps' (m, l, O) joined
+    // ---- the warps' (m, l, O) joined, 64 columns at a time, or all 128 where 8 rows
+    //      leave room (columns 64 .. 127 lie where rows 8 .. 15 would)
+    float l[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        float l = l_run[i];
-        l += __shfl_xor_sync(0xffffffffu, l, 1);
-        l += __shfl_xor_sync(0xffffffffu, l, 2);
-        if (tig == 0) w.sh_ml[w.warp * 16 + 8 * i + gid] = make_float2(m_run[i], l);
+        l[i] = l_run[i] + __shfl_xor_sync(0xffffffffu, l_run[i], 1);
+        l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
     }
+    // (all warps have left the tiles, and the last piece's join)
     if (!products_sync_and(ok)) return false;
-    const int64_t at = static_cast<int64_t>(it.slot) * (it.own ? p.w_own : p.w_pre);
-    float f[2];  // 2^(m of this warp - M) of this lane's rows
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float2* ml = w.sh_ml + rg * group * 16 + 8 * i + gid;  // [warp of the group][16]
-        float M = -INFINITY, l = 0.f;
-        for (int k = 0; k < group; ++k) M = fmaxf(M, ml[k * 16].x);
-        const float Mu = M == -INFINITY ? 0.f : M;
-        for (int k = 0; k < group; ++k) l += ex2_approx(ml[k * 16].x - Mu) * ml[k * 16].y;
-        f[i] = ex2_approx(m_run[i] - Mu);
-        const int row = 16 * rg + 8 * i + gid;
-        if (w.warp % group == 0 && tig == 0 && row < it.nrows)
-            reinterpret_cast<float2*>(it.own ? p.ml_own : p.ml_pre)[at + row] = make_float2(M, l);
-    }
     constexpr int kCols = 64, kStride = kCols + 8;  // rows 8 floats off a multiple of 32: no bank conflicts
+    const bool few = D > kCols && it.nrows <= 8;
+    const int64_t at = static_cast<int64_t>(it.slot) * (it.own ? p.w_own : p.w_pre);
     float* o_part = (it.own ? p.o_own : p.o_pre) + at * D;
-    const int tid = w.warp * 32 + lane;
+    float2* ml_part = reinterpret_cast<float2*>(it.own ? p.ml_own : p.ml_pre) + at;
+    float* mine = w.merge + w.warp * 16 * kStride + gid * kStride + 2 * tig;
+    const int tid = w.warp * 32 + lane, shift = few ? 5 : 4;  // float4s of a row in a round: 1 << shift
 #pragma unroll
     for (int c0 = 0; c0 < D; c0 += kCols) {
-        float* mine = w.merge + w.warp * 16 * kStride;
+        if (c0 > 0) {
+            if (few) break;
+            products_sync();
+        }
 #pragma unroll
-        for (int nt = 0; nt < kCols / 8; ++nt)
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                *reinterpret_cast<float2*>(mine + (8 * i + gid) * kStride + nt * 8 + 2 * tig) =
-                    make_float2(oc[c0 / 8 + nt][2 * i] * f[i], oc[c0 / 8 + nt][2 * i + 1] * f[i]);
-        products_sync();
-        for (int i = tid; i < it.nrows * (kCols / 4); i += kPaWarps * 32) {
-            const int row = i / (kCols / 4), c = i % (kCols / 4) * 4;
-            const float* src = w.merge + ((row >> 4) * group * 16 + (row & 15)) * kStride + c;
-            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-            for (int k = 0; k < group; ++k) {
-                const float4 v = *reinterpret_cast<const float4*>(src + k * 16 * kStride);
-                a.x += v.x, a.y += v.y, a.z += v.z, a.w += v.w;
-            }
-            *reinterpret_cast<float4*>(o_part + static_cast<int64_t>(row) * D + c0 + c) = a;
+        for (int nt = 0; nt < kCols / 8; ++nt) {
+            const float(&lo)[4] = oc[c0 / 8 + nt];
+            const float(&hi)[4] = oc[(D > kCols && c0 == 0 ? kCols / 8 : c0 / 8) + nt];
+            *reinterpret_cast<float2*>(mine + nt * 8) = make_float2(lo[0], lo[1]);
+            *reinterpret_cast<float2*>(mine + 8 * kStride + nt * 8) =
+                few ? make_float2(hi[0], hi[1]) : make_float2(lo[2], lo[3]);
+        }
+        if (c0 == 0 && tig == 0) {
+            w.sh_ml[w.warp * 16 + gid] = make_float2(m_run[0], l[0]);
+            w.sh_ml[w.warp * 16 + 8 + gid] = make_float2(m_run[1], l[1]);
         }
         products_sync();
+        for (int i = tid; i < it.nrows << shift; i += kPaWarps * 32) {
+            const int row = i >> shift, c = i & ((1 << shift) - 1);
+            const int from = split_rows ? (row >> 4) * 4 : 0;  // the row's first warp
+            const float2* ml = w.sh_ml + from * 16 + (row & 15);
+            float f[kPaWarps], M = -INFINITY, L = 0.f;
+            float2 part[kPaWarps];
+#pragma unroll
+            for (int k = 0; k < kPaWarps; ++k) {
+                part[k] = k < group ? ml[k * 16] : make_float2(-INFINITY, 0.f);
+                M = fmaxf(M, part[k].x);
+            }
+            const float Mu = M == -INFINITY ? 0.f : M;
+            const float* src = w.merge + (from * 16 + (few ? row + 8 * (c >> 4) : row & 15)) * kStride + (c & 15) * 4;
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < kPaWarps; ++k) {
+                f[k] = ex2_approx(part[k].x - Mu);
+                L += f[k] * part[k].y;
+                if (k < group) {
+                    const float4 v = *reinterpret_cast<const float4*>(src + k * 16 * kStride);
+                    a.x += f[k] * v.x, a.y += f[k] * v.y, a.z += f[k] * v.z, a.w += f[k] * v.w;
+                }
+            }
+            if (c0 == 0 && c == 0) ml_part[row] = make_float2(M, L);
+            *reinterpret_cast<float4*>(o_part + static_cast<int64_t>(row) * D + c0 + c * 4) = a;
+        }
     }
     return true;
 }
@@ -624,7 +640,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     int mine = 0;
     for (int b = tb0; b < tb1; ++b) {
         const OwnSeq o = own_seq(p, b);
-        mine += own_units<C::kRunCost>(p, o);
+        mine += own_units(p, o);
     }
     __syncwarp();
     int incl = mine;
@@ -640,7 +656,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     s.PT = (p.P + kPaTile - 1) / kPaTile;
     s.rt_pre = (N * p.G + kPaRows - 1) / kPaRows;
     s.wide = p.wq && s.rt_pre > p.rt_narrow;
-    s.K = N > 0 && p.P > 0 && !s.wide ? s.rt_pre * p.Hkv * (C::kRunCost + s.PT) : 0;
+    s.K = N > 0 && p.P > 0 && !s.wide ? s.rt_pre * p.Hkv * (kRunCost + s.PT) : 0;
     int excl = s.K + incl - mine;
     s.total = s.K;
     for (int k = 0; k < kPaThreads / 32; ++k) {
@@ -660,7 +676,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
         int base = excl, b = tb0;
         for (; b < tb1; ++b) {
             const OwnSeq o = own_seq(p, b);
-            const int units = own_units<C::kRunCost>(p, o);
+            const int units = own_units(p, o);
             if (iter.u < base + units) break;
             base += units;
         }
@@ -689,7 +705,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
             const uint64_t pol = policy_evict_first();
             int n = 0;
             bool ok = true;
-            while (ok && iter.template next<C::kRunCost>(p, s, &it)) {
+            while (ok && iter.next(p, s, &it)) {
                 // when all SMs fill their rings, their first tiles are 24 MB, and a load
                 // behind them takes 4 us
                 if (n == 0 && it.t1 - it.t0 > 1 && !(ok = mbar_wait(smem_u32(&bar_go), 0, &abort_flag))) break;
@@ -721,7 +737,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
             // planners take the pieces in turn, so that one's loads are in flight
             // (into registers) while the other waits for its Q buffer
             for (int piece = 0;; ++piece) {
-                const bool more = iter.template next<C::kRunCost>(p, s, &it);
+                const bool more = iter.next(p, s, &it);
                 const int qb = piece & 1;
                 if (piece % kPaPlanners != warp - kPaWarps - 1) {
                     if (!more) break;
@@ -1155,7 +1171,7 @@ size_t prefix_layout(const logo_dims& d, int n_new, int P, bool with_mass, char*
     // row tiles of the prefix up to which it is not wide
     const int64_t sms = device_sm_count(), PT = (P + kPaTile - 1ll) / kPaTile;
     const int64_t rt_pre = P > 0 ? (cap * G + kPaRows - 1) / kPaRows : 0;
-    const int64_t run_units = PT + (d.D == 128 ? PaCfg<128>::kRunCost : PaCfg<64>::kRunCost);
+    const int64_t run_units = PT + kRunCost;
     const int64_t rt_narrow =
         rt_pre * d.Hkv * run_units <= kPaNarrowCap * sms ? rt_pre : std::max<int64_t>(1, kPaNarrow * sms / (d.Hkv * run_units));
     const int64_t tiles = rt_narrow * d.Hkv * PT + d.B * d.Hkv * rt_own * ((d.T + kPaTile - 1) / kPaTile);
