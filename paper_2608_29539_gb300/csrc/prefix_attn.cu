@@ -158,6 +158,27 @@ __device__ __forceinline__ OwnSeq own_seq(const PaParams& p, int b)
     return o;
 }
 
+// The same from shared memory, where the batch fits there (seqs, else NULL): the
+// loads of one are two round trips, for every sequence that a share passes, and a
+// batch of which few are selected has many to pass.
+__device__ __forceinline__ OwnSeq seq_at(const PaParams& p, const OwnSeq* seqs, int b)
+{
+    return seqs ? seqs[b] : own_seq(p, b);
+}
+
+// Sequence of packed row r.
+__device__ __forceinline__ int seq_of(const PaParams& p, const OwnSeq* seqs, int r)
+{
+    if (!seqs) return seq_of_row(p.cu_q, p.B, r);
+    int lo = 0, hi = p.B - 1;  // the last one that starts at or before r
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (seqs[mid].row0 <= r) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
 // Units of a sequence on the line.
 __device__ __forceinline__ int own_units(const PaParams& p, const OwnSeq& o)
 {
@@ -190,7 +211,7 @@ struct PaIter {
     PaRun* run;             // of the last piece: where its run is noted,
     int run_end;            // ... and the run's last unit
 
-    __device__ __forceinline__ bool next(const PaParams& p, const PaSched& s, PaPiece* it)
+    __device__ __forceinline__ bool next(const PaParams& p, const PaSched& s, const OwnSeq* seqs, PaPiece* it)
     {
         for (;;) {
             if (u >= u1) return false;
@@ -209,12 +230,12 @@ struct PaIter {
                 it->slot = k + c;
                 run = p.run_pre + k;
             } else {
-                OwnSeq o = own_seq(p, b);
+                OwnSeq o = seq_at(p, seqs, b);
                 int units = own_units(p, o);
                 while (u - base >= units) {  // ends: u < u1 <= the line's length
                     base += units;
                     ++b;
-                    o = own_seq(p, b);
+                    o = seq_at(p, seqs, b);
                     units = own_units(p, o);
                 }
                 tiles = o.tiles;
@@ -553,7 +574,7 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
 // Items lie share by share, so that the SMs work on the same keys at the same
 // time.
 template <int D>
-__device__ __forceinline__ void wide_prep(const PaParams& p, const PaSched& s, int lane)
+__device__ __forceinline__ void wide_prep(const PaParams& p, const PaSched& s, const OwnSeq* seqs, int lane)
 {
     const int rows = s.wide ? s.N * p.G : 0, nRT = (rows + 127) / 128;
     // a row: [KV head][g][D] of q -> [KV head][D] for each g
@@ -564,7 +585,7 @@ __device__ __forceinline__ void wide_prep(const PaParams& p, const PaSched& s, i
             for (int v = lane; v < vecs; v += 32) dst[v] = make_uint4(0u, 0u, 0u, 0u);
             continue;
         }
-        const int r = M / p.G, g = M % p.G, b = seq_of_row(p.cu_q, p.B, r);
+        const int r = M / p.G, g = M % p.G, b = seq_of(p, seqs, r);
         const uint4* src =
             reinterpret_cast<const uint4*>(p.q + (static_cast<int64_t>(b) * p.n_new + token_of(p, r)) * p.Hq * D);
 #pragma unroll 4
@@ -614,6 +635,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     __shared__ float2 sh_ml[kPaWarps * 16];
     __shared__ int sh_vis[2][kPaRows], sh_scan[kPaThreads / 32], sh_base, sh_b0;
     __shared__ PaPiece sh_piece[2];
+    __shared__ OwnSeq sh_seq[kPaThreads];
     __shared__ volatile int abort_flag;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
@@ -637,10 +659,12 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     const int N = *p.n_sel;
     const int per = (p.B + kPaThreads - 1) / kPaThreads;  // sequences per thread
     const int tb0 = min(p.B, tid * per), tb1 = min(p.B, tb0 + per);
+    const OwnSeq* seqs = p.B <= kPaThreads ? sh_seq : nullptr;
     int mine = 0;
     for (int b = tb0; b < tb1; ++b) {
         const OwnSeq o = own_seq(p, b);
         mine += own_units(p, o);
+        if (seqs) sh_seq[b] = o;
     }
     __syncwarp();
     int incl = mine;
@@ -675,7 +699,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     if (iter.u < iter.u1 && iter.u >= excl && iter.u < excl + mine) {
         int base = excl, b = tb0;
         for (; b < tb1; ++b) {
-            const OwnSeq o = own_seq(p, b);
+            const OwnSeq o = seq_at(p, seqs, b);
             const int units = own_units(p, o);
             if (iter.u < base + units) break;
             base += units;
@@ -686,7 +710,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     if (cta == s.n % p.nCta) {  // for the join and the weights (by a CTA without a share, if there is one)
         if (tid == 0) *p.sched = s;
         for (int b = tb0; b < tb1; ++b) {
-            const OwnSeq o = own_seq(p, b);
+            const OwnSeq o = seq_at(p, seqs, b);
             p.seqs[b] = PaSeq{o.row0, o.n, o.len, o.tiles};
             for (int r = o.row0; r < o.row0 + o.n; ++r) p.rows[r] = make_int2(b, o.tiles > 0 ? o.row0 : -1);
         }
@@ -705,7 +729,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
             const uint64_t pol = policy_evict_first();
             int n = 0;
             bool ok = true;
-            while (ok && iter.next(p, s, &it)) {
+            while (ok && iter.next(p, s, seqs, &it)) {
                 // when all SMs fill their rings, their first tiles are 24 MB, and a load
                 // behind them takes 4 us
                 if (n == 0 && it.t1 - it.t0 > 1 && !(ok = mbar_wait(smem_u32(&bar_go), 0, &abort_flag))) break;
@@ -737,7 +761,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
             // planners take the pieces in turn, so that one's loads are in flight
             // (into registers) while the other waits for its Q buffer
             for (int piece = 0;; ++piece) {
-                const bool more = iter.next(p, s, &it);
+                const bool more = iter.next(p, s, seqs, &it);
                 const int qb = piece & 1;
                 if (piece % kPaPlanners != warp - kPaWarps - 1) {
                     if (!more) break;
@@ -751,7 +775,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
                 int64_t at = 0;
                 if (lane < it.nrows) {
                     const int m = it.row0 + lane, r = it.seg_row0 + m / p.G, g = m % p.G;
-                    const int b = it.own ? it.b : seq_of_row(p.cu_q, p.B, r);
+                    const int b = it.own ? it.b : seq_of(p, seqs, r);
                     const int i = token_of(p, r);
                     vis = it.own ? own_visible(it.len, p.n_new, i) : it.len;
                     at = ((static_cast<int64_t>(b) * p.n_new + i) * p.Hq + it.kvh * p.G + g) * D;
@@ -787,7 +811,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
                 if (!more) break;
             }
         } else if (warp == kPaWarps + 1 + kPaPlanners && p.wq) {
-            wide_prep<D>(p, s, lane);
+            wide_prep<D>(p, s, seqs, lane);
         }
         return;
     }
