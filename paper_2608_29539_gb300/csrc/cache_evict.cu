@@ -17,9 +17,9 @@
 // histograms meet in distributed shared memory, and the same CTAs then move the
 // rows (4 D bytes a moved row of K and V, read and written), so that the cut of a
 // whole batch is one launch.  The plan is bound by latency (barriers and round
-// trips): 64 pairs of 16384 rows cut to 2048 plan for 20 us, in which HBM idles,
-// and move 102 MB in 17, at 6.2 TB/s; 256 pairs of 2056 rows cut to 2048 plan for
-// 11 us and hardly move.
+// trips): 64 pairs of 16384 rows cut to 2048 take 37 us, the plan 20 of them, in
+// which HBM idles, and the moves 17 for 102 MB, 6.2 TB/s; 256 pairs of 2056 rows cut
+// to 2048 take 12 us and hardly move.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(EvParams p)
     if constexpr (IN_SMEM) {
         int i0 = 0;
         if (((reinterpret_cast<uintptr_t>(mass + s0) | reinterpret_cast<uintptr_t>(pos + s0)) & 15) == 0) {
-            // four at a time (1024 pairs of 2000 rows: 73 us a call, 84 one at a time;
+            // four at a time (1024 pairs of 2000 rows: 72 us a call, 84 one at a time;
             // 256 pairs of 2056: 11.9, 13.3); what is left over, or not aligned, below
             i0 = cnt & ~3;
 #pragma unroll 4
@@ -334,9 +334,9 @@ int check_evict(const logo_dims& d)
 // SMs hold two CTAs, plus a CTA's share of the rows to rank and to move, in units
 // of a row to rank (1.2 ns; moving one of D = 128 takes as long as ranking four).
 // Measured with 1 / 2 / 4 / 8 CTAs a pair (us): 16 pairs of 2100 rows, 2000 stay
-// 8.7 / 11.0 / 10.4 / 11.9; of 3000, 1500 stay 16.9 / 14.6 / 12.5 / 13.0; 4 pairs of
-// 16384, 12000 stay 65 / 38 / 24 / 19; 40 pairs of 6000, 5800 stay 14.7 / 14.8 / 16.1
-// / 32; 64 pairs of 16384, 2048 stay 82 / 52 / 42 / 66.
+// 7.7 / 10.1 / 10.0 / 12.9; of 3000, 1500 stay 15.4 / 13.9 / 12.1 / 13.9; 4 pairs of
+// 16384, 12000 stay 60 / 36 / 23 / 18; 40 pairs of 6000, 5800 stay 12.9 / 13.4 / 15.3
+// / 32; 64 pairs of 16384, 2048 stay 68 / 46 / 39 / 61.
 int evict_ctas(int64_t pairs, const logo_dims& d, int budget)
 {
     constexpr int64_t kCost[] = {0, 3500, 2600, 4400}, kCrowd[] = {0, 1500, 3300, 2200};
@@ -344,8 +344,8 @@ int evict_ctas(int64_t pairs, const logo_dims& d, int budget)
     const int64_t work = d.T + d.D / 32ll * std::max(0, std::min(budget, d.T - budget));
     int best = 1;
     int64_t least = work;
-    // (clusters do not fill the last places of a group of SMs: 76 of four CTAs take 38 us
-    // where 72 take 26)
+    // (clusters do not fill the last places of a group of SMs: 76 of four CTAs take 33.5
+    // us where 72 take 24.1)
     for (int k = 1; 1 << k <= kEvMaxCluster && (pairs << k) * 20 <= 2 * sms * 19; ++k) {
         const int64_t cost = kCost[k] + (pairs << k > sms ? kCrowd[k] : 0) + (work >> k);
         if (cost < least) {

@@ -56,16 +56,15 @@ constexpr int kPaMassThreads = 256;
 // A prefix is read again for each 32 rows by pa_rows_kernel up to this many units
 // (see PaSched) an SM, as counted at run time, and the tcgen05 kernel is not
 // launched where no selection can pass the second number.  Call times, read again
-// against tcgen05: 22 row tiles, 4 KV heads, 2 keys 41.6 us, 56.9; 16 and 16 and 500
-// keys (8 units) 50.3, 63.7.  With a launch saved (at most 15 units, all or half of
-// the rows selected; 16 row tiles, 8 KV heads, 2000 keys): 43.8 and 33.1,
-// against 41.4 and 39.3; 10 row tiles, 4 KV heads, 8000 keys 41.2 and 31.5, against
-// 40.7 and 36.8.
+// against tcgen05: 22 row tiles, 4 KV heads, 2 keys 41.1 us, 51.1; 16, 16 and 500
+// keys (10 units) 51.4, 62.0.  With all and with half of the rows selected: 16 row
+// tiles, 8 KV heads, 2000 keys (15 units) 43.5 and 33.1, against 41.3 and 37.7; 10
+// row tiles, 4 KV heads, 8000 keys (17 units) 40.8 and 31.5, against 39.4 and 36.8.
 constexpr int kPaNarrow = 8, kPaNarrowCap = 18;
 // A run's start and end (its Q, the join of the warps) are counted as this many
-// tiles when the shares are cut (with 1, D = 128: 16 sequences of 8192 tokens, 32
-// rows 51.1 us a call against 49.9; with 3, D = 64: 128 sequences of up to 400
-// tokens, two rows 29.1 against 27.9).
+// tiles when the shares are cut (with 1, 2 and 3: 16 sequences of 8192 tokens, 32
+// rows 51.6, 49.8 and 50.0 us a call; 256 rows, 2048 tokens 120, 110 and 115; 128
+// sequences of 512 tokens, four rows 70.2, 70.8 and 71.9).
 constexpr int kRunCost = 2;
 constexpr int kPaMaxR = 8192;        // n_new * (Hq / Hkv) at most (the weights' row statistics in shared memory)
 
@@ -302,8 +301,7 @@ __device__ __forceinline__ void products_sync() { asm volatile("barrier.cta.sync
 // products that use them, as two warps a scheduler hide little of each other's
 // latency; and there is one code path (a second one, met by a few SMs only, cost
 // them 8 us of instruction fetches).  16 sequences of up to 8192 keys, 8 KV heads,
-// 32 rows: 54.2 us a call, 271 MB at 74% of the measured HBM rate (56.1 with 16
-// keys after 16 keys).  Then the warps' results are joined in shared memory.
+// 32 rows: 49.8 us a call, 271 MB at 80% of the measured HBM rate.  Then the warps' results are joined in shared memory.
 // Returns false, to all warps, if a wait of any gave up.
 template <int D>
 __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, PaWarp& w, bool ok)
@@ -741,7 +739,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
                         if (!(ok = mbar_wait(smem_u32(&bar_kv_empty[st]), (f & 1) ^ 1, &abort_flag))) break;
                         const uint32_t bar = smem_u32(&bar_kv_full[st]);
                         // of an own cache only the boxes that hold tokens (74 sequences of 139
-                        // tokens in the mean, 16 KV heads: 67.5 us a call, 69.2 with whole tiles)
+                        // tokens in the mean, 16 KV heads: 64.4 us a call, 66.3 with whole tiles)
                         const int step = it.own ? kPaBox : kPaTile;
                         const int boxes = it.own ? min(kPaTile / kPaBox, (it.len - t * kPaTile + kPaBox - 1) / kPaBox) : 1;
                         mbar_arrive_expect_tx(bar, boxes * step * D * 2);
@@ -1115,9 +1113,9 @@ __device__ __forceinline__ void pa_mass(const PaParams& p, int block, int chunks
 // Up to kPaFusedR rows a (sequence, KV head), join and weights share a launch: a
 // block of the weights then forms its rows' lse from their parts itself, eight
 // lanes a row, which saves the launch between the two (call times, fused against
-// not: 44.4 us against 50.8 at 40 rows, 4 sequences; 90.6 against 98.0 at 64 rows,
-// 16 sequences of 4096; 111.8 against 117.7 at 256 rows, 16 sequences of 2048).
-// Every block does that work: at 512 rows it costs more (96.4 us against 94.1).
+// not: 41.9 us against 46.0 at 40 rows, 4 sequences; 90.5 against 97.1 at 64 rows,
+// 16 sequences of 4096; 110 against 115 at 256 rows, 16 sequences of 2048).  Every
+// block does that work: at 512 rows it costs more (96.3 us against 94.1).
 constexpr int kPaFusedR = 256;
 
 template <int D, int WPR, int CH>
@@ -1301,8 +1299,8 @@ int launch_prefix(PaParams& p, cudaStream_t st)
         if (rc != LOGO_OK) return rc;
     }
     // few (row, head) pairs: their parts are many and four warps join a pair (1024
-    // pairs, 22 parts: 54.8 us a call against 55.5 with one); more pairs keep the SMs
-    // busy with one (4096 pairs: 76.2 us against 83.5; 2976: 41.4 against 45.7)
+    // pairs, 22 parts: 52.9 us a call against 54.6 with one); more pairs keep the SMs
+    // busy with one (4096 pairs: 70.8 us against 77.5; 2976: 41.1 against 45.2)
     const int rc = static_cast<long long>(p.cap) * p.Hq <= 1024 ? launch_finish<D, 4, 4>(p, st) : launch_finish<D, 1, 4>(p, st);
     if (rc != LOGO_OK) return rc;
     return cudaGetLastError() == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
