@@ -163,6 +163,38 @@ def test_cache_offsets_beyond_32_bits():
     assert not bool(k[0, :200].any()) and not bool(k[1, :200, :63].any())
 
 
+def test_captures_in_a_graph_and_runs_on_another_stream():
+    from paper_2608_29539_gb300 import logo as Lg
+    g = torch.Generator().manual_seed(4)
+    B, L, H, D, budget = 2, 5000, 4, 64, 2000
+    k, v = (torch.randn((B, L, H, D), generator=g).bfloat16().cuda() for _ in range(2))
+    mass = torch.rand((B, H, L), generator=g).cuda()
+    pos = torch.arange(L, dtype=torch.int32).expand(B, H, L).contiguous().cuda()
+    lens = torch.tensor([L, 3100], dtype=torch.int32, device="cuda")
+    ws = Lg.logo_cache_evict_workspace(k)
+
+    def run(x):
+        return Lg.logo_cache_evict(x[0], x[1], x[2], x[3], lens, lens, budget, 100, new_len=x[4], workspace=ws)
+
+    state = lambda: [k.clone(), v.clone(), mass.clone(), pos.clone(), torch.zeros_like(lens)]  # noqa: E731
+    want, side, replayed = state(), state(), state()
+    run(want)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        run(side)
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(replayed)
+    assert torch.equal(replayed[2], mass)  # captured, not run
+    graph.replay()
+    torch.cuda.synchronize()
+    assert want[4].tolist() == [budget, budget]
+    for a, b, c in zip(want, side, replayed):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
 def test_refusals():
     from paper_2608_29539_gb300 import logo as Lg
     B, H, D, L = 2, 2, 64, 32

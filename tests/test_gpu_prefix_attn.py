@@ -150,6 +150,21 @@ def test_caches_that_end_inside_a_tile(n, G):
     _run(len(lens), n, 2 * G, 2, 128, 40, 230, lens, _z(len(lens), n, 1.0, G), seed=n)
 
 
+@pytest.mark.parametrize("P", [3, 130, 4000])
+def test_many_sequences(P):
+    """More than a CTA has threads; most of them not selected."""
+    B, n = 400, 2
+    lens = [(11 * b) % 19 + 1 for b in range(B)]
+    _run(B, n, 4, 2, 64, P, 21, lens, _z(B, n, 0.3, P), seed=P)
+
+
+@pytest.mark.parametrize("n,G,L", [(8, 40, 131), (33, 8, 200)])
+def test_many_rows_of_a_sequence(n, G, L):
+    """More rows than the join and the weights take in one launch."""
+    lens = [L, n, 130, 1]
+    _run(4, n, 2 * G, 2, 64, 70, L, lens, _z(4, n, 0.9, n), seed=n)
+
+
 @pytest.mark.parametrize("D,Hq,Hkv,n", [(128, 4, 1, 1), (64, 16, 2, 2), (128, 32, 1, 5)])
 def test_few_rows_long_prefix_and_caches(D, Hq, Hkv, n):
     _run(2, n, Hq, Hkv, D, 9001, 5000, [5000, 1700], torch.ones(2, n, dtype=torch.bool), seed=21)

@@ -127,6 +127,26 @@ def test_offsets_beyond_32_bits():
     assert n[0] == 0 and tokens[0, 0] == 0
 
 
+def test_captures_in_a_graph_and_runs_on_another_stream():
+    from paper_2608_29539_gb300 import logo as Lg
+    x = [t.cuda() for t in _inputs(5, 3, 20000, 6)]
+    want, n = Lg.logo_verify_draft(*x)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        side, n_side = Lg.logo_verify_draft(*x)
+    torch.cuda.current_stream().wait_stream(stream)
+    out, n_out = torch.full_like(want, -7), torch.full_like(n, -7)
+    ws = Lg.logo_verify_draft_workspace(x[2])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        Lg.logo_verify_draft(*x, tokens=out, n_accept=n_out, workspace=ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(want, side) and torch.equal(n, n_side)
+    assert torch.equal(want, out) and torch.equal(n, n_out)
+
+
 def test_refusals():
     from paper_2608_29539_gb300 import logo as Lg
     draft, q, p, u, e = (t.cuda() for t in _inputs(2, 2, 50, 1))
