@@ -9,6 +9,7 @@ there is no CPU path.  If the library has not been built, every call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -48,6 +49,11 @@ class LogoError(RuntimeError):
 
 class Dims(ctypes.Structure):
     _fields_ = [("B", _c_int), ("T", _c_int), ("Hq", _c_int), ("Hkv", _c_int), ("D", _c_int)]
+
+
+@functools.lru_cache(maxsize=256)
+def _dims(*sizes):  # passed by value: one struct for all calls of these sizes
+    return Dims(*sizes)
 
 
 _lib = None
@@ -128,8 +134,9 @@ def _p(t):
 
 
 def _stream():
-    # the raw handle of torch.cuda.current_stream() (0.1 us; the object costs 3)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    # the raw handle of torch.cuda.current_stream() (0.1 us; the object costs 3);
+    # a call has CUDA tensors, so CUDA has been initialised
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _call(name, *args):
@@ -191,6 +198,7 @@ def logo_num_sms() -> int:
 def logo_selftest_wait_expiry(budget_ns: int) -> None:
     """Launch one warp whose bounded mbarrier wait can never complete; after
     budget_ns it records LOGO_ERR_TIMEOUT (read it with logo_get_device_status)."""
+    torch.cuda.init()  # (no tensor has done so)
     _call("logo_selftest_wait_expiry", int(budget_ns), _stream())
 
 
@@ -442,7 +450,7 @@ def logo_decode_prefix_attn(q, k_prefix, v_prefix, k_cache, v_cache, seq_len, po
         lse_c = torch.empty((Hq, cap), dtype=torch.float32, device=q.device)
     else:
         _need(lse_c, torch.float32, "lse_c", (Hq, cap))
-    dims = Dims(B, Lc, Hq, Hkv, D)
+    dims = _dims(B, Lc, Hq, Hkv, D)
     if workspace is None:
         workspace = logo_decode_prefix_workspace(q, k_prefix, k_cache, mass_in is not None)
     _call("logo_decode_prefix_attn", q.data_ptr(), k_prefix.data_ptr() if P else None,
@@ -489,7 +497,7 @@ def logo_cache_evict(k_cache, v_cache, mass, slot_pos, seq_len, n_seen, budget: 
         workspace = logo_cache_evict_workspace(k_cache)
     _call("logo_cache_evict", k_cache.data_ptr(), v_cache.data_ptr(), mass.data_ptr(), slot_pos.data_ptr(),
           seq_len.data_ptr(), n_seen.data_ptr(), mass_out.data_ptr(), slot_pos_out.data_ptr(), new_len.data_ptr(),
-          Dims(B, Lc, Hkv, Hkv, D), int(budget), int(recent), workspace.data_ptr(), workspace.nbytes, _stream())
+          _dims(B, Lc, Hkv, Hkv, D), int(budget), int(recent), workspace.data_ptr(), workspace.nbytes, _stream())
     return mass_out, slot_pos_out, new_len
 
 
