@@ -329,28 +329,30 @@ int check_evict(const logo_dims& d)
     return LOGO_OK;
 }
 
-// CTAs per (sequence, KV head), up to nearly two per SM in all (as many as are
-// resident at once): the least of what the barriers and exchanges of a cluster cost, more where
-// SMs hold two CTAs, plus a CTA's share of the rows to rank and to move, in units
-// of a row to rank (1.2 ns; moving one of D = 128 takes as long as ranking four).
-// Measured with 1 / 2 / 4 / 8 CTAs a pair (us): 16 pairs of 2100 rows, 2000 stay
-// 7.7 / 10.1 / 10.0 / 12.9; of 3000, 1500 stay 15.4 / 13.9 / 12.1 / 13.9; 4 pairs of
-// 16384, 12000 stay 60 / 36 / 23 / 18; 40 pairs of 6000, 5800 stay 12.9 / 13.4 / 15.3
-// / 32; 64 pairs of 16384, 2048 stay 68 / 46 / 39 / 61.
+// CTAs per (sequence, KV head): the least of what the barriers and exchanges of a
+// cluster cost, more where SMs hold two CTAs, plus a CTA's share of the rows to
+// rank and to move, in units of a row to rank (1.2 ns; moving one of D = 128 takes
+// as long as ranking four).  All CTAs are to be resident at once, and clusters do
+// not fill the last places of a group of SMs: 76 of four take 33.5 us where 72
+// take 24.1, 48 of six 57 where 48 of five take 40.  Measured (us) with 1 to 8 CTAs
+// a pair: 24 pairs of 6000 rows, 5800 stay 12.2 13.4 11.7 11.7 12.3 13.0 16.8 18.8;
+// 8 of 15822, 8781 stay 74 44 33 28 25 24 23 21; 40 of 6000, 5800 stay 12.7 13.5 12.0
+// 15.3 15.9 17.2 26 32; 88 of 15822 (D = 64), 8781 stay 97 70 59 74 73 72 93 93.
 int evict_ctas(int64_t pairs, const logo_dims& d, int budget)
 {
-    constexpr int64_t kCost[] = {0, 3500, 2600, 4400}, kCrowd[] = {0, 1500, 3300, 2200};
+    constexpr int64_t kCost[] = {0, 3500, 2600, 2600, 3000, 3300, 3800, 4200};
+    constexpr int64_t kCrowd[] = {0, 3000, 4000, 4000, 4100, 4900, 5100, 5300};
+    static_assert(sizeof kCost / sizeof *kCost == kEvMaxCluster, "a cost for each cluster size");
     const int64_t sms = device_sm_count();
     const int64_t work = d.T + d.D / 32ll * std::max(0, std::min(budget, d.T - budget));
     int best = 1;
     int64_t least = work;
-    // (clusters do not fill the last places of a group of SMs: 76 of four CTAs take 33.5
-    // us where 72 take 24.1)
-    for (int k = 1; 1 << k <= kEvMaxCluster && (pairs << k) * 20 <= 2 * sms * 19; ++k) {
-        const int64_t cost = kCost[k] + (pairs << k > sms ? kCrowd[k] : 0) + (work >> k);
+    for (int cs = 2; cs <= kEvMaxCluster && pairs * cs <= 2 * sms * (cs <= 4 ? 95 : 83) / 100; ++cs) {
+        const int64_t crowd = pairs * cs > sms * 9 / 10 ? kCrowd[cs - 1] : 0;
+        const int64_t cost = kCost[cs - 1] + crowd + work / cs;
         if (cost < least) {
             least = cost;
-            best = 1 << k;
+            best = cs;
         }
     }
     return best;

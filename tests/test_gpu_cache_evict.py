@@ -70,7 +70,7 @@ def test_long_caches(B, H, L, budget):
     _run(B, H, 64, L, [L] * B, budget, 200, mass, slot_pos, n_seen)
 
 
-# one CTA, clusters of two, four and eight per (sequence, KV head); the first sequences shorter than one CTA's stretch
+# one CTA and clusters of three, six and eight per (sequence, KV head); the first sequences shorter than one CTA's stretch
 @pytest.mark.parametrize("B,H,L,budget", [(40, 2, 1500, 700), (40, 2, 6000, 3000), (5, 2, 6000, 3000),
                                           (5, 1, 20000, 9000)])
 def test_few_different_weights_in_many_ctas(B, H, L, budget):
