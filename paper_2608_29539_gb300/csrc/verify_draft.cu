@@ -171,11 +171,17 @@ extern "C" int logo_verify_draft(const int32_t* draft, const float* q_draft, con
     if (!workspace || workspace_bytes < logo_verify_draft_workspace_size(B, m, V) || !aligned16(workspace))
         return LOGO_ERR_WORKSPACE;
     VdParams p{draft, q_draft, p_target, u, noise, draft_len, tokens, n_accept, B, m, V};
-    // CTAs per sequence: up to two per SM in all (as many as are resident at once),
-    // stretches of a few loads a thread at least
-    const int64_t resident = 2ll * device_sm_count();
+    // CTAs per sequence: the largest cluster of which all are resident at once (two
+    // CTAs an SM, less what clusters of this size leave free in a group of SMs), with
+    // stretches of a few loads a thread at least.  Measured (us) with 1 to 7: 57
+    // sequences, V = 60000 28.7 18.9 16.4 14.4 13.1 20.0 20.4; 40, V = 100000 42 26 20
+    // 18.5 16.1 15.2 22.3; 96, V = 60000 29.2 21.8 17.3 25.5.
+    constexpr int kFill[] = {100, 95, 95, 95, 95, 91, 83, 95};  // per cent
+    static_assert(sizeof kFill / sizeof *kFill == kVdMaxCluster, "a share for each cluster size");
+    const int64_t places = 2ll * device_sm_count();
     int cs = 1;
-    while (cs < kVdMaxCluster && static_cast<int64_t>(B) * cs * 2 <= resident && V / (cs * 2) >= 2 * kVdThreads) cs *= 2;
+    for (int c = 2; c <= kVdMaxCluster && V / c >= 2 * kVdThreads; ++c)
+        if (B <= places * kFill[c - 1] / 100 / c) cs = c;
     cudaLaunchAttribute attr{};
     const cudaLaunchConfig_t cfg = cluster_config(static_cast<unsigned>(B) * cs, kVdThreads, cs, 0,
                                                   static_cast<cudaStream_t>(stream), &attr);

@@ -44,6 +44,11 @@ def test_sizes(B, m, V):
     _check(*_inputs(B, m, V, B + m + V))
 
 
+@pytest.mark.parametrize("B,V", [(130, 2100), (96, 4001), (70, 5002), (57, 6003), (46, 7004), (36, 7205), (9, 9000)])
+def test_clusters_of_every_size(B, V):
+    _check(*_inputs(B, 2, V, B))
+
+
 def test_no_drafts():
     _check(*_inputs(6, 0, 777, 3))
 
