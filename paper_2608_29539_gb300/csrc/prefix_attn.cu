@@ -38,6 +38,7 @@
 #include "attn_common.cuh"
 #include "host_common.h"
 #include "logo_status.cuh"
+#include "prefix_sched.h"
 #include "sm100.cuh"
 
 namespace logo {
@@ -61,11 +62,6 @@ constexpr int kPaMassThreads = 256;
 // tiles, 8 KV heads, 2000 keys (15 units) 43.5 and 33.1, against 41.3 and 37.7; 10
 // row tiles, 4 KV heads, 8000 keys (17 units) 40.8 and 31.5, against 39.4 and 36.8.
 constexpr int kPaNarrow = 8, kPaNarrowCap = 18;
-// A run's start and end (its Q, the join of the warps) are counted as this many
-// tiles when the shares are cut (with 1, 2 and 3: 16 sequences of 8192 tokens, 32
-// rows 51.6, 49.8 and 50.0 us a call; 256 rows, 2048 tokens 120, 110 and 115; 128
-// sequences of 512 tokens, four rows 70.2, 70.8 and 71.9).
-constexpr int kRunCost = 2;
 constexpr int kPaMaxR = 8192;        // n_new * (Hq / Hkv) at most (the weights' row statistics in shared memory)
 
 template <int D>
@@ -81,26 +77,19 @@ struct PaCfg {
     static constexpr int kSmemBytes = kOffMerge + kMergeBytes + 1024;
 };
 
-// All runs of a call (the tiles of one segment, KV head and row tile) lie on one
-// line: the prefix's KV heads, then the own caches' (sequence, KV head, row
-// tile).  A run takes kRunCost + tiles units, its tiles the last ones.  CTA c of
-// n takes the units [total c / n, total (c + 1) / n).
-struct PaSched {
-    int K;      // length of the prefix part; 0 if there is none, or if it is wide
-    int total;  // length of the line
-    int N, PT, n, wide, rt_pre;  // rt_pre: row tiles of a prefix that is not wide
-};
-
-// What the join and the weights need to know of a sequence.
+// What the weights need to know of a sequence (base: its first unit on the line).
 struct PaSeq {
-    int row0, n, len, tiles;
+    int row0, n, len, tiles, base;
 };
 
-// A row tile's keys of one segment and KV head: the first share that holds some
-// of them, and the number of shares.
-struct PaRun {
-    int c0, n;
+// ... and the join of a packed row: where its sequence's parts are.
+struct alignas(16) PaRow {
+    int row0, base, tiles;  // tiles 0: none of its sequence's keys is seen
+    uint32_t b_rts;         // sequence, row tiles - 1 (B <= 2^24, kPaMaxR / kPaRows row tiles at most)
+    __device__ __forceinline__ int b() const { return static_cast<int>(b_rts & 0xffffffu); }
+    __device__ __forceinline__ int rts() const { return static_cast<int>(b_rts >> 24) + 1; }
 };
+static_assert(kPaMaxR / kPaRows <= 256, "PaRow holds eight bits");
 
 struct PaParams {
     CUtensorMap tm_kp, tm_vp;  // prefix [1, P, Hkv, D]
@@ -114,8 +103,7 @@ struct PaParams {
     // workspace
     PaSched* sched;
     PaSeq* seqs;               // [B]
-    int2* rows;                // [cap]: sequence of each packed row, first packed row of that sequence (-1: none of its keys are seen)
-    PaRun *run_pre, *run_own;  // [Hkv][rt_pre], [B][Hkv][rt_own_max]
+    PaRow* rows;               // [cap]
     float *o_pre, *ml_pre;     // prefix pieces: [slot][w_pre][D], [slot][w_pre][2]
     float *o_own, *ml_own;
     float* lse2;               // [Hkv][cap * G] log2 units; +infinity for a row without a key
@@ -184,18 +172,6 @@ __device__ __forceinline__ int own_units(const PaParams& p, const OwnSeq& o)
     return o.tiles > 0 ? (kRunCost + o.tiles) * o.rts * p.Hkv : 0;
 }
 
-__device__ __forceinline__ int share_start(const PaSched& s, int c)
-{
-    return static_cast<int>(static_cast<long long>(s.total) * c / s.n);
-}
-
-// The CTA whose share holds tile u: the last c with floor(total c / n) <= u
-// (n <= total: no share is empty).
-__device__ __forceinline__ int share_owner(const PaSched& s, int u)
-{
-    return static_cast<int>(((u + 1ll) * s.n - 1) / s.total);
-}
-
 // One piece: key tiles [t0, t1) of a segment for one row tile and KV head.
 struct PaPiece {
     int own;
@@ -207,8 +183,6 @@ struct PaPiece {
 
 struct PaIter {
     int u, u1, base, c, b;  // position, end, first unit of sequence b, share, b
-    PaRun* run;             // of the last piece: where its run is noted,
-    int run_end;            // ... and the run's last unit
 
     __device__ __forceinline__ bool next(const PaParams& p, const PaSched& s, const OwnSeq* seqs, PaPiece* it)
     {
@@ -227,7 +201,6 @@ struct PaIter {
                 it->seg_row0 = 0;
                 it->len = p.P;
                 it->slot = k + c;
-                run = p.run_pre + k;
             } else {
                 OwnSeq o = seq_at(p, seqs, b);
                 int units = own_units(p, o);
@@ -250,20 +223,12 @@ struct PaIter {
                 it->len = o.len;
                 const int id = (b * p.Hkv + it->kvh) * p.rt_own_max + r;
                 it->slot = id + c;
-                run = p.run_own + id;
             }
             it->t0 = max(0, u - first - kRunCost);
             u = min(u1, first + kRunCost + tiles);
             it->t1 = max(0, u - first - kRunCost);
-            run_end = first + kRunCost + tiles - 1;
             if (it->t1 > it->t0) return true;  // else the share ends in the run's overhead
         }
-    }
-
-    // The piece that starts a run writes down where the run's pieces are.
-    __device__ __forceinline__ void note_run(const PaSched& s, const PaPiece& it) const
-    {
-        if (it.t0 == 0) *run = PaRun{c, share_owner(s, run_end) - c + 1};
     }
 };
 
@@ -686,6 +651,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
         s.total += sh_scan[k];
     }
     s.n = min(p.nCta, s.total);
+    s.rate = s.total > 0 ? static_cast<float>(s.n) / static_cast<float>(s.total) : 0.f;
     PaIter iter;
     iter.c = cta;
     iter.u = cta < s.n ? share_start(s, cta) : 0;
@@ -707,10 +673,13 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
     }
     if (cta == s.n % p.nCta) {  // for the join and the weights (by a CTA without a share, if there is one)
         if (tid == 0) *p.sched = s;
+        int base = excl;
         for (int b = tb0; b < tb1; ++b) {
             const OwnSeq o = seq_at(p, seqs, b);
-            p.seqs[b] = PaSeq{o.row0, o.n, o.len, o.tiles};
-            for (int r = o.row0; r < o.row0 + o.n; ++r) p.rows[r] = make_int2(b, o.tiles > 0 ? o.row0 : -1);
+            p.seqs[b] = PaSeq{o.row0, o.n, o.len, o.tiles, base};
+            const PaRow row{o.row0, base, o.tiles, static_cast<uint32_t>(b) | static_cast<uint32_t>(o.rts - 1) << 24};
+            for (int r = o.row0; r < o.row0 + o.n; ++r) p.rows[r] = row;
+            base += own_units(p, o);
         }
     }
     __syncwarp();  // whole warps from here on (setmaxnreg wants them)
@@ -802,10 +771,7 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
                 sh_vis[qb][lane] = vis;
                 if (lane == 0) sh_piece[qb] = it;
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(smem_u32(&bar_q_full[qb]));
-                    if (more) iter.note_run(s, it);
-                }
+                if (lane == 0) mbar_arrive(smem_u32(&bar_q_full[qb]));
                 if (!more) break;
             }
         } else if (warp == kPaWarps + 1 + kPaPlanners && p.wq) {
@@ -866,15 +832,16 @@ __device__ __forceinline__ PaPre pa_pre(const PaParams& p)
 }
 
 // Parts of packed row r, head g of KV head kvh: x[0] of the prefix, x[1] of the
-// cache of sequence b, whose first packed row is row0 (-1: no own key is seen).
+// cache of sequence b, whose first packed row is row0 and whose runs are rts row
+// tiles a KV head from unit `base` on (tiles 0: no own key is seen).
 template <int D>
 __device__ __forceinline__ void pa_parts(const PaParams& p, const PaSched& s, const PaPre& pre, int r, int b, int row0,
-                                         int kvh, int g, PaParts (&x)[2])
+                                         int base, int tiles, int rts, int kvh, int g, PaParts (&x)[2])
 {
     x[0] = x[1] = PaParts{nullptr, nullptr, nullptr, 0, 0, 0};
-    if (row0 >= 0) {
+    if (tiles > 0) {
         const int m = (r - row0) * p.G + g, id = (b * p.Hkv + kvh) * p.rt_own_max + m / kPaRows;
-        const PaRun run = p.run_own[id];
+        const PaRun run = run_of(s, base + (kvh * rts + m / kPaRows) * (kRunCost + tiles), tiles);
         const int64_t at = static_cast<int64_t>(id + run.c0) * p.w_own + m % kPaRows;
         x[1] = PaParts{p.ml_own + 2 * at, p.ml_own + 2 * at + 1, p.o_own + at * D, 2 * p.w_own,
                        static_cast<int64_t>(p.w_own) * D, run.n};
@@ -886,7 +853,7 @@ __device__ __forceinline__ void pa_parts(const PaParams& p, const PaSched& s, co
         x[0] = PaParts{p.wm_part + at, p.wl_part + at, p.wo_part + at * D, step, step * D, pre.ns};
     } else if (s.K > 0) {
         const int m = r * p.G + g, id = kvh * s.rt_pre + m / kPaRows;
-        const PaRun run = p.run_pre[id];
+        const PaRun run = run_of(s, id * (kRunCost + s.PT), s.PT);
         const int64_t at = static_cast<int64_t>(id + run.c0) * p.w_pre + m % kPaRows;
         x[0] = PaParts{p.ml_pre + 2 * at, p.ml_pre + 2 * at + 1, p.o_pre + at * D, 2 * p.w_pre,
                        static_cast<int64_t>(p.w_pre) * D, run.n};
@@ -911,7 +878,7 @@ __device__ __forceinline__ void pa_join(const PaParams& p, int block)
     const int r = min(task / p.Hq, p.cap - 1), h = task % p.Hq, kvh = h / p.G, g = h % p.G;
     // loads that depend on nothing, together
     const PaSched s = *p.sched;
-    const int2 row = p.rows[r];
+    const PaRow row = p.rows[r];
     const PaPre pre = pa_pre(p);
     const bool active = task / p.Hq < s.N;
     float acc[E], M = -INFINITY, Ls = 0.f;
@@ -919,7 +886,7 @@ __device__ __forceinline__ void pa_join(const PaParams& p, int block)
     for (int i = 0; i < E; ++i) acc[i] = 0.f;
     if (active) {
         PaParts x[2];
-        pa_parts<D>(p, s, pre, r, row.x, row.y, kvh, g, x);
+        pa_parts<D>(p, s, pre, r, row.b(), row.row0, row.base, row.tiles, row.rts(), kvh, g, x);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             for (int e0 = sub * CH; e0 < x[k].n; e0 += WPR * CH) {
@@ -1041,13 +1008,14 @@ __device__ __forceinline__ void pa_mass(const PaParams& p, int block, int chunks
     load(key, sub);
     if constexpr (FUSED) {
         // eight lanes a row
+        const int rts = (q.n * p.G + kPaRows - 1) / kPaRows;
         const int l8 = tid & 7;
         for (int m0 = 0; m0 < nm; m0 += kPaMassThreads / 8) {
             const int m = m0 + (tid >> 3);
             float M = -INFINITY, Ls = 0.f;
             if (m < nm) {
                 PaParts part[2];
-                pa_parts<D>(p, s, pre, q.row0 + m / p.G, b, q.row0, kvh, m % p.G, part);
+                pa_parts<D>(p, s, pre, q.row0 + m / p.G, b, q.row0, q.base, q.tiles, rts, kvh, m % p.G, part);
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
                     for (int e = l8; e < part[k].n; e += 8) {
@@ -1212,9 +1180,7 @@ size_t prefix_layout(const logo_dims& d, int n_new, int P, bool with_mass, char*
     };
     char* sched = take(sizeof(PaSched));
     char* seqs = take(d.B * sizeof(PaSeq));
-    char* row_info = take(cap * sizeof(int2));
-    char* run_pre = take(rt_narrow * d.Hkv * sizeof(PaRun));
-    char* run_own = take(runs_own * sizeof(PaRun));
+    char* row_info = take(cap * sizeof(PaRow));
     char* ml_pre = take(slots_pre * w_pre * 8);
     char* o_pre = take(slots_pre * w_pre * d.D * 4);
     char* ml_own = take(slots_own * w_own * 8);
@@ -1231,9 +1197,7 @@ size_t prefix_layout(const logo_dims& d, int n_new, int P, bool with_mass, char*
     if (p) {
         p->sched = reinterpret_cast<PaSched*>(sched);
         p->seqs = reinterpret_cast<PaSeq*>(seqs);
-        p->rows = reinterpret_cast<int2*>(row_info);
-        p->run_pre = reinterpret_cast<PaRun*>(run_pre);
-        p->run_own = reinterpret_cast<PaRun*>(run_own);
+        p->rows = reinterpret_cast<PaRow*>(row_info);
         p->ml_pre = reinterpret_cast<float*>(ml_pre);
         p->o_pre = reinterpret_cast<float*>(o_pre);
         p->ml_own = reinterpret_cast<float*>(ml_own);
