@@ -719,10 +719,10 @@ __global__ void __launch_bounds__(kPaThreads, 1) pa_rows_kernel(const __grid_con
                     }
                 }
             }
-            if (!ok) {  // let copies already issued land before the CTA exits
-                for (int k = max(0, n - C::kStages); k < n; ++k)
-                    mbar_wait_drain(smem_u32(&bar_kv_full[k % C::kStages]), (k / C::kStages) & 1);
-            }
+            // all copies land before the CTA exits (the products may have given up on
+            // one after the last was issued; else this finds them all there)
+            for (int k = max(0, n - C::kStages); k < n; ++k)
+                mbar_wait_drain(smem_u32(&bar_kv_full[k % C::kStages]), (k / C::kStages) & 1);
         } else if (warp > kPaWarps && warp <= kPaWarps + kPaPlanners) {
             // -------------------------------------------------- pieces and Q: the
             // planners take the pieces in turn, so that one's loads are in flight
