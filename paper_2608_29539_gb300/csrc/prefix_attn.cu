@@ -860,6 +860,11 @@ __device__ __forceinline__ void pa_parts(const PaParams& p, const PaSched& s, co
     }
 }
 
+// The maximum of a part with row sum l: -infinity where the row saw no key of it.
+// Maxima skip NaN, sums do not: a part whose logits were all NaN has the maximum of
+// an empty one, and must not pass for it.
+__device__ __forceinline__ float part_max(float m, float l) { return m == -INFINITY && l != l ? 0.f : m; }
+
 // lse of a row in log2 units for the weights exp2(x - lse2): x = -inf where the
 // row sees nothing, and a row that sees no key at all gets weights 0.
 __device__ __forceinline__ float weight_lse2(float M, float Ls) { return M == -INFINITY ? INFINITY : M + log2f(Ls); }
@@ -907,7 +912,7 @@ __device__ __forceinline__ void pa_join(const PaParams& p, int block)
                 }
 #pragma unroll
                 for (int e = 0; e < CH; ++e) {
-                    if (e0 + e >= x[k].n) vm[e] = -INFINITY;
+                    vm[e] = e0 + e < x[k].n ? part_max(vm[e], vl[e]) : -INFINITY;
                     top = fmaxf(top, vm[e]);
                 }
                 if (top == -INFINITY) continue;
@@ -952,7 +957,7 @@ __device__ __forceinline__ void pa_join(const PaParams& p, int block)
         }
     }
     if (active && sub == 0) {
-        const float inv = Ls > 0.f ? 1.0f / Ls : 0.f;
+        const float inv = Ls == 0.f ? 0.f : 1.0f / Ls;  // (0: no key is seen)
         uint32_t* dst = reinterpret_cast<uint32_t*>(p.o + (static_cast<int64_t>(r) * p.Hq + h) * D + lane * E);
 #pragma unroll
         for (int i = 0; i < E; i += 2) dst[i / 2] = cvt_bf16x2(acc[i] * inv, acc[i + 1] * inv);
@@ -1019,7 +1024,8 @@ __device__ __forceinline__ void pa_mass(const PaParams& p, int block, int chunks
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
                     for (int e = l8; e < part[k].n; e += 8) {
-                        const float vm = __ldg(part[k].m + e * part[k].s_ml), vl = __ldg(part[k].l + e * part[k].s_ml);
+                        const float vl = __ldg(part[k].l + e * part[k].s_ml);
+                        const float vm = part_max(__ldg(part[k].m + e * part[k].s_ml), vl);
                         if (vm == -INFINITY) continue;
                         const float top = fmaxf(M, vm);
                         Ls = Ls * ex2_approx(M - top) + vl * ex2_approx(vm - top);
