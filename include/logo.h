@@ -216,6 +216,8 @@ LOGO_API int logo_decode_global_sparse_attn(const logo_bf16* q, const logo_bf16*
  *       themselves.  Rows s >= len may hold anything.  The order of the other
  *       rows does not matter (logo_cache_evict changes it).
  *   A row that sees no key gets o = 0 and lse = -infinity.
+ *   What a row does not see does not enter its results, infinities and NaN
+ *   included; what it does see shows in them (a NaN query: o and lse are NaN).
  * Out: o_c [B*n_new, Hq, D] bf16 packed and lse_c [Hq, B*n_new] float32 packed
  *      (may be NULL): rows >= n_sel_total are left untouched.
  *      mass_out [B, Hkv, L] float32 (NULL: not wanted; then mass_in is not

@@ -1,8 +1,11 @@
-"""logo_decode_prefix_attn with infinities and NaN: in what a row sees, or in its
-query, they show in its output.  """
+"""logo_decode_prefix_attn with infinities and NaN: in the keys and values of
+drafts that a row does not see they change nothing; in what a row sees, or in its
+query, they show in its output.  Bounds as in test_gpu_prefix_attn."""
+import numpy as np
 import pytest
 import torch
 
+import serving_ref as R
 import test_gpu_prefix_attn as T
 
 pytestmark = pytest.mark.gpu
@@ -20,6 +23,47 @@ def _call(q, kp, vp, kc, vc, lens, pos, cu, ns, mass):
     torch.cuda.synchronize()
     assert Lg.logo_get_device_status() == 0
     return out
+
+
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("D,G,n,P", [(128, 4, 3, 0), (128, 2, 8, 70), (64, 1, 5, 0), (64, 16, 2, 200), (128, 9, 7, 0)])
+def test_unseen_drafts_change_nothing(D, G, n, P, where):
+    """Sequence b's draft c[b] and all after it hold infinities and NaN; the rows
+    before it are compared, of up to 63 (row, head) pairs a KV head."""
+    Hkv, L = 2, 300
+    lens = [n, 31 + n, 128, 129, 160, 257, 300]
+    B = len(lens)
+    q, kp, vp, kc, vc = T._inputs(B, n, G * Hkv, Hkv, D, P, L, 40 + n)
+    mass = torch.rand((B, Hkv, L), generator=torch.Generator().manual_seed(1))
+    pos, cu, ns, rows = T._pack(torch.ones(B, n, dtype=torch.bool))
+    first = [1 + b % (n - 1) for b in range(B)]
+    ref = R.prefix_attn(q, kp, vp, kc, vc, lens, rows, mass)
+    bad = kc if where == "k" else vc
+    for b in range(B):
+        for j in range(first[b], n):
+            row = bad[b, lens[b] - n + j]
+            if (b + j) % 3 == 0:
+                row[:] = NAN
+            elif (b + j) % 3 == 1:
+                row[:, ::5] = INF
+                row[:, 1::7] = -INF
+            else:
+                row[:, (11 * b + j) % D] = -INF
+    o, lse, m = _call(q, kp, vp, kc, vc, lens, pos, cu, ns, mass)
+    keep = [r for r, (b, i) in enumerate(rows) if i < first[b]]
+    T._check(o[keep], lse[:, keep], None, {k: ref[k][:, keep] if k == "lse" else ref[k][keep] for k in ("o", "lse", "absv")}
+             | {"big": ref["big"]}, keep, D, lens)
+    for r, (b, i) in enumerate(rows):
+        for h in range(G * Hkv):
+            got = o[r, h].float().cpu()
+            if where == "v":  # a seen row's infinity or NaN is in its column, and only there
+                seen = torch.stack([vc[b, lens[b] - n + j, h // G] for j in range(i + 1)]).float()
+                assert torch.equal(~torch.isfinite(got), ~torch.isfinite(seen).all(0)), (r, h)
+    if where == "v":  # weights do not depend on V
+        for b, length in enumerate(lens):
+            want, add = ref["mass"][b, :, :length], ref["add"][b, :, :length]
+            err = np.abs(m[b, :, :length].cpu().numpy().astype(np.float64) - want)
+            assert (err <= (2 * 2.0 ** -24 * D * ref["big"] + 2.0 ** -18) * add + 2.0 ** -22 * want).all()
 
 
 @pytest.mark.parametrize("P,wide", [(0, False), (300, False), (None, True)])
