@@ -1162,21 +1162,17 @@ size_t global_bwd_ws_layout(const logo_dims& d, char* base, BwdWs* ws)
 template <int D, bool GLOBAL>
 int launch_bwd(const BwdParams& prm, cudaStream_t st)
 {
-    static bool attr_done = false;  // benign race: setting the attribute twice is harmless
+    static OncePerDevice limit;
     const int n_items = prm.B * prm.nblk * prm.Hkv;
     const int grid = max(1, min(n_items, device_sm_count()));
     if (D == 128) {
-        if (!attr_done) {
-            if (set_smem_limit(attn_bwd2_kernel<GLOBAL>, Bwd2Cfg::kSmemBytes) != cudaSuccess) return LOGO_ERR_CUDA;
-            attr_done = true;
-        }
+        if (limit([] { return set_smem_limit(attn_bwd2_kernel<GLOBAL>, Bwd2Cfg::kSmemBytes); }) != cudaSuccess)
+            return LOGO_ERR_CUDA;
         attn_bwd2_kernel<GLOBAL><<<grid, Bwd2Cfg::kThreads, Bwd2Cfg::kSmemBytes, st>>>(prm);
     } else {
         using C = BwdCfg<D>;
-        if (!attr_done) {
-            if (set_smem_limit(attn_bwd_kernel<D, GLOBAL>, C::kSmemBytes) != cudaSuccess) return LOGO_ERR_CUDA;
-            attr_done = true;
-        }
+        if (limit([] { return set_smem_limit(attn_bwd_kernel<D, GLOBAL>, C::kSmemBytes); }) != cudaSuccess)
+            return LOGO_ERR_CUDA;
         attn_bwd_kernel<D, GLOBAL><<<grid, 192, C::kSmemBytes, st>>>(prm);
     }
     return cudaGetLastError() == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;

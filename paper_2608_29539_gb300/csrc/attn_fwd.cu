@@ -966,11 +966,9 @@ template <int D, bool GLOBAL>
 int launch_fwd(const FwdParams& prm, int n_items_upper, cudaStream_t st)
 {
     using C = FwdCfg<D>;
-    static bool attr_done = false;  // benign race: setting the attribute twice is harmless
-    if (!attr_done) {
-        if (set_smem_limit(attn_fwd_kernel<D, GLOBAL>, C::kSmemBytes) != cudaSuccess) return LOGO_ERR_CUDA;
-        attr_done = true;
-    }
+    static OncePerDevice limit;
+    if (limit([] { return set_smem_limit(attn_fwd_kernel<D, GLOBAL>, C::kSmemBytes); }) != cudaSuccess)
+        return LOGO_ERR_CUDA;
     const int grid = max(1, min(n_items_upper, device_sm_count()));
     attn_fwd_kernel<D, GLOBAL><<<grid, C::kThreads, C::kSmemBytes, st>>>(prm);
     return cudaGetLastError() == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;

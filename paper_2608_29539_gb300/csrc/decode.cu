@@ -471,12 +471,10 @@ int check_decode(const logo_dims& d)
 template <int D, bool RING>
 int launch_decode(DecParams& prm, cudaStream_t st)
 {
-    static bool attr_done = false;  // benign race: setting the attribute twice is harmless
-    if (!attr_done) {
-        if (set_smem_limit(decode_attn_kernel<D, RING>, DecCfg<D>::smem_bytes(kDecMaxGroup)) != cudaSuccess)
-            return LOGO_ERR_CUDA;
-        attr_done = true;
-    }
+    static OncePerDevice limit;
+    if (limit([] { return set_smem_limit(decode_attn_kernel<D, RING>, DecCfg<D>::smem_bytes(kDecMaxGroup)); }) !=
+        cudaSuccess)
+        return LOGO_ERR_CUDA;
     // as many resident CTAs as fit (each keeps up to three sub-tiles' K/V loads in
     // flight); the merge buffer, and so the fit, depends on the group size
     const int group = prm.Hq / prm.Hkv;

@@ -4,6 +4,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 
@@ -27,12 +28,34 @@ bool encode_bf16_4d(CUtensorMap* map, const void* base, uint64_t d0, uint64_t d1
 // Round up to a multiple of `a`.
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-// Allow a kernel more than 48 KB of dynamic shared memory (once per kernel).
+// Allow a kernel more than 48 KB of dynamic shared memory, on the current device.
 template <typename K>
 inline cudaError_t set_smem_limit(K kernel, int bytes)
 {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
+
+// For a launcher's static: runs `set` once per device, as a kernel's limit holds on
+// one device only.  (Two threads may both run it, which is harmless; a device past
+// the 64th gets it every time.)
+class OncePerDevice {
+public:
+    template <typename F>
+    cudaError_t operator()(F set)
+    {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+        if (done_.load(std::memory_order_acquire) & bit) return cudaSuccess;
+        e = set();
+        if (e == cudaSuccess) done_.fetch_or(bit, std::memory_order_release);
+        return e;
+    }
+
+private:
+    std::atomic<uint64_t> done_{0};
+};
 
 // Per-translation-unit status readers (each .cu owns one device word).
 int select_tu_status(int clear);

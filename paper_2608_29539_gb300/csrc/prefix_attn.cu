@@ -1288,16 +1288,11 @@ template <int D>
 int launch_prefix(PaParams& p, cudaStream_t st)
 {
     using C = PaCfg<D>;
-    static bool attr_done = false;  // benign race: setting the attribute twice is harmless
-    if (!attr_done) {
-        if (set_smem_limit(pa_rows_kernel<D, false>, C::kSmemBytes) != cudaSuccess ||
-            set_smem_limit(pa_rows_kernel<D, true>, C::kSmemBytes) != cudaSuccess)
-            return LOGO_ERR_CUDA;
-        attr_done = true;
-    }
+    const auto rows_kernel = p.n_new > 1 ? pa_rows_kernel<D, true> : pa_rows_kernel<D, false>;
+    static OncePerDevice limit[2];
+    if (limit[p.n_new > 1]([&] { return set_smem_limit(rows_kernel, C::kSmemBytes); }) != cudaSuccess) return LOGO_ERR_CUDA;
     p.n_sm = device_sm_count();
-    if (p.n_new > 1) pa_rows_kernel<D, true><<<p.nCta, kPaThreads, C::kSmemBytes, st>>>(p);
-    else pa_rows_kernel<D, false><<<p.nCta, kPaThreads, C::kSmemBytes, st>>>(p);
+    rows_kernel<<<p.nCta, kPaThreads, C::kSmemBytes, st>>>(p);
     if (p.wq) {
         const int64_t rts = (static_cast<int64_t>(p.cap) * p.G + 127) / 128;
         TileShares t{};
