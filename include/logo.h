@@ -260,8 +260,8 @@ LOGO_API int logo_decode_prefix_attn(const logo_bf16* q, const logo_bf16* k_pref
  *   k_cache, v_cache [B, L, Hkv, D] bf16: changed in place, rows >= end left as
  *   they are.  mass, slot_pos are read; mass_out, slot_pos_out [B, Hkv, L]
  *   receive entries < end (the others untouched) and may be mass / slot_pos.
- *   new_len [B] int32 = end (not seq_len itself: it is read throughout the
- *   call).  budget in [1, L], recent in [0, budget].
+ *   new_len [B] int32 = end (not seq_len or n_seen itself: they are read
+ *   throughout the call).  budget in [1, L], recent in [0, budget].
  *   dims: B, T = L, Hkv, D in {64, 128} (Hq is not read).
  *   Results are exact and deterministic.  Workspace:
  *   logo_cache_evict_workspace_size(dims) bytes.

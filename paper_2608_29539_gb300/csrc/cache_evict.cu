@@ -383,7 +383,7 @@ extern "C" int logo_cache_evict(logo_bf16* k_cache, logo_bf16* v_cache, const fl
     if (rc != LOGO_OK) return rc;
     if (!k_cache || !v_cache || !mass || !slot_pos || !seq_len || !n_seen || !mass_out || !slot_pos_out || !new_len)
         return LOGO_ERR_INVALID_ARG;
-    if (new_len == seq_len) return LOGO_ERR_INVALID_ARG;
+    if (new_len == seq_len || new_len == n_seen) return LOGO_ERR_INVALID_ARG;  // CTAs that start later read both
     if (budget < 1 || budget > dims.T || recent < 0 || recent > budget) return LOGO_ERR_INVALID_ARG;
     if (!aligned16(k_cache) || !aligned16(v_cache)) return LOGO_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < evict_ws_bytes(dims) || !aligned16(workspace)) return LOGO_ERR_WORKSPACE;
