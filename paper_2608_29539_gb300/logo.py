@@ -168,8 +168,15 @@ def dims_of(q: torch.Tensor, k: torch.Tensor) -> Dims:
     return Dims(B, T, Hq, k.shape[2], D)
 
 
+def _given_workspace(ws):
+    if not ws.is_cuda or not ws.is_contiguous():  # the library takes an address and a size
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    return ws
+
+
 def _workspace(nbytes: int, device, ws=None):
     if ws is not None:
+        _given_workspace(ws)
         if ws.numel() * ws.element_size() < nbytes:
             raise ValueError("workspace too small")
         return ws
@@ -453,6 +460,8 @@ def logo_decode_prefix_attn(q, k_prefix, v_prefix, k_cache, v_cache, seq_len, po
     dims = _dims(B, Lc, Hq, Hkv, D)
     if workspace is None:
         workspace = logo_decode_prefix_workspace(q, k_prefix, k_cache, mass_in is not None)
+    else:
+        _given_workspace(workspace)
     _call("logo_decode_prefix_attn", q.data_ptr(), k_prefix.data_ptr() if P else None,
           v_prefix.data_ptr() if P else None, k_cache.data_ptr(), v_cache.data_ptr(), seq_len.data_ptr(),
           pos.data_ptr(), cu_q.data_ptr(), n_sel_total.data_ptr(), o_c.data_ptr(), lse_c.data_ptr(),
@@ -495,6 +504,8 @@ def logo_cache_evict(k_cache, v_cache, mass, slot_pos, seq_len, n_seen, budget: 
         _need(new_len, torch.int32, "new_len", (B,))
     if workspace is None:
         workspace = logo_cache_evict_workspace(k_cache)
+    else:
+        _given_workspace(workspace)
     _call("logo_cache_evict", k_cache.data_ptr(), v_cache.data_ptr(), mass.data_ptr(), slot_pos.data_ptr(),
           seq_len.data_ptr(), n_seen.data_ptr(), mass_out.data_ptr(), slot_pos_out.data_ptr(), new_len.data_ptr(),
           _dims(B, Lc, Hkv, Hkv, D), int(budget), int(recent), workspace.data_ptr(), workspace.nbytes, _stream())
@@ -535,6 +546,8 @@ def logo_verify_draft(draft, q_draft, p_target, u, noise, draft_len=None, tokens
         _need(n_accept, torch.int32, "n_accept", (B,))
     if workspace is None:
         workspace = logo_verify_draft_workspace(p_target)
+    else:
+        _given_workspace(workspace)
     _call("logo_verify_draft", draft.data_ptr() if m else None, q_draft.data_ptr() if m else None,
           p_target.data_ptr(), u.data_ptr() if m else None, noise.data_ptr(),
           None if draft_len is None else draft_len.data_ptr(), tokens.data_ptr(), n_accept.data_ptr(), B, m, V,
