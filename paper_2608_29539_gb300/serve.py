@@ -50,7 +50,10 @@ class ServeBatch:
 
     k_prefix / v_prefix [P, Hkv, D] bf16, or None.  Positions count from the
     prefix's first token.  At most slack / n_new + 1 steps may pass without an
-    eviction: a cache holds budget + n_new + slack rows."""
+    eviction: a cache holds budget + n_new + slack rows.  A step that might not fit
+    is refused, counting rejected drafts too, as their number stays on the device.
+    Replays of a captured CUDA graph are not seen here: once a call was captured
+    nothing is refused, and a step that finds no room overwrites the latest rows."""
 
     def __init__(self, cfg: ServeConfig, k_prefix=None, v_prefix=None, device="cuda"):
         if cfg.budget < 1 or cfg.n_new < 1 or cfg.slack < 0 or not 0 <= cfg.recent <= cfg.budget:
@@ -78,6 +81,8 @@ class ServeBatch:
         self.new_len = z((c.B,), torch.int32)
         self._b = torch.arange(c.B, device=dev)[:, None]
         self._i = torch.arange(c.n_new, device=dev, dtype=torch.int32)
+        self._rows_used = 0     # at most this many rows of any cache hold a token
+        self._captured = False  # whether a graph holds some of the calls
         dims = L.Dims(c.B, self.rows, c.Hq, c.Hkv, c.D)
         lib = L.lib()
         nbytes = max(int(lib.logo_decode_prefix_workspace_size(dims, c.n_new, P, 1)),
@@ -85,15 +90,25 @@ class ServeBatch:
                      int(lib.logo_select_workspace_size(L.Dims(c.B, c.n_new, 1, 1, 64))))
         self.ws = torch.empty((max(nbytes, 256),), dtype=torch.uint8, device=dev)  # the calls are stream-ordered
 
+    def _counts(self):
+        """Are all calls seen here?"""
+        self._captured |= self.k.is_cuda and torch.cuda.is_current_stream_capturing()
+        return not self._captured
+
     def append(self, k_new, v_new):
         """K and V [B, n_new, Hkv, D] of the new tokens into the caches' next rows."""
+        n = self.cfg.n_new
+        if self._counts() and self._rows_used + n > self.rows:
+            raise ValueError(f"{n} more rows may not fit: up to {self._rows_used} of {self.rows} are in use; evict first")
+        self.seq_len.clamp_(max=self.rows - n)  # (a replay may come here with full caches)
         slots = (self.seq_len[:, None] + self._i).long()
         self.k[self._b, slots] = k_new
         self.v[self._b, slots] = v_new
         at = (self.n_seen[:, None] + self._i)[:, None].expand(-1, self.cfg.Hkv, -1)
         self.slot_pos.scatter_(2, slots[:, None].expand(-1, self.cfg.Hkv, -1), at)
-        self.seq_len += self.cfg.n_new
-        self.n_seen += self.cfg.n_new
+        self.seq_len += n
+        self.n_seen += n
+        self._rows_used += n
 
     def step(self, q, k_new, v_new, gate_p):
         """q [B, n_new, Hq, D], k_new / v_new [B, n_new, Hkv, D] bf16, gate_p
@@ -124,3 +139,5 @@ class ServeBatch:
         L.logo_cache_evict(self.k, self.v, self.mass, self.slot_pos, self.seq_len, self.n_seen, c.budget, c.recent,
                            new_len=self.new_len, workspace=self.ws)
         self.seq_len, self.new_len = self.new_len, self.seq_len
+        self._counts()
+        self._rows_used = min(self._rows_used, c.budget)
