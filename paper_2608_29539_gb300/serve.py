@@ -134,10 +134,11 @@ class ServeBatch:
         return tokens, n_accept
 
     def evict(self):
-        """Every cache back to at most `budget` rows."""
+        """Every cache back to at most `budget` rows.  Lengths keep their place in
+        memory, so that the call can be part of a captured graph."""
         c = self.cfg
         L.logo_cache_evict(self.k, self.v, self.mass, self.slot_pos, self.seq_len, self.n_seen, c.budget, c.recent,
                            new_len=self.new_len, workspace=self.ws)
-        self.seq_len, self.new_len = self.new_len, self.seq_len
+        self.seq_len.copy_(self.new_len)
         self._counts()
         self._rows_used = min(self._rows_used, c.budget)

@@ -58,3 +58,15 @@ def test_full_caches_are_not_written_past(serve):
     assert batch.n_seen.tolist() == [27, 27]
     assert batch.k[0, :, 0, 0].tolist() == [1, 1, 1, 2, 2, 2, 3, 3, 9, 9, 9]
     assert batch.slot_pos[0, 0, 8:].tolist() == [24, 25, 26]
+
+
+def test_an_eviction_keeps_the_lengths_where_they_are(serve, monkeypatch):
+    """A graph's replays read and write the buffers of the capture."""
+    _evict(serve, monkeypatch)
+    batch = _batch(serve, n=3, budget=4, slack=2)
+    at = batch.seq_len.data_ptr(), batch.new_len.data_ptr(), batch.n_seen.data_ptr()
+    for want in ([3, 3], [4, 4], [4, 4]):
+        batch.append(*_new(2, 3))
+        batch.evict()
+        assert batch.seq_len.tolist() == want
+        assert (batch.seq_len.data_ptr(), batch.new_len.data_ptr(), batch.n_seen.data_ptr()) == at
