@@ -82,6 +82,7 @@ class ServeBatch:
         self._b = torch.arange(c.B, device=dev)[:, None]
         self._i = torch.arange(c.n_new, device=dev, dtype=torch.int32)
         self._rows_used = 0     # at most this many rows of any cache hold a token
+        self._latest_last = True  # the latest step's rows are the caches' last ones, and all there
         self._captured = False  # whether a graph holds some of the calls
         dims = L.Dims(c.B, self.rows, c.Hq, c.Hkv, c.D)
         lib = L.lib()
@@ -99,7 +100,7 @@ class ServeBatch:
         """K and V [B, n_new, Hkv, D] of the new tokens into the caches' next rows."""
         n = self.cfg.n_new
         if self._counts() and self._rows_used + n > self.rows:
-            raise ValueError(f"{n} more rows may not fit: up to {self._rows_used} of {self.rows} are in use; evict first")
+            raise ValueError(f"{n} more rows may not fit, {self._rows_used} of {self.rows} may be in use: evict first")
         self.seq_len.clamp_(max=self.rows - n)  # (a replay may come here with full caches)
         slots = (self.seq_len[:, None] + self._i).long()
         self.k[self._b, slots] = k_new
@@ -109,6 +110,7 @@ class ServeBatch:
         self.seq_len += n
         self.n_seen += n
         self._rows_used += n
+        self._latest_last = True
 
     def step(self, q, k_new, v_new, gate_p):
         """q [B, n_new, Hq, D], k_new / v_new [B, n_new, Hkv, D] bf16, gate_p
@@ -126,8 +128,12 @@ class ServeBatch:
     def verify(self, draft, q_draft, p_target, u, noise):
         """The step's drafts (n_new - 1 per sequence) against the target's
         probabilities [B, n_new, V]; the rejected tokens leave the caches.
-        Returns (tokens [B, n_new], n_accept [B])."""
+        Returns (tokens [B, n_new], n_accept [B]).  Once a step and before evict,
+        which moves the rows that are dropped from the end here."""
+        if self._counts() and self.cfg.n_new > 1 and not self._latest_last:
+            raise ValueError("the drafts were verified, or the caches cut, since the last step")
         tokens, n_accept = L.logo_verify_draft(draft, q_draft, p_target, u, noise, workspace=self.ws)
+        self._latest_last = False
         dropped = self.cfg.n_new - 1 - n_accept
         self.seq_len -= dropped
         self.n_seen -= dropped
@@ -141,4 +147,5 @@ class ServeBatch:
                            new_len=self.new_len, workspace=self.ws)
         self.seq_len.copy_(self.new_len)
         self._counts()
+        self._latest_last = False
         self._rows_used = min(self._rows_used, c.budget)

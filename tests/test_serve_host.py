@@ -70,3 +70,50 @@ def test_an_eviction_keeps_the_lengths_where_they_are(serve, monkeypatch):
         batch.evict()
         assert batch.seq_len.tolist() == want
         assert (batch.seq_len.data_ptr(), batch.new_len.data_ptr(), batch.n_seen.data_ptr()) == at
+
+
+def _verify(serve, monkeypatch, accepted):
+    def verdict(draft, q_draft, p_target, u, noise, draft_len=None, workspace=None):
+        if draft is None:
+            raise ValueError("draft must be a CUDA tensor")
+        tokens = torch.zeros(draft.shape[0], draft.shape[1] + 1, dtype=torch.int32)
+        return tokens, torch.tensor(accepted, dtype=torch.int32)
+    monkeypatch.setattr(serve.L, "logo_verify_draft", verdict)
+    args = torch.zeros(2, 2, dtype=torch.int32), None, None, None, None
+    return lambda batch: batch.verify(*args)
+
+
+def test_drafts_are_verified_once_and_before_the_cut(serve, monkeypatch):
+    """The rejected drafts' rows are dropped from the caches' ends, which holds until an
+    eviction moves rows, and once."""
+    _evict(serve, monkeypatch)
+    verify = _verify(serve, monkeypatch, [0, 1])
+    batch = _batch(serve, n=3, budget=4, slack=4)
+    for start in ([0, 0], [1, 2]):
+        batch.append(*_new(2, 3))
+        assert batch.seq_len.tolist() == [a + 3 for a in start]
+        with pytest.raises(ValueError, match="CUDA"):
+            batch.verify(None, None, None, None, None)  # a call that was refused has verified nothing
+        verify(batch)
+        assert batch.seq_len.tolist() == [start[0] + 1, start[1] + 2]
+        with pytest.raises(ValueError, match="since the last step"):
+            verify(batch)
+        assert batch.seq_len.tolist() == [start[0] + 1, start[1] + 2]
+    batch.append(*_new(2, 3))
+    batch.evict()
+    with pytest.raises(ValueError, match="since the last step"):
+        verify(batch)
+    assert batch.seq_len.tolist() == [4, 4]
+    batch.append(*_new(2, 3))
+    verify(batch)
+    assert batch.seq_len.tolist() == [5, 6]
+
+
+def test_one_new_token_has_no_drafts_to_drop(serve, monkeypatch):
+    _evict(serve, monkeypatch)
+    verify = _verify(serve, monkeypatch, [0, 0])
+    batch = _batch(serve, n=1, budget=4, slack=4)
+    batch.append(*_new(2, 1))
+    batch.evict()
+    verify(batch)
+    assert batch.seq_len.tolist() == [1, 1]
