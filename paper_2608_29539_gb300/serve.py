@@ -115,8 +115,12 @@ class ServeBatch:
     def step(self, q, k_new, v_new, gate_p):
         """q [B, n_new, Hq, D], k_new / v_new [B, n_new, Hkv, D] bf16, gate_p
         [B, n_new] float32.  Returns (o_c [B*n_new, Hq, D] packed, z, row_of):
-        what logo_combine takes on (B, n_new)."""
+        what logo_combine takes on (B, n_new); the next step writes to the same
+        buffers."""
         c = self.cfg
+        # what is refused is refused before the caches change
+        L._need(q, torch.bfloat16, "q", (c.B, c.n_new, c.Hq, c.D))
+        L._need(gate_p, torch.float32, "gate_p", (c.B, c.n_new))
         self.append(k_new, v_new)
         L.logo_select(gate_p, c.mode, c.b_th, c.ratio, self.z, self.pos, self.cu_q, self.row_of, self.n_sel,
                       workspace=self.ws)

@@ -117,3 +117,15 @@ def test_one_new_token_has_no_drafts_to_drop(serve, monkeypatch):
     batch.evict()
     verify(batch)
     assert batch.seq_len.tolist() == [1, 1]
+
+
+def test_a_refused_step_leaves_the_caches_alone(serve):
+    """Tensors that the calls do not take (here: on the CPU) are refused before the new
+    tokens join the caches."""
+    batch = _batch(serve, n=3, budget=8)
+    k, v = _new(2, 3)
+    for q, gate in ((torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 3)), (None, None)):
+        with pytest.raises(ValueError):
+            batch.step(q, k, v, gate)
+        assert batch.seq_len.tolist() == [0, 0] and batch.n_seen.tolist() == [0, 0]
+        assert float(batch.k.abs().sum()) == 0
