@@ -129,14 +129,17 @@ class ServeBatch:
                                   workspace=self.ws)
         return self.o_c, self.z, self.row_of
 
-    def verify(self, draft, q_draft, p_target, u, noise):
-        """The step's drafts (n_new - 1 per sequence) against the target's
-        probabilities [B, n_new, V]; the rejected tokens leave the caches.
+    def verify(self, draft, q_draft, p_target, u, noise, draft_len=None):
+        """The step's drafts (n_new - 1 per sequence, of which the first draft_len [B]
+        int32 count where it is given: a rejection past them would draw the next
+        token from the wrong distribution) against the target's probabilities
+        [B, n_new, V]; the tokens that are not accepted leave the caches.
         Returns (tokens [B, n_new], n_accept [B]).  Once a step and before evict,
         which moves the rows that are dropped from the end here."""
         if self._counts() and self.cfg.n_new > 1 and not self._latest_last:
             raise ValueError("the drafts were verified, or the caches cut, since the last step")
-        tokens, n_accept = L.logo_verify_draft(draft, q_draft, p_target, u, noise, workspace=self.ws)
+        tokens, n_accept = L.logo_verify_draft(draft, q_draft, p_target, u, noise, draft_len=draft_len,
+                                                workspace=self.ws)
         self._latest_last = False
         dropped = self.cfg.n_new - 1 - n_accept
         self.seq_len -= dropped
