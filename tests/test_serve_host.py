@@ -79,8 +79,8 @@ def _verify(serve, monkeypatch, accepted):
         tokens = torch.zeros(draft.shape[0], draft.shape[1] + 1, dtype=torch.int32)
         return tokens, torch.tensor(accepted, dtype=torch.int32)
     monkeypatch.setattr(serve.L, "logo_verify_draft", verdict)
-    args = torch.zeros(2, 2, dtype=torch.int32), None, None, None, None
-    return lambda batch: batch.verify(*args)
+    args = torch.zeros(2, 2, dtype=torch.int32), None
+    return lambda batch: batch.verify(*args, torch.zeros(2, batch.cfg.n_new, 5), None, None)
 
 
 def test_drafts_are_verified_once_and_before_the_cut(serve, monkeypatch):
@@ -93,7 +93,7 @@ def test_drafts_are_verified_once_and_before_the_cut(serve, monkeypatch):
         batch.append(*_new(2, 3))
         assert batch.seq_len.tolist() == [a + 3 for a in start]
         with pytest.raises(ValueError, match="CUDA"):
-            batch.verify(None, None, None, None, None)  # a call that was refused has verified nothing
+            batch.verify(None, None, torch.zeros(2, 3, 5), None, None)  # a call that was refused has verified nothing
         verify(batch)
         assert batch.seq_len.tolist() == [start[0] + 1, start[1] + 2]
         with pytest.raises(ValueError, match="since the last step"):
@@ -129,3 +129,15 @@ def test_a_refused_step_leaves_the_caches_alone(serve):
             batch.step(q, k, v, gate)
         assert batch.seq_len.tolist() == [0, 0] and batch.n_seen.tolist() == [0, 0]
         assert float(batch.k.abs().sum()) == 0
+
+
+@pytest.mark.parametrize("shape", [(2, 4, 5), (1, 3, 5), (3, 3, 5)])
+def test_more_drafts_or_sequences_than_the_step_had_are_refused(serve, monkeypatch, shape):
+    """(more accepted tokens than the step brought would lengthen the caches)"""
+    _verify(serve, monkeypatch, [shape[1] - 1] * shape[0])
+    batch = _batch(serve, n=3, budget=8)
+    batch.append(*_new(2, 3))
+    draft = torch.zeros(shape[0], shape[1] - 1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="p_target"):
+        batch.verify(draft, None, torch.zeros(shape), None, None)
+    assert batch.seq_len.tolist() == [3, 3] and batch.n_seen.tolist() == [3, 3]
