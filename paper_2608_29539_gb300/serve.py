@@ -139,7 +139,8 @@ class ServeBatch:
         if self._counts() and self.cfg.n_new > 1 and not self._latest_last:
             raise ValueError("the drafts were verified, or the caches cut, since the last step")
         if p_target.shape[0] != self.cfg.B or p_target.shape[1] > self.cfg.n_new:
-            raise ValueError(f"p_target has shape {tuple(p_target.shape)}, expected ({self.cfg.B}, {self.cfg.n_new}, V)")
+            want = f"({self.cfg.B}, {self.cfg.n_new}, V)"
+            raise ValueError(f"p_target has shape {tuple(p_target.shape)}, expected {want}")
         tokens, n_accept = L.logo_verify_draft(draft, q_draft, p_target, u, noise, draft_len=draft_len,
                                                 workspace=self.ws)
         self._latest_last = False
