@@ -231,7 +231,11 @@ LOGO_API int logo_decode_global_sparse_attn(const logo_bf16* q, const logo_bf16*
  *   Products in bf16 with fp32 accumulation, softmax and weights in fp32.
  *   Results do not depend on the order in which the GPU runs the blocks.
  *   Workspace: logo_decode_prefix_workspace_size(...) bytes, one per call in
- *   flight (with_mass: whether mass_out will be given).
+ *   flight (with_mass: whether mass_out will be given).  It is sized for every
+ *   token being selected: with weights it holds a logit for each of them and own
+ *   cache row, 4 * B * n_new * Hq * L bytes (64 sequences, 5 new tokens, 64 heads,
+ *   32K caches: 2.7 GB), and where many rows meet a long prefix the parts of
+ *   128-row tiles, at least 1216 of 128 * (D + 2) * 4 bytes (81 MB at D = 128).
  *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer or a size out of range;
  *   LOGO_ERR_UNSUPPORTED for D, Hq % Hkv, 16-byte alignment of a bf16 pointer,
  *   or a size past what the kernels count in: with G = Hq / Hkv, B * n_new <=

@@ -19,7 +19,8 @@
 // whole batch is one launch.  The plan is bound by latency (barriers and round
 // trips): 64 pairs of 16384 rows cut to 2048 take 37 us, the plan 20 of them, in
 // which HBM idles, and the moves 17 for 102 MB, 6.2 TB/s; 256 pairs of 2056 rows cut
-// to 2048 take 12 us and hardly move.
+// to 2048 take 12 us and hardly move: that time is the plan's own passes and
+// barriers, four or five walks over the rows.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -334,10 +335,12 @@ int check_evict(const logo_dims& d)
 // rank and to move, in units of a row to rank (1.2 ns; moving one of D = 128 takes
 // as long as ranking four).  All CTAs are to be resident at once, and clusters do
 // not fill the last places of a group of SMs: 76 of four take 33.5 us where 72
-// take 24.1, 48 of six 57 where 48 of five take 40.  Measured (us) with 1 to 8 CTAs
-// a pair: 24 pairs of 6000 rows, 5800 stay 12.2 13.4 11.7 11.7 12.3 13.0 16.8 18.8;
-// 8 of 15822, 8781 stay 74 44 33 28 25 24 23 21; 40 of 6000, 5800 stay 12.7 13.5 12.0
-// 15.3 15.9 17.2 26 32; 88 of 15822 (D = 64), 8781 stay 97 70 59 74 73 72 93 93.
+// take 24.1, 48 of six 57 where 48 of five take 40.  Both tables were set by hand to
+// come near the best of 1 to 8 CTAs a pair.  Measured (us) with each: 24 pairs of 6000
+// rows, 5800 stay 11.9 13.5 11.6 11.7 12.2 15.5 18.2 19.9; 8 of 15822, 8781 stay 73 44
+// 32 28 25 24 23 22; 40 of 6000, 5800 stay 11.8 13.5 12.0 15.4 16.0 17.1 29 32; 88 of
+// 15822 (D = 64), 8781 stay 93 69 55 73 72 72 94 94.  Over 60 shapes the choice is
+// within 8% of the best but for one: 16 of 15822 (D = 64) 27.2 us, 22.2 with six.
 int evict_ctas(int64_t pairs, const logo_dims& d, int budget)
 {
     constexpr int64_t kCost[] = {0, 3500, 2600, 2600, 3000, 3300, 3800, 4200};

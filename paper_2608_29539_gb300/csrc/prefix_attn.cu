@@ -20,16 +20,18 @@
 //   bounds it (a tile's 64 KB take 2790 clocks at an SM's share of it).  Each
 //   warp takes its own keys with its own running maximum and sum, so that none
 //   waits for another inside a piece.  8 sequences, 16 heads, D = 128, own caches
-//   of up to 16384: 395 MB in 69 us, 5.8 TB/s.
+//   of up to 16384: 566 MB in 92 us, 6.2 TB/s.  Caches of 1000 to 2000 rows are read
+//   at 2.6 to 4.5 TB/s: their runs are short, and start, Q and joins are latency.
 // Many rows of a long prefix per KV head are bound by the products and go to the
 //   tcgen05 kernel of the prefill's global branch instead ("wide" below), in tiles
 //   of 128 rows and shares of the prefix (pa_rows_kernel lays them out first, on the
 //   device as the count of rows is known only there).
 // pa_finish_kernel (or pa_join_kernel, then pa_mass_kernel): joins each (row,
 //   head)'s pieces, and adds up the weights exp(x - lse) of every own cache row from
-//   the logits that pa_rows_kernel wrote down (4 bytes a row and key, against
-//   4 D bytes of K and V a key for all rows; reading K again would cost half of
-//   the cache traffic).  10 us of that call, latency most of it.
+//   the logits that pa_rows_kernel wrote down (4 bytes a row and key, written and
+//   read; reading K again, and multiplying again, would be 2 D bytes a key for all
+//   rows: fewer from D / 4 rows a sequence and KV head on, a form that was not
+//   built).  11 us of that call, latency most of it.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -467,7 +469,9 @@ __device__ __forceinline__ bool pa_piece(const PaParams& p, const PaPiece& it, P
                     sc[st][nt][i] = ex2_approx(sc[st][nt][i] - (i < 2 ? m0 : m1));
                     l_run[i >> 1] += sc[st][nt][i];  // this lane's keys; the quad's are added at the end
                 }
-            // P as the A fragment: rows = rows, k = the 16 keys
+            // P as the A fragment: rows = rows, k = the 16 keys; rounded to bf16, the
+            // type that V has and the product takes (2^-8 of each weight at most; l is
+            // summed before it)
             pa[st][0] = pack_bf16x2(sc[st][0][0], sc[st][0][1]);
             pa[st][1] = pack_bf16x2(sc[st][0][2], sc[st][0][3]);
             pa[st][2] = pack_bf16x2(sc[st][1][0], sc[st][1][1]);
