@@ -20,6 +20,11 @@
  *   logo_decode_prefix_attn, logo_cache_evict, logo_verify_draft
  *                                serving: drafted tokens of a batch over a shared
  *                                prefix and bounded caches
+ *   logo_cache4_append, logo_cache4_read, logo_decode_cache4_attn
+ *                                serving: a cache held in 4 bits, written, read back
+ *                                and attended
+ *   logo_target_probs            serving: logits to the probabilities that
+ *                                logo_verify_draft takes
  *
  * Conventions shared by every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller.  The
@@ -303,6 +308,110 @@ LOGO_API size_t logo_verify_draft_workspace_size(int B, int m, int V);
 LOGO_API int logo_verify_draft(const int32_t* draft, const float* q_draft, const float* p_target, const float* u,
                 const float* noise, const int32_t* draft_len, int32_t* tokens, int32_t* n_accept, int B, int m, int V,
                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* logo_cache4 -- a key-value cache held in 4 bits (4.5 with the scales), each KV
+ *   head's rows in a row: k, v [B, Hkv, L, D/2] bytes and k_scale, v_scale
+ *   [B, Hkv, L, D/16] bytes, caller-owned device memory.
+ *   A row's D channels go in groups of 16.  A group's scale is an unsigned float of
+ *   5 exponent bits (bias 15) and 3 mantissa bits (code 8e + m: (8 + m) 2^(e - 18),
+ *   or m 2^-17 for e = 0): the group's largest magnitude / 6, rounded to nearest even,
+ *   at most 10240 (code 226).  A channel's code is a 4-bit float (bit 3 the sign;
+ *   magnitudes 0 0.5 1 1.5 2 3 4 6): the channel / scale, rounded to nearest even,
+ *   at most 6; byte j of a row holds channel 2j in its low half and 2j + 1 in its high
+ *   half.  The value held is code * scale, exact in bf16.  The
+ *   error of a channel is at most about a sixth of its group's largest magnitude, and
+ *   a quarter of the scale near zero.  Groups below 6 * 2^-18 are held as zeros,
+ *   magnitudes above 61440 as 61440.  A group with a NaN or an infinity gets
+ *   scale code 255, and all of it reads as NaN. */
+typedef struct {
+    uint8_t *k, *v;
+    uint8_t *k_scale, *v_scale;
+} logo_cache4;
+
+/* logo_cache4_append -- new tokens' K and V, quantised into the cache.
+ *   k_new, v_new [B, n_new, Hkv, D] bf16.  seq_len [B] int32 counts each sequence's
+ *   tokens with the new ones, as the attention calls take it; n_valid [B] int32
+ *   (clamped to [0, n_new]; NULL: n_new for all) counts the new ones, the first of the
+ *   sequence's n_new.  Token i < n_valid[b] goes to cache row seq_len[b] - n_valid[b]
+ *   + i; rows outside [0, L) are not written, nor is any other row touched.
+ *   dims: B, T = L, Hkv, D in {64, 128} (Hq is not read).  Codes are exact: a value
+ *   between two codes goes to the nearer, whatever the arithmetic.
+ *   Errors: LOGO_ERR_INVALID_ARG; LOGO_ERR_UNSUPPORTED (D, 16-byte alignment of a
+ *   pointer to bf16, codes or scales, B * L or B * n_new > 2^30, Hkv > 2^16,
+ *   B * n_new * Hkv > 2^34). */
+LOGO_API int logo_cache4_append(logo_cache4 cache, const logo_bf16* k_new, const logo_bf16* v_new,
+                const int32_t* seq_len, const int32_t* n_valid, logo_dims dims, int n_new, void* stream);
+
+/* logo_cache4_read -- rows of the cache as the bf16 values that they hold (exact).
+ *   rows [B, m] int32: the row numbers wanted of each sequence, in any order, with
+ *   repetitions (NULL: rows 0 .. m-1).  Out: k, v [B, m, Hkv, D] bf16, the layout of
+ *   the bf16 entry points; zeros where the row number is outside [0, min(seq_len[b],
+ *   L)).  dims, limits (m for n_new) and errors as logo_cache4_append. */
+LOGO_API int logo_cache4_read(logo_cache4 cache, const int32_t* seq_len, const int32_t* rows, logo_bf16* k,
+                logo_bf16* v, logo_dims dims, int m, void* stream);
+
+/* logo_decode_cache4_attn -- one serving step of the global branch (Eq. 8) over
+ *   caches held in 4 bits: logo_decode_prefix_attn's own-cache half.
+ *   q [B, n_new, Hq, D] bf16; packed row r of the selection (logo_select on dims
+ *   (B, T = n_new)) is token pos[r] of its sequence b and attends the cache rows
+ *   s < min(len, max(0, len - n_new + pos[r] + 1)), len = seq_len[b] clamped to
+ *   [0, L] counting the new tokens: the drafts are causal among themselves.  Rows
+ *   s >= len may hold anything.
+ *   A row that sees no key gets o = 0 and lse = -infinity.  What a row does not see
+ *   does not enter its results, NaN included; what it does see shows in them: a query
+ *   with a NaN or an infinity has NaN in o and lse.
+ * Out: o_c [B*n_new, Hq, D] bf16 packed, lse_c [Hq, B*n_new] float32 packed (may be
+ *   NULL); rows >= n_sel_total are left untouched.
+ *   Products in fp16 (the cache's values are exact in it; queries are scaled by a
+ *   power of two a row, so they are too but for channels 2^-30 of the row's largest
+ *   or less) with fp32 accumulation, softmax in fp32, weights rounded to fp16 for the
+ *   product.  Results do not depend on the order in which the GPU runs the blocks.
+ *   dims: B, T = L, Hq, Hkv, D in {64, 128}; scale as elsewhere.
+ *   Workspace: logo_decode_cache4_workspace_size(dims, n_new) bytes, one per call in
+ *   flight.
+ *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer or a size out of range;
+ *   LOGO_ERR_UNSUPPORTED for D, Hq % Hkv, 16-byte alignment, B * n_new > 2^24,
+ *   n_new * Hq / Hkv > 8192, Hkv > 2^16, B * n_new * Hq > 2^30; LOGO_ERR_WORKSPACE. */
+LOGO_API size_t logo_decode_cache4_workspace_size(logo_dims dims, int n_new);
+LOGO_API int logo_decode_cache4_attn(const logo_bf16* q, logo_cache4 cache, const int32_t* seq_len,
+                const int32_t* pos, const int32_t* cu_q, const int32_t* n_sel_total, logo_bf16* o_c, float* lse_c,
+                logo_dims dims, int n_new, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* logo_target_probs -- the target's logits to the probabilities that
+ *   logo_verify_draft takes, with what a request asks of its sampling.
+ *   logits [B, m1, V] float32, or bf16 when logits_bf16 is not 0: row i of a sequence
+ *   gives the token after its i-th draft (m1 = drafts + 1).  With x = logits[b,i,v] in
+ *   float32, in this order:
+ *   penalty [B, 3] float32 (NULL: none): repetition r > 0, frequency f, presence q.
+ *     history [B, H] int32 (or NULL) holds in its first hist_len[b] entries the
+ *     sequence's tokens, the prompt's n_prompt[b] (NULL: 0) first; draft [B, m1 - 1]
+ *     int32 (or NULL) the drafts, of which the first i count for row i.  A token that
+ *     occurs in either: x = x / r if x > 0, else x * r.  One that occurs c > 0 times
+ *     among the generated tokens (the history's past the prompt, of which the latest
+ *     LOGO_PROBS_MAX_COUNTED, and the drafts): x = x - (c * f + q).
+ *   bias_tok [B, K] int32, bias_val [B, K] float32 (NULL with K = 0): x = x + the sum,
+ *     in the list's order, of the values listed for v.
+ *   allowed [B, m1, ceil(V / 32)] int32 (NULL: all): bit v % 32 of word v / 32 is 0
+ *     for a token that a grammar rules out; bits past V are not read as tokens.
+ *   temperature [B] float32 (NULL: 1): T > 0: p = softmax over the allowed tokens of
+ *     x / T; T = 0: 1 for the largest x, the lowest v among equals, 0 for the others.
+ *   Each operation named is one float32 operation; the softmax's sum is float32.
+ *   Token numbers outside [0, V) in a list count for nothing (padding).
+ * Out: p [B, m1, V] float32; may be logits themselves if those are float32.  0 for
+ *   every token that is not allowed; a row that allows none, or only tokens of x =
+ *   -infinity, is all 0.  A NaN among a row's allowed tokens (or for T > 0 an infinite
+ *   x) makes p NaN for all of them.
+ *   Results are deterministic.  No workspace.
+ *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer, history without hist_len,
+ *   n_prompt without history, history or draft without penalty, draft with m1 = 1, or
+ *   sizes out of range; LOGO_ERR_UNSUPPORTED for V > LOGO_PROBS_MAX_VOCAB, m1 > 1024,
+ *   K > 4096, B * m1 > 2^24, 16-byte alignment of logits or p, bf16 logits in p. */
+#define LOGO_PROBS_MAX_COUNTED 16384
+#define LOGO_PROBS_MAX_VOCAB 294912
+LOGO_API int logo_target_probs(const void* logits, int logits_bf16, const float* temperature, const float* penalty,
+                const int32_t* history, const int32_t* hist_len, const int32_t* n_prompt, const int32_t* draft,
+                const int32_t* bias_tok, const float* bias_val, const int32_t* allowed, float* p, int B, int m1, int V,
+                int H, int K, void* stream);
 
 /* logo_select_noalloc -- logo_select for callers that cannot allocate.
  *   No counterpart in the paper: this is a deployment variant of logo_select.

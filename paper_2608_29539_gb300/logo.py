@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import typing
 
 import torch
 
@@ -49,6 +50,19 @@ class LogoError(RuntimeError):
 
 class Dims(ctypes.Structure):
     _fields_ = [("B", _c_int), ("T", _c_int), ("Hq", _c_int), ("Hkv", _c_int), ("D", _c_int)]
+
+
+class Cache4(typing.NamedTuple):
+    """A key-value cache held in 4 bits: codes k, v [B, Hkv, L, D/2] and scales
+    k_scale, v_scale [B, Hkv, L, D/16], uint8 (the format is in include/logo.h)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+class _Cache4Ptrs(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp)]
 
 
 @functools.lru_cache(maxsize=256)
@@ -90,6 +104,13 @@ _SIGS = {
     "logo_verify_draft_workspace_size": (_c_size, [_c_int, _c_int, _c_int]),
     "logo_verify_draft": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _c_int, _vp, _c_size,
                                    _vp]),
+    "logo_cache4_append": (_c_int, [_Cache4Ptrs, _vp, _vp, _vp, _vp, Dims, _c_int, _vp]),
+    "logo_cache4_read": (_c_int, [_Cache4Ptrs, _vp, _vp, _vp, _vp, Dims, _c_int, _vp]),
+    "logo_decode_cache4_workspace_size": (_c_size, [Dims, _c_int]),
+    "logo_decode_cache4_attn": (_c_int, [_vp, _Cache4Ptrs, _vp, _vp, _vp, _vp, _vp, _vp, Dims, _c_int, _c_float, _vp,
+                                         _c_size, _vp]),
+    "logo_target_probs": (_c_int, [_vp, _c_int, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int,
+                                   _c_int, _c_int, _c_int, _vp]),
     "logo_local_attn_fwd": (_c_int, [_vp, _vp, _vp, _vp, _vp, Dims, _c_int, _c_float, _vp]),
     "logo_local_attn_bwd_workspace_size": (_c_size, [Dims]),
     "logo_local_attn_bwd": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, Dims, _c_int, _c_float, _vp,
@@ -553,6 +574,194 @@ def logo_verify_draft(draft, q_draft, p_target, u, noise, draft_len=None, tokens
           None if draft_len is None else draft_len.data_ptr(), tokens.data_ptr(), n_accept.data_ptr(), B, m, V,
           workspace.data_ptr(), workspace.nbytes, _stream())
     return tokens, n_accept
+
+
+def logo_cache4_empty(B: int, L: int, Hkv: int, D: int, device="cuda") -> Cache4:
+    """A 4-bit cache of L rows a sequence; the rows hold nothing yet."""
+    e = lambda w: torch.zeros((B, Hkv, L, w), dtype=torch.uint8, device=device)  # noqa: E731
+    return Cache4(e(D // 2), e(D // 2), e(D // 16), e(D // 16))
+
+
+def _cache4(cache):
+    """(its addresses, B, Hkv, L, D) of a Cache4."""
+    k, v, ks, vs = cache
+    _need(k, torch.uint8, "cache.k")
+    if k.dim() != 4:
+        raise ValueError("cache.k must be [B, Hkv, L, D/2]")
+    B, Hkv, L, half = k.shape
+    _need(v, torch.uint8, "cache.v", k.shape)
+    scales = (B, Hkv, L, half // 8)
+    _need(ks, torch.uint8, "cache.k_scale", scales)
+    _need(vs, torch.uint8, "cache.v_scale", scales)
+    return _Cache4Ptrs(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr()), B, Hkv, L, 2 * half
+
+
+def _here(*tensors):
+    """The kernels run on the current device: tensors on another are refused."""
+    dev = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def logo_cache4_append(cache: Cache4, k_new, v_new, seq_len, n_valid=None):
+    """Quantise new tokens' k_new, v_new [B, n_new, Hkv, D] bf16 into the 4-bit
+    cache.  seq_len [B] int32 counts each sequence's tokens, the new ones included;
+    of those the first n_valid [B] int32 of the n_new are new ones (None: all), and
+    go to the rows that end at seq_len.  Returns the cache."""
+    ptrs, B, Hkv, L, D = _cache4(cache)
+    _need(k_new, torch.bfloat16, "k_new")
+    if k_new.dim() != 4:
+        raise ValueError("k_new must be [B, n_new, Hkv, D]")
+    n = k_new.shape[1]
+    _need(k_new, torch.bfloat16, "k_new", (B, n, Hkv, D))
+    _need(v_new, torch.bfloat16, "v_new", (B, n, Hkv, D))
+    _need(seq_len, torch.int32, "seq_len", (B,))
+    if n_valid is not None:
+        _need(n_valid, torch.int32, "n_valid", (B,))
+    _here(*cache, k_new, v_new, seq_len, n_valid)
+    _call("logo_cache4_append", ptrs, k_new.data_ptr(), v_new.data_ptr(), seq_len.data_ptr(),
+          None if n_valid is None else n_valid.data_ptr(), _dims(B, L, Hkv, Hkv, D), n, _stream())
+    return cache
+
+
+def logo_cache4_read(cache: Cache4, seq_len, rows=None, m=None, k=None, v=None):
+    """Rows of a 4-bit cache as the bf16 values that they hold: the listed rows
+    [B, m] int32, or rows 0 .. m-1 (m None: as k has, or all L).  Rows outside
+    [0, seq_len) read as zeros.  Returns (k, v) [B, m, Hkv, D]."""
+    ptrs, B, Hkv, L, D = _cache4(cache)
+    _need(seq_len, torch.int32, "seq_len", (B,))
+    if rows is not None:
+        _need(rows, torch.int32, "rows")
+        if rows.dim() != 2 or (m is not None and m != rows.shape[1]):
+            raise ValueError("rows must be [B, m]")
+        m = rows.shape[1]
+        _need(rows, torch.int32, "rows", (B, m))
+    elif m is None:
+        m = L if k is None else k.shape[1]
+    shape = (B, m, Hkv, D)
+    k = torch.empty(shape, dtype=torch.bfloat16, device=seq_len.device) if k is None else k
+    v = torch.empty(shape, dtype=torch.bfloat16, device=seq_len.device) if v is None else v
+    _need(k, torch.bfloat16, "k", shape)
+    _need(v, torch.bfloat16, "v", shape)
+    _here(*cache, seq_len, rows, k, v)
+    _call("logo_cache4_read", ptrs, seq_len.data_ptr(), None if rows is None else rows.data_ptr(), k.data_ptr(),
+          v.data_ptr(), _dims(B, L, Hkv, Hkv, D), m, _stream())
+    return k, v
+
+
+def logo_decode_cache4_workspace(q, cache: Cache4):
+    """A workspace for logo_decode_cache4_attn calls of these shapes (one per call
+    in flight)."""
+    B, n_new, Hq, D = q.shape
+    dims = Dims(B, cache.k.shape[2], Hq, cache.k.shape[1], D)
+    return _workspace(int(lib().logo_decode_cache4_workspace_size(dims, n_new)), q.device)
+
+
+def logo_decode_cache4_attn(q, cache: Cache4, seq_len, pos, cu_q, n_sel_total, scale: float = 0.0, o_c=None,
+                            lse_c=None, workspace=None):
+    """One serving step of the global branch (Eq. 8) over 4-bit caches.
+
+    q [B, n_new, Hq, D] bf16; seq_len [B] int32 (tokens of each cache, the n_new new
+    ones included and last); pos, cu_q, n_sel_total from logo_select on (B, n_new)
+    gates.  Returns (o_c [B*n_new, Hq, D], lse_c [Hq, B*n_new]); packed rows >=
+    n_sel_total are untouched."""
+    ptrs, B, Hkv, L, D = _cache4(cache)
+    _need(q, torch.bfloat16, "q")
+    if q.dim() != 4 or q.shape[0] != B or q.shape[3] != D:
+        raise ValueError(f"q has shape {tuple(q.shape)}, expected ({B}, n_new, Hq, {D})")
+    _, n_new, Hq, _ = q.shape
+    cap = B * n_new
+    _need(seq_len, torch.int32, "seq_len", (B,))
+    _need(pos, torch.int32, "pos", (cap,))
+    _need(cu_q, torch.int32, "cu_q", (B + 1,))
+    _need(n_sel_total, torch.int32, "n_sel_total", (1,))
+    if o_c is None:
+        o_c = torch.empty((cap, Hq, D), dtype=torch.bfloat16, device=q.device)
+    else:
+        _need(o_c, torch.bfloat16, "o_c", (cap, Hq, D))
+    if lse_c is None:
+        lse_c = torch.empty((Hq, cap), dtype=torch.float32, device=q.device)
+    else:
+        _need(lse_c, torch.float32, "lse_c", (Hq, cap))
+    if workspace is None:
+        workspace = logo_decode_cache4_workspace(q, cache)
+    else:
+        _given_workspace(workspace)
+    _here(*cache, q, seq_len, pos, cu_q, n_sel_total, o_c, lse_c, workspace)
+    _call("logo_decode_cache4_attn", q.data_ptr(), ptrs, seq_len.data_ptr(), pos.data_ptr(), cu_q.data_ptr(),
+          n_sel_total.data_ptr(), o_c.data_ptr(), lse_c.data_ptr(), _dims(B, L, Hq, Hkv, D), n_new, float(scale),
+          workspace.data_ptr(), workspace.nbytes, _stream())
+    return o_c, lse_c
+
+
+def logo_target_probs(logits, temperature=None, penalty=None, history=None, hist_len=None, n_prompt=None, draft=None,
+                      bias_tok=None, bias_val=None, allowed=None, p=None):
+    """The target's probabilities [B, m1, V] float32, as logo_verify_draft takes
+    them, from logits [B, m1, V] (float32 or bf16).
+
+    penalty [B, 3] float32: repetition (over the history and the drafts before the
+    row), frequency and presence (over the generated ones of these); history [B, H]
+    int32 with hist_len [B] int32 tokens of which the first n_prompt [B] int32 are the
+    prompt's; draft [B, m1 - 1] int32.  bias_tok [B, K] int32 with bias_val [B, K]
+    float32: added to the listed tokens.  allowed [B, m1, ceil(V / 32)] int32: a bit
+    per token.  temperature [B] float32, 0 for greedy.  Token numbers outside [0, V)
+    count for nothing.  p may be float32 logits themselves."""
+    if not isinstance(logits, torch.Tensor) or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("logits must be a float32 or bf16 CUDA tensor")
+    _need(logits, logits.dtype, "logits")
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, m1, V]")
+    B, m1, V = logits.shape
+    H = K = 0
+    if temperature is not None:
+        _need(temperature, torch.float32, "temperature", (B,))
+    if penalty is not None:
+        _need(penalty, torch.float32, "penalty", (B, 3))
+    elif history is not None or draft is not None:
+        raise ValueError("history and draft need penalty")
+    if history is not None:
+        _need(history, torch.int32, "history")
+        if history.dim() != 2:
+            raise ValueError("history must be [B, H]")
+        H = history.shape[1]
+        _need(history, torch.int32, "history", (B, H))
+        if hist_len is None:
+            raise ValueError("history needs hist_len")
+        _need(hist_len, torch.int32, "hist_len", (B,))
+        if n_prompt is not None:
+            _need(n_prompt, torch.int32, "n_prompt", (B,))
+    elif hist_len is not None or n_prompt is not None:
+        raise ValueError("hist_len and n_prompt need history")
+    if draft is not None:
+        _need(draft, torch.int32, "draft", (B, m1 - 1))
+    if (bias_tok is None) != (bias_val is None):
+        raise ValueError("bias_tok and bias_val come together")
+    if bias_tok is not None:
+        _need(bias_tok, torch.int32, "bias_tok")
+        if bias_tok.dim() != 2:
+            raise ValueError("bias_tok must be [B, K]")
+        K = bias_tok.shape[1]
+        _need(bias_tok, torch.int32, "bias_tok", (B, K))
+        _need(bias_val, torch.float32, "bias_val", (B, K))
+    if allowed is not None:
+        _need(allowed, torch.int32, "allowed", (B, m1, (V + 31) // 32))
+    if p is None:
+        p = torch.empty((B, m1, V), dtype=torch.float32, device=logits.device)
+    else:
+        _need(p, torch.float32, "p", (B, m1, V))
+    _here(logits, temperature, penalty, history, hist_len, n_prompt, draft, bias_tok, bias_val, allowed, p)
+    a = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    if H == 0:  # an empty list is no list
+        history = hist_len = n_prompt = None
+    if m1 == 1:
+        draft = None
+    if K == 0:
+        bias_tok = bias_val = None
+    _call("logo_target_probs", logits.data_ptr(), int(logits.dtype is torch.bfloat16), a(temperature), a(penalty),
+          a(history), a(hist_len), a(n_prompt), a(draft), a(bias_tok), a(bias_val), a(allowed), p.data_ptr(), B, m1, V,
+          H, K, _stream())
+    return p
 
 
 def logo_select_noalloc(gate_p, mode: int, b_th: float = 0.5, ratio: float = 0.0, z=None, pos=None, cu_q=None,
