@@ -18,11 +18,13 @@
 //   - code * scale is exact in fp16.  Queries go through fp16 scaled by a power of two
 //     a row.  P is rounded to fp16; it comes out of S^T's fragments by a transposition
 //     in registers.
-// The batch's (sequence, KV head, 32 rows, 128 keys) units form a line, sequences
-// without a selected row left out; each CTA takes an equal stretch of it, its four warps
-// 32 keys of a unit each through a ring of their own in shared memory (cp.async; no warp
-// waits for another before a stretch of one run ends).  A run (sequence, KV head, rows)
-// that spans several CTAs is joined by a second launch from their parts, in order.
+// The batch's (sequence, KV head, rows, 128 keys) units form a line, sequences without a
+// selected row left out.  Each group of four warps takes an equal stretch of it, a cell,
+// its warps 32 keys of a unit each through a ring of their own in shared memory (cp.async;
+// no warp waits for another inside a run).  All groups of an SM are one CTA: as CTAs of
+// their own the hardware favoured the first ones, and the last finished a quarter later.
+// A run (sequence, KV head, rows) that spans several cells is joined from their parts, in
+// order, by a second launch.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -37,13 +39,30 @@
 namespace logo {
 namespace {
 
-constexpr int kCaWarps = 4;
-constexpr int kCaThreads = 32 * kCaWarps;
+#ifndef CA_ST
+#define CA_ST 2
+#endif
+#ifndef CA_C1
+#define CA_C1 4
+#endif
+#ifndef CA_C2
+#define CA_C2 3
+#endif
+constexpr int kCaWarps = 4;                   // of a group
+constexpr int kCaGroup = 32 * kCaWarps;
 constexpr int kCaKeys = 32;                   // keys of a warp's step
 constexpr int kCaUnit = kCaKeys * kCaWarps;   // keys of a unit
-constexpr int kCaStages = 2;
+constexpr int kCaStages = CA_ST;
 constexpr float kCaSlack = 8.f;               // a maximum may grow by 2^8 before what is summed is rescaled
 constexpr int kCaMaxTiles = 4;                // tiles of 8 rows that a warp holds
+constexpr int kJoinThreads = 256;
+
+// A run that a cell begins and does not end: its packed rows from r0 and KV head, of which
+// its rows are row0 ..., the last cell that has a part of it (-1: there is no such run).
+struct __align__(16) CaOpen {
+    int r0, h, row0, nrow, last;
+    int pad[3];
+};
 
 struct CaParams {
     const uint16_t* q;
@@ -51,30 +70,48 @@ struct CaParams {
     const int32_t *len, *pos, *cu_q, *n_sel;
     uint16_t* o;
     float* lse;
-    float* parts;   // [2 * grid][rows * D, then rows of (max, sum)]
-    int4* table;    // [grid]: (sequence or -1, KV head, row block, last CTA) of the run that goes on past a CTA's end
+    float* parts;   // [2 * cells][rows * D, then rows of (max, sum)]
+    CaOpen* table;  // [cells]
     int B, n, Hq, Hkv, G, L;
-    float scale2;   // scale * log2(e)
+    uint32_t magic;  // ceil(2^32 / G), 0 for G = 1
+    float scale2;    // scale * log2(e)
+
+    __device__ __forceinline__ int token_of(int row) const { return magic ? __umulhi(row, magic) : row; }  // row / G
 };
 
 template <int D, int NT>
 struct CaShape {
     static constexpr int kRows = 8 * NT;
+    static constexpr int kGroups = NT == 1 ? CA_C1 : NT == 2 ? CA_C2 : 2;  // an SM
+    static constexpr int kThreads = kGroups * kCaGroup;
     static constexpr int kCodes = kCaKeys * D / 2, kScales = kCaKeys * D / 16;  // bytes a step, K or V
     static constexpr int kStage = 2 * (kCodes + kScales);
     static constexpr int kSteps = D / 16;                      // k steps of S^T, m tiles of O^T
     static constexpr int kRowBytes = 4 * D + 16;               // a row of the warps' results (padded for the banks)
     static constexpr int kRing = kCaWarps * kCaStages * kStage;
     static constexpr int kQ = NT * kSteps * 32 * 8;            // fragments of Q
-    static constexpr int kMerge = kCaWarps * kRows * kRowBytes;
-    static constexpr int kSmem = kRing + kQ + kMerge + kCaWarps * kRows * 8 + kRows * 8;
+    static constexpr int kMerge = kCaWarps * kRows * kRowBytes;  // (ahead of a run: its queries)
+    static constexpr int kStats = (kCaWarps + 1) * kRows * 8 + kRows * 8;
+    static constexpr int kGroupBytes = kRing + kQ + kMerge + kStats;
+    static constexpr int kSmem = kGroups * kGroupBytes;
     static constexpr int kPart = kRows * (D + 2);              // floats of a part
-    static constexpr int kCtas = NT == 1 ? 4 : NT == 2 ? 3 : 2;  // an SM
 };
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// (the first `bytes`, then zeros)
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void cp_async_small(uint32_t dst, const void* src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(N) : "memory");
 }
 
 template <int N>
@@ -91,31 +128,9 @@ __device__ __forceinline__ void cp_async_wait()
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-__device__ __forceinline__ uint2 ld_shared_v2(uint32_t addr)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
-    return v;
-}
-
-__device__ __forceinline__ uint32_t ld_shared_u16(uint32_t addr)
-{
-    uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
-    return v;
-}
-
-__device__ __forceinline__ uint32_t ld_shared_u8(uint32_t addr)
-{
-    uint32_t v;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
-    return v;
-}
-
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -134,16 +149,20 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
     return r;
 }
 
-__device__ __forceinline__ uint32_t dup16(uint32_t x) { return __byte_perm(x, 0, 0x1010); }
-
 // Where byte `at` (a multiple of 4) of a step's key row lies: the 16-byte pieces of
 // 128-byte lines exchanged so that both kinds of loads below meet every bank once.
+// The exchange repeats every 8 keys.
 template <int D>
 __device__ __forceinline__ uint32_t piece(uint32_t key, uint32_t at)
 {
     const uint32_t x = key * (D / 2) + at, line = x >> 7;
     const uint32_t f = D == 128 ? ((line & 1) << 1) | ((line & 2) << 1) : (line & 1) << 2;
     return x ^ (f << 4);
+}
+
+__device__ __forceinline__ void group_sync(int group)
+{
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kCaGroup) : "memory");
 }
 
 // A run: the units of one (sequence, KV head, row block), in the line's order.
@@ -155,15 +174,13 @@ struct CaRun {
 // Whether sequence b has selected rows; its part of the run's description.
 __device__ __forceinline__ bool ca_sequence(const CaParams& p, int b, int rows, CaRun& r)
 {
-    const int n_sel = *p.n_sel;
-    r.r0 = p.cu_q[b];
-    r.cnt = min(min(p.cu_q[b + 1], n_sel) - r.r0, p.n);
-    if (r.cnt <= 0) return false;
     r.b = b;
+    r.r0 = p.cu_q[b];
+    r.cnt = min(min(p.cu_q[b + 1], *p.n_sel) - r.r0, p.n);
     r.len = max(0, min(p.len[b], p.L));
     r.units = max(1, (r.len + kCaUnit - 1) / kCaUnit);
     r.nrb = (r.cnt * p.G + rows - 1) / rows;
-    return true;
+    return r.cnt > 0;
 }
 
 __device__ __forceinline__ void ca_next(const CaParams& p, int rows, CaRun& r)
@@ -172,171 +189,229 @@ __device__ __forceinline__ void ca_next(const CaParams& p, int rows, CaRun& r)
     r.rb = 0;
     if (++r.h < p.Hkv) return;
     r.h = 0;
-    for (int b = r.b + 1; b < p.B; ++b)
-        if (ca_sequence(p, b, rows, r)) return;
-    r.units = 0;  // the line's end
+    int b = r.b + 1;
+#pragma unroll 1
+    for (; b < p.B - 1; ++b)
+        if (min(p.cu_q[b + 1], *p.n_sel) > p.cu_q[b]) break;
+    ca_sequence(p, b, rows, r);  // (only called where another run follows)
 }
 
-__device__ __forceinline__ long long ca_weight(const CaParams& p, int b, int rows)
+__device__ __forceinline__ uint32_t ca_weight(const CaParams& p, int b, int rows)
 {
     CaRun r;
-    return b < p.B && ca_sequence(p, b, rows, r) ? static_cast<long long>(r.units) * r.nrb * p.Hkv : 0;
+    return b < p.B && ca_sequence(p, b, rows, r) ? static_cast<uint32_t>(r.units) * r.nrb * p.Hkv : 0u;
 }
 
-// The line's length and, for a place x on it that depends on the length, the sequence
-// that holds it and where its units begin.  All threads of the CTA.
-struct CaLine {
-    long long total, x0, x1, base;
-    int b;
+// How the line is cut: SM i has `each` units, one more where i < extra, in `cells` equal
+// cells, one for each group as long as there are units for all.
+struct CaCut {
+    uint32_t each, extra, cells;
+
+    __device__ __forceinline__ CaCut(uint32_t total, uint32_t sms, uint32_t groups)
+        : each(total / sms), extra(total % sms), cells(max(1u, min(each, groups)))
+    {
+    }
+    __device__ __forceinline__ uint32_t units(uint32_t sm) const { return each + (sm < extra); }
+    __device__ __forceinline__ uint32_t begin(uint32_t sm) const { return each * sm + min(sm, extra); }
+    // first unit of cell k of an SM with u units, which are no fewer than its cells
+    __device__ __forceinline__ uint32_t cell(uint32_t u, uint32_t k) const { return u * k / cells; }
+    __device__ __forceinline__ uint32_t cell_of(uint32_t x) const
+    {
+        const uint32_t big = extra * (each + 1);
+        const uint32_t sm = x < big ? x / (each + 1) : extra + (x - big) / each;  // (each = 0: x < big)
+        const uint32_t in = x - begin(sm), u = units(sm);
+        return sm * cells + ((in + 1) * cells - 1) / u;
+    }
 };
 
-__device__ __forceinline__ void ca_line(const CaParams& p, int rows, CaLine& at, long long* sh)
+// The line's length; all threads of the CTA.
+__device__ __forceinline__ uint32_t ca_length(const CaParams& p, int rows, uint32_t* sh)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long w = 0;
-    for (int b = threadIdx.x; b < p.B; b += kCaThreads) w += ca_weight(p, b, rows);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) w += __shfl_xor_sync(0xffffffffu, w, d);
-    if (lane == 0) sh[warp] = w;
+    if (p.B <= 32) return __reduce_add_sync(0xffffffffu, ca_weight(p, threadIdx.x % 32, rows));  // every warp for itself
+    uint32_t w = 0;
+#pragma unroll 1
+    for (int b = threadIdx.x; b < p.B; b += blockDim.x) w += ca_weight(p, b, rows);
+    w = __reduce_add_sync(0xffffffffu, w);
+    if (threadIdx.x % 32 == 0) sh[threadIdx.x / 32] = w;
     __syncthreads();
-    long long total = 0;
-#pragma unroll
-    for (int i = 0; i < kCaWarps; ++i) total += sh[i];
-    const long long ctas = min(static_cast<long long>(gridDim.x), total);
-    at.total = total;
-    at.x0 = at.x1 = 0;
-    if (blockIdx.x >= ctas) return;
-    at.x0 = total * blockIdx.x / ctas;
-    at.x1 = total * (blockIdx.x + 1) / ctas;
-    long long base = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 32) {  // every warp for itself
-        const long long mine = ca_weight(p, b0 + lane, rows);
-        long long upto = mine;
+    const int lane = threadIdx.x & 31;
+    return __reduce_add_sync(0xffffffffu, lane < blockDim.x / 32 ? sh[lane] : 0u);
+}
+
+// The sequence whose runs hold unit x of the line, and its first unit; every warp for itself.
+__device__ __forceinline__ uint2 ca_find(const CaParams& p, int rows, uint32_t x)
+{
+    const int lane = threadIdx.x & 31;
+    uint32_t base = 0;
+#pragma unroll 1
+    for (int b0 = 0;; b0 += 32) {
+        const uint32_t mine = ca_weight(p, b0 + lane, rows);
+        uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, upto, d);
+            const uint32_t y = __shfl_up_sync(0xffffffffu, upto, d);
             if (lane >= d) upto += y;
         }
-        const uint32_t past = __ballot_sync(0xffffffffu, base + upto > at.x0);
-        if (past) {
-            const int k = __ffs(past) - 1;
-            at.b = b0 + k;
-            at.base = base + __shfl_sync(0xffffffffu, upto - mine, k);
-            return;
+        const uint32_t past = __ballot_sync(0xffffffffu, base + upto > x);
+        if (past || b0 + 32 >= p.B) {
+            const int k = past ? __ffs(past) - 1 : 31;
+            return make_uint2(b0 + k, base + __shfl_sync(0xffffffffu, upto - mine, k));
         }
         base += __shfl_sync(0xffffffffu, upto, 31);
     }
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kCaThreads, CaShape<D, NT>::kCtas) cache4_attn_kernel(CaParams p)
+__global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_attn_kernel(CaParams p)
 {
     using S = CaShape<D, NT>;
     constexpr int NS = S::kSteps;
-    extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long sh_line[kCaWarps];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const uint32_t ring = smem_u32(smem) + warp * (kCaStages * S::kStage);
+    extern __shared__ __align__(128) uint8_t smem_all[];
+    __shared__ uint32_t sh_line[32];
+    const int group = threadIdx.x / kCaGroup, tid = threadIdx.x % kCaGroup;
+    const int lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    uint8_t* const smem = smem_all + group * S::kGroupBytes;
+    const uint8_t* const my_ring = smem + warp * (kCaStages * S::kStage);
+    const uint32_t ring = smem_u32(my_ring);
     uint2* const q_frag = reinterpret_cast<uint2*>(smem + S::kRing);
     uint8_t* const merge = smem + S::kRing + S::kQ;
-    float2* const stats = reinterpret_cast<float2*>(merge + S::kMerge);  // [warp][row] (max, sum)
-    int* const row_vis = reinterpret_cast<int*>(stats + kCaWarps * S::kRows);
+    float2* const stats = reinterpret_cast<float2*>(merge + S::kMerge);  // [warp, all][row] (max, sum)
+    int* const row_vis = reinterpret_cast<int*>(stats + (kCaWarps + 1) * S::kRows);
     float* const row_mul = reinterpret_cast<float*>(row_vis + S::kRows);
+    // a thread's pieces: of K, keys (g >> 1) + 4 (g & 1) + 8 i; of V, keys t + 8 i and t + 4 + 8 i
+    const int my_key = (g >> 1) + 4 * (g & 1);
+    const uint32_t k_at = piece<D>(my_key, t * (D / 8)), k_sc = 2 * S::kCodes + my_key * (D / 16) + t * (D / 64);
+    const uint32_t v_at[2] = {S::kCodes + piece<D>(t, g * (D / 16)), S::kCodes + piece<D>(t + 4, g * (D / 16))};
+    const uint32_t v_sc = 2 * S::kCodes + S::kScales + t * (D / 16) + (D == 128 ? g : g >> 1);
+    const uint32_t to0 = ring + piece<D>(lane * 16 / (D / 2), lane * 16 % (D / 2));
+    const uint32_t to1 = ring + 2 * S::kCodes + lane * (D / 16);
 
-    CaLine at;
-    ca_line(p, S::kRows, at, sh_line);
-    int4 goes_on = make_int4(-1, 0, 0, 0);
-    if (at.x0 < at.x1) {
-        const long long ctas = min(static_cast<long long>(gridDim.x), at.total);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const uint32_t total = ca_length(p, S::kRows, sh_line);
+    const CaCut cut(total, gridDim.x, S::kGroups);
+    const uint32_t my_units = cut.units(blockIdx.x), my_begin = cut.begin(blockIdx.x);
+    // the entries of the table that no cell below writes
+    const uint32_t spare = S::kGroups - cut.cells;
+    if (threadIdx.x < spare) p.table[gridDim.x * cut.cells + blockIdx.x * spare + threadIdx.x].last = -1;
+    if (my_units == 0) {
+        if (threadIdx.x < cut.cells) p.table[blockIdx.x * cut.cells + threadIdx.x].last = -1;
+        return;
+    }
+    uint32_t fill = 0, use = 0;  // stages
+    const uint32_t cell = group;
+    if (cell < cut.cells) {
+        const uint32_t x0 = my_begin + cut.cell(my_units, cell), x1 = my_begin + cut.cell(my_units, cell + 1);
         CaRun run{};
-        ca_sequence(p, at.b, S::kRows, run);
-        long long off = at.x0 - at.base;
-        run.h = static_cast<int>(off / (static_cast<long long>(run.units) * run.nrb));
-        off -= static_cast<long long>(run.h) * run.units * run.nrb;
-        run.rb = static_cast<int>(off / run.units);
-        int unit = static_cast<int>(off - static_cast<long long>(run.rb) * run.units);
+        const uint2 at = ca_find(p, S::kRows, x0);
+        ca_sequence(p, at.x, S::kRows, run);
+        uint32_t base = (x0 - at.y) / run.units;  // of the run, on the line
+        run.h = base / run.nrb, run.rb = base % run.nrb;
+        base = at.y + base * run.units;
+        int unit = x0 - base;
+        CaOpen open{0, 0, 0, 0, -1, {0, 0, 0}};
 
         // ---- loads: a cursor of its own, kCaStages - 1 units ahead
         CaRun ahead = run;
-        int ahead_unit = unit;
-        long long ahead_left = at.x1 - at.x0;
-        uint32_t fill = 0;
+        int ahead_unit = unit, ahead_left = x1 - x0;
+        const uint8_t *k, *v, *ks, *vs;  // this lane's first pieces of the step ahead
+        auto point = [&] {
+            const int64_t row0 = (static_cast<int64_t>(ahead.b) * p.Hkv + ahead.h) * p.L + ahead_unit * kCaUnit + warp * kCaKeys;
+            k = p.k + row0 * (D / 2) + lane * 16;
+            v = p.v + row0 * (D / 2) + lane * 16;
+            ks = p.ks + (row0 + lane) * (D / 16);
+            vs = p.vs + (row0 + lane) * (D / 16);
+        };
+        point();
         auto issue = [&] {
             if (ahead_left > 0) {
-                const int key0 = ahead_unit * kCaUnit + warp * kCaKeys;
-                if (key0 < ahead.len) {
-                    const uint32_t st = ring + fill * S::kStage;
-                    const int64_t row0 = (static_cast<int64_t>(ahead.b) * p.Hkv + ahead.h) * p.L + key0;
-                    const int rows = ahead.len - key0;  // rows past the end are written as zeros
+                const int rows = ahead.len - ahead_unit * kCaUnit - warp * kCaKeys;
+                const uint32_t st = fill * S::kStage;
+                if (rows >= kCaKeys) {
 #pragma unroll
                     for (int i = 0; i < S::kCodes / 512; ++i) {
-                        const uint32_t x = (i * 32 + lane) * 16, key = x / (D / 2);
-                        const bool in = static_cast<int>(key) < rows;
-                        const uint32_t to = st + piece<D>(key, x % (D / 2));
-                        const int64_t from = in ? row0 * (D / 2) + x : 0;
-                        cp_async16(to, p.k + from, in ? 16 : 0);
-                        cp_async16(to + S::kCodes, p.v + from, in ? 16 : 0);
+                        cp_async16(to0 + st + i * 512, k + i * 512);
+                        cp_async16(to0 + st + i * 512 + S::kCodes, v + i * 512);
+                    }
+                    cp_async_small<D / 16>(to1 + st, ks);
+                    cp_async_small<D / 16>(to1 + st + S::kScales, vs);
+                } else if (rows > 0) {  // rows past the end are written as zeros
+#pragma unroll 1
+                    for (int i = 0; i < S::kCodes / 512; ++i) {
+                        const bool in = (i * 512 + lane * 16) / (D / 2) < rows;
+                        cp_async16(to0 + st + i * 512, in ? k + i * 512 : p.k, in ? 16 : 0);
+                        cp_async16(to0 + st + i * 512 + S::kCodes, in ? v + i * 512 : p.v, in ? 16 : 0);
                     }
                     const bool in = lane < rows;
-                    const int64_t from = in ? (row0 + lane) * (D / 16) : 0;
-                    const uint32_t to = st + 2 * S::kCodes + lane * (D / 16);
-                    cp_async_small<D / 16>(to, p.ks + from, in ? D / 16 : 0);
-                    cp_async_small<D / 16>(to + S::kScales, p.vs + from, in ? D / 16 : 0);
+                    cp_async_small<D / 16>(to1 + st, in ? ks : p.ks, in ? D / 16 : 0);
+                    cp_async_small<D / 16>(to1 + st + S::kScales, in ? vs : p.vs, in ? D / 16 : 0);
                 }
                 --ahead_left;
-                if (++ahead_unit == ahead.units) {
+                k += kCaUnit * (D / 2), v += kCaUnit * (D / 2), ks += kCaUnit * (D / 16), vs += kCaUnit * (D / 16);
+                if (++ahead_unit == ahead.units && ahead_left > 0) {
                     ahead_unit = 0;
-                    if (ahead_left > 0) ca_next(p, S::kRows, ahead);
+                    ca_next(p, S::kRows, ahead);
+                    point();
                 }
             }
             cp_async_commit();
             fill = fill + 1 == kCaStages ? 0 : fill + 1;
         };
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < kCaStages - 1; ++i) issue();
 
-        uint32_t use = 0;
-        for (long long left = at.x1 - at.x0; left > 0;) {
+#pragma unroll 1
+        for (int left = x1 - x0; left > 0;) {
             // ---- a stretch of one run
-            const int first = unit, last = static_cast<int>(min(static_cast<long long>(run.units), unit + left));
+            const int first = unit, last = min(run.units, unit + left);
             const int row0 = run.rb * S::kRows, nrow = min(S::kRows, run.cnt * p.G - row0);
             const int tiles = NT == 1 ? 1 : (nrow + 7) / 8;
-            __syncthreads();  // the rows of the stretch before are no longer read
-            for (int r = warp; r < S::kRows; r += kCaWarps) {
-                uint2 w = make_uint2(0, 0);
+            group_sync(group);  // the rows of the stretch before are no longer read
+            // queries: bf16 rows, then fp16 fragments scaled by a power of two a row
+            uint16_t* const q_raw = reinterpret_cast<uint16_t*>(merge);
+#pragma unroll 1
+            for (int x = tid; x < S::kRows * (D / 8); x += kCaGroup) {
+                const int r = x / (D / 8), token = p.token_of(row0 + r);
+                uint4 w = make_uint4(0, 0, 0, 0);
                 int vis = 0;
                 if (r < nrow) {
-                    const int i = max(0, min(p.pos[run.r0 + (row0 + r) / p.G], p.n - 1));
-                    const int64_t at_q = ((static_cast<int64_t>(run.b) * p.n + i) * p.Hq + run.h * p.G + (row0 + r) % p.G) * D;
-                    if (lane < D / 4) w = __ldg(reinterpret_cast<const uint2*>(p.q + at_q) + lane);
+                    const int i = max(0, min(p.pos[run.r0 + token], p.n - 1));
                     vis = min(run.len, max(0, run.len - p.n + i + 1));
+                    const int64_t at_q = (static_cast<int64_t>(run.b) * p.n + i) * p.Hq + run.h * p.G + row0 + r - token * p.G;
+                    w = __ldg(reinterpret_cast<const uint4*>(p.q + at_q * D) + x % (D / 8));
                 }
+                reinterpret_cast<uint4*>(q_raw)[x] = w;
+                if (x % (D / 8) == 0) row_vis[r] = vis;
+            }
+            group_sync(group);
+#pragma unroll 1
+            for (int r = warp; r < S::kRows; r += kCaWarps) {
                 // the row times 2^(140 - e), e the largest exponent: below 2^14
+                uint2 w = make_uint2(0, 0);
+                if (lane < D / 4) w = reinterpret_cast<const uint2*>(q_raw + r * D)[lane];
                 uint32_t top = 0;
-                uint32_t bits[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
+                const uint32_t bits[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t e = bits[j] >> 23 & 0xff;
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t e = bits[c] >> 23 & 0xff;
                     if (e != 0xff) top = max(top, e);
                 }
                 top = max(16u, __reduce_max_sync(0xffffffffu, top));
                 const float up = __uint_as_float((267u - top) << 23);
                 float f[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    f[j] = (bits[j] >> 23 & 0xff) == 0xff ? __uint_as_float(0x7fc00000u) : __uint_as_float(bits[j]) * up;
+                for (int c = 0; c < 4; ++c)
+                    f[c] = (bits[c] >> 23 & 0xff) == 0xff ? __uint_as_float(0x7fc00000u) : __uint_as_float(bits[c]) * up;
                 if (lane < D / 4)  // channels 4 lane ... 4 lane + 3: of thread lane / NS, step lane % NS
                     q_frag[((r >> 3) * NS + lane % NS) * 32 + (r & 7) * 4 + lane / NS] =
                         make_uint2(pack_f16(f[0], f[1]), pack_f16(f[2], f[3]));
-                if (lane == 0) {
-                    row_vis[r] = vis;
-                    // (2^(top - 140) alone may not be a normal number)
-                    row_mul[r] = fmaxf(ldexpf(p.scale2, static_cast<int>(top) - 140), 1.2e-38f);
-                }
+                if (lane == 0) row_mul[r] = fmaxf(p.scale2 * __uint_as_float((top - 13) << 23), 1.2e-38f);  // 2^(top - 140)
             }
-            __syncthreads();
-            float mul[NT][2], m[NT][2], l[NT][2], o[NT][NS][4];
+            group_sync(group);
+            float mul[NT][2], l[NT][2], o[NT][NS][4];
+            float m[NT][2], lim[NT][2];  // the maximum that is subtracted (0 before there is one) and q.k above which it moves
             int vis[NT][2], vis_min = run.len;
+            uint32_t poison = 0;  // bit 2 nt + j: row nt, 2t + j sees a value that is not finite in this thread's group
             uint2 q1[NS];
             if (NT == 1)
 #pragma unroll
@@ -347,18 +422,19 @@ __global__ void __launch_bounds__(kCaThreads, CaShape<D, NT>::kCtas) cache4_attn
                 for (int j = 0; j < 2; ++j) {
                     const int r = nt * 8 + 2 * t + j;
                     mul[nt][j] = row_mul[r], vis[nt][j] = row_vis[r];
-                    m[nt][j] = -INFINITY, l[nt][j] = 0.f;
+                    m[nt][j] = 0.f, lim[nt][j] = -INFINITY, l[nt][j] = 0.f;
 #pragma unroll
                     for (int i = 0; i < NS; ++i) o[nt][i][j] = o[nt][i][j + 2] = 0.f;
                 }
-            for (int r = lane; r < nrow; r += 32) vis_min = min(vis_min, row_vis[r]);
+            if (lane < nrow) vis_min = row_vis[lane];
             vis_min = __reduce_min_sync(0xffffffffu, vis_min);
 
+#pragma unroll 1
             for (; unit < last; ++unit, --left) {
                 cp_async_wait<kCaStages - 2>();
                 __syncwarp();
                 issue();
-                const uint32_t st = ring + use * S::kStage;
+                const uint8_t* const st = my_ring + use * S::kStage;
                 use = use + 1 == kCaStages ? 0 : use + 1;
                 const int key0 = unit * kCaUnit + warp * kCaKeys;
                 if (key0 >= run.len) continue;
@@ -376,17 +452,18 @@ __global__ void __launch_bounds__(kCaThreads, CaShape<D, NT>::kCtas) cache4_attn
                     for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const uint32_t key = 16 * mt + 8 * e + (g >> 1) + 4 * (g & 1);
-                            const uint32_t sa = st + 2 * S::kCodes + key * (D / 16);
+                            // (8 keys are a whole number of the exchange's periods)
+                            const uint8_t* at_k = st + k_at + (16 * mt + 8 * e) * (D / 2);
+                            const uint8_t* at_s = st + k_sc + (16 * mt + 8 * e) * (D / 16);
                             if (D == 128) {
-                                const uint4 x = ld_shared_v4(st + piece<D>(key, 16 * t));
+                                const uint4 x = *reinterpret_cast<const uint4*>(at_k);
                                 kw[mt][e][0] = x.x, kw[mt][e][1] = x.y, kw[mt][e][2 % (NS / 2)] = x.z;
                                 kw[mt][e][3 % (NS / 2)] = x.w;
-                                sc[mt][e] = ld_shared_u16(sa + 2 * t);
+                                sc[mt][e] = *reinterpret_cast<const uint16_t*>(at_s);
                             } else {
-                                const uint2 x = ld_shared_v2(st + piece<D>(key, 8 * t));
+                                const uint2 x = *reinterpret_cast<const uint2*>(at_k);
                                 kw[mt][e][0] = x.x, kw[mt][e][1] = x.y;
-                                sc[mt][e] = ld_shared_u8(sa + t);
+                                sc[mt][e] = *at_s;
                             }
                         }
 #pragma unroll
@@ -397,8 +474,8 @@ __global__ void __launch_bounds__(kCaThreads, CaShape<D, NT>::kCtas) cache4_attn
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 c4_decode(kw[mt][e][w], h[mt][e]);
-                                const uint32_t code = D == 128 && w >= NS / 4 ? sc[mt][e] >> 8 : sc[mt][e] & 0xff;
-                                const uint32_t f = dup16(c4_scale_f16(code));
+                                // the scale's f16 twice: code << 7 | code << 23
+                                const uint32_t f = (D == 128 && w >= NS / 4 ? sc[mt][e] >> 8 : sc[mt][e] & 0xff) * 0x800080u;
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) h[mt][e][j] = h2_mul(h[mt][e][j], f);
                             }
@@ -418,57 +495,56 @@ __global__ void __launch_bounds__(kCaThreads, CaShape<D, NT>::kCtas) cache4_attn
                     }
                 }
                 // ---- what a row does not see; softmax
-                const bool cut = key0 + kCaKeys > vis_min;
-                const bool drafts = cut && vis_min < run.len;  // keys that some rows see and some do not
+                const bool cut_here = key0 + kCaKeys > vis_min;
+                const bool drafts = cut_here && vis_min < run.len;  // keys that some rows see and some do not
                 uint32_t pb[2][NT][2];
-                uint32_t vb[2][NT][2];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     if (NT > 1 && nt >= tiles) break;
-                    if (cut) {
+                    if (cut_here) {
 #pragma unroll
-                        for (int mt = 0; mt < 2; ++mt) {
-                            const int key = key0 + 16 * mt + (g >> 1) + 4 * (g & 1);
-                            bool in[4];
+                        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                in[j] = key + 8 * (j >> 1) < vis[nt][j & 1];
-                                if (!in[j]) s[mt][nt][j] = -INFINITY;
-                            }
-                            vb[mt][nt][0] = (in[0] ? 0x3c00u : 0u) | (in[1] ? 0x3c000000u : 0u);
-                            vb[mt][nt][1] = (in[2] ? 0x3c00u : 0u) | (in[3] ? 0x3c000000u : 0u);
-                        }
+                            for (int j = 0; j < 4; ++j)
+                                if (key0 + 16 * mt + my_key + 8 * (j >> 1) >= vis[nt][j & 1]) s[mt][nt][j] = -INFINITY;
                     }
                     float top[2];
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
-                        top[j] = fmaxf(fmaxf(s[0][nt][j], s[0][nt][j + 2]), fmaxf(s[1][nt][j], s[1][nt][j + 2])) * mul[nt][j];
-                    if (__any_sync(0xffffffffu, top[0] > m[nt][0] + kCaSlack || top[1] > m[nt][1] + kCaSlack)) {
+                        top[j] = fmaxf(max3f(s[0][nt][j], s[0][nt][j + 2], s[1][nt][j]), s[1][nt][j + 2]);
+                    if (__any_sync(0xffffffffu, top[0] > lim[nt][0] || top[1] > lim[nt][1])) {
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
 #pragma unroll
                             for (int d = 4; d < 32; d <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], d));
-                            const float now = fmaxf(m[nt][j], top[j]);
-                            const float keep = m[nt][j] == -INFINITY ? 0.f : ex2_approx(m[nt][j] - now);
-                            // (a sum that is NaN stays so; nothing but zeros is summed where m is -infinity)
-                            l[nt][j] = m[nt][j] == -INFINITY ? l[nt][j] : l[nt][j] * keep;
+                            const bool none = lim[nt][j] == -INFINITY;  // nothing seen so far: all sums are 0 (or NaN)
+                            if (top[j] == -INFINITY) continue;
+                            const float now = none ? top[j] * mul[nt][j] : fmaxf(m[nt][j], top[j] * mul[nt][j]);
+                            const float keep = none ? 1.f : ex2_approx(m[nt][j] - now);
+                            l[nt][j] *= keep;
 #pragma unroll
                             for (int i = 0; i < NS; ++i) {
                                 o[nt][i][j] *= keep;
                                 o[nt][i][j + 2] *= keep;
                             }
                             m[nt][j] = now;
+                            lim[nt][j] = __fdividef(now + kCaSlack, mul[nt][j]);
                         }
                     }
-                    const float mu[2] = {m[nt][0] == -INFINITY ? 0.f : m[nt][0], m[nt][1] == -INFINITY ? 0.f : m[nt][1]};
+                    const uint64_t mu = f2_pack(-m[nt][0], -m[nt][1]);
+                    const uint64_t by = f2_pack(mul[nt][0], mul[nt][1]);
+                    uint64_t sum = f2_pack(l[nt][0], l[nt][1]);
 #pragma unroll
                     for (int mt = 0; mt < 2; ++mt) {
                         float e[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            e[j] = ex2_approx(fmaf(s[mt][nt][j], mul[nt][j & 1], -mu[j & 1]));
-                            l[nt][j & 1] += e[j];
+                        for (int j = 0; j < 4; j += 2) {
+                            f2_unpack(f2_fma(f2_pack(s[mt][nt][j], s[mt][nt][j + 1]), by, mu), e[j], e[j + 1]);
+                            e[j] = ex2_approx(e[j]);
+                            e[j + 1] = ex2_approx(e[j + 1]);
+                            sum = f2_add(sum, f2_pack(e[j], e[j + 1]));
                         }
+                        if (mt == 1) f2_unpack(sum, l[nt][0], l[nt][1]);
                         pb[mt][nt][0] = transpose8(pack_f16(e[0], e[1]));
                         pb[mt][nt][1] = transpose8(pack_f16(e[2], e[3]));
                     }
@@ -481,18 +557,17 @@ __global__ void __launch_bounds__(kCaThreads, CaShape<D, NT>::kCtas) cache4_attn
                         uint32_t code[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const uint32_t key = 16 * mt + 4 * j + t;
-                            const uint32_t va = st + S::kCodes;
+                            const uint8_t* at_v = st + v_at[j & 1] + (16 * mt + 8 * (j >> 1)) * (D / 2);
                             if (D == 128) {
-                                const uint2 x = ld_shared_v2(va + piece<D>(key, 8 * g));
+                                const uint2 x = *reinterpret_cast<const uint2*>(at_v);
                                 vw[j][0] = x.x, vw[j][1 % (NS / 4)] = x.y;
                             } else {
-                                vw[j][0] = ld_shared_u32(va + piece<D>(key, 4 * g));
+                                vw[j][0] = *reinterpret_cast<const uint32_t*>(at_v);
                             }
-                            code[j] = ld_shared_u8(st + 2 * S::kCodes + S::kScales + key * (D / 16) + (D == 128 ? g : g >> 1));
+                            code[j] = st[v_sc + (16 * mt + 4 * j) * (D / 16)];
                         }
-                        f[0] = (code[0] << 7) | (code[1] << 23);
-                        f[1] = (code[2] << 7) | (code[3] << 23);
+                        f[0] = code[1] * 0x800000u + code[0] * 0x80u;
+                        f[1] = code[3] * 0x800000u + code[2] * 0x80u;
                     }
                     if (drafts) {
                         // a value that is not finite counts for the rows that see it alone: its product is
@@ -511,12 +586,14 @@ __global__ void __launch_bounds__(kCaThreads, CaShape<D, NT>::kCtas) cache4_attn
                             for (int nt = 0; nt < NT; ++nt) {
                                 if (NT > 1 && nt >= tiles) break;
                                 float seen[4] = {0.f, 0.f, 0.f, 0.f};
-                                mma_f16(seen, a, transpose8(vb[mt][nt][0]), transpose8(vb[mt][nt][1]));
+                                uint32_t b[2];
 #pragma unroll
-                                for (int i = 0; i < NS; ++i)
-#pragma unroll
-                                    for (int j = 0; j < 4; ++j)
-                                        if (seen[j & 1] > 0.f) o[nt][i][j] = __uint_as_float(0x7fc00000u);
+                                for (int j = 0; j < 2; ++j) {
+                                    const int key = key0 + 16 * mt + my_key + 8 * j;
+                                    b[j] = transpose8((key < vis[nt][0] ? 0x3c00u : 0u) | (key < vis[nt][1] ? 0x3c000000u : 0u));
+                                }
+                                mma_f16(seen, a, b[0], b[1]);
+                                poison |= (seen[0] > 0.f ? 1u : 0u) << (2 * nt) | (seen[1] > 0.f ? 2u : 0u) << (2 * nt);
                             }
                         }
                     }
@@ -526,7 +603,7 @@ __global__ void __launch_bounds__(kCaThreads, CaShape<D, NT>::kCtas) cache4_attn
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const uint32_t a = vw[2 * e][w], b = vw[2 * e + 1][w];
-                            c4_decode((a & 0x0f0f0f0fu) | ((b << 4) & 0xf0f0f0f0u), h[e][0]);
+                            c4_decode((a & 0x0f0f0f0fu) | ((b * 16) & 0xf0f0f0f0u), h[e][0]);
                             c4_decode(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), h[e][1]);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
@@ -554,9 +631,21 @@ __global__ void __launch_bounds__(kCaThreads, CaShape<D, NT>::kCtas) cache4_attn
                 for (int j = 0; j < 2; ++j) {
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], d);
+                    if (lim[nt][j] == -INFINITY) m[nt][j] = -INFINITY;
                     if (g == 0) stats[warp * S::kRows + nt * 8 + 2 * t + j] = make_float2(m[nt][j], l[nt][j]);
                 }
-            __syncthreads();
+            group_sync(group);
+            if (tid < nrow) {
+                float top = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < kCaWarps; ++w) top = fmaxf(top, stats[w * S::kRows + tid].x);
+#pragma unroll
+                for (int w = 0; w < kCaWarps; ++w) {
+                    const float2 x = stats[w * S::kRows + tid];
+                    sum += x.x == -INFINITY ? x.y : x.y * ex2_approx(x.x - top);
+                }
+                stats[kCaWarps * S::kRows + tid] = make_float2(top, sum);
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -565,97 +654,127 @@ __global__ void __launch_bounds__(kCaThreads, CaShape<D, NT>::kCtas) cache4_attn
                     float top = -INFINITY;
 #pragma unroll
                     for (int w = 0; w < kCaWarps; ++w) top = fmaxf(top, stats[w * S::kRows + r].x);
-                    const float keep = m[nt][j] == -INFINITY ? 1.f : ex2_approx(m[nt][j] - top);
+                    float keep = m[nt][j] == -INFINITY ? 1.f : ex2_approx(m[nt][j] - top);
+                    if (poison >> (2 * nt + j) & 1) keep = __uint_as_float(0x7fc00000u);
                     if (r < nrow) {
                         float2* to = reinterpret_cast<float2*>(merge + (warp * S::kRows + r) * S::kRowBytes);
 #pragma unroll
                         for (int i = 0; i < NS; ++i) to[i * 8 + g] = make_float2(o[nt][i][j] * keep, o[nt][i][j + 2] * keep);
                     }
                 }
-            __syncthreads();
+            group_sync(group);
             const bool whole = first == 0 && last == run.units;
-            float* part = p.parts + (2ll * blockIdx.x + (first == 0)) * S::kPart;
-            for (int x = tid; x < nrow * (D / 2); x += kCaThreads) {
+            const uint32_t slot = 2 * (blockIdx.x * cut.cells + cell) + (first == 0);
+            float* part = p.parts + static_cast<int64_t>(slot) * S::kPart;
+#pragma unroll 1
+            for (int x = tid; x < nrow * (D / 2); x += kCaGroup) {
                 const int r = x / (D / 2), y = x % (D / 2);
                 // whole: channels 2y, 2y + 1; a part: in the fragments' order
-                const int slot = whole ? (y & (NS - 1)) * 8 + y / NS : y;
+                const int at = whole ? (y & (NS - 1)) * 8 + y / NS : y;
                 float2 sum = make_float2(0.f, 0.f);
-                float top = -INFINITY, total = 0.f;
 #pragma unroll
                 for (int w = 0; w < kCaWarps; ++w) {
-                    const float2 v = reinterpret_cast<const float2*>(merge + (w * S::kRows + r) * S::kRowBytes)[slot];
+                    const float2 v = reinterpret_cast<const float2*>(merge + (w * S::kRows + r) * S::kRowBytes)[at];
                     sum.x += v.x, sum.y += v.y;
-                    top = fmaxf(top, stats[w * S::kRows + r].x);
                 }
-#pragma unroll
-                for (int w = 0; w < kCaWarps; ++w) {
-                    const float2 st2 = stats[w * S::kRows + r];
-                    total += st2.x == -INFINITY ? st2.y : st2.y * ex2_approx(st2.x - top);
-                }
+                const float2 all = stats[kCaWarps * S::kRows + r];
                 if (!whole) {
                     reinterpret_cast<float2*>(part)[x] = sum;
-                    if (y == 0) reinterpret_cast<float2*>(part + S::kRows * D)[r] = make_float2(top, total);
+                    if (y == 0) reinterpret_cast<float2*>(part + S::kRows * D)[r] = all;
                     continue;
                 }
-                const int pr = run.r0 + (row0 + r) / p.G, hq = run.h * p.G + (row0 + r) % p.G;
-                const bool any = row_vis[r] > 0;
-                const float inv = 1.f / total;
+                const int token = p.token_of(row0 + r), hq = run.h * p.G + row0 + r - token * p.G, pr = run.r0 + token;
+                const bool any = all.y != 0.f;  // (a NaN is not)
+                const float inv = 1.f / all.y;
                 reinterpret_cast<uint32_t*>(p.o + (static_cast<int64_t>(pr) * p.Hq + hq) * D)[y] =
                     any ? cvt_bf16x2(sum.x * inv, sum.y * inv) : 0u;
                 if (y == 0 && p.lse)
-                    p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? (top + log2f(total)) * 0.693147181f : -INFINITY;
+                    p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? (all.x + log2f(all.y)) * 0.693147181f : -INFINITY;
             }
-            if (last < run.units && first == 0) {
-                const long long end = at.x1 + run.units - last;  // the unit after the run's last
-                goes_on = make_int4(run.b, run.h, run.rb, static_cast<int>((end * ctas - 1) / at.total));
-            }
-            if (last == run.units) {
+            if (last < run.units && first == 0)
+                open = CaOpen{run.r0, run.h, row0, nrow, static_cast<int>(cut.cell_of(base + run.units - 1)), {0, 0, 0}};
+            if (last == run.units && left > 0) {
                 unit = 0;
-                if (left > 0) ca_next(p, S::kRows, run);
+                base += run.units;
+                ca_next(p, S::kRows, run);
             }
         }
+        if (tid == 0) p.table[blockIdx.x * cut.cells + cell] = open;
     }
     cp_async_wait<0>();
-    if (tid == 0) p.table[blockIdx.x] = goes_on;
 }
 
-// Joins the parts of the run that goes on past CTA blockIdx.x of the first launch:
-// one row a CTA.
+// Joins the parts of the run that goes on past cell blockIdx.x, 8 rows a CTA: each row by
+// as many warps as there are for it, which share the parts.
 template <int D, int NT>
-__global__ void __launch_bounds__(kCaThreads) cache4_join_kernel(CaParams p)
+__global__ void __launch_bounds__(kJoinThreads) cache4_join_kernel(CaParams p)
 {
     using S = CaShape<D, NT>;
-    const int4 e = p.table[blockIdx.x];
-    if (e.x < 0) return;
-    CaRun run{};
-    ca_sequence(p, e.x, S::kRows, run);
-    const int row0 = e.z * S::kRows, r = blockIdx.y, tid = threadIdx.x;
-    if (r >= min(S::kRows, run.cnt * p.G - row0)) return;
-    const int first = blockIdx.x, n = e.w - first + 1;
-    auto slot = [&](int i) { return p.parts + (2ll * (first + i) + (i == 0)) * S::kPart; };
-    float top = -INFINITY;
-    for (int i = 0; i < n; ++i) top = fmaxf(top, slot(i)[S::kRows * D + 2 * r]);
-    float total = 0.f;
-    float2 sum = make_float2(0.f, 0.f);
-    for (int i = 0; i < n; ++i) {
-        const float2 st = reinterpret_cast<const float2*>(slot(i) + S::kRows * D)[r];
-        const float keep = st.x == -INFINITY ? 1.f : ex2_approx(st.x - top);
-        total += st.y * keep;
-        if (tid < D / 2) {
-            const float2 v = reinterpret_cast<const float2*>(slot(i))[r * (D / 2) + tid];
-            sum.x += v.x * keep, sum.y += v.y * keep;
+    constexpr int C = D / 32, W = kJoinThreads / 32;
+    __shared__ float sh[W][D + 1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, first = blockIdx.x;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const CaOpen e = p.table[first];
+    const int rows = min(8, e.nrow - static_cast<int>(blockIdx.y) * 8);
+    if (e.last < 0 || rows <= 0) return;
+    const int ways = rows > 4 ? W / 8 : rows > 2 ? W / 4 : rows > 1 ? W / 2 : W;  // warps a row
+    const int row = warp / ways, way = warp % ways, r = blockIdx.y * 8 + row, n = e.last - first + 1;
+    const auto part = [&](int i) { return p.parts + (2ll * (first + i) + (i == 0)) * S::kPart; };
+    float top = -INFINITY, total = 0.f, sum[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) sum[c] = 0.f;
+    if (row < rows) {
+        for (int i = lane; i < n; i += 32) top = fmaxf(top, part(i)[S::kRows * D + 2 * r]);
+        constexpr int AT = 4;  // parts in flight
+#pragma unroll 1
+        for (int i0 = way; i0 < n; i0 += AT * ways) {
+            float2 st[AT];
+            float v[AT][C];
+#pragma unroll
+            for (int k = 0; k < AT; ++k) {
+                const int i = i0 + k * ways;
+                st[k] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+                for (int c = 0; c < C; ++c) v[k][c] = 0.f;
+                if (i < n) {
+                    st[k] = reinterpret_cast<const float2*>(part(i) + S::kRows * D)[r];
+                    const float2* x = reinterpret_cast<const float2*>(part(i) + r * D) + lane * (C / 2);
+#pragma unroll
+                    for (int c = 0; c < C; c += 2) v[k][c] = x[c / 2].x, v[k][c + 1] = x[c / 2].y;
+                }
+            }
+            if (i0 == way)
+#pragma unroll
+                for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+#pragma unroll
+            for (int k = 0; k < AT; ++k) {
+                const float keep = st[k].x == -INFINITY ? 1.f : ex2_approx(st[k].x - top);
+                total += st[k].y * keep;
+#pragma unroll
+                for (int c = 0; c < C; ++c) sum[c] += v[k][c] * keep;
+            }
         }
+#pragma unroll
+        for (int c = 0; c < C; ++c) sh[warp][lane * C + c] = sum[c];
+        if (lane == 0) sh[warp][D] = total;
     }
-    const int pr = run.r0 + (row0 + r) / p.G, hq = e.y * p.G + (row0 + r) % p.G;
-    const int i = max(0, min(p.pos[pr], p.n - 1));
-    const bool any = min(run.len, max(0, run.len - p.n + i + 1)) > 0;
-    if (tid < D / 2) {
-        const int y = (tid & 7) * S::kSteps + tid / 8;  // fragment (i, g) holds channels 2 (g * steps + i), + 1
-        const float inv = 1.f / total;
-        reinterpret_cast<uint32_t*>(p.o + (static_cast<int64_t>(pr) * p.Hq + hq) * D)[y] =
-            any ? cvt_bf16x2(sum.x * inv, sum.y * inv) : 0u;
+    __syncthreads();
+    if (row >= rows || way > 0) return;
+    for (int w = 1; w < min(ways, n); ++w) {
+        total += sh[warp + w][D];
+#pragma unroll
+        for (int c = 0; c < C; ++c) sum[c] += sh[warp + w][lane * C + c];
     }
-    if (tid == 0 && p.lse)
+    const int token = p.token_of(e.row0 + r), hq = e.h * p.G + e.row0 + r - token * p.G, pr = e.r0 + token;
+    const bool any = total != 0.f;
+    const float inv = 1.f / total;
+    uint32_t* out = reinterpret_cast<uint32_t*>(p.o + (static_cast<int64_t>(pr) * p.Hq + hq) * D);
+#pragma unroll
+    for (int c = 0; c < C; c += 2) {
+        const int x = (lane * C + c) / 2;  // fragment (x / 8, g = x % 8) holds channels 2 (g * steps + x / 8), + 1
+        out[(x & 7) * S::kSteps + x / 8] = any ? cvt_bf16x2(sum[c] * inv, sum[c + 1] * inv) : 0u;
+    }
+    if (lane == 0 && p.lse)
         p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? (top + log2f(total)) * 0.693147181f : -INFINITY;
 }
 
@@ -667,6 +786,10 @@ int check_cache4_attn(const logo_dims& d, int n_new)
     if (static_cast<int64_t>(d.B) * n_new > (1 << 24) || d.Hkv > (1 << 16) ||
         static_cast<int64_t>(n_new) * (d.Hq / d.Hkv) > 8192 || static_cast<int64_t>(d.B) * n_new * d.Hq > (1 << 30))
         return LOGO_ERR_UNSUPPORTED;
+    // the line's units are counted in 31 bits
+    const int64_t units = (static_cast<int64_t>(d.T) + kCaUnit - 1) / kCaUnit;
+    const int64_t blocks = (static_cast<int64_t>(n_new) * (d.Hq / d.Hkv) + 8 * kCaMaxTiles - 1) / (8 * kCaMaxTiles);
+    if (units * d.B * d.Hkv > (1ll << 31) / blocks - 1) return LOGO_ERR_UNSUPPORTED;
     return LOGO_OK;
 }
 
@@ -692,9 +815,9 @@ int ca_dispatch(int D, int tiles, F f)
 }
 
 template <int D, int NT>
-int ca_grid(CaShape<D, NT>)
+int ca_cells(CaShape<D, NT>)
 {
-    return device_sm_count() * CaShape<D, NT>::kCtas;
+    return device_sm_count() * CaShape<D, NT>::kGroups;
 }
 
 template <int D, int NT>
@@ -703,10 +826,22 @@ int ca_launch(CaShape<D, NT> s, CaParams& p, cudaStream_t st)
     using S = CaShape<D, NT>;
     static OncePerDevice once;
     if (once([] { return set_smem_limit(cache4_attn_kernel<D, NT>, S::kSmem); }) != cudaSuccess) return LOGO_ERR_CUDA;
-    const unsigned grid = ca_grid(s);
-    cache4_attn_kernel<D, NT><<<grid, kCaThreads, S::kSmem, st>>>(p);
-    cache4_join_kernel<D, NT><<<dim3(grid, S::kRows), kCaThreads, 0, st>>>(p);
-    return cudaGetLastError() == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
+    // each launch is set up while the one before it on the stream runs (and waits for its end itself)
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(device_sm_count());
+    cfg.blockDim = dim3(S::kThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, cache4_attn_kernel<D, NT>, p) != cudaSuccess) return LOGO_ERR_CUDA;
+    cfg.gridDim = dim3(ca_cells(s), NT);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, cache4_join_kernel<D, NT>, p) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }
 
 }  // namespace
@@ -720,8 +855,8 @@ extern "C" size_t logo_decode_cache4_workspace_size(logo_dims dims, int n_new)
     size_t bytes = 0;
     ca_dispatch(dims.D, ca_tiles(dims, n_new), [&](auto s) {
         using S = decltype(s);
-        const size_t grid = ca_grid(s);
-        bytes = round_up(grid * sizeof(int4), 256) + 2 * grid * S::kPart * sizeof(float);
+        const size_t cells = ca_cells(s);
+        bytes = round_up(cells * sizeof(CaOpen), 256) + 2 * cells * S::kPart * sizeof(float);
         return 0;
     });
     return bytes;
@@ -746,10 +881,11 @@ extern "C" int logo_decode_cache4_attn(const logo_bf16* q, logo_cache4 cache, co
     p.q = q, p.k = cache.k, p.v = cache.v, p.ks = cache.k_scale, p.vs = cache.v_scale;
     p.len = seq_len, p.pos = pos, p.cu_q = cu_q, p.n_sel = n_sel_total, p.o = o_c, p.lse = lse_c;
     p.B = dims.B, p.n = n_new, p.Hq = dims.Hq, p.Hkv = dims.Hkv, p.G = dims.Hq / dims.Hkv, p.L = dims.T;
+    p.magic = p.G > 1 ? 0xffffffffu / p.G + 1 : 0;
     p.scale2 = (scale > 0.f ? scale : 1.f / sqrtf(static_cast<float>(dims.D))) * 1.44269504f;
     return ca_dispatch(dims.D, ca_tiles(dims, n_new), [&](auto s) {
-        p.table = static_cast<int4*>(workspace);
-        p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + round_up(ca_grid(s) * sizeof(int4), 256));
+        p.table = static_cast<CaOpen*>(workspace);
+        p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + round_up(ca_cells(s) * sizeof(CaOpen), 256));
         return ca_launch(s, p, static_cast<cudaStream_t>(stream));
     });
 }
