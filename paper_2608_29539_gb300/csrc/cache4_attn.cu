@@ -48,6 +48,9 @@ namespace {
 #ifndef CA_C2
 #define CA_C2 3
 #endif
+#ifndef CA_RC
+#define CA_RC 2
+#endif
 constexpr int kCaWarps = 4;                   // of a group
 constexpr int kCaGroup = 32 * kCaWarps;
 constexpr int kCaKeys = 32;                   // keys of a warp's step
@@ -79,19 +82,24 @@ struct CaParams {
     __device__ __forceinline__ int token_of(int row) const { return magic ? __umulhi(row, magic) : row; }  // row / G
 };
 
+// Sizes of the kernel for one tile of rows (NT = 1), whose warps have all channels of
+// their keys, and of the one for more, whose warps have a quarter of the channels of all keys.
 template <int D, int NT>
 struct CaShape {
+    static constexpr bool kWide = NT > 1;
     static constexpr int kRows = 8 * NT;
-    static constexpr int kGroups = NT == 1 ? CA_C1 : NT == 2 ? CA_C2 : 2;  // an SM
+    static constexpr int kGroups = NT < 3 ? CA_C1 : CA_C2;     // an SM
     static constexpr int kThreads = kGroups * kCaGroup;
+    static constexpr int kRunCost = CA_RC;                     // units that beginning a run costs about as much as
     static constexpr int kCodes = kCaKeys * D / 2, kScales = kCaKeys * D / 16;  // bytes a step, K or V
     static constexpr int kStage = 2 * (kCodes + kScales);
     static constexpr int kSteps = D / 16;                      // k steps of S^T, m tiles of O^T
-    static constexpr int kRowBytes = 4 * D + 16;               // a row of the warps' results (padded for the banks)
     static constexpr int kRing = kCaWarps * kCaStages * kStage;
     static constexpr int kQ = NT * kSteps * 32 * 8;            // fragments of Q
-    static constexpr int kMerge = kCaWarps * kRows * kRowBytes;  // (ahead of a run: its queries)
-    static constexpr int kStats = (kCaWarps + 1) * kRows * 8 + kRows * 8;
+    // the warps' results: rows padded for the banks; or P's fragments (and the queries as they come)
+    static constexpr int kRowBytes = 4 * D + 16;
+    static constexpr int kMerge = kWide ? NT * 2048 : kCaWarps * kRows * kRowBytes;
+    static constexpr int kStats = (kCaWarps + 1) * kRows * 8 + 4 * kRows * 4;
     static constexpr int kGroupBytes = kRing + kQ + kMerge + kStats;
     static constexpr int kSmem = kGroups * kGroupBytes;
     static constexpr int kPart = kRows * (D + 2);              // floats of a part
@@ -165,7 +173,23 @@ __device__ __forceinline__ void group_sync(int group)
     asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kCaGroup) : "memory");
 }
 
-// A run: the units of one (sequence, KV head, row block), in the line's order.
+// Whether x holds in any thread of the group, which all arrive.
+__device__ __forceinline__ bool group_any(int group, bool x)
+{
+    int r;
+    asm volatile(
+        "{\n\t.reg .pred P, Q;\n\t"
+        "setp.ne.s32 P, %3, 0;\n\t"
+        "bar.red.or.pred Q, %1, %2, P;\n\t"
+        "selp.s32 %0, 1, 0, Q;\n\t}"
+        : "=r"(r)
+        : "r"(group + 1), "n"(kCaGroup), "r"(static_cast<int>(x))
+        : "memory");
+    return r != 0;
+}
+
+// A run: the units of one (sequence, KV head, row block), in the line's order.  On the line
+// it has room for what beginning it costs, then its units.
 struct CaRun {
     int b, h, rb;
     int nrb, units, len, r0, cnt;   // of the sequence
@@ -196,10 +220,10 @@ __device__ __forceinline__ void ca_next(const CaParams& p, int rows, CaRun& r)
     ca_sequence(p, b, rows, r);  // (only called where another run follows)
 }
 
-__device__ __forceinline__ uint32_t ca_weight(const CaParams& p, int b, int rows)
+__device__ __forceinline__ uint32_t ca_weight(const CaParams& p, int b, int rows, int cost)
 {
     CaRun r;
-    return b < p.B && ca_sequence(p, b, rows, r) ? static_cast<uint32_t>(r.units) * r.nrb * p.Hkv : 0u;
+    return b < p.B && ca_sequence(p, b, rows, r) ? static_cast<uint32_t>(r.units + cost) * r.nrb * p.Hkv : 0u;
 }
 
 // How the line is cut: SM i has `each` units, one more where i < extra, in `cells` equal
@@ -225,12 +249,12 @@ struct CaCut {
 };
 
 // The line's length; all threads of the CTA.
-__device__ __forceinline__ uint32_t ca_length(const CaParams& p, int rows, uint32_t* sh)
+__device__ __forceinline__ uint32_t ca_length(const CaParams& p, int rows, int cost, uint32_t* sh)
 {
-    if (p.B <= 32) return __reduce_add_sync(0xffffffffu, ca_weight(p, threadIdx.x % 32, rows));  // every warp for itself
+    if (p.B <= 32) return __reduce_add_sync(0xffffffffu, ca_weight(p, threadIdx.x % 32, rows, cost));  // every warp for itself
     uint32_t w = 0;
 #pragma unroll 1
-    for (int b = threadIdx.x; b < p.B; b += blockDim.x) w += ca_weight(p, b, rows);
+    for (int b = threadIdx.x; b < p.B; b += blockDim.x) w += ca_weight(p, b, rows, cost);
     w = __reduce_add_sync(0xffffffffu, w);
     if (threadIdx.x % 32 == 0) sh[threadIdx.x / 32] = w;
     __syncthreads();
@@ -239,13 +263,13 @@ __device__ __forceinline__ uint32_t ca_length(const CaParams& p, int rows, uint3
 }
 
 // The sequence whose runs hold unit x of the line, and its first unit; every warp for itself.
-__device__ __forceinline__ uint2 ca_find(const CaParams& p, int rows, uint32_t x)
+__device__ __forceinline__ uint2 ca_find(const CaParams& p, int rows, int cost, uint32_t x)
 {
     const int lane = threadIdx.x & 31;
     uint32_t base = 0;
 #pragma unroll 1
     for (int b0 = 0;; b0 += 32) {
-        const uint32_t mine = ca_weight(p, b0 + lane, rows);
+        const uint32_t mine = ca_weight(p, b0 + lane, rows, cost);
         uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -261,10 +285,240 @@ __device__ __forceinline__ uint2 ca_find(const CaParams& p, int rows, uint32_t x
     }
 }
 
-template <int D, int NT>
-__global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_attn_kernel(CaParams p)
+// A group's stretch of the line and where it begins: run, unit of it, units left to the
+// stretch's end.
+struct CaCell {
+    uint32_t cell, cells, x1, base;  // base: of the run, on the line
+    CaCut cut;
+    CaRun run;
+    int unit;
+    bool any;
+};
+
+template <typename S>
+__device__ __forceinline__ CaCell ca_cell(const CaParams& p, int group, uint32_t* sh)
 {
-    using S = CaShape<D, NT>;
+    const uint32_t total = ca_length(p, S::kRows, S::kRunCost, sh);
+    const CaCut cut(total, gridDim.x, S::kGroups);
+    CaCell c{0, cut.cells, 0, 0, cut, {}, 0, false};
+    const uint32_t units = cut.units(blockIdx.x), begin = cut.begin(blockIdx.x);
+    // the entries of the table that no cell writes
+    const uint32_t spare = S::kGroups - cut.cells, mine = units ? 0 : cut.cells;
+    if (threadIdx.x < spare) p.table[gridDim.x * cut.cells + blockIdx.x * spare + threadIdx.x].last = -1;
+    if (threadIdx.x < mine) p.table[blockIdx.x * cut.cells + threadIdx.x].last = -1;
+    if (units == 0 || group >= cut.cells) return c;
+    c.any = true;
+    c.cell = blockIdx.x * cut.cells + group;
+    const uint32_t x0 = begin + cut.cell(units, group);
+    c.x1 = begin + cut.cell(units, group + 1);
+    const uint2 at = ca_find(p, S::kRows, S::kRunCost, x0);
+    ca_sequence(p, at.x, S::kRows, c.run);
+    const uint32_t weight = c.run.units + S::kRunCost, i = (x0 - at.y) / weight;
+    c.run.h = i / c.run.nrb, c.run.rb = i % c.run.nrb;
+    c.base = at.y + i * weight;
+    c.unit = max(0, static_cast<int>(x0 - c.base) - S::kRunCost);
+    return c;
+}
+
+// Units of the run that begins at `base` on the line which lie before x.
+template <typename S>
+__device__ __forceinline__ int ca_before(const CaRun& r, uint32_t base, uint32_t x)
+{
+    return max(0, min(r.units, static_cast<int>(min(x - base, 0x40000000u)) - S::kRunCost));
+}
+
+// The copies of a warp's steps into its ring, with a place on the line of their own.
+template <int D, typename S>
+struct CaCopies {
+    const CaParams& p;
+    uint32_t to_codes, to_scales;  // this lane's first pieces of a stage, in shared memory
+    int warp, lane;
+    CaRun run;
+    int unit;
+    uint32_t base, x1, fill = 0;
+    const uint8_t *k, *v, *ks, *vs;
+
+    __device__ __forceinline__ CaCopies(const CaParams& p_, uint32_t ring, int warp_, int lane_, const CaCell& c)
+        : p(p_), to_codes(ring + piece<D>(lane_ * 16 / (D / 2), lane_ * 16 % (D / 2))),
+          to_scales(ring + 2 * S::kCodes + lane_ * (D / 16)), warp(warp_), lane(lane_), run(c.run), unit(c.unit),
+          base(c.base), x1(c.x1)
+    {
+        point();
+    }
+    __device__ __forceinline__ void point()
+    {
+        const int64_t row0 = (static_cast<int64_t>(run.b) * p.Hkv + run.h) * p.L + static_cast<int64_t>(unit) * kCaUnit + warp * kCaKeys;
+        k = p.k + row0 * (D / 2) + lane * 16;
+        v = p.v + row0 * (D / 2) + lane * 16;
+        ks = p.ks + (row0 + lane) * (D / 16);
+        vs = p.vs + (row0 + lane) * (D / 16);
+    }
+    // The next step's copies, one group (an empty one past the stretch's end).
+    __device__ __forceinline__ void issue()
+    {
+        if (base + S::kRunCost + unit < x1) {
+            const int rows = run.len - unit * kCaUnit - warp * kCaKeys;
+            const uint32_t to = to_codes + fill * S::kStage, tos = to_scales + fill * S::kStage;
+            if (rows >= kCaKeys) {
+#pragma unroll
+                for (int i = 0; i < S::kCodes / 512; ++i) {
+                    cp_async16(to + i * 512, k + i * 512);
+                    cp_async16(to + i * 512 + S::kCodes, v + i * 512);
+                }
+                cp_async_small<D / 16>(tos, ks);
+                cp_async_small<D / 16>(tos + S::kScales, vs);
+            } else if (rows > 0) {  // rows past the end are written as zeros
+#pragma unroll 1
+                for (int i = 0; i < S::kCodes / 512; ++i) {
+                    const bool in = (i * 512 + lane * 16) / (D / 2) < rows;
+                    cp_async16(to + i * 512, in ? k + i * 512 : p.k, in ? 16 : 0);
+                    cp_async16(to + i * 512 + S::kCodes, in ? v + i * 512 : p.v, in ? 16 : 0);
+                }
+                const bool in = lane < rows;
+                cp_async_small<D / 16>(tos, in ? ks : p.ks, in ? D / 16 : 0);
+                cp_async_small<D / 16>(tos + S::kScales, in ? vs : p.vs, in ? D / 16 : 0);
+            }
+            k += kCaUnit * (D / 2), v += kCaUnit * (D / 2), ks += kCaUnit * (D / 16), vs += kCaUnit * (D / 16);
+            if (++unit == run.units) {
+                base += run.units + S::kRunCost;
+                unit = 0;
+                if (base + S::kRunCost < x1) {
+                    ca_next(p, S::kRows, run);
+                    point();
+                }
+            }
+        }
+        cp_async_commit();
+        fill = fill + 1 == kCaStages ? 0 : fill + 1;
+    }
+};
+
+// A run's queries: bf16 rows into `raw`, then fp16 fragments scaled by a power of two a row;
+// what each row sees, and the factor from its products to logits (in powers of two).
+// Begins and ends with a barrier of the group.
+template <int D, typename S>
+__device__ __forceinline__ void ca_queries(const CaParams& p, const CaRun& run, int row0, int nrow, int group, int tid,
+                                           uint8_t* raw, uint2* q_frag, int* row_vis, float* row_mul)
+{
+    constexpr int NS = S::kSteps;
+    const int lane = tid & 31, warp = tid >> 5;
+    group_sync(group);  // the rows of the stretch before are no longer read
+#pragma unroll 1
+    for (int x = tid; x < S::kRows * (D / 8); x += kCaGroup) {
+        const int r = x / (D / 8), token = p.token_of(row0 + r);
+        uint4 w = make_uint4(0, 0, 0, 0);
+        int vis = 0;
+        if (r < nrow) {
+            const int i = max(0, min(p.pos[run.r0 + token], p.n - 1));
+            vis = min(run.len, max(0, run.len - p.n + i + 1));
+            const int64_t at_q = (static_cast<int64_t>(run.b) * p.n + i) * p.Hq + run.h * p.G + row0 + r - token * p.G;
+            w = __ldg(reinterpret_cast<const uint4*>(p.q + at_q * D) + x % (D / 8));
+        }
+        reinterpret_cast<uint4*>(raw)[x] = w;
+        if (x % (D / 8) == 0) row_vis[r] = vis;
+    }
+    group_sync(group);
+#pragma unroll 1
+    for (int r = warp; r < S::kRows; r += kCaWarps) {
+        // the row times 2^(140 - e), e the largest exponent: below 2^14
+        uint2 w = make_uint2(0, 0);
+        if (lane < D / 4) w = reinterpret_cast<const uint2*>(raw + r * D * 2)[lane];
+        uint32_t top = 0;
+        const uint32_t bits[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint32_t e = bits[c] >> 23 & 0xff;
+            if (e != 0xff) top = max(top, e);
+        }
+        top = max(16u, __reduce_max_sync(0xffffffffu, top));
+        const float up = __uint_as_float((267u - top) << 23);
+        float f[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            f[c] = (bits[c] >> 23 & 0xff) == 0xff ? __uint_as_float(0x7fc00000u) : __uint_as_float(bits[c]) * up;
+        if (lane < D / 4)  // channels 4 lane ... 4 lane + 3: of thread lane / NS, step lane % NS
+            q_frag[((r >> 3) * NS + lane % NS) * 32 + (r & 7) * 4 + lane / NS] = make_uint2(pack_f16(f[0], f[1]), pack_f16(f[2], f[3]));
+        if (lane == 0) row_mul[r] = fmaxf(p.scale2 * __uint_as_float((top - 13) << 23), 1.2e-38f);  // 2^(top - 140)
+    }
+    group_sync(group);
+}
+
+// S^T of a warp's step, raw products: row g of a tile is key (g >> 1) + 4 (g & 1), row g + 8
+// that plus 8; columns are rows of Q.  st: the stage; k_at, k_sc: this thread's pieces.
+template <int D, int NT, typename F>
+__device__ __forceinline__ void ca_scores(const uint8_t* st, uint32_t k_at, uint32_t k_sc, int tiles, F frag, float (&s)[2][NT][4])
+{
+    constexpr int NS = D / 16;
+    uint32_t kw[2][2][NS / 2], sc[2][2];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[mt][nt][j] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            // (8 keys are a whole number of the exchange's periods)
+            const uint8_t* at_k = st + k_at + (16 * mt + 8 * e) * (D / 2);
+            const uint8_t* at_s = st + k_sc + (16 * mt + 8 * e) * (D / 16);
+            if (D == 128) {
+                const uint4 x = *reinterpret_cast<const uint4*>(at_k);
+                kw[mt][e][0] = x.x, kw[mt][e][1] = x.y, kw[mt][e][2 % (NS / 2)] = x.z;
+                kw[mt][e][3 % (NS / 2)] = x.w;
+                sc[mt][e] = *reinterpret_cast<const uint16_t*>(at_s);
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(at_k);
+                kw[mt][e][0] = x.x, kw[mt][e][1] = x.y;
+                sc[mt][e] = *at_s;
+            }
+        }
+    }
+#pragma unroll
+    for (int w = 0; w < NS / 2; ++w) {
+        uint32_t h[2][2][4];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                c4_decode(kw[mt][e][w], h[mt][e]);
+                // the scale's f16 twice: code << 7 | code << 23
+                const uint32_t f = (D == 128 && w >= NS / 4 ? sc[mt][e] >> 8 : sc[mt][e] & 0xff) * 0x800080u;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) h[mt][e][j] = h2_mul(h[mt][e][j], f);
+            }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (NT > 1 && nt >= tiles) break;
+                const uint2 qf = frag(nt, 2 * w + half);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    const uint32_t a[4] = {h[mt][0][2 * half], h[mt][1][2 * half], h[mt][0][2 * half + 1], h[mt][1][2 * half + 1]};
+                    mma_f16(s[mt][nt], a, qf.x, qf.y);
+                }
+            }
+    }
+}
+
+// Scales of four keys that are not finite are taken out of f; the mask of their halves.
+__device__ __forceinline__ void ca_take_bad(uint32_t (&f)[2], uint32_t (&bad)[2])
+{
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint32_t lo = (f[j] & 0x7c00u) == 0x7c00u ? 0xffffu : 0u;
+        const uint32_t hi = (f[j] & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
+        bad[j] = lo | hi;
+        f[j] &= ~bad[j];
+    }
+}
+
+__device__ __forceinline__ float ca_lse(float top, float total) { return (top + log2f(total)) * 0.693147181f; }
+
+template <int D>
+__global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel(CaParams p)
+{
+    using S = CaShape<D, 1>;
     constexpr int NS = S::kSteps;
     extern __shared__ __align__(128) uint8_t smem_all[];
     __shared__ uint32_t sh_line[32];
@@ -272,7 +526,6 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_attn_kerne
     const int lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     uint8_t* const smem = smem_all + group * S::kGroupBytes;
     const uint8_t* const my_ring = smem + warp * (kCaStages * S::kStage);
-    const uint32_t ring = smem_u32(my_ring);
     uint2* const q_frag = reinterpret_cast<uint2*>(smem + S::kRing);
     uint8_t* const merge = smem + S::kRing + S::kQ;
     float2* const stats = reinterpret_cast<float2*>(merge + S::kMerge);  // [warp, all][row] (max, sum)
@@ -283,318 +536,134 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_attn_kerne
     const uint32_t k_at = piece<D>(my_key, t * (D / 8)), k_sc = 2 * S::kCodes + my_key * (D / 16) + t * (D / 64);
     const uint32_t v_at[2] = {S::kCodes + piece<D>(t, g * (D / 16)), S::kCodes + piece<D>(t + 4, g * (D / 16))};
     const uint32_t v_sc = 2 * S::kCodes + S::kScales + t * (D / 16) + (D == 128 ? g : g >> 1);
-    const uint32_t to0 = ring + piece<D>(lane * 16 / (D / 2), lane * 16 % (D / 2));
-    const uint32_t to1 = ring + 2 * S::kCodes + lane * (D / 16);
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const uint32_t total = ca_length(p, S::kRows, sh_line);
-    const CaCut cut(total, gridDim.x, S::kGroups);
-    const uint32_t my_units = cut.units(blockIdx.x), my_begin = cut.begin(blockIdx.x);
-    // the entries of the table that no cell below writes
-    const uint32_t spare = S::kGroups - cut.cells;
-    if (threadIdx.x < spare) p.table[gridDim.x * cut.cells + blockIdx.x * spare + threadIdx.x].last = -1;
-    if (my_units == 0) {
-        if (threadIdx.x < cut.cells) p.table[blockIdx.x * cut.cells + threadIdx.x].last = -1;
-        return;
-    }
-    uint32_t fill = 0, use = 0;  // stages
-    const uint32_t cell = group;
-    if (cell < cut.cells) {
-        const uint32_t x0 = my_begin + cut.cell(my_units, cell), x1 = my_begin + cut.cell(my_units, cell + 1);
-        CaRun run{};
-        const uint2 at = ca_find(p, S::kRows, x0);
-        ca_sequence(p, at.x, S::kRows, run);
-        uint32_t base = (x0 - at.y) / run.units;  // of the run, on the line
-        run.h = base / run.nrb, run.rb = base % run.nrb;
-        base = at.y + base * run.units;
-        int unit = x0 - base;
-        CaOpen open{0, 0, 0, 0, -1, {0, 0, 0}};
-
-        // ---- loads: a cursor of its own, kCaStages - 1 units ahead
-        CaRun ahead = run;
-        int ahead_unit = unit, ahead_left = x1 - x0;
-        const uint8_t *k, *v, *ks, *vs;  // this lane's first pieces of the step ahead
-        auto point = [&] {
-            const int64_t row0 = (static_cast<int64_t>(ahead.b) * p.Hkv + ahead.h) * p.L + ahead_unit * kCaUnit + warp * kCaKeys;
-            k = p.k + row0 * (D / 2) + lane * 16;
-            v = p.v + row0 * (D / 2) + lane * 16;
-            ks = p.ks + (row0 + lane) * (D / 16);
-            vs = p.vs + (row0 + lane) * (D / 16);
-        };
-        point();
-        auto issue = [&] {
-            if (ahead_left > 0) {
-                const int rows = ahead.len - ahead_unit * kCaUnit - warp * kCaKeys;
-                const uint32_t st = fill * S::kStage;
-                if (rows >= kCaKeys) {
-#pragma unroll
-                    for (int i = 0; i < S::kCodes / 512; ++i) {
-                        cp_async16(to0 + st + i * 512, k + i * 512);
-                        cp_async16(to0 + st + i * 512 + S::kCodes, v + i * 512);
-                    }
-                    cp_async_small<D / 16>(to1 + st, ks);
-                    cp_async_small<D / 16>(to1 + st + S::kScales, vs);
-                } else if (rows > 0) {  // rows past the end are written as zeros
+    CaCell c = ca_cell<S>(p, group, sh_line);
+    if (!c.any) return;
+    CaRun& run = c.run;
+    CaCopies<D, S> copies(p, smem_u32(my_ring), warp, lane, c);
+    CaOpen open{0, 0, 0, 0, -1, {0, 0, 0}};
+    uint32_t use = 0;  // stage
 #pragma unroll 1
-                    for (int i = 0; i < S::kCodes / 512; ++i) {
-                        const bool in = (i * 512 + lane * 16) / (D / 2) < rows;
-                        cp_async16(to0 + st + i * 512, in ? k + i * 512 : p.k, in ? 16 : 0);
-                        cp_async16(to0 + st + i * 512 + S::kCodes, in ? v + i * 512 : p.v, in ? 16 : 0);
-                    }
-                    const bool in = lane < rows;
-                    cp_async_small<D / 16>(to1 + st, in ? ks : p.ks, in ? D / 16 : 0);
-                    cp_async_small<D / 16>(to1 + st + S::kScales, in ? vs : p.vs, in ? D / 16 : 0);
-                }
-                --ahead_left;
-                k += kCaUnit * (D / 2), v += kCaUnit * (D / 2), ks += kCaUnit * (D / 16), vs += kCaUnit * (D / 16);
-                if (++ahead_unit == ahead.units && ahead_left > 0) {
-                    ahead_unit = 0;
-                    ca_next(p, S::kRows, ahead);
-                    point();
-                }
-            }
-            cp_async_commit();
-            fill = fill + 1 == kCaStages ? 0 : fill + 1;
-        };
+    for (int i = 0; i < kCaStages - 1; ++i) copies.issue();
 #pragma unroll 1
-        for (int i = 0; i < kCaStages - 1; ++i) issue();
-
-#pragma unroll 1
-        for (int left = x1 - x0; left > 0;) {
-            // ---- a stretch of one run
-            const int first = unit, last = min(run.units, unit + left);
-            const int row0 = run.rb * S::kRows, nrow = min(S::kRows, run.cnt * p.G - row0);
-            const int tiles = NT == 1 ? 1 : (nrow + 7) / 8;
-            group_sync(group);  // the rows of the stretch before are no longer read
-            // queries: bf16 rows, then fp16 fragments scaled by a power of two a row
-            uint16_t* const q_raw = reinterpret_cast<uint16_t*>(merge);
-#pragma unroll 1
-            for (int x = tid; x < S::kRows * (D / 8); x += kCaGroup) {
-                const int r = x / (D / 8), token = p.token_of(row0 + r);
-                uint4 w = make_uint4(0, 0, 0, 0);
-                int vis = 0;
-                if (r < nrow) {
-                    const int i = max(0, min(p.pos[run.r0 + token], p.n - 1));
-                    vis = min(run.len, max(0, run.len - p.n + i + 1));
-                    const int64_t at_q = (static_cast<int64_t>(run.b) * p.n + i) * p.Hq + run.h * p.G + row0 + r - token * p.G;
-                    w = __ldg(reinterpret_cast<const uint4*>(p.q + at_q * D) + x % (D / 8));
-                }
-                reinterpret_cast<uint4*>(q_raw)[x] = w;
-                if (x % (D / 8) == 0) row_vis[r] = vis;
-            }
-            group_sync(group);
-#pragma unroll 1
-            for (int r = warp; r < S::kRows; r += kCaWarps) {
-                // the row times 2^(140 - e), e the largest exponent: below 2^14
-                uint2 w = make_uint2(0, 0);
-                if (lane < D / 4) w = reinterpret_cast<const uint2*>(q_raw + r * D)[lane];
-                uint32_t top = 0;
-                const uint32_t bits[4] = {w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint32_t e = bits[c] >> 23 & 0xff;
-                    if (e != 0xff) top = max(top, e);
-                }
-                top = max(16u, __reduce_max_sync(0xffffffffu, top));
-                const float up = __uint_as_float((267u - top) << 23);
-                float f[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    f[c] = (bits[c] >> 23 & 0xff) == 0xff ? __uint_as_float(0x7fc00000u) : __uint_as_float(bits[c]) * up;
-                if (lane < D / 4)  // channels 4 lane ... 4 lane + 3: of thread lane / NS, step lane % NS
-                    q_frag[((r >> 3) * NS + lane % NS) * 32 + (r & 7) * 4 + lane / NS] =
-                        make_uint2(pack_f16(f[0], f[1]), pack_f16(f[2], f[3]));
-                if (lane == 0) row_mul[r] = fmaxf(p.scale2 * __uint_as_float((top - 13) << 23), 1.2e-38f);  // 2^(top - 140)
-            }
-            group_sync(group);
-            float mul[NT][2], l[NT][2], o[NT][NS][4];
-            float m[NT][2], lim[NT][2];  // the maximum that is subtracted (0 before there is one) and q.k above which it moves
-            int vis[NT][2], vis_min = run.len;
-            uint32_t poison = 0;  // bit 2 nt + j: row nt, 2t + j sees a value that is not finite in this thread's group
+    for (int unit = c.unit; c.base < c.x1; unit = 0) {
+        // ---- a stretch of one run
+        const int first = unit, last = ca_before<S>(run, c.base, c.x1), nrow = run.cnt * p.G;
+        if (first < last) {
+            ca_queries<D, S>(p, run, 0, nrow, group, tid, merge, q_frag, row_vis, row_mul);
+            float mul[2], l[2], o[NS][4];
+            float m[2], lim[2];  // the maximum that is subtracted (0 before there is one) and q.k above which it moves
+            int vis[2], vis_min = run.len;
+            uint32_t poison = 0;  // bit j: row 2t + j sees a value that is not finite in this thread's group
             uint2 q1[NS];
-            if (NT == 1)
 #pragma unroll
-                for (int ks = 0; ks < NS; ++ks) q1[ks] = q_frag[ks * 32 + lane];
+            for (int i = 0; i < NS; ++i) {
+                q1[i] = q_frag[i * 32 + lane];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+            }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int r = nt * 8 + 2 * t + j;
-                    mul[nt][j] = row_mul[r], vis[nt][j] = row_vis[r];
-                    m[nt][j] = 0.f, lim[nt][j] = -INFINITY, l[nt][j] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < NS; ++i) o[nt][i][j] = o[nt][i][j + 2] = 0.f;
-                }
+            for (int j = 0; j < 2; ++j) {
+                mul[j] = row_mul[2 * t + j], vis[j] = row_vis[2 * t + j];
+                m[j] = 0.f, lim[j] = -INFINITY, l[j] = 0.f;
+            }
             if (lane < nrow) vis_min = row_vis[lane];
             vis_min = __reduce_min_sync(0xffffffffu, vis_min);
 
 #pragma unroll 1
-            for (; unit < last; ++unit, --left) {
+            for (; unit < last; ++unit) {
                 cp_async_wait<kCaStages - 2>();
                 __syncwarp();
-                issue();
+                copies.issue();
                 const uint8_t* const st = my_ring + use * S::kStage;
                 use = use + 1 == kCaStages ? 0 : use + 1;
                 const int key0 = unit * kCaUnit + warp * kCaKeys;
                 if (key0 >= run.len) continue;
-                // ---- S^T: row g of a tile is key (g >> 1) + 4 (g & 1), row g + 8 that plus 8
-                float s[2][NT][4];
-#pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) s[mt][nt][j] = 0.f;
-                {
-                    uint32_t kw[2][2][NS / 2], sc[2][2];
-#pragma unroll
-                    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            // (8 keys are a whole number of the exchange's periods)
-                            const uint8_t* at_k = st + k_at + (16 * mt + 8 * e) * (D / 2);
-                            const uint8_t* at_s = st + k_sc + (16 * mt + 8 * e) * (D / 16);
-                            if (D == 128) {
-                                const uint4 x = *reinterpret_cast<const uint4*>(at_k);
-                                kw[mt][e][0] = x.x, kw[mt][e][1] = x.y, kw[mt][e][2 % (NS / 2)] = x.z;
-                                kw[mt][e][3 % (NS / 2)] = x.w;
-                                sc[mt][e] = *reinterpret_cast<const uint16_t*>(at_s);
-                            } else {
-                                const uint2 x = *reinterpret_cast<const uint2*>(at_k);
-                                kw[mt][e][0] = x.x, kw[mt][e][1] = x.y;
-                                sc[mt][e] = *at_s;
-                            }
-                        }
-#pragma unroll
-                    for (int w = 0; w < NS / 2; ++w) {
-                        uint32_t h[2][2][4];
-#pragma unroll
-                        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                c4_decode(kw[mt][e][w], h[mt][e]);
-                                // the scale's f16 twice: code << 7 | code << 23
-                                const uint32_t f = (D == 128 && w >= NS / 4 ? sc[mt][e] >> 8 : sc[mt][e] & 0xff) * 0x800080u;
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) h[mt][e][j] = h2_mul(h[mt][e][j], f);
-                            }
-#pragma unroll
-                        for (int half = 0; half < 2; ++half)
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                if (NT > 1 && nt >= tiles) break;
-                                const uint2 qf = NT == 1 ? q1[2 * w + half] : q_frag[(nt * NS + 2 * w + half) * 32 + lane];
-#pragma unroll
-                                for (int mt = 0; mt < 2; ++mt) {
-                                    const uint32_t a[4] = {h[mt][0][2 * half], h[mt][1][2 * half], h[mt][0][2 * half + 1],
-                                                           h[mt][1][2 * half + 1]};
-                                    mma_f16(s[mt][nt], a, qf.x, qf.y);
-                                }
-                            }
-                    }
-                }
+                float s[2][1][4];
+                ca_scores<D, 1>(st, k_at, k_sc, 1, [&](int, int i) { return q1[i]; }, s);
                 // ---- what a row does not see; softmax
                 const bool cut_here = key0 + kCaKeys > vis_min;
                 const bool drafts = cut_here && vis_min < run.len;  // keys that some rows see and some do not
-                uint32_t pb[2][NT][2];
+                if (cut_here) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    if (NT > 1 && nt >= tiles) break;
-                    if (cut_here) {
+                    for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                        for (int mt = 0; mt < 2; ++mt)
+                        for (int j = 0; j < 4; ++j)
+                            if (key0 + 16 * mt + my_key + 8 * (j >> 1) >= vis[j & 1]) s[mt][0][j] = -INFINITY;
+                }
+                float top[2];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                if (key0 + 16 * mt + my_key + 8 * (j >> 1) >= vis[nt][j & 1]) s[mt][nt][j] = -INFINITY;
-                    }
-                    float top[2];
+                for (int j = 0; j < 2; ++j) top[j] = fmaxf(max3f(s[0][0][j], s[0][0][j + 2], s[1][0][j]), s[1][0][j + 2]);
+                if (__any_sync(0xffffffffu, top[0] > lim[0] || top[1] > lim[1])) {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        top[j] = fmaxf(max3f(s[0][nt][j], s[0][nt][j + 2], s[1][nt][j]), s[1][nt][j + 2]);
-                    if (__any_sync(0xffffffffu, top[0] > lim[nt][0] || top[1] > lim[nt][1])) {
+                    for (int j = 0; j < 2; ++j) {
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
+                        for (int d = 4; d < 32; d <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], d));
+                        const bool none = lim[j] == -INFINITY;  // nothing seen so far: all sums are 0 (or NaN)
+                        if (top[j] == -INFINITY) continue;
+                        const float now = none ? top[j] * mul[j] : fmaxf(m[j], top[j] * mul[j]);
+                        const float keep = none ? 1.f : ex2_approx(m[j] - now);
+                        l[j] *= keep;
 #pragma unroll
-                            for (int d = 4; d < 32; d <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], d));
-                            const bool none = lim[nt][j] == -INFINITY;  // nothing seen so far: all sums are 0 (or NaN)
-                            if (top[j] == -INFINITY) continue;
-                            const float now = none ? top[j] * mul[nt][j] : fmaxf(m[nt][j], top[j] * mul[nt][j]);
-                            const float keep = none ? 1.f : ex2_approx(m[nt][j] - now);
-                            l[nt][j] *= keep;
-#pragma unroll
-                            for (int i = 0; i < NS; ++i) {
-                                o[nt][i][j] *= keep;
-                                o[nt][i][j + 2] *= keep;
-                            }
-                            m[nt][j] = now;
-                            lim[nt][j] = __fdividef(now + kCaSlack, mul[nt][j]);
+                        for (int i = 0; i < NS; ++i) {
+                            o[i][j] *= keep;
+                            o[i][j + 2] *= keep;
                         }
-                    }
-                    const uint64_t mu = f2_pack(-m[nt][0], -m[nt][1]);
-                    const uint64_t by = f2_pack(mul[nt][0], mul[nt][1]);
-                    uint64_t sum = f2_pack(l[nt][0], l[nt][1]);
-#pragma unroll
-                    for (int mt = 0; mt < 2; ++mt) {
-                        float e[4];
-#pragma unroll
-                        for (int j = 0; j < 4; j += 2) {
-                            f2_unpack(f2_fma(f2_pack(s[mt][nt][j], s[mt][nt][j + 1]), by, mu), e[j], e[j + 1]);
-                            e[j] = ex2_approx(e[j]);
-                            e[j + 1] = ex2_approx(e[j + 1]);
-                            sum = f2_add(sum, f2_pack(e[j], e[j + 1]));
-                        }
-                        if (mt == 1) f2_unpack(sum, l[nt][0], l[nt][1]);
-                        pb[mt][nt][0] = transpose8(pack_f16(e[0], e[1]));
-                        pb[mt][nt][1] = transpose8(pack_f16(e[2], e[3]));
+                        m[j] = now;
+                        lim[j] = __fdividef(now + kCaSlack, mul[j]);
                     }
                 }
+                uint32_t pb[2][2];
+                const uint64_t mu = f2_pack(-m[0], -m[1]), by = f2_pack(mul[0], mul[1]);
+                uint64_t sum = f2_pack(l[0], l[1]);
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt) {
+                    float e[4];
+#pragma unroll
+                    for (int j = 0; j < 4; j += 2) {
+                        f2_unpack(f2_fma(f2_pack(s[mt][0][j], s[mt][0][j + 1]), by, mu), e[j], e[j + 1]);
+                        e[j] = ex2_approx(e[j]);
+                        e[j + 1] = ex2_approx(e[j + 1]);
+                        sum = f2_add(sum, f2_pack(e[j], e[j + 1]));
+                    }
+                    pb[mt][0] = transpose8(pack_f16(e[0], e[1]));
+                    pb[mt][1] = transpose8(pack_f16(e[2], e[3]));
+                }
+                f2_unpack(sum, l[0], l[1]);
                 // ---- O^T: columns 2t, 2t + 1, 2t + 8, 2t + 9 of a tile are keys t, t + 4, t + 8, t + 12
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt) {
-                    uint32_t vw[4][NS / 4], f[2];
-                    {
-                        uint32_t code[4];
+                    uint32_t vw[4][NS / 4], code[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint8_t* at_v = st + v_at[j & 1] + (16 * mt + 8 * (j >> 1)) * (D / 2);
-                            if (D == 128) {
-                                const uint2 x = *reinterpret_cast<const uint2*>(at_v);
-                                vw[j][0] = x.x, vw[j][1 % (NS / 4)] = x.y;
-                            } else {
-                                vw[j][0] = *reinterpret_cast<const uint32_t*>(at_v);
-                            }
-                            code[j] = st[v_sc + (16 * mt + 4 * j) * (D / 16)];
+                    for (int j = 0; j < 4; ++j) {
+                        const uint8_t* at_v = st + v_at[j & 1] + (16 * mt + 8 * (j >> 1)) * (D / 2);
+                        if (D == 128) {
+                            const uint2 x = *reinterpret_cast<const uint2*>(at_v);
+                            vw[j][0] = x.x, vw[j][1 % (NS / 4)] = x.y;
+                        } else {
+                            vw[j][0] = *reinterpret_cast<const uint32_t*>(at_v);
                         }
-                        f[0] = code[1] * 0x800000u + code[0] * 0x80u;
-                        f[1] = code[3] * 0x800000u + code[2] * 0x80u;
+                        code[j] = st[v_sc + (16 * mt + 4 * j) * (D / 16)];
                     }
+                    uint32_t f[2] = {code[1] * 0x800000u + code[0] * 0x80u, code[3] * 0x800000u + code[2] * 0x80u};
                     if (drafts) {
                         // a value that is not finite counts for the rows that see it alone: its product is
                         // left out, and the rows that see it are found by a product of their own
                         uint32_t bad[2];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const uint32_t lo = (f[j] & 0x7c00u) == 0x7c00u ? 0xffffu : 0u;
-                            const uint32_t hi = (f[j] & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
-                            bad[j] = lo | hi;
-                            f[j] &= ~bad[j];
-                        }
+                        ca_take_bad(f, bad);
                         if (__any_sync(0xffffffffu, (bad[0] | bad[1]) != 0)) {
                             const uint32_t a[4] = {bad[0] & 0x3c003c00u, 0u, bad[1] & 0x3c003c00u, 0u};
+                            float seen[4] = {0.f, 0.f, 0.f, 0.f};
+                            uint32_t b[2];
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                if (NT > 1 && nt >= tiles) break;
-                                float seen[4] = {0.f, 0.f, 0.f, 0.f};
-                                uint32_t b[2];
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) {
-                                    const int key = key0 + 16 * mt + my_key + 8 * j;
-                                    b[j] = transpose8((key < vis[nt][0] ? 0x3c00u : 0u) | (key < vis[nt][1] ? 0x3c000000u : 0u));
-                                }
-                                mma_f16(seen, a, b[0], b[1]);
-                                poison |= (seen[0] > 0.f ? 1u : 0u) << (2 * nt) | (seen[1] > 0.f ? 2u : 0u) << (2 * nt);
+                            for (int j = 0; j < 2; ++j) {
+                                const int key = key0 + 16 * mt + my_key + 8 * j;
+                                b[j] = transpose8((key < vis[0] ? 0x3c00u : 0u) | (key < vis[1] ? 0x3c000000u : 0u));
                             }
+                            mma_f16(seen, a, b[0], b[1]);
+                            poison |= (seen[0] > 0.f ? 1u : 0u) | (seen[1] > 0.f ? 2u : 0u);
                         }
                     }
 #pragma unroll
@@ -612,13 +681,9 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_attn_kerne
                             }
                         }
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            if (NT > 1 && nt >= tiles) break;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint32_t a[4] = {h[0][0][i], h[0][1][i], h[1][0][i], h[1][1][i]};
-                                mma_f16(o[nt][4 * w + i], a, pb[mt][nt][0], pb[mt][nt][1]);
-                            }
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t a[4] = {h[0][0][i], h[0][1][i], h[1][0][i], h[1][1][i]};
+                            mma_f16(o[4 * w + i], a, pb[mt][0], pb[mt][1]);
                         }
                     }
                 }
@@ -626,14 +691,12 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_attn_kerne
 
             // ---- the four warps' results of the stretch
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int j = 0; j < 2; ++j) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], d);
-                    if (lim[nt][j] == -INFINITY) m[nt][j] = -INFINITY;
-                    if (g == 0) stats[warp * S::kRows + nt * 8 + 2 * t + j] = make_float2(m[nt][j], l[nt][j]);
-                }
+                for (int d = 4; d < 32; d <<= 1) l[j] += __shfl_xor_sync(0xffffffffu, l[j], d);
+                if (lim[j] == -INFINITY) m[j] = -INFINITY;
+                if (g == 0) stats[warp * S::kRows + 2 * t + j] = make_float2(m[j], l[j]);
+            }
             group_sync(group);
             if (tid < nrow) {
                 float top = -INFINITY, sum = 0.f;
@@ -647,34 +710,29 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_attn_kerne
                 stats[kCaWarps * S::kRows + tid] = make_float2(top, sum);
             }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int j = 0; j < 2; ++j) {
+                const int r = 2 * t + j;
+                float top = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int r = nt * 8 + 2 * t + j;
-                    float top = -INFINITY;
+                for (int w = 0; w < kCaWarps; ++w) top = fmaxf(top, stats[w * S::kRows + r].x);
+                float keep = m[j] == -INFINITY ? 1.f : ex2_approx(m[j] - top);
+                if (poison >> j & 1) keep = __uint_as_float(0x7fc00000u);
+                if (r < nrow) {
+                    float2* to = reinterpret_cast<float2*>(merge + (warp * S::kRows + r) * S::kRowBytes);
 #pragma unroll
-                    for (int w = 0; w < kCaWarps; ++w) top = fmaxf(top, stats[w * S::kRows + r].x);
-                    float keep = m[nt][j] == -INFINITY ? 1.f : ex2_approx(m[nt][j] - top);
-                    if (poison >> (2 * nt + j) & 1) keep = __uint_as_float(0x7fc00000u);
-                    if (r < nrow) {
-                        float2* to = reinterpret_cast<float2*>(merge + (warp * S::kRows + r) * S::kRowBytes);
-#pragma unroll
-                        for (int i = 0; i < NS; ++i) to[i * 8 + g] = make_float2(o[nt][i][j] * keep, o[nt][i][j + 2] * keep);
-                    }
+                    for (int i = 0; i < NS; ++i) to[i * 8 + g] = make_float2(o[i][j] * keep, o[i][j + 2] * keep);
                 }
+            }
             group_sync(group);
             const bool whole = first == 0 && last == run.units;
-            const uint32_t slot = 2 * (blockIdx.x * cut.cells + cell) + (first == 0);
-            float* part = p.parts + static_cast<int64_t>(slot) * S::kPart;
+            float* part = p.parts + (2ll * c.cell + (first == 0)) * S::kPart;
 #pragma unroll 1
             for (int x = tid; x < nrow * (D / 2); x += kCaGroup) {
-                const int r = x / (D / 2), y = x % (D / 2);
-                // whole: channels 2y, 2y + 1; a part: in the fragments' order
-                const int at = whole ? (y & (NS - 1)) * 8 + y / NS : y;
+                const int r = x / (D / 2), y = x % (D / 2);  // channels 2y, 2y + 1
                 float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < kCaWarps; ++w) {
-                    const float2 v = reinterpret_cast<const float2*>(merge + (w * S::kRows + r) * S::kRowBytes)[at];
+                    const float2 v = reinterpret_cast<const float2*>(merge + (w * S::kRows + r) * S::kRowBytes)[y % NS * 8 + y / NS];
                     sum.x += v.x, sum.y += v.y;
                 }
                 const float2 all = stats[kCaWarps * S::kRows + r];
@@ -683,24 +741,288 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_attn_kerne
                     if (y == 0) reinterpret_cast<float2*>(part + S::kRows * D)[r] = all;
                     continue;
                 }
-                const int token = p.token_of(row0 + r), hq = run.h * p.G + row0 + r - token * p.G, pr = run.r0 + token;
+                const int token = p.token_of(r), hq = run.h * p.G + r - token * p.G, pr = run.r0 + token;
                 const bool any = all.y != 0.f;  // (a NaN is not)
                 const float inv = 1.f / all.y;
                 reinterpret_cast<uint32_t*>(p.o + (static_cast<int64_t>(pr) * p.Hq + hq) * D)[y] =
                     any ? cvt_bf16x2(sum.x * inv, sum.y * inv) : 0u;
-                if (y == 0 && p.lse)
-                    p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? (all.x + log2f(all.y)) * 0.693147181f : -INFINITY;
+                if (y == 0 && p.lse) p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? ca_lse(all.x, all.y) : -INFINITY;
             }
             if (last < run.units && first == 0)
-                open = CaOpen{run.r0, run.h, row0, nrow, static_cast<int>(cut.cell_of(base + run.units - 1)), {0, 0, 0}};
-            if (last == run.units && left > 0) {
-                unit = 0;
-                base += run.units;
-                ca_next(p, S::kRows, run);
-            }
+                open = CaOpen{run.r0, run.h, 0, nrow, static_cast<int>(c.cut.cell_of(c.base + S::kRunCost + run.units - 1)), {0, 0, 0}};
         }
-        if (tid == 0) p.table[blockIdx.x * cut.cells + cell] = open;
+        c.base += run.units + S::kRunCost;
+        if (c.base < c.x1) ca_next(p, S::kRows, run);
     }
+    if (tid == 0) p.table[c.cell] = open;
+    cp_async_wait<0>();
+}
+
+// The same for more rows: V's codes are turned into operands once for all rows, so a warp
+// has all rows' sums over all keys of the group, of a quarter of the channels.  P goes
+// through shared memory, and the running maxima are the group's.
+template <int D, int NT>
+__global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kernel(CaParams p)
+{
+    using S = CaShape<D, NT>;
+    constexpr int NS = S::kSteps, MT = D / 64;  // m tiles of a warp's channels
+    extern __shared__ __align__(128) uint8_t smem_all[];
+    __shared__ uint32_t sh_line[32];
+    const int group = threadIdx.x / kCaGroup, tid = threadIdx.x % kCaGroup;
+    const int lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    uint8_t* const smem = smem_all + group * S::kGroupBytes;
+    const uint8_t* const my_ring = smem + warp * (kCaStages * S::kStage);
+    uint2* const q_frag = reinterpret_cast<uint2*>(smem + S::kRing);
+    uint2* const p_frag = reinterpret_cast<uint2*>(smem + S::kRing + S::kQ);  // [16 keys][tile of rows][lane]
+    float* const wtop = reinterpret_cast<float*>(smem + S::kRing + S::kQ + S::kMerge);  // [warp][row]: maxima, then sums
+    int* const row_vis = reinterpret_cast<int*>(wtop + kCaWarps * S::kRows);
+    float* const row_mul = reinterpret_cast<float*>(row_vis + S::kRows);
+    float* const row_m = row_mul + S::kRows;    // the maximum that is subtracted (0 before there is one)
+    float* const row_lim = row_m + S::kRows;    // q.k above which it moves
+    const int my_key = (g >> 1) + 4 * (g & 1);
+    const uint32_t k_at = piece<D>(my_key, t * (D / 8)), k_sc = 2 * S::kCodes + my_key * (D / 16) + t * (D / 64);
+    // of V: D / 32 channels, from warp * D / 4 + g * D / 32, of keys t + 8 i and t + 4 + 8 i
+    const uint32_t at = warp * (D / 8) + g * (D / 64);
+    const uint32_t v_at[2] = {S::kCodes + piece<D>(t, at), S::kCodes + piece<D>(t + 4, at)};
+    const uint32_t v_sc = 2 * S::kCodes + S::kScales + t * (D / 16) + (D == 128 ? 2 * warp + (g >> 2) : warp);
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    CaCell c = ca_cell<S>(p, group, sh_line);
+    if (!c.any) return;
+    CaRun& run = c.run;
+    CaCopies<D, S> copies(p, smem_u32(my_ring), warp, lane, c);
+    CaOpen open{0, 0, 0, 0, -1, {0, 0, 0}};
+    uint32_t use = 0;  // stage
+#pragma unroll 1
+    for (int i = 0; i < kCaStages - 1; ++i) copies.issue();
+#pragma unroll 1
+    for (int unit = c.unit; c.base < c.x1; unit = 0) {
+        // ---- a stretch of one run
+        const int first = unit, last = ca_before<S>(run, c.base, c.x1);
+        const int row0 = run.rb * S::kRows, nrow = min(S::kRows, run.cnt * p.G - row0), tiles = (nrow + 7) / 8;
+        if (first < last) {
+            ca_queries<D, S>(p, run, row0, nrow, group, tid, reinterpret_cast<uint8_t*>(p_frag), q_frag, row_vis, row_mul);
+            float l[NT][2], o[NT][MT][4];
+            uint32_t poison = 0;  // bit 2 nt + j: row 8 nt + 2t + j sees a value that is not finite in this thread's channels
+            if (tid < S::kRows) row_m[tid] = 0.f, row_lim[tid] = -INFINITY;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                l[nt][0] = l[nt][1] = 0.f;
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.f;
+            }
+            int vis_min = lane < nrow ? row_vis[lane] : run.len;
+            vis_min = __reduce_min_sync(0xffffffffu, vis_min);
+            group_sync(group);
+
+#pragma unroll 1
+            for (; unit < last; ++unit) {
+                cp_async_wait<kCaStages - 2>();
+                __syncwarp();
+                const uint32_t stage = use * S::kStage;
+                use = use + 1 == kCaStages ? 0 : use + 1;
+                const int key0 = unit * kCaUnit + warp * kCaKeys;
+                const bool mine = key0 < run.len;
+                const bool cut_here = unit * kCaUnit + kCaUnit > vis_min;  // (of any of the group's warps)
+                float s[2][NT][4];
+                bool moves = false;
+                if (mine) {
+                    ca_scores<D, NT>(my_ring + stage, k_at, k_sc, tiles, [&](int nt, int i) { return q_frag[(nt * NS + i) * 32 + lane]; }, s);
+                    if (cut_here) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const int2 vis = reinterpret_cast<const int2*>(row_vis)[nt * 4 + t];
+#pragma unroll
+                            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    if (key0 + 16 * mt + my_key + 8 * (j >> 1) >= (j & 1 ? vis.y : vis.x)) s[mt][nt][j] = -INFINITY;
+                        }
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (nt >= tiles) break;
+                        const float2 lim = reinterpret_cast<const float2*>(row_lim)[nt * 4 + t];
+                        moves |= fmaxf(max3f(s[0][nt][0], s[0][nt][2], s[1][nt][0]), s[1][nt][2]) > lim.x;
+                        moves |= fmaxf(max3f(s[0][nt][1], s[0][nt][3], s[1][nt][1]), s[1][nt][3]) > lim.y;
+                    }
+                }
+                // (all copies of the unit are there, and P of the unit before has been read)
+                if (group_any(group, moves)) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            float top = -INFINITY;
+                            if (mine && nt < tiles) top = fmaxf(max3f(s[0][nt][j], s[0][nt][j + 2], s[1][nt][j]), s[1][nt][j + 2]);
+#pragma unroll
+                            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                            if (g == 0) wtop[warp * S::kRows + nt * 8 + 2 * t + j] = top;
+                        }
+                    group_sync(group);
+                    float now[NT][2];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int r = nt * 8 + 2 * t + j;
+                            float top = wtop[r];
+#pragma unroll
+                            for (int w = 1; w < kCaWarps; ++w) top = fmaxf(top, wtop[w * S::kRows + r]);
+                            const float was = row_m[r];
+                            const bool none = row_lim[r] == -INFINITY;  // nothing seen so far: all sums are 0 (or NaN)
+                            now[nt][j] = top == -INFINITY ? was : none ? top * row_mul[r] : fmaxf(was, top * row_mul[r]);
+                            const float keep = none ? 1.f : ex2_approx(was - now[nt][j]);
+                            l[nt][j] *= keep;
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) {
+                                o[nt][i][j] *= keep;
+                                o[nt][i][j + 2] *= keep;
+                            }
+                            if (none && top == -INFINITY) now[nt][j] = -INFINITY;
+                        }
+                    group_sync(group);
+                    if (warp == 0 && g == 0) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const int r = nt * 8 + 2 * t + j;
+                                if (now[nt][j] == -INFINITY) continue;
+                                row_m[r] = now[nt][j];
+                                row_lim[r] = __fdividef(now[nt][j] + kCaSlack, row_mul[r]);
+                            }
+                    }
+                    group_sync(group);
+                }
+                copies.issue();  // into the stage that the unit before has left
+                if (mine) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (nt >= tiles) break;
+                        const float2 mm = reinterpret_cast<const float2*>(row_m)[nt * 4 + t];
+                        const float2 mul = reinterpret_cast<const float2*>(row_mul)[nt * 4 + t];
+                        const uint64_t mu = f2_pack(-mm.x, -mm.y), by = f2_pack(mul.x, mul.y);
+                        uint64_t sum = f2_pack(l[nt][0], l[nt][1]);
+#pragma unroll
+                        for (int mt = 0; mt < 2; ++mt) {
+                            float e[4];
+#pragma unroll
+                            for (int j = 0; j < 4; j += 2) {
+                                f2_unpack(f2_fma(f2_pack(s[mt][nt][j], s[mt][nt][j + 1]), by, mu), e[j], e[j + 1]);
+                                e[j] = ex2_approx(e[j]);
+                                e[j + 1] = ex2_approx(e[j + 1]);
+                                sum = f2_add(sum, f2_pack(e[j], e[j + 1]));
+                            }
+                            p_frag[((warp * 2 + mt) * NT + nt) * 32 + lane] =
+                                make_uint2(transpose8(pack_f16(e[0], e[1])), transpose8(pack_f16(e[2], e[3])));
+                        }
+                        f2_unpack(sum, l[nt][0], l[nt][1]);
+                    }
+                }
+                group_sync(group);
+                // ---- O^T: columns 2t, 2t + 1, 2t + 8, 2t + 9 of a tile are keys t, t + 4, t + 8, t + 12
+                const int steps = 2 * min(kCaWarps, (run.len - unit * kCaUnit + kCaKeys - 1) / kCaKeys);
+                const bool drafts = cut_here && vis_min < run.len;  // keys that some rows see and some do not
+#pragma unroll 2
+                for (int ks = 0; ks < steps; ++ks) {
+                    const uint8_t* const st = smem + (ks >> 1) * (kCaStages * S::kStage) + stage;
+                    const int key_at = (ks & 1) * 16;
+                    uint32_t vw[4], code[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint8_t* at_v = st + v_at[j & 1] + (key_at + 8 * (j >> 1)) * (D / 2);
+                        vw[j] = D == 128 ? *reinterpret_cast<const uint16_t*>(at_v) : *at_v;
+                        code[j] = st[v_sc + (key_at + 4 * j) * (D / 16)];
+                    }
+                    uint32_t f[2] = {code[1] * 0x800000u + code[0] * 0x80u, code[3] * 0x800000u + code[2] * 0x80u};
+                    if (drafts) {  // (as for one tile)
+                        uint32_t bad[2];
+                        ca_take_bad(f, bad);
+                        if (__any_sync(0xffffffffu, (bad[0] | bad[1]) != 0)) {
+                            const uint32_t a[4] = {bad[0] & 0x3c003c00u, 0u, bad[1] & 0x3c003c00u, 0u};
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                if (nt >= tiles) break;
+                                const int room = row_vis[nt * 8 + g] - unit * kCaUnit - ks * 16 - t;  // of keys t, t + 4 ...
+                                float seen[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma_f16(seen, a, (room > 0 ? 0x3c00u : 0u) | (room > 4 ? 0x3c000000u : 0u),
+                                        (room > 8 ? 0x3c00u : 0u) | (room > 12 ? 0x3c000000u : 0u));
+                                poison |= ((seen[0] > 0.f ? 1u : 0u) | (seen[1] > 0.f ? 2u : 0u)) << (2 * nt);
+                            }
+                        }
+                    }
+                    // keys 0 and 2 in one word, 1 and 3 in the other; then even channels of both, odd ones of both
+                    const uint32_t a = vw[0] + vw[2] * (D == 128 ? 0x10000u : 0x100u), b = vw[1] + vw[3] * (D == 128 ? 0x10000u : 0x100u);
+                    uint32_t ev[4], od[4];
+                    c4_decode((a & 0x0f0f0f0fu) | ((b * 16) & 0xf0f0f0f0u), ev);
+                    c4_decode(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), od);
+                    uint32_t ha[MT][4];
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        ha[i][0] = h2_mul(ev[i], f[0]), ha[i][1] = h2_mul(od[i], f[0]);
+                        ha[i][2] = h2_mul(ev[MT + i], f[1]), ha[i][3] = h2_mul(od[MT + i], f[1]);
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (nt >= tiles) break;
+                        const uint2 pf = p_frag[(ks * NT + nt) * 32 + lane];
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) mma_f16(o[nt][i], ha[i], pf.x, pf.y);
+                    }
+                }
+            }
+
+            // ---- the stretch's results: sums over the warps' keys, then a thread's channels of its rows
+            group_sync(group);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], d);
+                    if (g == 0) wtop[warp * S::kRows + nt * 8 + 2 * t + j] = l[nt][j];
+                }
+            group_sync(group);
+            const bool whole = first == 0 && last == run.units;
+            float* part = p.parts + (2ll * c.cell + (first == 0)) * S::kPart;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int r = nt * 8 + 2 * t + j, ch = warp * (D / 4) + g * (D / 32);
+                    if (r >= nrow) continue;
+                    const float total = wtop[r] + wtop[S::kRows + r] + wtop[2 * S::kRows + r] + wtop[3 * S::kRows + r];
+                    const float top = row_lim[r] == -INFINITY ? -INFINITY : row_m[r];
+                    const bool any = total != 0.f;  // (a NaN is not)
+                    float keep = whole ? 1.f / total : 1.f;
+                    if (poison >> (2 * nt + j) & 1) keep = __uint_as_float(0x7fc00000u);
+                    float x[D / 32];
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) x[2 * i] = o[nt][i][j] * keep, x[2 * i + 1] = o[nt][i][j + 2] * keep;
+                    const bool one = warp == 0 && g == 0;  // of a row's threads
+                    if (!whole) {
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) reinterpret_cast<float2*>(part + r * D + ch)[i] = make_float2(x[2 * i], x[2 * i + 1]);
+                        if (one) reinterpret_cast<float2*>(part + S::kRows * D)[r] = make_float2(top, total);
+                        continue;
+                    }
+                    const int token = p.token_of(row0 + r), hq = run.h * p.G + row0 + r - token * p.G, pr = run.r0 + token;
+                    uint32_t* out = reinterpret_cast<uint32_t*>(p.o + (static_cast<int64_t>(pr) * p.Hq + hq) * D + ch);
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) out[i] = any ? cvt_bf16x2(x[2 * i], x[2 * i + 1]) : 0u;
+                    if (one && p.lse) p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? ca_lse(top, total) : -INFINITY;
+                }
+            if (last < run.units && first == 0)
+                open = CaOpen{run.r0, run.h, row0, nrow, static_cast<int>(c.cut.cell_of(c.base + S::kRunCost + run.units - 1)), {0, 0, 0}};
+        }
+        c.base += run.units + S::kRunCost;
+        if (c.base < c.x1) ca_next(p, S::kRows, run);
+    }
+    if (tid == 0) p.table[c.cell] = open;
     cp_async_wait<0>();
 }
 
@@ -768,14 +1090,10 @@ __global__ void __launch_bounds__(kJoinThreads) cache4_join_kernel(CaParams p)
     const int token = p.token_of(e.row0 + r), hq = e.h * p.G + e.row0 + r - token * p.G, pr = e.r0 + token;
     const bool any = total != 0.f;
     const float inv = 1.f / total;
-    uint32_t* out = reinterpret_cast<uint32_t*>(p.o + (static_cast<int64_t>(pr) * p.Hq + hq) * D);
+    uint32_t* out = reinterpret_cast<uint32_t*>(p.o + (static_cast<int64_t>(pr) * p.Hq + hq) * D + lane * C);
 #pragma unroll
-    for (int c = 0; c < C; c += 2) {
-        const int x = (lane * C + c) / 2;  // fragment (x / 8, g = x % 8) holds channels 2 (g * steps + x / 8), + 1
-        out[(x & 7) * S::kSteps + x / 8] = any ? cvt_bf16x2(sum[c] * inv, sum[c + 1] * inv) : 0u;
-    }
-    if (lane == 0 && p.lse)
-        p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? (top + log2f(total)) * 0.693147181f : -INFINITY;
+    for (int c = 0; c < C; c += 2) out[c / 2] = any ? cvt_bf16x2(sum[c] * inv, sum[c + 1] * inv) : 0u;
+    if (lane == 0 && p.lse) p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? ca_lse(top, total) : -INFINITY;
 }
 
 int check_cache4_attn(const logo_dims& d, int n_new)
@@ -787,7 +1105,7 @@ int check_cache4_attn(const logo_dims& d, int n_new)
         static_cast<int64_t>(n_new) * (d.Hq / d.Hkv) > 8192 || static_cast<int64_t>(d.B) * n_new * d.Hq > (1 << 30))
         return LOGO_ERR_UNSUPPORTED;
     // the line's units are counted in 31 bits
-    const int64_t units = (static_cast<int64_t>(d.T) + kCaUnit - 1) / kCaUnit;
+    const int64_t units = (static_cast<int64_t>(d.T) + kCaUnit - 1) / kCaUnit + 4;  // (and a run's cost)
     const int64_t blocks = (static_cast<int64_t>(n_new) * (d.Hq / d.Hkv) + 8 * kCaMaxTiles - 1) / (8 * kCaMaxTiles);
     if (units * d.B * d.Hkv > (1ll << 31) / blocks - 1) return LOGO_ERR_UNSUPPORTED;
     return LOGO_OK;
@@ -824,8 +1142,11 @@ template <int D, int NT>
 int ca_launch(CaShape<D, NT> s, CaParams& p, cudaStream_t st)
 {
     using S = CaShape<D, NT>;
+    void (*kernel)(CaParams);
+    if constexpr (NT == 1) kernel = cache4_attn_kernel<D>;
+    else kernel = cache4_wide_kernel<D, NT>;
     static OncePerDevice once;
-    if (once([] { return set_smem_limit(cache4_attn_kernel<D, NT>, S::kSmem); }) != cudaSuccess) return LOGO_ERR_CUDA;
+    if (once([&] { return set_smem_limit(kernel, S::kSmem); }) != cudaSuccess) return LOGO_ERR_CUDA;
     // each launch is set up while the one before it on the stream runs (and waits for its end itself)
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -837,7 +1158,7 @@ int ca_launch(CaShape<D, NT> s, CaParams& p, cudaStream_t st)
     cfg.stream = st;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, cache4_attn_kernel<D, NT>, p) != cudaSuccess) return LOGO_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) return LOGO_ERR_CUDA;
     cfg.gridDim = dim3(ca_cells(s), NT);
     cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = 0;
