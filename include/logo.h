@@ -394,24 +394,30 @@ LOGO_API int logo_decode_cache4_attn(const logo_bf16* q, logo_cache4 cache, cons
  *   allowed [B, m1, ceil(V / 32)] int32 (NULL: all): bit v % 32 of word v / 32 is 0
  *     for a token that a grammar rules out; bits past V are not read as tokens.
  *   temperature [B] float32 (NULL: 1): T > 0: p = softmax over the allowed tokens of
- *     x / T; T = 0: 1 for the largest x, the lowest v among equals, 0 for the others.
- *   Each operation named is one float32 operation; the softmax's sum is float32.
+ *     x / T, as 2^((x - max x) log2(e) / T) over their sum; T = 0: 1 for the largest x,
+ *     the lowest v among equals, 0 for the others; a T below 0 or NaN makes them NaN.
+ *   Each operation named up to x is one float32 operation, exponentials and sum are
+ *   float32.
  *   Token numbers outside [0, V) in a list count for nothing (padding).
  * Out: p [B, m1, V] float32; may be logits themselves if those are float32.  0 for
  *   every token that is not allowed; a row that allows none, or only tokens of x =
  *   -infinity, is all 0.  A NaN among a row's allowed tokens (or for T > 0 an infinite
  *   x) makes p NaN for all of them.
- *   Results are deterministic.  No workspace.
+ *   Results are deterministic.  Workspace:
+ *   logo_target_probs_workspace_size(...) bytes, one per call in flight: a row's 8 bytes per
+ *   2048 tokens, and for lists 3 V / 8 and 8 for each token that they can name.
  *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer, history without hist_len,
  *   n_prompt without history, history or draft without penalty, draft with m1 = 1, or
  *   sizes out of range; LOGO_ERR_UNSUPPORTED for V > LOGO_PROBS_MAX_VOCAB, m1 > 1024,
- *   K > 4096, B * m1 > 2^24, 16-byte alignment of logits or p, bf16 logits in p. */
+ *   K > 4096, B * m1 > 2^24, 16-byte alignment of logits or p, bf16 logits in p;
+ *   LOGO_ERR_WORKSPACE. */
 #define LOGO_PROBS_MAX_COUNTED 16384
-#define LOGO_PROBS_MAX_VOCAB 294912
+#define LOGO_PROBS_MAX_VOCAB 278528
+LOGO_API size_t logo_target_probs_workspace_size(int B, int m1, int V, int H, int K);
 LOGO_API int logo_target_probs(const void* logits, int logits_bf16, const float* temperature, const float* penalty,
                 const int32_t* history, const int32_t* hist_len, const int32_t* n_prompt, const int32_t* draft,
                 const int32_t* bias_tok, const float* bias_val, const int32_t* allowed, float* p, int B, int m1, int V,
-                int H, int K, void* stream);
+                int H, int K, void* workspace, size_t workspace_bytes, void* stream);
 
 /* logo_select_noalloc -- logo_select for callers that cannot allocate.
  *   No counterpart in the paper: this is a deployment variant of logo_select.

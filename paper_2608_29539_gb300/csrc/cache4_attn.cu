@@ -446,7 +446,7 @@ __device__ __forceinline__ void ca_queries(const CaParams& p, const CaRun& run, 
 // S^T of a warp's step, raw products: row g of a tile is key (g >> 1) + 4 (g & 1), row g + 8
 // that plus 8; columns are rows of Q.  st: the stage; k_at, k_sc: this thread's pieces.
 template <int D, int NT, typename F>
-__device__ __forceinline__ void ca_scores(const uint8_t* st, uint32_t k_at, uint32_t k_sc, int tiles, F frag, float (&s)[2][NT][4])
+__device__ __forceinline__ void ca_scores(const uint8_t* st, uint32_t k_at, uint32_t k_sc, F frag, float (&s)[2][NT][4])
 {
     constexpr int NS = D / 16;
     uint32_t kw[2][2][NS / 2], sc[2][2];
@@ -490,7 +490,6 @@ __device__ __forceinline__ void ca_scores(const uint8_t* st, uint32_t k_at, uint
         for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                if (NT > 1 && nt >= tiles) break;
                 const uint2 qf = frag(nt, 2 * w + half);
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt) {
@@ -582,7 +581,7 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
                 const int key0 = unit * kCaUnit + warp * kCaKeys;
                 if (key0 >= run.len) continue;
                 float s[2][1][4];
-                ca_scores<D, 1>(st, k_at, k_sc, 1, [&](int, int i) { return q1[i]; }, s);
+                ca_scores<D, 1>(st, k_at, k_sc, [&](int, int i) { return q1[i]; }, s);
                 // ---- what a row does not see; softmax
                 const bool cut_here = key0 + kCaKeys > vis_min;
                 const bool drafts = cut_here && vis_min < run.len;  // keys that some rows see and some do not
@@ -800,7 +799,7 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
     for (int unit = c.unit; c.base < c.x1; unit = 0) {
         // ---- a stretch of one run
         const int first = unit, last = ca_before<S>(run, c.base, c.x1);
-        const int row0 = run.rb * S::kRows, nrow = min(S::kRows, run.cnt * p.G - row0), tiles = (nrow + 7) / 8;
+        const int row0 = run.rb * S::kRows, nrow = min(S::kRows, run.cnt * p.G - row0);
         if (first < last) {
             ca_queries<D, S>(p, run, row0, nrow, group, tid, reinterpret_cast<uint8_t*>(p_frag), q_frag, row_vis, row_mul);
             float l[NT][2], o[NT][MT][4];
@@ -830,7 +829,7 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                 float s[2][NT][4];
                 bool moves = false;
                 if (mine) {
-                    ca_scores<D, NT>(my_ring + stage, k_at, k_sc, tiles, [&](int nt, int i) { return q_frag[(nt * NS + i) * 32 + lane]; }, s);
+                    ca_scores<D, NT>(my_ring + stage, k_at, k_sc, [&](int nt, int i) { return q_frag[(nt * NS + i) * 32 + lane]; }, s);
                     if (cut_here) {
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
@@ -844,7 +843,6 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        if (nt >= tiles) break;
                         const float2 lim = reinterpret_cast<const float2*>(row_lim)[nt * 4 + t];
                         moves |= fmaxf(max3f(s[0][nt][0], s[0][nt][2], s[1][nt][0]), s[1][nt][2]) > lim.x;
                         moves |= fmaxf(max3f(s[0][nt][1], s[0][nt][3], s[1][nt][1]), s[1][nt][3]) > lim.y;
@@ -857,7 +855,7 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
                             float top = -INFINITY;
-                            if (mine && nt < tiles) top = fmaxf(max3f(s[0][nt][j], s[0][nt][j + 2], s[1][nt][j]), s[1][nt][j + 2]);
+                            if (mine) top = fmaxf(max3f(s[0][nt][j], s[0][nt][j + 2], s[1][nt][j]), s[1][nt][j + 2]);
 #pragma unroll
                             for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
                             if (g == 0) wtop[warp * S::kRows + nt * 8 + 2 * t + j] = top;
@@ -902,7 +900,6 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                 if (mine) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        if (nt >= tiles) break;
                         const float2 mm = reinterpret_cast<const float2*>(row_m)[nt * 4 + t];
                         const float2 mul = reinterpret_cast<const float2*>(row_mul)[nt * 4 + t];
                         const uint64_t mu = f2_pack(-mm.x, -mm.y), by = f2_pack(mul.x, mul.y);
@@ -946,7 +943,6 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                             const uint32_t a[4] = {bad[0] & 0x3c003c00u, 0u, bad[1] & 0x3c003c00u, 0u};
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
-                                if (nt >= tiles) break;
                                 const int room = row_vis[nt * 8 + g] - unit * kCaUnit - ks * 16 - t;  // of keys t, t + 4 ...
                                 float seen[4] = {0.f, 0.f, 0.f, 0.f};
                                 mma_f16(seen, a, (room > 0 ? 0x3c00u : 0u) | (room > 4 ? 0x3c000000u : 0u),
@@ -968,7 +964,6 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                     }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        if (nt >= tiles) break;
                         const uint2 pf = p_frag[(ks * NT + nt) * 32 + lane];
 #pragma unroll
                         for (int i = 0; i < MT; ++i) mma_f16(o[nt][i], ha[i], pf.x, pf.y);

@@ -109,8 +109,9 @@ _SIGS = {
     "logo_decode_cache4_workspace_size": (_c_size, [Dims, _c_int]),
     "logo_decode_cache4_attn": (_c_int, [_vp, _Cache4Ptrs, _vp, _vp, _vp, _vp, _vp, _vp, Dims, _c_int, _c_float, _vp,
                                          _c_size, _vp]),
+    "logo_target_probs_workspace_size": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int]),
     "logo_target_probs": (_c_int, [_vp, _c_int, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int,
-                                   _c_int, _c_int, _c_int, _vp]),
+                                   _c_int, _c_int, _c_int, _vp, _c_size, _vp]),
     "logo_local_attn_fwd": (_c_int, [_vp, _vp, _vp, _vp, _vp, Dims, _c_int, _c_float, _vp]),
     "logo_local_attn_bwd_workspace_size": (_c_size, [Dims]),
     "logo_local_attn_bwd": (_c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, Dims, _c_int, _c_float, _vp,
@@ -695,8 +696,15 @@ def logo_decode_cache4_attn(q, cache: Cache4, seq_len, pos, cu_q, n_sel_total, s
     return o_c, lse_c
 
 
+def logo_target_probs_workspace(logits, H: int = 0, K: int = 0):
+    """A workspace for logo_target_probs calls on logits of this shape with histories
+    [B, H] and biases [B, K] (one per call in flight)."""
+    B, m1, V = logits.shape
+    return _workspace(int(lib().logo_target_probs_workspace_size(B, m1, V, H, K)), logits.device)
+
+
 def logo_target_probs(logits, temperature=None, penalty=None, history=None, hist_len=None, n_prompt=None, draft=None,
-                      bias_tok=None, bias_val=None, allowed=None, p=None):
+                      bias_tok=None, bias_val=None, allowed=None, p=None, workspace=None):
     """The target's probabilities [B, m1, V] float32, as logo_verify_draft takes
     them, from logits [B, m1, V] (float32 or bf16).
 
@@ -750,7 +758,11 @@ def logo_target_probs(logits, temperature=None, penalty=None, history=None, hist
         p = torch.empty((B, m1, V), dtype=torch.float32, device=logits.device)
     else:
         _need(p, torch.float32, "p", (B, m1, V))
-    _here(logits, temperature, penalty, history, hist_len, n_prompt, draft, bias_tok, bias_val, allowed, p)
+    if workspace is None:
+        workspace = logo_target_probs_workspace(logits, H, K)
+    else:
+        _given_workspace(workspace)
+    _here(logits, temperature, penalty, history, hist_len, n_prompt, draft, bias_tok, bias_val, allowed, p, workspace)
     a = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     if H == 0:  # an empty list is no list
         history = hist_len = n_prompt = None
@@ -760,7 +772,7 @@ def logo_target_probs(logits, temperature=None, penalty=None, history=None, hist
         bias_tok = bias_val = None
     _call("logo_target_probs", logits.data_ptr(), int(logits.dtype is torch.bfloat16), a(temperature), a(penalty),
           a(history), a(hist_len), a(n_prompt), a(draft), a(bias_tok), a(bias_val), a(allowed), p.data_ptr(), B, m1, V,
-          H, K, _stream())
+          H, K, workspace.data_ptr(), workspace.nbytes, _stream())
     return p
 
 

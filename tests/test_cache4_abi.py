@@ -86,17 +86,23 @@ def test_probs_host_checks(logo):
     L = logo.lib()
 
     def call(x=fake, half=0, T=null, pen=fake, hist=fake, hl=fake, npr=null, draft=null, bt=null, bv=null, ok=null,
-             p=other, B=2, m1=3, V=1000, H=10, K=0):
-        return L.logo_target_probs(x, half, T, pen, hist, hl, npr, draft, bt, bv, ok, p, B, m1, V, H, K, null)
+             p=other, B=2, m1=3, V=1000, H=10, K=0, w=fake, wb=1 << 30):
+        return L.logo_target_probs(x, half, T, pen, hist, hl, npr, draft, bt, bv, ok, p, B, m1, V, H, K, w, wb, null)
 
     for kw in (dict(x=null), dict(p=null), dict(B=0), dict(m1=0), dict(V=0), dict(H=-1), dict(K=-1), dict(hl=null),
                dict(hist=null), dict(hist=null, hl=null, npr=fake, H=0), dict(hist=null, hl=null), dict(H=0),
                dict(pen=null), dict(draft=fake, m1=1), dict(bt=fake), dict(bt=fake, bv=fake), dict(K=4),
                dict(K=4, bt=fake), dict(K=4, bv=fake), dict(pen=null, hist=null, hl=null, H=0, draft=fake)):
         assert call(**kw) == logo.LOGO_ERR_INVALID_ARG, kw
-    for kw in (dict(x=odd), dict(p=odd), dict(V=294913), dict(m1=1025), dict(K=4097, bt=fake, bv=fake),
+    for kw in (dict(x=odd), dict(p=odd), dict(V=278529), dict(m1=1025), dict(K=4097, bt=fake, bv=fake),
                dict(B=1 << 20, m1=17), dict(half=1, p=fake)):
         assert call(**kw) == logo.LOGO_ERR_UNSUPPORTED, kw
+    ws = L.logo_target_probs_workspace_size(2, 3, 1000, 10, 0)
+    assert 0 < ws < L.logo_target_probs_workspace_size(2, 3, 1000, 10, 90)
+    for bad in ((0, 3, 10, 0, 0), (2, 0, 10, 0, 0), (2, 3, 0, 0, 0), (2, 3, 278529, 0, 0), (2, 3, 10, -1, 0)):
+        assert L.logo_target_probs_workspace_size(*bad) == 0
+    for kw in (dict(w=null), dict(w=odd), dict(wb=ws - 1)):
+        assert call(**kw) == logo.LOGO_ERR_WORKSPACE, kw
 
 
 def test_definition_of_the_format():

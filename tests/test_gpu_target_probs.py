@@ -90,7 +90,7 @@ def _check(s, ok, p):
 @pytest.mark.parametrize("B,m1,V,H,K,half", [
     (1, 1, 1, 3, 1, False), (2, 1, 31, 0, 0, False), (1, 2, 33, 5, 3, True), (3, 4, 1000, 40, 7, True),
     (2, 3, 4099, 700, 30, False), (1, 1, 32000, 300, 0, False), (5, 2, 50021, 2000, 200, True), (1, 8, 131072, 64, 5, True),
-    (1, 1, 262143, 100, 300, False), (1, 1, 294912, 10, 2, True), (40, 1, 2053, 9, 1, False), (2, 300, 257, 50, 3, True)])
+    (1, 1, 262143, 100, 300, False), (1, 1, 278528, 10, 2, True), (40, 1, 2053, 9, 1, False), (2, 300, 257, 50, 3, True)])
 def test_against_the_definition(B, m1, V, H, K, half):
     s, ok = _random(B, m1, V, H, K, V + H, half=half)
     _check(s, ok, _run(s))
