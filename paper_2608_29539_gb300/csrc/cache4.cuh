@@ -17,6 +17,8 @@
 
 #include <cstdint>
 
+#include "sm100.cuh"
+
 namespace logo {
 
 constexpr int kC4Group = 16;            // channels that share a scale
@@ -54,14 +56,13 @@ __device__ __forceinline__ float c4_inverse(uint32_t code)
 // least) it stays on its side.
 __device__ __forceinline__ uint32_t c4_codes(const uint32_t (&x)[4], float inv)
 {
+    const uint64_t by = f2_pack(inv, inv), up = f2_pack(1536.f, 1536.f), down = f2_pack(-1536.f, -1536.f);
     float y[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        y[2 * i] = __uint_as_float(x[i] << 16) * inv;
-        y[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u) * inv;
+        const uint64_t q = f2_mul(f2_pack(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u)), by);
+        f2_unpack(f2_add(f2_add(q, up), down), y[2 * i], y[2 * i + 1]);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = __fsub_rn(__fadd_rn(y[i], 1536.f), 1536.f);
     uint32_t r;
     asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
         "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"

@@ -37,7 +37,6 @@ constexpr uint32_t kTpSeen = 1u << 31, kTpBiased = 1u << 30, kTpTwice = 1u << 29
 constexpr int kTpBiasAt = 15, kTpTake = 4;                 // listed tokens of a thread at a time
 static_assert(LOGO_PROBS_MAX_COUNTED + 1024 <= kTpCount, "counts have room");
 constexpr int kTpRowThreads = 512;
-constexpr unsigned kTpGridRows = 1u << 15;                 // rows of a grid's second dimension
 
 struct TpParams {
     const void* logits;
@@ -207,7 +206,7 @@ __device__ __forceinline__ TpGroup group_of(const TpParams& a, int row, int chun
 __device__ __forceinline__ uint32_t bits_of(const uint32_t* row, int words, int v)
 {
     const int w = max(v, 0) / 32;
-    const uint32_t lo = row[w], hi = (v & 31) > 24 && w + 1 < words ? row[w + 1] : 0;  // (never where a row begins at a multiple of eight)
+    const uint32_t lo = row[w], hi = row[w + (w + 1 < words)];
     return (v < 0 ? lo << -v : __funnelshift_r(lo, hi, v & 31)) & 0xffu;
 }
 
@@ -366,8 +365,7 @@ __global__ void __launch_bounds__(kTpThreads) target_stats_kernel(TpParams a)
 {
     __shared__ float2 sh[kTpThreads / 32];
     wait_for_stream();
-    const int row = blockIdx.z * kTpGridRows + blockIdx.y, chunk = blockIdx.x;
-    if (row >= a.B * a.m1) return;
+    const int row = blockIdx.x, chunk = blockIdx.y;  // (rows first: the tokens that lists name are often neighbours)
     const float T = a.temperature ? a.temperature[row / a.m1] : 1.f, c = steepness(T);
     float x[kTpGroups * 8];
     TpTokens<HALF>(a, row, chunk, std::true_type()).logits(x);
@@ -445,8 +443,7 @@ template <bool HALF>
 __global__ void __launch_bounds__(kTpThreads) target_write_kernel(TpParams a)
 {
     wait_for_stream();
-    const int row = a.B * a.m1 - 1 - (blockIdx.z * kTpGridRows + blockIdx.y), chunk = a.chunks - 1 - blockIdx.x;  // what was read last comes first
-    if (row < 0) return;
+    const int row = a.B * a.m1 - 1 - blockIdx.x, chunk = a.chunks - 1 - blockIdx.y;  // what was read last comes first
     const float T = a.temperature ? a.temperature[row / a.m1] : 1.f, c = steepness(T);
     const float2 total = a.totals[row];
     const TpTokens<HALF> tokens(a, row, chunk, std::false_type());
@@ -561,13 +558,13 @@ int tp_launch(const TpParams& a, cudaStream_t st)
         if (cudaLaunchKernelEx(&cfg, target_lists_kernel, a) != cudaSuccess) return LOGO_ERR_CUDA;
         cfg.dynamicSmemBytes = 0;
     }
-    cfg.gridDim = dim3(a.chunks, std::min(rows, kTpGridRows), (rows + kTpGridRows - 1) / kTpGridRows);
+    cfg.gridDim = dim3(rows, a.chunks);
     cfg.blockDim = dim3(kTpThreads);
     if (cudaLaunchKernelEx(&cfg, target_stats_kernel<HALF>, a) != cudaSuccess) return LOGO_ERR_CUDA;
     cfg.gridDim = dim3(rows);
     cfg.blockDim = dim3(kTpRowThreads);
     if (cudaLaunchKernelEx(&cfg, target_rows_kernel<HALF>, a) != cudaSuccess) return LOGO_ERR_CUDA;
-    cfg.gridDim = dim3(a.chunks, std::min(rows, kTpGridRows), (rows + kTpGridRows - 1) / kTpGridRows);
+    cfg.gridDim = dim3(rows, a.chunks);
     cfg.blockDim = dim3(kTpThreads);
     return cudaLaunchKernelEx(&cfg, target_write_kernel<HALF>, a) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }
