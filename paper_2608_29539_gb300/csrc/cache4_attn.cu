@@ -83,7 +83,7 @@ struct CaParams {
 };
 
 // Sizes of the kernel for one tile of rows (NT = 1), whose warps have all channels of
-// their keys, and of the one for more, whose warps have a quarter of the channels of all keys.
+// their keys, and of the one for more, whose warps have half of the channels of half of the keys.
 template <int D, int NT>
 struct CaShape {
     static constexpr bool kWide = NT > 1;
@@ -102,6 +102,7 @@ struct CaShape {
     static constexpr int kStats = (kCaWarps + 1) * kRows * 8 + 4 * kRows * 4;
     static constexpr int kGroupBytes = kRing + kQ + kMerge + kStats;
     static constexpr int kSmem = kGroups * kGroupBytes;
+    static_assert(!kWide || kQ + kMerge >= kRows * D * 4, "half of the sums go where Q and P were");
     static constexpr int kPart = kRows * (D + 2);              // floats of a part
 };
 
@@ -757,14 +758,15 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
     cp_async_wait<0>();
 }
 
-// The same for more rows: V's codes are turned into operands once for all rows, so a warp
-// has all rows' sums over all keys of the group, of a quarter of the channels.  P goes
-// through shared memory, and the running maxima are the group's.
+// The same for more rows, whose sums over all channels a warp cannot hold: a warp has all
+// rows' sums over half of the group's keys (of V), of half of the channels.  So V's codes are
+// still turned into operands once.  P goes through shared memory, and the running maxima are
+// the group's.
 template <int D, int NT>
 __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kernel(CaParams p)
 {
     using S = CaShape<D, NT>;
-    constexpr int NS = S::kSteps, MT = D / 64;  // m tiles of a warp's channels
+    constexpr int NS = S::kSteps, MT = D / 32;  // m tiles of a warp's channels
     extern __shared__ __align__(128) uint8_t smem_all[];
     __shared__ uint32_t sh_line[32];
     const int group = threadIdx.x / kCaGroup, tid = threadIdx.x % kCaGroup;
@@ -780,10 +782,11 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
     float* const row_lim = row_m + S::kRows;    // q.k above which it moves
     const int my_key = (g >> 1) + 4 * (g & 1);
     const uint32_t k_at = piece<D>(my_key, t * (D / 8)), k_sc = 2 * S::kCodes + my_key * (D / 16) + t * (D / 64);
-    // of V: D / 32 channels, from warp * D / 4 + g * D / 32, of keys t + 8 i and t + 4 + 8 i
-    const uint32_t at = warp * (D / 8) + g * (D / 64);
+    // of V: D / 16 channels, from half * D / 2 + g * D / 16, of keys t + 8 i and t + 4 + 8 i
+    const int half = warp & 1, keys = warp >> 1;
+    const uint32_t at = half * (D / 4) + g * (D / 32);
     const uint32_t v_at[2] = {S::kCodes + piece<D>(t, at), S::kCodes + piece<D>(t + 4, at)};
-    const uint32_t v_sc = 2 * S::kCodes + S::kScales + t * (D / 16) + (D == 128 ? 2 * warp + (g >> 2) : warp);
+    const uint32_t v_sc = 2 * S::kCodes + S::kScales + t * (D / 16) + half * (D / 32) + (D == 128 ? g >> 1 : g >> 2);
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -922,17 +925,17 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                 }
                 group_sync(group);
                 // ---- O^T: columns 2t, 2t + 1, 2t + 8, 2t + 9 of a tile are keys t, t + 4, t + 8, t + 12
-                const int steps = 2 * min(kCaWarps, (run.len - unit * kCaUnit + kCaKeys - 1) / kCaKeys);
+                const int steps = 2 * min(kCaWarps, (run.len - unit * kCaUnit + kCaKeys - 1) / kCaKeys);  // of 16 keys
                 const bool drafts = cut_here && vis_min < run.len;  // keys that some rows see and some do not
 #pragma unroll 2
-                for (int ks = 0; ks < steps; ++ks) {
+                for (int ks = 4 * keys; ks < min(steps, 4 * keys + 4); ++ks) {
                     const uint8_t* const st = smem + (ks >> 1) * (kCaStages * S::kStage) + stage;
                     const int key_at = (ks & 1) * 16;
                     uint32_t vw[4], code[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const uint8_t* at_v = st + v_at[j & 1] + (key_at + 8 * (j >> 1)) * (D / 2);
-                        vw[j] = D == 128 ? *reinterpret_cast<const uint16_t*>(at_v) : *at_v;
+                        vw[j] = D == 128 ? *reinterpret_cast<const uint32_t*>(at_v) : *reinterpret_cast<const uint16_t*>(at_v);
                         code[j] = st[v_sc + (key_at + 4 * j) * (D / 16)];
                     }
                     uint32_t f[2] = {code[1] * 0x800000u + code[0] * 0x80u, code[3] * 0x800000u + code[2] * 0x80u};
@@ -951,11 +954,17 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                             }
                         }
                     }
-                    // keys 0 and 2 in one word, 1 and 3 in the other; then even channels of both, odd ones of both
-                    const uint32_t a = vw[0] + vw[2] * (D == 128 ? 0x10000u : 0x100u), b = vw[1] + vw[3] * (D == 128 ? 0x10000u : 0x100u);
-                    uint32_t ev[4], od[4];
-                    c4_decode((a & 0x0f0f0f0fu) | ((b * 16) & 0xf0f0f0f0u), ev);
-                    c4_decode(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), od);
+                    // even channels of two keys, odd ones of two keys (D = 64: of four, two words in one)
+                    uint32_t ev[MT == 4 ? 8 : 4], od[MT == 4 ? 8 : 4];
+#pragma unroll
+                    for (int e = 0; e < MT / 2; ++e) {
+                        const uint32_t a = MT == 4 ? vw[2 * e] : vw[0] + vw[2] * 0x10000u, b = MT == 4 ? vw[2 * e + 1] : vw[1] + vw[3] * 0x10000u;
+                        uint32_t x[4], y[4];
+                        c4_decode((a & 0x0f0f0f0fu) | ((b * 16) & 0xf0f0f0f0u), x);
+                        c4_decode(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), y);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) ev[4 * e + j] = x[j], od[4 * e + j] = y[j];
+                    }
                     uint32_t ha[MT][4];
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
@@ -973,13 +982,22 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
 
             // ---- the stretch's results: sums over the warps' keys, then a thread's channels of its rows
             group_sync(group);
+            float* const other = reinterpret_cast<float*>(q_frag);  // [row][channel]: the other half's (Q and P are done with)
+            const int ch = half * (D / 2) + g * (D / 16);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
+                    const int r = nt * 8 + 2 * t + j;
+                    const float keep = poison >> (2 * nt + j) & 1 ? __uint_as_float(0x7fc00000u) : 1.f;
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], d);
-                    if (g == 0) wtop[warp * S::kRows + nt * 8 + 2 * t + j] = l[nt][j];
+                    if (g == 0) wtop[warp * S::kRows + r] = l[nt][j];
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        o[nt][i][j] *= keep, o[nt][i][j + 2] *= keep;
+                        if (keys == 1) *reinterpret_cast<float2*>(other + r * D + ch + 2 * i) = make_float2(o[nt][i][j], o[nt][i][j + 2]);
+                    }
                 }
             group_sync(group);
             const bool whole = first == 0 && last == run.units;
@@ -988,27 +1006,29 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const int r = nt * 8 + 2 * t + j, ch = warp * (D / 4) + g * (D / 32);
-                    if (r >= nrow) continue;
+                    const int r = nt * 8 + 2 * t + j;
+                    if (keys == 1 || r >= nrow) continue;
                     const float total = wtop[r] + wtop[S::kRows + r] + wtop[2 * S::kRows + r] + wtop[3 * S::kRows + r];
                     const float top = row_lim[r] == -INFINITY ? -INFINITY : row_m[r];
                     const bool any = total != 0.f;  // (a NaN is not)
-                    float keep = whole ? 1.f / total : 1.f;
-                    if (poison >> (2 * nt + j) & 1) keep = __uint_as_float(0x7fc00000u);
-                    float x[D / 32];
+                    const float scale = whole ? 1.f / total : 1.f;
+                    float2 x[MT];
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) x[2 * i] = o[nt][i][j] * keep, x[2 * i + 1] = o[nt][i][j + 2] * keep;
-                    const bool one = warp == 0 && g == 0;  // of a row's threads
+                    for (int i = 0; i < MT; ++i) {
+                        const float2 y = *reinterpret_cast<const float2*>(other + r * D + ch + 2 * i);
+                        x[i] = make_float2((o[nt][i][j] + y.x) * scale, (o[nt][i][j + 2] + y.y) * scale);
+                    }
+                    const bool one = half == 0 && g == 0;  // of a row's threads
                     if (!whole) {
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) reinterpret_cast<float2*>(part + r * D + ch)[i] = make_float2(x[2 * i], x[2 * i + 1]);
+                        for (int i = 0; i < MT; ++i) reinterpret_cast<float2*>(part + r * D + ch)[i] = x[i];
                         if (one) reinterpret_cast<float2*>(part + S::kRows * D)[r] = make_float2(top, total);
                         continue;
                     }
                     const int token = p.token_of(row0 + r), hq = run.h * p.G + row0 + r - token * p.G, pr = run.r0 + token;
                     uint32_t* out = reinterpret_cast<uint32_t*>(p.o + (static_cast<int64_t>(pr) * p.Hq + hq) * D + ch);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) out[i] = any ? cvt_bf16x2(x[2 * i], x[2 * i + 1]) : 0u;
+                    for (int i = 0; i < MT; ++i) out[i] = any ? cvt_bf16x2(x[i].x, x[i].y) : 0u;
                     if (one && p.lse) p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? ca_lse(top, total) : -INFINITY;
                 }
             if (last < run.units && first == 0)
