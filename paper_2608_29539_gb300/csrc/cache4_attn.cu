@@ -39,23 +39,10 @@
 namespace logo {
 namespace {
 
-#ifndef CA_ST
-#define CA_ST 2
-#endif
-#ifndef CA_C1
-#define CA_C1 4
-#endif
-#ifndef CA_C2
-#define CA_C2 3
-#endif
-#ifndef CA_RC
-#define CA_RC 2
-#endif
 constexpr int kCaWarps = 4;                   // of a group
 constexpr int kCaGroup = 32 * kCaWarps;
 constexpr int kCaKeys = 32;                   // keys of a warp's step
 constexpr int kCaUnit = kCaKeys * kCaWarps;   // keys of a unit
-constexpr int kCaStages = CA_ST;
 constexpr float kCaSlack = 8.f;               // a maximum may grow by 2^8 before what is summed is rescaled
 constexpr int kCaMaxTiles = 4;                // tiles of 8 rows that a warp holds
 constexpr int kJoinThreads = 256;
@@ -88,17 +75,20 @@ template <int D, int NT>
 struct CaShape {
     static constexpr bool kWide = NT > 1;
     static constexpr int kRows = 8 * NT;
-    static constexpr int kGroups = NT < 3 ? CA_C1 : CA_C2;     // an SM
+    // groups an SM and steps of a warp's ring: as many warps as registers allow (one tile of rows:
+    // 32 sequences of 16K rows, one token 41.3 us with four groups, 42.5 with three; three tiles, 64
+    // x 5 drafts: 141 with three, 195 with four, which spill, 161 with two)
+    static constexpr int kGroups = kWide ? 3 : 4, kStages = NT == 2 || NT == 3 ? 3 : 2;
     static constexpr int kThreads = kGroups * kCaGroup;
-    static constexpr int kRunCost = CA_RC;                     // units that beginning a run costs about as much as
+    static constexpr int kRunCost = 2;                         // units that beginning a run costs about as much as
     static constexpr int kCodes = kCaKeys * D / 2, kScales = kCaKeys * D / 16;  // bytes a step, K or V
     static constexpr int kStage = 2 * (kCodes + kScales);
     static constexpr int kSteps = D / 16;                      // k steps of S^T, m tiles of O^T
-    static constexpr int kRing = kCaWarps * kCaStages * kStage;
+    static constexpr int kRing = kCaWarps * kStages * kStage;
     static constexpr int kQ = NT * kSteps * 32 * 8;            // fragments of Q
-    // the warps' results: rows padded for the banks; or P's fragments (and the queries as they come)
+    // the warps' results: rows padded for the banks; or P's fragments of two units (and the queries as they come)
     static constexpr int kRowBytes = 4 * D + 16;
-    static constexpr int kMerge = kWide ? NT * 2048 : kCaWarps * kRows * kRowBytes;
+    static constexpr int kMerge = kWide ? 2 * NT * 2048 : kCaWarps * kRows * kRowBytes;
     static constexpr int kStats = (kCaWarps + 1) * kRows * 8 + 4 * kRows * 4;
     static constexpr int kGroupBytes = kRing + kQ + kMerge + kStats;
     static constexpr int kSmem = kGroups * kGroupBytes;
@@ -390,7 +380,7 @@ struct CaCopies {
             }
         }
         cp_async_commit();
-        fill = fill + 1 == kCaStages ? 0 : fill + 1;
+        fill = fill + 1 == S::kStages ? 0 : fill + 1;
     }
 };
 
@@ -501,16 +491,30 @@ __device__ __forceinline__ void ca_scores(const uint8_t* st, uint32_t k_at, uint
     }
 }
 
-// Scales of four keys that are not finite are taken out of f; the mask of their halves.
-__device__ __forceinline__ void ca_take_bad(uint32_t (&f)[2], uint32_t (&bad)[2])
+// A value that is not finite counts for the rows that see it alone: its product is left out,
+// and the rows that see it are found by a product of their own.  scales: those of this
+// thread's group of keys t, t + 4, t + 8, t + 12 of a tile, `step` bytes apart; room: how many
+// of the keys from t on row g of a tile of rows sees.  Bits 0 and 1: whether rows 2t and
+// 2t + 1 see a value that is not finite in this thread's group.
+__device__ __forceinline__ uint32_t ca_seen_bad(const uint8_t* scales, int step, int room)
+{
+    uint32_t bad[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bad[j] = scales[j * step] >= 0xf8 ? 0x3c00u : 0u;
+    if (!__any_sync(0xffffffffu, (bad[0] | bad[1] | bad[2] | bad[3]) != 0)) return 0;
+    const uint32_t a[4] = {bad[0] | bad[1] << 16, 0u, bad[2] | bad[3] << 16, 0u};
+    float seen[4] = {0.f, 0.f, 0.f, 0.f};
+    mma_f16(seen, a, (room > 0 ? 0x3c00u : 0u) | (room > 4 ? 0x3c000000u : 0u),
+            (room > 8 ? 0x3c00u : 0u) | (room > 12 ? 0x3c000000u : 0u));
+    return (seen[0] > 0.f ? 1u : 0u) | (seen[1] > 0.f ? 2u : 0u);
+}
+
+// Takes the scales that are not finite out of a warp's step.
+__device__ __forceinline__ void ca_drop_bad(uint8_t* scales, int step)
 {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const uint32_t lo = (f[j] & 0x7c00u) == 0x7c00u ? 0xffffu : 0u;
-        const uint32_t hi = (f[j] & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u;
-        bad[j] = lo | hi;
-        f[j] &= ~bad[j];
-    }
+    for (int j = 0; j < 8; ++j)
+        if (scales[j * step] >= 0xf8) scales[j * step] = 0;
 }
 
 __device__ __forceinline__ float ca_lse(float top, float total) { return (top + log2f(total)) * 0.693147181f; }
@@ -525,7 +529,7 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
     const int group = threadIdx.x / kCaGroup, tid = threadIdx.x % kCaGroup;
     const int lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     uint8_t* const smem = smem_all + group * S::kGroupBytes;
-    const uint8_t* const my_ring = smem + warp * (kCaStages * S::kStage);
+    uint8_t* const my_ring = smem + warp * (S::kStages * S::kStage);
     uint2* const q_frag = reinterpret_cast<uint2*>(smem + S::kRing);
     uint8_t* const merge = smem + S::kRing + S::kQ;
     float2* const stats = reinterpret_cast<float2*>(merge + S::kMerge);  // [warp, all][row] (max, sum)
@@ -546,7 +550,7 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
     CaOpen open{0, 0, 0, 0, -1, {0, 0, 0}};
     uint32_t use = 0;  // stage
 #pragma unroll 1
-    for (int i = 0; i < kCaStages - 1; ++i) copies.issue();
+    for (int i = 0; i < S::kStages - 1; ++i) copies.issue();
 #pragma unroll 1
     for (int unit = c.unit; c.base < c.x1; unit = 0) {
         // ---- a stretch of one run
@@ -574,11 +578,11 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
 
 #pragma unroll 1
             for (; unit < last; ++unit) {
-                cp_async_wait<kCaStages - 2>();
+                cp_async_wait<S::kStages - 2>();
                 __syncwarp();
                 copies.issue();
-                const uint8_t* const st = my_ring + use * S::kStage;
-                use = use + 1 == kCaStages ? 0 : use + 1;
+                uint8_t* const st = my_ring + use * S::kStage;
+                use = use + 1 == S::kStages ? 0 : use + 1;
                 const int key0 = unit * kCaUnit + warp * kCaKeys;
                 if (key0 >= run.len) continue;
                 float s[2][1][4];
@@ -632,6 +636,16 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
                     pb[mt][1] = transpose8(pack_f16(e[2], e[3]));
                 }
                 f2_unpack(sum, l[0], l[1]);
+                if (__builtin_expect(drafts, 0)) {
+#pragma unroll 1
+                    for (int mt = 0; mt < 2; ++mt) {
+                        const int room = row_vis[g] - key0 - 16 * mt - t;  // of keys t, t + 4 ...
+                        poison |= ca_seen_bad(st + v_sc + 16 * mt * (D / 16), D / 4, room);
+                    }
+                    __syncwarp();
+                    ca_drop_bad(st + v_sc, D / 4);
+                    __syncwarp();
+                }
                 // ---- O^T: columns 2t, 2t + 1, 2t + 8, 2t + 9 of a tile are keys t, t + 4, t + 8, t + 12
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt) {
@@ -647,25 +661,7 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
                         }
                         code[j] = st[v_sc + (16 * mt + 4 * j) * (D / 16)];
                     }
-                    uint32_t f[2] = {code[1] * 0x800000u + code[0] * 0x80u, code[3] * 0x800000u + code[2] * 0x80u};
-                    if (drafts) {
-                        // a value that is not finite counts for the rows that see it alone: its product is
-                        // left out, and the rows that see it are found by a product of their own
-                        uint32_t bad[2];
-                        ca_take_bad(f, bad);
-                        if (__any_sync(0xffffffffu, (bad[0] | bad[1]) != 0)) {
-                            const uint32_t a[4] = {bad[0] & 0x3c003c00u, 0u, bad[1] & 0x3c003c00u, 0u};
-                            float seen[4] = {0.f, 0.f, 0.f, 0.f};
-                            uint32_t b[2];
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                const int key = key0 + 16 * mt + my_key + 8 * j;
-                                b[j] = transpose8((key < vis[0] ? 0x3c00u : 0u) | (key < vis[1] ? 0x3c000000u : 0u));
-                            }
-                            mma_f16(seen, a, b[0], b[1]);
-                            poison |= (seen[0] > 0.f ? 1u : 0u) | (seen[1] > 0.f ? 2u : 0u);
-                        }
-                    }
+                    const uint32_t f[2] = {code[1] * 0x800000u + code[0] * 0x80u, code[3] * 0x800000u + code[2] * 0x80u};
 #pragma unroll
                     for (int w = 0; w < NS / 4; ++w) {
                         uint32_t h[2][2][4];  // [keys 0 1 | 2 3][even | odd channel]
@@ -772,9 +768,10 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
     const int group = threadIdx.x / kCaGroup, tid = threadIdx.x % kCaGroup;
     const int lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     uint8_t* const smem = smem_all + group * S::kGroupBytes;
-    const uint8_t* const my_ring = smem + warp * (kCaStages * S::kStage);
+    uint8_t* const my_ring = smem + warp * (S::kStages * S::kStage);
     uint2* const q_frag = reinterpret_cast<uint2*>(smem + S::kRing);
-    uint2* const p_frag = reinterpret_cast<uint2*>(smem + S::kRing + S::kQ);  // [16 keys][tile of rows][lane]
+    uint2* const p_both = reinterpret_cast<uint2*>(smem + S::kRing + S::kQ);  // of two units, [16 keys][tile of rows][lane]
+    uint2* p_frag = p_both;
     float* const wtop = reinterpret_cast<float*>(smem + S::kRing + S::kQ + S::kMerge);  // [warp][row]: maxima, then sums
     int* const row_vis = reinterpret_cast<int*>(wtop + kCaWarps * S::kRows);
     float* const row_mul = reinterpret_cast<float*>(row_vis + S::kRows);
@@ -797,14 +794,14 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
     CaOpen open{0, 0, 0, 0, -1, {0, 0, 0}};
     uint32_t use = 0;  // stage
 #pragma unroll 1
-    for (int i = 0; i < kCaStages - 1; ++i) copies.issue();
+    for (int i = 0; i < S::kStages - 1; ++i) copies.issue();
 #pragma unroll 1
     for (int unit = c.unit; c.base < c.x1; unit = 0) {
         // ---- a stretch of one run
         const int first = unit, last = ca_before<S>(run, c.base, c.x1);
         const int row0 = run.rb * S::kRows, nrow = min(S::kRows, run.cnt * p.G - row0);
         if (first < last) {
-            ca_queries<D, S>(p, run, row0, nrow, group, tid, reinterpret_cast<uint8_t*>(p_frag), q_frag, row_vis, row_mul);
+            ca_queries<D, S>(p, run, row0, nrow, group, tid, reinterpret_cast<uint8_t*>(p_both), q_frag, row_vis, row_mul);
             float l[NT][2], o[NT][MT][4];
             uint32_t poison = 0;  // bit 2 nt + j: row 8 nt + 2t + j sees a value that is not finite in this thread's channels
             if (tid < S::kRows) row_m[tid] = 0.f, row_lim[tid] = -INFINITY;
@@ -822,10 +819,11 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
 
 #pragma unroll 1
             for (; unit < last; ++unit) {
-                cp_async_wait<kCaStages - 2>();
+                cp_async_wait<S::kStages - 2>();
                 __syncwarp();
                 const uint32_t stage = use * S::kStage;
-                use = use + 1 == kCaStages ? 0 : use + 1;
+                use = use + 1 == S::kStages ? 0 : use + 1;
+                p_frag = p_both + (unit & 1) * (S::kMerge / 16);  // (of the unit before some warps may still read theirs)
                 const int key0 = unit * kCaUnit + warp * kCaKeys;
                 const bool mine = key0 < run.len;
                 const bool cut_here = unit * kCaUnit + kCaUnit > vis_min;  // (of any of the group's warps)
@@ -851,7 +849,33 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                         moves |= fmaxf(max3f(s[0][nt][1], s[0][nt][3], s[1][nt][1]), s[1][nt][3]) > lim.y;
                     }
                 }
-                // (all copies of the unit are there, and P of the unit before has been read)
+                // P by the maxima so far, and its sums
+                float more[NT][2];
+                const auto weights = [&] {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const float2 mm = reinterpret_cast<const float2*>(row_m)[nt * 4 + t];
+                        const float2 mul = reinterpret_cast<const float2*>(row_mul)[nt * 4 + t];
+                        const uint64_t mu = f2_pack(-mm.x, -mm.y), by = f2_pack(mul.x, mul.y);
+                        uint64_t sum = f2_pack(0.f, 0.f);
+#pragma unroll
+                        for (int mt = 0; mt < 2; ++mt) {
+                            float e[4];
+#pragma unroll
+                            for (int j = 0; j < 4; j += 2) {
+                                f2_unpack(f2_fma(f2_pack(s[mt][nt][j], s[mt][nt][j + 1]), by, mu), e[j], e[j + 1]);
+                                e[j] = ex2_approx(e[j]);
+                                e[j + 1] = ex2_approx(e[j + 1]);
+                                sum = f2_add(sum, f2_pack(e[j], e[j + 1]));
+                            }
+                            p_frag[((warp * 2 + mt) * NT + nt) * 32 + lane] =
+                                make_uint2(transpose8(pack_f16(e[0], e[1])), transpose8(pack_f16(e[2], e[3])));
+                        }
+                        f2_unpack(sum, more[nt][0], more[nt][1]);
+                    }
+                };
+                if (mine) weights();
+                // (past this all copies of the unit are there, and all have P and are done with the unit before)
                 if (group_any(group, moves)) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -898,84 +922,65 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                             }
                     }
                     group_sync(group);
+                    if (mine) weights();
+                    group_sync(group);
                 }
-                copies.issue();  // into the stage that the unit before has left
                 if (mine) {
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const float2 mm = reinterpret_cast<const float2*>(row_m)[nt * 4 + t];
-                        const float2 mul = reinterpret_cast<const float2*>(row_mul)[nt * 4 + t];
-                        const uint64_t mu = f2_pack(-mm.x, -mm.y), by = f2_pack(mul.x, mul.y);
-                        uint64_t sum = f2_pack(l[nt][0], l[nt][1]);
-#pragma unroll
-                        for (int mt = 0; mt < 2; ++mt) {
-                            float e[4];
-#pragma unroll
-                            for (int j = 0; j < 4; j += 2) {
-                                f2_unpack(f2_fma(f2_pack(s[mt][nt][j], s[mt][nt][j + 1]), by, mu), e[j], e[j + 1]);
-                                e[j] = ex2_approx(e[j]);
-                                e[j + 1] = ex2_approx(e[j + 1]);
-                                sum = f2_add(sum, f2_pack(e[j], e[j + 1]));
-                            }
-                            p_frag[((warp * 2 + mt) * NT + nt) * 32 + lane] =
-                                make_uint2(transpose8(pack_f16(e[0], e[1])), transpose8(pack_f16(e[2], e[3])));
-                        }
-                        f2_unpack(sum, l[nt][0], l[nt][1]);
-                    }
+                    for (int nt = 0; nt < NT; ++nt) l[nt][0] += more[nt][0], l[nt][1] += more[nt][1];
                 }
-                group_sync(group);
+                copies.issue();  // into the stage that the unit before has left
                 // ---- O^T: columns 2t, 2t + 1, 2t + 8, 2t + 9 of a tile are keys t, t + 4, t + 8, t + 12
-                const int steps = 2 * min(kCaWarps, (run.len - unit * kCaUnit + kCaKeys - 1) / kCaKeys);  // of 16 keys
                 const bool drafts = cut_here && vis_min < run.len;  // keys that some rows see and some do not
-#pragma unroll 2
-                for (int ks = 4 * keys; ks < min(steps, 4 * keys + 4); ++ks) {
-                    const uint8_t* const st = smem + (ks >> 1) * (kCaStages * S::kStage) + stage;
-                    const int key_at = (ks & 1) * 16;
-                    uint32_t vw[4], code[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint8_t* at_v = st + v_at[j & 1] + (key_at + 8 * (j >> 1)) * (D / 2);
-                        vw[j] = D == 128 ? *reinterpret_cast<const uint32_t*>(at_v) : *reinterpret_cast<const uint16_t*>(at_v);
-                        code[j] = st[v_sc + (key_at + 4 * j) * (D / 16)];
-                    }
-                    uint32_t f[2] = {code[1] * 0x800000u + code[0] * 0x80u, code[3] * 0x800000u + code[2] * 0x80u};
-                    if (drafts) {  // (as for one tile)
-                        uint32_t bad[2];
-                        ca_take_bad(f, bad);
-                        if (__any_sync(0xffffffffu, (bad[0] | bad[1]) != 0)) {
-                            const uint32_t a[4] = {bad[0] & 0x3c003c00u, 0u, bad[1] & 0x3c003c00u, 0u};
-#pragma unroll
+#pragma unroll 1
+                for (int w = 2 * keys; w < 2 * keys + 2 && unit * kCaUnit + w * kCaKeys < run.len; ++w) {
+                    uint8_t* const st = smem + w * (S::kStages * S::kStage) + stage;
+                    if (__builtin_expect(drafts, 0)) {
+#pragma unroll 1
+                        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll 1
                             for (int nt = 0; nt < NT; ++nt) {
-                                const int room = row_vis[nt * 8 + g] - unit * kCaUnit - ks * 16 - t;  // of keys t, t + 4 ...
-                                float seen[4] = {0.f, 0.f, 0.f, 0.f};
-                                mma_f16(seen, a, (room > 0 ? 0x3c00u : 0u) | (room > 4 ? 0x3c000000u : 0u),
-                                        (room > 8 ? 0x3c00u : 0u) | (room > 12 ? 0x3c000000u : 0u));
-                                poison |= ((seen[0] > 0.f ? 1u : 0u) | (seen[1] > 0.f ? 2u : 0u)) << (2 * nt);
+                                const int room = row_vis[nt * 8 + g] - unit * kCaUnit - w * kCaKeys - 16 * mt - t;  // of keys t, t + 4 ...
+                                poison |= ca_seen_bad(st + v_sc + 16 * mt * (D / 16), D / 4, room) << (2 * nt);
                             }
+                        __syncwarp();
+                        ca_drop_bad(st + v_sc, D / 4);
+                        __syncwarp();
+                    }
+                    const uint2* const pf = p_frag + w * 2 * NT * 32 + lane;
+#pragma unroll
+                    for (int mt = 0; mt < 2; ++mt) {
+                        uint32_t vw[4], code[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint8_t* at_v = st + v_at[j & 1] + (16 * mt + 8 * (j >> 1)) * (D / 2);
+                            vw[j] = D == 128 ? *reinterpret_cast<const uint32_t*>(at_v) : *reinterpret_cast<const uint16_t*>(at_v);
+                            code[j] = st[v_sc + (16 * mt + 4 * j) * (D / 16)];
                         }
-                    }
-                    // even channels of two keys, odd ones of two keys (D = 64: of four, two words in one)
-                    uint32_t ev[MT == 4 ? 8 : 4], od[MT == 4 ? 8 : 4];
+                        const uint32_t f[2] = {code[1] * 0x800000u + code[0] * 0x80u, code[3] * 0x800000u + code[2] * 0x80u};
+                        // even channels of two keys, odd ones of two keys (D = 64: of four, two words in one)
+                        uint32_t ev[2 * MT], od[2 * MT];
 #pragma unroll
-                    for (int e = 0; e < MT / 2; ++e) {
-                        const uint32_t a = MT == 4 ? vw[2 * e] : vw[0] + vw[2] * 0x10000u, b = MT == 4 ? vw[2 * e + 1] : vw[1] + vw[3] * 0x10000u;
-                        uint32_t x[4], y[4];
-                        c4_decode((a & 0x0f0f0f0fu) | ((b * 16) & 0xf0f0f0f0u), x);
-                        c4_decode(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), y);
+                        for (int e = 0; e < MT / 2; ++e) {
+                            const uint32_t a = MT == 4 ? vw[2 * e] : vw[0] + vw[2] * 0x10000u, b = MT == 4 ? vw[2 * e + 1] : vw[1] + vw[3] * 0x10000u;
+                            uint32_t x[4], y[4];
+                            c4_decode((a & 0x0f0f0f0fu) | ((b * 16) & 0xf0f0f0f0u), x);
+                            c4_decode(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), y);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) ev[4 * e + j] = x[j], od[4 * e + j] = y[j];
-                    }
-                    uint32_t ha[MT][4];
+                            for (int j = 0; j < 4; ++j) ev[4 * e + j] = x[j], od[4 * e + j] = y[j];
+                        }
+                        uint32_t ha[MT][4];
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        ha[i][0] = h2_mul(ev[i], f[0]), ha[i][1] = h2_mul(od[i], f[0]);
-                        ha[i][2] = h2_mul(ev[MT + i], f[1]), ha[i][3] = h2_mul(od[MT + i], f[1]);
-                    }
+                        for (int i = 0; i < MT; ++i) {
+                            ha[i][0] = h2_mul(ev[i], f[0]), ha[i][1] = h2_mul(od[i], f[0]);
+                            ha[i][2] = h2_mul(ev[MT + i], f[1]), ha[i][3] = h2_mul(od[MT + i], f[1]);
+                        }
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const uint2 pf = p_frag[(ks * NT + nt) * 32 + lane];
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint2 pp = pf[(mt * NT + nt) * 32];
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) mma_f16(o[nt][i], ha[i], pf.x, pf.y);
+                            for (int i = 0; i < MT; ++i) mma_f16(o[nt][i], ha[i], pp.x, pp.y);
+                        }
                     }
                 }
             }
