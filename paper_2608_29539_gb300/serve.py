@@ -19,6 +19,10 @@ Nothing here waits for the GPU, and all lengths stay on the device.  Rejected
 drafts have added to the weights by then; their own rows are gone.  The rest of
 the layer (projections, the local branch, ContextNorm and fusion) is the
 caller's, by logo_decode_local_attn and logo_combine where n_new is 1.
+
+``ServeBatch4`` is the same loop for sequences whose own caches are kept whole, in
+4 bits a value: prompts are filled in, nothing is evicted, and verification starts
+from the target's logits and what each request asks of its sampling.
 """
 from __future__ import annotations
 
@@ -159,3 +163,134 @@ class ServeBatch:
         self._counts()
         self._latest_last = False
         self._rows_used = min(self._rows_used, c.budget)
+
+
+@dataclasses.dataclass
+class Serve4Config:
+    B: int             # sequences
+    n_new: int         # tokens a step brings per sequence (drafts + 1)
+    Hq: int
+    Hkv: int
+    D: int
+    rows: int          # cache rows per sequence
+    mode: int = L.LOGO_SELECT_THRESHOLD
+    b_th: float = 0.5
+    ratio: float = 1.0
+    scale: float = 0.0
+
+
+class ServeBatch4:
+    """A batch over caches of its own that are held in 4 bits.
+
+        batch.fill(k, v, n_valid)             prompts, or the next chunk of them
+        batch.context(m)                      the rows held so far, for a chunk's dense attention
+        batch.step(q, k_new, v_new, gate_p)   the new tokens join; gate, packing, attention
+        batch.verify(draft, q_draft, logits, u, noise, ...)
+                                              logits to probabilities, verdict, rejected rows dropped
+
+    What might not fit the caches is refused, counting rejected drafts too, as their
+    number stays on the device (recount() reads it back).  Replays of a captured graph are
+    not seen here: once a call was captured nothing is refused, and a call that finds no
+    room for all its rows overwrites the latest ones."""
+
+    def __init__(self, cfg: Serve4Config, device="cuda"):
+        if cfg.B < 1 or cfg.n_new < 1 or cfg.rows < cfg.n_new:
+            raise ValueError("need B >= 1, n_new >= 1 and rows >= n_new")
+        self.cfg = c = cfg
+        dev = torch.device(device)
+        z = lambda shape, dt: torch.zeros(shape, dtype=dt, device=dev)  # noqa: E731
+        self.cache = L.logo_cache4_empty(c.B, c.rows, c.Hkv, c.D, dev)
+        self.seq_len = z((c.B,), torch.int32)
+        cap = c.B * c.n_new
+        self.z = z((c.B, c.n_new), torch.uint8)
+        self.pos = z((cap,), torch.int32)
+        self.cu_q = z((c.B + 1,), torch.int32)
+        self.row_of = z((c.B, c.n_new), torch.int32)
+        self.n_sel = z((1,), torch.int32)
+        self.o_c = z((cap, c.Hq, c.D), torch.bfloat16)
+        self.lse_c = z((c.Hq, cap), torch.float32)
+        lib = L.lib()
+        nbytes = max(int(lib.logo_decode_cache4_workspace_size(L.Dims(c.B, c.rows, c.Hq, c.Hkv, c.D), c.n_new)),
+                     int(lib.logo_select_workspace_size(L.Dims(c.B, c.n_new, 1, 1, 64))))
+        self.ws = torch.empty((max(nbytes, 256),), dtype=torch.uint8, device=dev)  # the calls are stream-ordered
+        self._rows_used = 0       # at most this many rows of any cache hold a token
+        self._latest_step = False  # the caches' last rows are the latest step's, and all there
+        self._captured = False    # whether a graph holds some of the calls
+
+    _counts = ServeBatch._counts
+
+    @property
+    def k(self):  # (what _counts looks at)
+        return self.cache.k
+
+    def _room(self, n):
+        if self._counts() and self._rows_used + n > self.cfg.rows:
+            raise ValueError(f"{n} more rows may not fit, {self._rows_used} of {self.cfg.rows} may be in use")
+
+    def recount(self):
+        """Counts the rows in use, which waits for the GPU; returns the largest count."""
+        self._rows_used = int(self.seq_len.max())
+        return self._rows_used
+
+    def fill(self, k, v, n_valid=None):
+        """K and V [B, n, Hkv, D] bf16 behind what the caches hold; of sequence b the first
+        n_valid[b] (int32; None: all n)."""
+        n = k.shape[1]
+        if n > self.cfg.rows:
+            raise ValueError(f"{n} rows do not fit caches of {self.cfg.rows}")
+        self._room(n)
+        if n_valid is not None:
+            L._need(n_valid, torch.int32, "n_valid", (self.cfg.B,))
+            n_valid = n_valid.clamp(0, n)
+        # (a replay may come here with full caches)
+        seq_len = self.seq_len.clamp(max=self.cfg.rows - n) + (n if n_valid is None else n_valid)
+        L.logo_cache4_append(self.cache, k, v, seq_len, n_valid)
+        self.seq_len.copy_(seq_len)
+        self._rows_used += n
+        self._latest_step = False
+
+    def context(self, m=None):
+        """The first m rows (None: all) of every cache as bf16 (k, v) [B, m, Hkv, D], zeros
+        past a sequence's tokens."""
+        return L.logo_cache4_read(self.cache, self.seq_len, m=m)
+
+    def step(self, q, k_new, v_new, gate_p):
+        """q [B, n_new, Hq, D], k_new / v_new [B, n_new, Hkv, D] bf16, gate_p [B, n_new]
+        float32.  Returns (o_c [B*n_new, Hq, D] packed, z, row_of): what logo_combine takes
+        on (B, n_new); the next step writes to the same buffers."""
+        c = self.cfg
+        # what is refused is refused before the caches change
+        L._need(q, torch.bfloat16, "q", (c.B, c.n_new, c.Hq, c.D))
+        L._need(gate_p, torch.float32, "gate_p", (c.B, c.n_new))
+        for name, t in (("k_new", k_new), ("v_new", v_new)):
+            L._need(t, torch.bfloat16, name, (c.B, c.n_new, c.Hkv, c.D))
+        self._room(c.n_new)
+        self.seq_len.clamp_(max=c.rows - c.n_new)  # (a replay may come here with full caches)
+        self.seq_len += c.n_new
+        L.logo_cache4_append(self.cache, k_new, v_new, self.seq_len)
+        self._rows_used += c.n_new
+        self._latest_step = True
+        L.logo_select(gate_p, c.mode, c.b_th, c.ratio, self.z, self.pos, self.cu_q, self.row_of, self.n_sel,
+                      workspace=self.ws)
+        L.logo_decode_cache4_attn(q, self.cache, self.seq_len, self.pos, self.cu_q, self.n_sel, c.scale, o_c=self.o_c,
+                                  lse_c=self.lse_c, workspace=self.ws)
+        return self.o_c, self.z, self.row_of
+
+    def verify(self, draft, q_draft, logits, u, noise, draft_len=None, **sampling):
+        """The step's drafts (n_new - 1 per sequence, of which the first draft_len [B] int32
+        count where it is given) against the target's logits [B, n_new, V]; sampling: what
+        logo_target_probs takes beside them (its draft is given here where there is a
+        penalty).  The tokens that are not accepted leave the caches.  Returns (tokens [B,
+        n_new], n_accept [B]).  Once a step."""
+        c = self.cfg
+        if self._counts() and c.n_new > 1 and not self._latest_step:
+            raise ValueError("the drafts were verified, or rows filled in, since the last step")
+        if logits.dim() != 3 or logits.shape[0] != c.B or logits.shape[1] != c.n_new:
+            raise ValueError(f"logits has shape {tuple(logits.shape)}, expected ({c.B}, {c.n_new}, V)")
+        if sampling.get("penalty") is not None and c.n_new > 1:
+            sampling.setdefault("draft", draft)
+        p = L.logo_target_probs(logits, **sampling)
+        tokens, n_accept = L.logo_verify_draft(draft, q_draft, p, u, noise, draft_len=draft_len)
+        self._latest_step = False
+        self.seq_len -= c.n_new - 1 - n_accept
+        return tokens, n_accept
