@@ -371,7 +371,9 @@ LOGO_API int logo_cache4_read(logo_cache4 cache, const int32_t* seq_len, const i
  *   flight.
  *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer or a size out of range;
  *   LOGO_ERR_UNSUPPORTED for D, Hq % Hkv, 16-byte alignment, B * n_new > 2^24,
- *   n_new * Hq / Hkv > 8192, Hkv > 2^16, B * n_new * Hq > 2^30; LOGO_ERR_WORKSPACE. */
+ *   n_new * Hq / Hkv > 8192, Hkv > 2^16, B * n_new * Hq > 2^30, 2^31 pieces of 128 cache
+ *   rows and 32 query rows or more ((ceil(L / 128) + 4) * B * Hkv * ceil(n_new * Hq /
+ *   Hkv / 32)); LOGO_ERR_WORKSPACE. */
 LOGO_API size_t logo_decode_cache4_workspace_size(logo_dims dims, int n_new);
 LOGO_API int logo_decode_cache4_attn(const logo_bf16* q, logo_cache4 cache, const int32_t* seq_len,
                 const int32_t* pos, const int32_t* cu_q, const int32_t* n_sel_total, logo_bf16* o_c, float* lse_c,
@@ -405,11 +407,11 @@ LOGO_API int logo_decode_cache4_attn(const logo_bf16* q, logo_cache4 cache, cons
  *   x) makes p NaN for all of them.
  *   Results are deterministic.  Workspace:
  *   logo_target_probs_workspace_size(...) bytes, one per call in flight: a row's 8 bytes per
- *   2048 tokens, and for lists 3 V / 8 and 8 for each token that they can name.
+ *   4096 tokens, and for lists 3 V / 8 and 8 for each token that they can name.
  *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer, history without hist_len,
  *   n_prompt without history, history or draft without penalty, draft with m1 = 1, or
  *   sizes out of range; LOGO_ERR_UNSUPPORTED for V > LOGO_PROBS_MAX_VOCAB, m1 > 1024,
- *   K > 4096, B * m1 > 2^24, 16-byte alignment of logits or p, bf16 logits in p;
+ *   K > 4096, B * m1 > 2^24, B * H > 2^40, 16-byte alignment of logits or p, bf16 logits in p;
  *   LOGO_ERR_WORKSPACE. */
 #define LOGO_PROBS_MAX_COUNTED 16384
 #define LOGO_PROBS_MAX_VOCAB 278528

@@ -36,9 +36,6 @@ __device__ __forceinline__ uint32_t c4_scale_code(uint32_t amax)
     return min(u - ((127u - 15u) << 3), kC4MaxScale);
 }
 
-// Two scales' codes in bytes 0 and 1 -> f16x2 (code 255: NaN).
-__device__ __forceinline__ uint32_t c4_scale_f16(uint32_t code) { return code << 7; }
-
 __device__ __forceinline__ float c4_scale(uint32_t code)
 {
     return __half2float(__ushort_as_half(static_cast<unsigned short>(code << 7)));

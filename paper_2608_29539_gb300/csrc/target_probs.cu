@@ -4,7 +4,7 @@
 //
 // HBM bounds it: 2 or 4 bytes read, 1/8 of one for the mask and 4 written per token.  Two
 // streaming passes, the second of which finds most logits in L2 (it goes through the rows
-// backwards): the first leaves a maximum and a sum of exponentials per 2048 tokens, the
+// backwards): the first leaves a maximum and a sum of exponentials per 4096 tokens, the
 // second takes all of a row's and writes.  (One pass that kept a row in the registers of a
 // thread-block cluster between its read and its write took 122 us for 240 rows of 131072:
 // clusters follow one another, wait for their slowest CTA and do the lists' work eight

@@ -74,7 +74,8 @@ def test_attn_host_checks(logo):
                dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf)):
         assert call(**kw) == logo.LOGO_ERR_INVALID_ARG, kw
     for kw in (dict(q=odd), dict(o=odd), dict(dims=logo.Dims(4, 256, 8, 2, 80)), dict(dims=logo.Dims(4, 256, 9, 2, 128)),
-               dict(n_new=4096)):
+               dict(n_new=4096), dict(dims=logo.Dims(1, 1 << 30, 512, 512, 64), n_new=1),
+               dict(dims=logo.Dims(1 << 20, 1 << 10, 1 << 12, 1 << 8, 64), n_new=16)):
         assert call(**kw) == logo.LOGO_ERR_UNSUPPORTED, kw
     for c, want in _bad_caches(logo):
         assert call(c=c) == want

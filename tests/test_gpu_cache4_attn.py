@@ -247,6 +247,42 @@ def test_same_bits_in_a_graph_and_on_other_streams():
             assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("n,G", [(1, 4), (3, 4)])
+def test_offsets_past_32_bits(n, G):
+    """Rows written, read and attended past 2^32 bytes of codes.  All other rows hold zeros:
+    a logit of 0 each and nothing added to the sums."""
+    logo = _logo()
+    B, Hkv, D, L = 2, 8, 128, 2 ** 22 + 2 ** 18 + 77
+    assert B * Hkv * L * (D // 2) > 2 ** 32 > (B * Hkv - 1) * L * (D // 2)
+    g = torch.Generator().manual_seed(n)
+    bf = lambda *s: torch.randn(s, generator=g).to(torch.bfloat16)  # noqa: E731
+    q, k, v = bf(B, n, G * Hkv, D), bf(B, 5, Hkv, D) * 4, bf(B, 5, Hkv, D)
+    cache = logo.logo_cache4_empty(B, L, Hkv, D)
+    lens = [700, L]
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    logo.logo_cache4_append(cache, k.cuda(), v.cuda(), seq)
+    k, v = (R.values(*R.quantise(x)) for x in (k, v))
+    rows = (seq[:, None] - 5 + torch.arange(5, device="cuda")).int()
+    for got, want in zip(logo.logo_cache4_read(cache, seq, rows=rows), (k, v)):
+        assert torch.equal(got.double().cpu(), want)
+    pos, cu, ns, packed = (t.cuda() if torch.is_tensor(t) else t for t in _pack(torch.ones((B, n), dtype=torch.bool)))
+    o, lse = logo.logo_decode_cache4_attn(q.cuda(), cache, seq, pos, cu, ns)
+    for r in range(B * n):
+        b, i = divmod(r, n)
+        m = 5 - n + i + 1  # of the rows that are not zeros it sees these
+        for h in range(G * Hkv):
+            kk, vv, qq = k[b, :m, h // G], v[b, :m, h // G], q[b, i, h].double()
+            w = torch.exp(kk @ qq / D ** 0.5)
+            total = w.sum() + lens[b] - n + i + 1 - m
+            want, absv = w @ vv / total, w @ vv.abs() / total
+            x = (D + 8) * 2.0 ** -24 * float((kk.abs() @ qq.abs()).max()) / D ** 0.5 + 2.0 ** -20
+            # no thread adds more than 4 weights for each of 1/456 of the 8 heads' units of 128 rows
+            sums = 3000 * 2.0 ** -24
+            tol = 2.0 ** -8 * want.abs() + absv * (2.0 ** -11 + 2 * x + 2 * sums) + 2.0 ** -25 * w.max() / total * vv.abs().sum(0)
+            assert ((o[r, h].double().cpu() - want).abs() <= 1.01 * tol).all()
+            assert abs(float(lse[h, r]) - float(torch.log(total))) <= x + sums + 2.0 ** -23 * abs(float(torch.log(total)))
+
+
 def test_refusals():
     logo = _logo()
     cache = logo.logo_cache4_empty(2, 16, 2, 64)

@@ -106,6 +106,30 @@ def test_parts_left_out(drop):
     _check(s, None if "allowed" in drop else ok, _run(s))
 
 
+@pytest.mark.parametrize("B,m1,V,H,K,half", [(1, 2, 30011, 12000, 3, False), (2, 1, 9001, 9500, 0, True)])
+def test_long_lists(B, m1, V, H, K, half):
+    """More listed tokens than are counted in shared memory, in place where that can be."""
+    s, ok = _random(B, m1, V, H, K, V + H, half=half)
+    _check(s, ok, _run(s))
+    if not half:
+        d = {k: v.cuda() for k, v in s.items()}
+        _check(s, ok, _logo().logo_target_probs(**d, p=d["logits"]))
+
+
+def test_offsets_past_32_bits():
+    """The last rows of 2^32 tokens and more; those ahead of them are uniform."""
+    B, m1, V = 15421, 1, 278528
+    s, ok = _random(2, m1, V, 40, 3, 12, mask=False, half=True)
+    grow = lambda t, x=0: torch.cat([t.new_full((B - 2, *t.shape[1:]), x).cuda(), t.cuda()])  # noqa: E731
+    d = {k: grow(v, 1 if k in ("temperature", "penalty") else 0) for k, v in s.items()}
+    d["bias_tok"][:-2] = -1
+    p = _logo().logo_target_probs(**d)
+    assert (B - 2) * V < 2 ** 32 < B * V
+    _check(s, None, p[-2:])
+    for b in (0, B // 2, B - 3):
+        assert ((p[b] * V - 1).abs() < 1e-4).all()
+
+
 def test_in_place():
     s, ok = _random(2, 3, 40013, 60, 9, 5)
     x = s["logits"].cuda()
