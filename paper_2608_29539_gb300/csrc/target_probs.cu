@@ -30,13 +30,12 @@ constexpr int kTpThreads = 256;
 constexpr int kTpGroups = 2;                               // groups of eight tokens a thread
 constexpr int kTpChunk = kTpThreads * kTpGroups;           // groups a CTA
 constexpr int kTpListThreads = 512;
-constexpr int kTpAt = 8;                                   // list entries in flight per thread
+constexpr int kTpAt = 4;                                   // list entries in flight per thread
 constexpr int kTpNear = 8192;                              // listed tokens that are counted in shared memory
 // a listed token's word: how often it was generated, its place among the biases (plus one), flags
 constexpr uint32_t kTpSeen = 1u << 31, kTpBiased = 1u << 30, kTpTwice = 1u << 29, kTpCount = (1u << 15) - 1;
-constexpr int kTpBiasAt = 15, kTpTake = 4;                 // listed tokens of a thread at a time
+constexpr int kTpBiasAt = 15, kTpTake = 8;                 // listed tokens of a thread at a time
 static_assert(LOGO_PROBS_MAX_COUNTED + 1024 <= kTpCount, "counts have room");
-constexpr int kTpRowThreads = 512;
 
 struct TpParams {
     const void* logits;
@@ -49,14 +48,14 @@ struct TpParams {
     int chunks;         // CTAs a row
     int words;          // of a bit a token: ceil(V / 32)
     int64_t listed;     // room for listed tokens a row (0: no lists)
-    float2* stats;      // [rows][chunks] (maximum, sum)
-    float2* totals;     // [rows]
+    int pairs;          // of a row: one a chunk, then its listed tokens'
+    float2* stats;      // [rows][pairs] (maximum, sum)
     uint32_t* marks;    // [rows][words]: a bit a listed token
     uint16_t* bits;     // [rows][chunks * groups]: of eight tokens, those allowed and not listed; in the upper byte those listed
-    int32_t* n_listed;  // [rows]
-    int32_t* tokens;    // [rows][listed]: the listed tokens, ascending
-    uint32_t* counts;   // [rows][listed]: how often each was generated, and flags
+    uint2* far;         // [rows][listed], where that is more than shared memory is used for
 };
+
+
 
 __device__ __forceinline__ float ex2(float x) { return ex2_approx(x); }
 
@@ -210,11 +209,14 @@ __device__ __forceinline__ uint32_t bits_of(const uint32_t* row, int words, int 
     return (v < 0 ? lo << -v : __funnelshift_r(lo, hi, v & 31)) & 0xffu;
 }
 
-// A row's listed tokens with their counts and flags, and what is left to the passes.
+// A row's lists: the listed tokens counted, then adjusted, into p; their pair, and what is
+// left to the passes.
+template <bool HALF>
 __global__ void __launch_bounds__(kTpListThreads) target_lists_kernel(TpParams a)
 {
     extern __shared__ __align__(16) uint32_t smem[];
     __shared__ uint32_t sh_sum[kTpListThreads / 32];
+    __shared__ float2 sh_pair[kTpListThreads / 32];
     const int row = blockIdx.x, b = row / a.m1, i = row - b * a.m1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int room = (a.words + 3) / 4 * 4;
     uint32_t *const bits = smem, *const before = smem + room;
@@ -226,7 +228,12 @@ __global__ void __launch_bounds__(kTpListThreads) target_lists_kernel(TpParams a
     const int32_t* draft = a.draft + static_cast<int64_t>(b) * (a.m1 - 1);
     const int n_draft = a.draft ? i : 0;
     const int32_t* tok = a.bias_tok + static_cast<int64_t>(b) * a.K;
+    const float* val = a.bias_val + static_cast<int64_t>(b) * a.K;
+    const float T = a.temperature ? a.temperature[b] : 1.f, c = steepness(T);
+    const float rep = a.penalty ? a.penalty[3 * b] : 1.f, freq = a.penalty ? a.penalty[3 * b + 1] : 0.f,
+                pres = a.penalty ? a.penalty[3 * b + 2] : 0.f;
     __syncthreads();
+    const int64_t row0 = static_cast<int64_t>(row) * a.V;
     const auto mark = [&](uint32_t t, int) { atomicOr(bits + t / 32, 1u << (t & 31)); };
     each_token(hist, old, a.V, mark);
     each_token(draft, n_draft, a.V, mark);
@@ -263,38 +270,69 @@ __global__ void __launch_bounds__(kTpListThreads) target_lists_kernel(TpParams a
         if (in) *reinterpret_cast<uint4*>(before + w + 4 * lane) = make_uint4(b0, b1, b2, b2 + __popc(y.z));
         at += __shfl_sync(0xffffffffu, upto, 31);
     }
-    // counts in shared memory where there is room, else in the workspace
-    const bool near = a.listed <= kTpNear;
-    int32_t* const tokens = a.tokens + row * a.listed;
-    uint32_t* const far_counts = a.counts + row * a.listed;
-    uint32_t* const counts = near ? smem + 2 * room : far_counts;
-    for (uint32_t k = tid; k < n; k += kTpListThreads) counts[k] = 0;
-    if (tid == 0) a.n_listed[row] = n;
+    // the tokens and their words in shared memory where there is room, else in the workspace
+    uint2* const list = a.listed <= kTpNear ? reinterpret_cast<uint2*>(smem + 2 * room) : a.far + row * a.listed;
+    for (uint32_t k = tid; k < n; k += kTpListThreads) list[k] = make_uint2(0, 0);
     __syncthreads();
     for (int w = tid; w < a.words; w += kTpListThreads) a.marks[static_cast<int64_t>(row) * a.words + w] = bits[w];
-    const auto place = [&](uint32_t t) { return before[t / 32] + __popc(bits[t / 32] & ((1u << (t & 31)) - 1)); };
+    const auto place = [&](uint32_t t) {
+        uint2* const to = list + before[t / 32] + __popc(bits[t / 32] & ((1u << (t & 31)) - 1));
+        to->x = t;  // (the same from all entries)
+        return &to->y;
+    };
     each_token(hist, old, a.V, [&](uint32_t t, int k) {
-        const uint32_t to = place(t);
-        tokens[to] = t;  // (the same from all entries)
-        if (k >= prompt) atomicAdd(counts + to, 1u);
-        else atomicOr(counts + to, kTpSeen);
+        if (k >= prompt) atomicAdd(place(t), 1u);
+        else atomicOr(place(t), kTpSeen);
     });
-    each_token(draft, n_draft, a.V, [&](uint32_t t, int) {
-        const uint32_t to = place(t);
-        tokens[to] = t;
-        atomicAdd(counts + to, 1u);
-    });
+    each_token(draft, n_draft, a.V, [&](uint32_t t, int) { atomicAdd(place(t), 1u); });
     each_token(tok, a.K, a.V, [&](uint32_t t, int k) {
-        const uint32_t to = place(t);
-        tokens[to] = t;
+        uint32_t* const to = place(t);
         // (a second entry leaves the first's place and a mark that there are several)
-        if (atomicOr(counts + to, kTpBiased) & kTpBiased) atomicOr(counts + to, kTpTwice);
-        else atomicAdd(counts + to, static_cast<uint32_t>(k + 1) << kTpBiasAt);
+        if (atomicOr(to, kTpBiased) & kTpBiased) atomicOr(to, kTpTwice);
+        else atomicAdd(to, static_cast<uint32_t>(k + 1) << kTpBiasAt);
     });
-    if (near) {
-        __syncthreads();
-        for (uint32_t k = tid; k < n; k += kTpListThreads) far_counts[k] = counts[k];
+    __syncthreads();
+    // adjusted in the tokens' order
+    const uint32_t* allowed = a.allowed ? a.allowed + static_cast<int64_t>(row) * a.words : nullptr;
+    float2 pair = nothing(T, a.V);
+#pragma unroll 1
+    for (uint32_t k0 = tid; k0 < n + tid; k0 += kTpTake * kTpListThreads) {
+        uint2 e[kTpTake];
+        uint32_t in[kTpTake];
+        float x[kTpTake];
+#pragma unroll
+        for (int j = 0; j < kTpTake; ++j) {
+            const uint32_t k = k0 + j * kTpListThreads;
+            e[j] = k < n ? list[k] : make_uint2(a.V, 0);
+            x[j] = k < n ? logit<HALF>(a, row0 + e[j].x) : -INFINITY;
+            in[j] = allowed && k < n ? __ldg(allowed + e[j].x / 32) >> (e[j].x & 31) & 1 : 1;
+        }
+#pragma unroll
+        for (int j = 0; j < kTpTake; ++j) {
+            const uint32_t t = e[j].x, w = e[j].y, count = w & kTpCount;
+            if (t == a.V) continue;
+            float y = x[j];
+            if (count || w & kTpSeen) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
+            if (count) y = __fsub_rn(y, __fadd_rn(__fmul_rn(static_cast<float>(count), freq), pres));
+            if (w & kTpBiased) {
+                float sum = 0.f;
+                if (w & kTpTwice) {  // all that is listed for it, in the list's order
+#pragma unroll 8
+                    for (int q = 0; q < a.K; ++q)
+                        if (__ldg(tok + q) == t) sum = __fadd_rn(sum, val[q]);
+                } else {
+                    sum = val[(w >> kTpBiasAt & 0x1fff) - 1];
+                }
+                y = __fadd_rn(y, sum);
+            }
+            if (!in[j]) y = -INFINITY;
+            a.p[row0 + t] = y;
+            x[j] = y;
+        }
+        pair = join(pair, pair_of(x, T, c, a.V, [&](int j) { return static_cast<int>(e[j].x); }), T, c);
     }
+    pair = join_block<W>(pair, T, c, sh_pair);
+    if (tid == 0) a.stats[static_cast<int64_t>(row) * a.pairs + a.chunks] = pair;
 }
 
 // A thread's tokens as they come; of each group, the bits of those that count here and, in the
@@ -371,82 +409,25 @@ __global__ void __launch_bounds__(kTpThreads) target_stats_kernel(TpParams a)
     TpTokens<HALF>(a, row, chunk, std::true_type()).logits(x);
     float2 pair = pair_of(x, T, c, a.V, [&](int k) { return group_of(a, row, chunk, k / 8).v + k % 8; });
     pair = join_block<kTpThreads / 32>(pair, T, c, sh);
-    if (threadIdx.x == 0) a.stats[static_cast<int64_t>(row) * a.chunks + chunk] = pair;
-}
-
-// Between the passes: a row's listed tokens are adjusted, into p, and its pairs joined.
-template <bool HALF>
-__global__ void __launch_bounds__(kTpRowThreads) target_rows_kernel(TpParams a)
-{
-    __shared__ float2 sh_pair[kTpRowThreads / 32];
-    wait_for_stream();
-    const int row = blockIdx.x, b = row / a.m1, tid = threadIdx.x;
-    const float T = a.temperature ? a.temperature[b] : 1.f, c = steepness(T);
-    float2 pair = nothing(T, a.V);
-    for (int k = tid; k < a.chunks; k += kTpRowThreads) pair = join(pair, a.stats[static_cast<int64_t>(row) * a.chunks + k], T, c);
-    pair = join_warp(pair, T, c);
-    if (a.listed) {
-        const float rep = a.penalty ? a.penalty[3 * b] : 1.f, freq = a.penalty ? a.penalty[3 * b + 1] : 0.f,
-                    pres = a.penalty ? a.penalty[3 * b + 2] : 0.f;
-        const int32_t* tok = a.bias_tok + static_cast<int64_t>(b) * a.K;
-        const float* val = a.bias_val + static_cast<int64_t>(b) * a.K;
-        const int32_t* tokens = a.tokens + row * a.listed;
-        const uint32_t* counts = a.counts + row * a.listed;
-        const uint32_t* allowed = a.allowed ? a.allowed + static_cast<int64_t>(row) * a.words : nullptr;
-        const uint32_t n = a.n_listed[row];
-#pragma unroll 1
-        for (uint32_t k0 = tid; k0 < n + tid; k0 += kTpTake * kTpRowThreads) {
-            int t[kTpTake];
-            uint32_t w[kTpTake], in[kTpTake];
-            float x[kTpTake];
-#pragma unroll
-            for (int j = 0; j < kTpTake; ++j) {
-                const uint32_t k = k0 + j * kTpRowThreads;
-                t[j] = k < n ? tokens[k] : a.V;
-                w[j] = k < n ? counts[k] : 0;
-            }
-#pragma unroll
-            for (int j = 0; j < kTpTake; ++j) {
-                x[j] = t[j] < a.V ? logit<HALF>(a, static_cast<int64_t>(row) * a.V + t[j]) : -INFINITY;
-                in[j] = allowed && t[j] < a.V ? __ldg(allowed + t[j] / 32) >> (t[j] & 31) & 1 : 1;
-            }
-#pragma unroll
-            for (int j = 0; j < kTpTake; ++j) {
-                if (t[j] == a.V) continue;
-                float y = x[j];
-                const uint32_t count = w[j] & kTpCount;
-                if (count || w[j] & kTpSeen) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
-                if (count) y = __fsub_rn(y, __fadd_rn(__fmul_rn(static_cast<float>(count), freq), pres));
-                if (w[j] & kTpBiased) {
-                    float sum = 0.f;
-                    if (w[j] & kTpTwice) {  // all that is listed for it, in the list's order
-#pragma unroll 8
-                        for (int q = 0; q < a.K; ++q)
-                            if (__ldg(tok + q) == t[j]) sum = __fadd_rn(sum, val[q]);
-                    } else {
-                        sum = val[(w[j] >> kTpBiasAt & 0x1fff) - 1];
-                    }
-                    y = __fadd_rn(y, sum);
-                }
-                if (!in[j]) y = -INFINITY;
-                a.p[static_cast<int64_t>(row) * a.V + t[j]] = y;
-                x[j] = y;
-            }
-            pair = join(pair, pair_of(x, T, c, a.V, [&](int j) { return t[j]; }), T, c);
-        }
-    }
-    pair = join_block<kTpRowThreads / 32>(pair, T, c, sh_pair);
-    if (tid == 0) a.totals[row] = pair;
+    if (threadIdx.x == 0) a.stats[static_cast<int64_t>(row) * a.pairs + chunk] = pair;
 }
 
 template <bool HALF>
 __global__ void __launch_bounds__(kTpThreads) target_write_kernel(TpParams a)
 {
+    __shared__ float2 sh_total;
     wait_for_stream();
     const int row = a.B * a.m1 - 1 - blockIdx.x, chunk = a.chunks - 1 - blockIdx.y;  // what was read last comes first
     const float T = a.temperature ? a.temperature[row / a.m1] : 1.f, c = steepness(T);
-    const float2 total = a.totals[row];
     const TpTokens<HALF> tokens(a, row, chunk, std::false_type());
+    if (threadIdx.x < 32) {
+        float2 pair = nothing(T, a.V);
+        for (int k = threadIdx.x; k < a.pairs; k += 32) pair = join(pair, a.stats[static_cast<int64_t>(row) * a.pairs + k], T, c);
+        pair = join_warp(pair, T, c);
+        if (threadIdx.x == 0) sh_total = pair;
+    }
+    __syncthreads();
+    const float2 total = sh_total;
     float x[kTpGroups * 8];
     tokens.logits(x);
 #pragma unroll
@@ -508,7 +489,7 @@ int64_t tp_chunks(int V) { return (V / 8 + 2 + kTpChunk - 1) / kTpChunk; }
 
 // Offsets of the workspace's parts; the last is its size.
 struct TpRoom {
-    size_t totals, marks, bits, n_listed, tokens, counts, bytes;
+    size_t marks, bits, far, bytes;
     int64_t listed;
 };
 
@@ -517,13 +498,10 @@ TpRoom tp_room(int B, int m1, int V, int H, int K)
     const size_t rows = static_cast<size_t>(B) * m1;
     TpRoom r;
     r.listed = std::min<int64_t>(V, static_cast<int64_t>(H) + (m1 - 1) + K);
-    r.totals = round_up(rows * tp_chunks(V) * sizeof(float2), 256);
-    r.marks = r.totals + round_up(rows * sizeof(float2), 256);
+    r.marks = round_up(rows * (tp_chunks(V) + 1) * sizeof(float2), 256);
     r.bits = r.marks + (r.listed ? round_up(rows * ((V + 31) / 32) * 4, 256) : 0);
-    r.n_listed = r.bits + (r.listed ? round_up(rows * tp_chunks(V) * kTpChunk * 2, 256) : 0);
-    r.tokens = r.n_listed + round_up(rows * 4, 256);
-    r.counts = r.tokens + round_up(rows * r.listed * 4, 256);
-    r.bytes = r.counts + round_up(rows * r.listed * 4, 256);
+    r.far = r.bits + (r.listed ? round_up(rows * tp_chunks(V) * kTpChunk * 2, 256) : 0);
+    r.bytes = r.far + (r.listed > kTpNear ? round_up(rows * r.listed * sizeof(uint2), 256) : 0);
     return r;
 }
 
@@ -539,9 +517,9 @@ int check_probs(int B, int m1, int V, int H, int K)
 template <bool HALF>
 int tp_launch(const TpParams& a, cudaStream_t st)
 {
-    const int lists_smem = (a.words + 3) / 4 * 32 + (a.listed <= kTpNear ? static_cast<int>(a.listed) * 4 : 0);
+    const int lists_smem = (a.words + 3) / 4 * 32 + (a.listed <= kTpNear ? static_cast<int>(a.listed * sizeof(uint2)) : 0);
     static OncePerDevice once;
-    if (once([] { return set_smem_limit(target_lists_kernel, (LOGO_PROBS_MAX_VOCAB + 127) / 128 * 32 + kTpNear * 4); }) != cudaSuccess)
+    if (once([] { return set_smem_limit(target_lists_kernel<HALF>, (LOGO_PROBS_MAX_VOCAB + 127) / 128 * 32 + kTpNear * static_cast<int>(sizeof(uint2))); }) != cudaSuccess)
         return LOGO_ERR_CUDA;
     const unsigned rows = static_cast<unsigned>(a.B) * a.m1;
     cudaLaunchAttribute attr{};
@@ -555,17 +533,12 @@ int tp_launch(const TpParams& a, cudaStream_t st)
         cfg.gridDim = dim3(rows);
         cfg.blockDim = dim3(kTpListThreads);
         cfg.dynamicSmemBytes = lists_smem;
-        if (cudaLaunchKernelEx(&cfg, target_lists_kernel, a) != cudaSuccess) return LOGO_ERR_CUDA;
+        if (cudaLaunchKernelEx(&cfg, target_lists_kernel<HALF>, a) != cudaSuccess) return LOGO_ERR_CUDA;
         cfg.dynamicSmemBytes = 0;
     }
     cfg.gridDim = dim3(rows, a.chunks);
     cfg.blockDim = dim3(kTpThreads);
     if (cudaLaunchKernelEx(&cfg, target_stats_kernel<HALF>, a) != cudaSuccess) return LOGO_ERR_CUDA;
-    cfg.gridDim = dim3(rows);
-    cfg.blockDim = dim3(kTpRowThreads);
-    if (cudaLaunchKernelEx(&cfg, target_rows_kernel<HALF>, a) != cudaSuccess) return LOGO_ERR_CUDA;
-    cfg.gridDim = dim3(rows, a.chunks);
-    cfg.blockDim = dim3(kTpThreads);
     return cudaLaunchKernelEx(&cfg, target_write_kernel<HALF>, a) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }
 
@@ -603,10 +576,9 @@ extern "C" int logo_target_probs(const void* logits, int logits_bf16, const floa
     a.B = B, a.m1 = m1, a.V = V, a.H = H, a.K = K;
     a.chunks = static_cast<int>(tp_chunks(V)), a.words = (V + 31) / 32;
     a.listed = history || draft || K > 0 ? room.listed : 0;
-    a.stats = reinterpret_cast<float2*>(ws), a.totals = reinterpret_cast<float2*>(ws + room.totals);
-    a.marks = reinterpret_cast<uint32_t*>(ws + room.marks);
-    a.bits = reinterpret_cast<uint16_t*>(ws + room.bits), a.n_listed = reinterpret_cast<int32_t*>(ws + room.n_listed);
-    a.tokens = reinterpret_cast<int32_t*>(ws + room.tokens), a.counts = reinterpret_cast<uint32_t*>(ws + room.counts);
+    a.pairs = a.chunks + (a.listed > 0);
+    a.stats = reinterpret_cast<float2*>(ws), a.marks = reinterpret_cast<uint32_t*>(ws + room.marks);
+    a.bits = reinterpret_cast<uint16_t*>(ws + room.bits), a.far = reinterpret_cast<uint2*>(ws + room.far);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return logits_bf16 ? tp_launch<true>(a, st) : tp_launch<false>(a, st);
 }
