@@ -4,15 +4,17 @@
 //
 // HBM bounds it: 2 or 4 bytes read, 1/8 of one for the mask and 4 written per token.  Two
 // streaming passes, the second of which finds most logits in L2 (it goes through the rows
-// backwards): the first leaves a maximum and a sum of exponentials per 4096 tokens, the
+// backwards): the first leaves a maximum and a sum of exponentials per part of a row, the
 // second takes all of a row's and writes.  (One pass that kept a row in the registers of a
 // thread-block cluster between its read and its write took 122 us for 240 rows of 131072:
 // clusters follow one another, wait for their slowest CTA and do the lists' work eight
-// times.)
+// times.)  At the HBM rate an SM has little more than an instruction a token to spend, so
+// both passes are laid out to save them: logits come through a ring of a warp's own in shared
+// memory, and a thread of the first has 32 tokens in a row, whose masks are a word.
 // The lists of tokens (history, drafts, biases) are counted ahead of that, a CTA a row.  The
-// listed tokens are left out of the first pass; between the passes, when their logits are in
-// L2, they are adjusted, in the tokens' order, so that sums do not depend on the order of
-// atomics, and lie in p until the second pass takes them from there.
+// first pass leaves listed tokens out of its stretches and then takes each chunk's from the
+// list, a thread one, with their logits from the ring; the second writes their probabilities
+// over the zeros that it left.  Sums do not depend on the order of atomics.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -26,15 +28,17 @@
 namespace logo {
 namespace {
 
-constexpr int kTpThreads = 256;
-constexpr int kTpGroups = 2;                               // groups of eight tokens a thread
-constexpr int kTpChunk = kTpThreads * kTpGroups;           // groups a CTA
+constexpr int kTpThreads = 128, kTpWarps = kTpThreads / 32;
+constexpr int kTpChunk = 1024;                             // tokens of a warp at a time
+constexpr int kTpWords = 36;                               // room for the 33 words of a bit a token that they are in
+constexpr int kTpFew = 32;                                 // chunks an SM, up to which a warp takes one, else two
 constexpr int kTpListThreads = 512;
 constexpr int kTpAt = 4;                                   // list entries in flight per thread
+constexpr int kTpMaxBiases = 4096;
 constexpr int kTpNear = 8192;                              // listed tokens that are counted in shared memory
 // a listed token's word: how often it was generated, its place among the biases (plus one), flags
 constexpr uint32_t kTpSeen = 1u << 31, kTpBiased = 1u << 30, kTpTwice = 1u << 29, kTpCount = (1u << 15) - 1;
-constexpr int kTpBiasAt = 15, kTpTake = 8;                 // listed tokens of a thread at a time
+constexpr int kTpBiasAt = 15, kTpTake = 4;                 // listed tokens of a thread at a time
 static_assert(LOGO_PROBS_MAX_COUNTED + 1024 <= kTpCount, "counts have room");
 
 struct TpParams {
@@ -45,14 +49,16 @@ struct TpParams {
     const uint32_t* allowed;
     float* p;
     int B, m1, V, H, K;
-    int chunks;         // CTAs a row
+    int chunks;         // of a row
+    int each, parts;    // chunks of a warp: a part of a row; parts of a row
     int words;          // of a bit a token: ceil(V / 32)
     int64_t listed;     // room for listed tokens a row (0: no lists)
-    int pairs;          // of a row: one a chunk, then its listed tokens'
-    float2* stats;      // [rows][pairs] (maximum, sum)
-    uint32_t* marks;    // [rows][words]: a bit a listed token
-    uint16_t* bits;     // [rows][chunks * groups]: of eight tokens, those allowed and not listed; in the upper byte those listed
-    uint2* far;         // [rows][listed], where that is more than shared memory is used for
+    float2* stats;      // [rows][parts] (maximum, sum)
+    uint32_t *marks, *before;  // [rows][words]: a bit a listed token; how many are ahead of a word's
+    uint32_t* bits;     // [rows * chunks][kTpChunk / 32]: a bit a token that counts in the passes
+    uint2* part;        // [rows * chunks]: of the row's list, the first that is in the chunk, and how many are
+    uint2* list;        // [rows][listed]: listed tokens, ascending, with their words
+    float* adjusted;    // [rows][listed]: their biases, then their adjusted logits
 };
 
 
@@ -118,58 +124,6 @@ __device__ __forceinline__ float2 join_warp(float2 p, float T, float c)
 
 __device__ __forceinline__ float2 nothing(float T, int V) { return make_float2(-INFINITY, T == 0.f ? __int_as_float(V) : 0.f); }
 
-// Over a CTA's warps, in its first one; sh: a pair per warp.
-template <int WARPS>
-__device__ __forceinline__ float2 join_block(float2 p, float T, float c, float2* sh)
-{
-    if (threadIdx.x % 32 == 0) sh[threadIdx.x / 32] = p;
-    __syncthreads();
-    if (threadIdx.x >= 32) return p;
-    return join_warp(threadIdx.x < WARPS ? sh[threadIdx.x] : make_float2(-INFINITY, T == 0.f ? __int_as_float(0x7f7fffff) : 0.f), T, c);
-}
-
-// A warp's pair: its largest x, then the sum.  tokens(k): the token of x[k], ascending.
-template <int N, typename F>
-__device__ __forceinline__ float2 pair_of(const float (&x)[N], float T, float c, int V, F tokens)
-{
-    float top = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < N; k += 2) top = max3f(top, x[k], x[k + 1]);
-    top = unordered(__reduce_max_sync(0xffffffffu, ordered(top)));
-    if (T == 0.f) {
-        int chosen = V;
-        bool nan = false;
-#pragma unroll
-        for (int k = N - 1; k >= 0; --k) {
-            if (x[k] == top && top > -INFINITY) chosen = tokens(k);
-            nan |= x[k] != x[k];
-        }
-        chosen = __reduce_min_sync(0xffffffffu, chosen);
-        return make_float2(top, __any_sync(0xffffffffu, nan) ? NAN : __int_as_float(chosen));
-    }
-    const float mid = top == -INFINITY ? 0.f : top;
-    uint64_t part = f2_pack(0.f, 0.f);
-    const uint64_t off = f2_pack(-mid, -mid), by = f2_pack(c, c);
-    float lo, hi;
-#pragma unroll
-    for (int k = 0; k < N; k += 2) {
-        f2_unpack(f2_mul(f2_add(f2_pack(x[k], x[k + 1]), off), by), lo, hi);
-        part = f2_add(part, f2_pack(ex2(lo), ex2(hi)));
-    }
-    f2_unpack(part, lo, hi);
-    float sum = lo + hi;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    return make_float2(top, sum);
-}
-
-template <bool HALF>
-__device__ __forceinline__ float logit(const TpParams& a, int64_t e)
-{
-    return HALF ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(a.logits)[e]) << 16)
-                : static_cast<const float*>(a.logits)[e];
-}
-
 // f(token, index) for the entries of a list that are tokens, kTpAt loads in flight.
 template <typename F>
 __device__ __forceinline__ void each_token(const int32_t* list, int len, int V, F f)
@@ -178,28 +132,33 @@ __device__ __forceinline__ void each_token(const int32_t* list, int len, int V, 
     for (int k0 = threadIdx.x; k0 < len; k0 += kTpAt * kTpListThreads) {
         uint32_t t[kTpAt];
 #pragma unroll
-        for (int k = 0; k < kTpAt; ++k) t[k] = k0 + k * kTpListThreads < len ? __ldg(list + k0 + k * kTpListThreads) : 0xffffffffu;
+        for (int k = 0; k < kTpAt; ++k) t[k] = k0 + k * kTpListThreads < len ? list[k0 + k * kTpListThreads] : 0xffffffffu;
 #pragma unroll
         for (int k = 0; k < kTpAt; ++k)
             if (t[k] < static_cast<uint32_t>(V)) f(t[k], k0 + k * kTpListThreads);
     }
 }
 
-// Eight tokens of a row.  Groups begin at multiples of eight of the whole tensor's
-// elements, so all but a row's first and last are whole and aligned.
-struct TpGroup {
-    int64_t g;     // of the tensor
-    int v;         // its first token; less than 0 in a row's first group
-    bool in;       // a group of the row
+// A chunk of a row.  Chunks begin at multiples of eight of the whole tensor's elements, so
+// that groups of eight tokens are aligned, and all but a row's first and last are whole.
+struct TpPlace {
+    int64_t item;  // among all rows' chunks
+    int64_t g;     // its first group, of the tensor
+    int v;         // its first token, of the row; less than 0 in a row's first chunk, if that begins in the row before
+
+    __device__ __forceinline__ TpPlace(const TpParams& a, int row, int chunk)
+    {
+        const int64_t e0 = static_cast<int64_t>(row) * a.V;
+        item = static_cast<int64_t>(row) * a.chunks + chunk;
+        g = e0 / 8 + chunk * (kTpChunk / 8);
+        v = chunk * kTpChunk - static_cast<int>(e0 & 7);
+    }
+    __device__ __forceinline__ void step() { ++item, g += kTpChunk / 8, v += kTpChunk; }
+    __device__ __forceinline__ bool whole(const TpParams& a) const { return v >= 0 && v + kTpChunk <= a.V; }
 };
 
-__device__ __forceinline__ TpGroup group_of(const TpParams& a, int row, int chunk, int k)
-{
-    const int64_t e0 = static_cast<int64_t>(row) * a.V;
-    const uint32_t at = chunk * kTpChunk + k * kTpThreads + threadIdx.x;
-    const int v = static_cast<int>(at * 8) - static_cast<int>(e0 & 7);
-    return TpGroup{e0 / 8 + at, v, v < a.V};
-}
+// Are the eight tokens from v on all the row's?
+__device__ __forceinline__ bool whole8(const TpParams& a, int v) { return static_cast<uint32_t>(v) < static_cast<uint32_t>(max(a.V - 7, 0)); }
 
 // Bits of eight tokens from a row of a bit a token.
 __device__ __forceinline__ uint32_t bits_of(const uint32_t* row, int words, int v)
@@ -209,17 +168,16 @@ __device__ __forceinline__ uint32_t bits_of(const uint32_t* row, int words, int 
     return (v < 0 ? lo << -v : __funnelshift_r(lo, hi, v & 31)) & 0xffu;
 }
 
-// A row's lists: the listed tokens counted, then adjusted, into p; their pair, and what is
-// left to the passes.
-template <bool HALF>
+// A row's lists: the listed tokens in their order, with a word each, and what the passes take.
 __global__ void __launch_bounds__(kTpListThreads) target_lists_kernel(TpParams a)
 {
     extern __shared__ __align__(16) uint32_t smem[];
     __shared__ uint32_t sh_sum[kTpListThreads / 32];
-    __shared__ float2 sh_pair[kTpListThreads / 32];
     const int row = blockIdx.x, b = row / a.m1, i = row - b * a.m1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int room = (a.words + 3) / 4 * 4;
     uint32_t *const bits = smem, *const before = smem + room;
+    int32_t* const bias_tok = reinterpret_cast<int32_t*>(smem + 2 * room);
+    float* const bias_val = reinterpret_cast<float*>(bias_tok) + a.K;
     for (int w = tid; w < room; w += kTpListThreads) bits[w] = 0;
     wait_for_stream();
     const int old = a.history ? max(0, min(a.hist_len[b], a.H)) : 0;
@@ -227,17 +185,15 @@ __global__ void __launch_bounds__(kTpListThreads) target_lists_kernel(TpParams a
     const int32_t* hist = a.history + static_cast<int64_t>(b) * a.H;
     const int32_t* draft = a.draft + static_cast<int64_t>(b) * (a.m1 - 1);
     const int n_draft = a.draft ? i : 0;
-    const int32_t* tok = a.bias_tok + static_cast<int64_t>(b) * a.K;
-    const float* val = a.bias_val + static_cast<int64_t>(b) * a.K;
-    const float T = a.temperature ? a.temperature[b] : 1.f, c = steepness(T);
-    const float rep = a.penalty ? a.penalty[3 * b] : 1.f, freq = a.penalty ? a.penalty[3 * b + 1] : 0.f,
-                pres = a.penalty ? a.penalty[3 * b + 2] : 0.f;
+    for (int k = tid; k < a.K; k += kTpListThreads) {
+        bias_tok[k] = a.bias_tok[static_cast<int64_t>(b) * a.K + k];
+        bias_val[k] = a.bias_val[static_cast<int64_t>(b) * a.K + k];
+    }
     __syncthreads();
-    const int64_t row0 = static_cast<int64_t>(row) * a.V;
     const auto mark = [&](uint32_t t, int) { atomicOr(bits + t / 32, 1u << (t & 31)); };
     each_token(hist, old, a.V, mark);
     each_token(draft, n_draft, a.V, mark);
-    each_token(tok, a.K, a.V, mark);
+    each_token(bias_tok, a.K, a.V, mark);
     __syncthreads();
     // listed tokens before each word's: a warp a stretch of words, a lane four at a time
     constexpr int W = kTpListThreads / 32;
@@ -270,11 +226,16 @@ __global__ void __launch_bounds__(kTpListThreads) target_lists_kernel(TpParams a
         if (in) *reinterpret_cast<uint4*>(before + w + 4 * lane) = make_uint4(b0, b1, b2, b2 + __popc(y.z));
         at += __shfl_sync(0xffffffffu, upto, 31);
     }
-    // the tokens and their words in shared memory where there is room, else in the workspace
-    uint2* const list = a.listed <= kTpNear ? reinterpret_cast<uint2*>(smem + 2 * room) : a.far + row * a.listed;
+    // put together in shared memory where there is room, else in the workspace
+    const bool near = a.listed <= kTpNear;
+    uint2* const far_list = a.list + row * a.listed;
+    uint2* const list = near ? reinterpret_cast<uint2*>(bias_val + a.K) : far_list;
     for (uint32_t k = tid; k < n; k += kTpListThreads) list[k] = make_uint2(0, 0);
     __syncthreads();
-    for (int w = tid; w < a.words; w += kTpListThreads) a.marks[static_cast<int64_t>(row) * a.words + w] = bits[w];
+    for (int w = tid; w < a.words; w += kTpListThreads) {
+        a.marks[static_cast<int64_t>(row) * a.words + w] = bits[w];
+        a.before[static_cast<int64_t>(row) * a.words + w] = before[w];
+    }
     const auto place = [&](uint32_t t) {
         uint2* const to = list + before[t / 32] + __popc(bits[t / 32] & ((1u << (t & 31)) - 1));
         to->x = t;  // (the same from all entries)
@@ -285,241 +246,445 @@ __global__ void __launch_bounds__(kTpListThreads) target_lists_kernel(TpParams a
         else atomicOr(place(t), kTpSeen);
     });
     each_token(draft, n_draft, a.V, [&](uint32_t t, int) { atomicAdd(place(t), 1u); });
-    each_token(tok, a.K, a.V, [&](uint32_t t, int k) {
+    each_token(bias_tok, a.K, a.V, [&](uint32_t t, int k) {
         uint32_t* const to = place(t);
         // (a second entry leaves the first's place and a mark that there are several)
         if (atomicOr(to, kTpBiased) & kTpBiased) atomicOr(to, kTpTwice);
         else atomicAdd(to, static_cast<uint32_t>(k + 1) << kTpBiasAt);
     });
+    if (!near && !a.K) return;
     __syncthreads();
-    // adjusted in the tokens' order
-    const uint32_t* allowed = a.allowed ? a.allowed + static_cast<int64_t>(row) * a.words : nullptr;
-    float2 pair = nothing(T, a.V);
-#pragma unroll 1
-    for (uint32_t k0 = tid; k0 < n + tid; k0 += kTpTake * kTpListThreads) {
-        uint2 e[kTpTake];
-        uint32_t in[kTpTake];
-        float x[kTpTake];
-#pragma unroll
-        for (int j = 0; j < kTpTake; ++j) {
-            const uint32_t k = k0 + j * kTpListThreads;
-            e[j] = k < n ? list[k] : make_uint2(a.V, 0);
-            x[j] = k < n ? logit<HALF>(a, row0 + e[j].x) : -INFINITY;
-            in[j] = allowed && k < n ? __ldg(allowed + e[j].x / 32) >> (e[j].x & 31) & 1 : 1;
-        }
-#pragma unroll
-        for (int j = 0; j < kTpTake; ++j) {
-            const uint32_t t = e[j].x, w = e[j].y, count = w & kTpCount;
-            if (t == a.V) continue;
-            float y = x[j];
-            if (count || w & kTpSeen) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
-            if (count) y = __fsub_rn(y, __fadd_rn(__fmul_rn(static_cast<float>(count), freq), pres));
-            if (w & kTpBiased) {
-                float sum = 0.f;
-                if (w & kTpTwice) {  // all that is listed for it, in the list's order
+    for (uint32_t k = tid; k < n; k += kTpListThreads) {
+        const uint2 e = list[k];
+        if (near) far_list[k] = e;
+        if (!(e.y & kTpBiased)) continue;
+        float sum = bias_val[(e.y >> kTpBiasAt & 0x1fff) - 1];
+        if (e.y & kTpTwice) {  // all that is listed for it, in the list's order
+            sum = 0.f;
 #pragma unroll 8
-                    for (int q = 0; q < a.K; ++q)
-                        if (__ldg(tok + q) == t) sum = __fadd_rn(sum, val[q]);
-                } else {
-                    sum = val[(w >> kTpBiasAt & 0x1fff) - 1];
-                }
-                y = __fadd_rn(y, sum);
-            }
-            if (!in[j]) y = -INFINITY;
-            a.p[row0 + t] = y;
-            x[j] = y;
+            for (int q = 0; q < a.K; ++q)
+                if (bias_tok[q] == static_cast<int>(e.x)) sum = __fadd_rn(sum, bias_val[q]);
         }
-        pair = join(pair, pair_of(x, T, c, a.V, [&](int j) { return static_cast<int>(e[j].x); }), T, c);
+        a.adjusted[row * a.listed + k] = sum;
     }
-    pair = join_block<W>(pair, T, c, sh_pair);
-    if (tid == 0) a.stats[static_cast<int64_t>(row) * a.pairs + a.chunks] = pair;
 }
 
-// A thread's tokens as they come; of each group, the bits of those that count here and, in the
-// upper byte, of those that are listed.
-template <bool HALF>
-struct TpTokens {
-    uint4 raw[kTpGroups][2];
-    uint32_t ok[kTpGroups];
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 
-    // FIRST: the bits are put together, and written for the second pass, else read.
-    template <bool FIRST>
-    __device__ __forceinline__ TpTokens(const TpParams& a, int row, int chunk, std::bool_constant<FIRST>)
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// A warp's chunks on their way through a ring of its own in shared memory: no warp waits for
+// another.  FIRST: the first pass, in which a thread has 32 tokens in a row, a word of the
+// masks; the second: four times eight, a sector of what it writes.
+template <bool HALF, bool FIRST>
+struct TpRing {
+    static constexpr int kResident = HALF ? 8 : 6;                  // CTAs an SM
+    static constexpr int kStages = 2;
+    static constexpr int kPieces = HALF ? 4 : 8;                    // of 16 bytes: a thread's 32 tokens
+    static constexpr int kLogits = 32 * kPieces * 16;
+    static constexpr int kStage = kLogits + 3 * kTpWords * 4;       // (allowed, listed, listed ones ahead)
+    static constexpr int kSmem = kTpWarps * kStages * kStage;
+
+    const TpParams& a;
+    const int lane;
+    uint8_t* const smem;
+    TpPlace next;                // to copy
+    int left;
+    const uint32_t *allowed, *marks, *before;  // the row's
+    uint32_t fill = 0, use = 0;  // bytes
+
+    __device__ __forceinline__ TpRing(const TpParams& a_, uint8_t* smem_, int row, const TpPlace& first, int chunks)
+        : a(a_), lane(threadIdx.x & 31), smem(smem_ + threadIdx.x / 32 * (kStages * kStage)), next(first), left(chunks)
     {
-#pragma unroll
-        for (int k = 0; k < kTpGroups; ++k) {
-            const TpGroup t = group_of(a, row, chunk, k);
-            ok[k] = 0;
-            raw[k][0] = raw[k][1] = make_uint4(0, 0, 0, 0);
-            if (!t.in) continue;
-            uint16_t* const bits = a.bits + static_cast<int64_t>(row) * a.chunks * kTpChunk + chunk * kTpChunk + k * kTpThreads + threadIdx.x;
-            if (!FIRST && a.listed) {
-                ok[k] = *bits;
-            } else {
-                const int64_t words = static_cast<int64_t>(row) * a.words;
-                ok[k] = inside(a.V, t.v) & (a.allowed ? bits_of(a.allowed + words, a.words, t.v) : 0xffu);
-                if (a.listed) {
-                    const uint32_t listed = inside(a.V, t.v) & bits_of(a.marks + words, a.words, t.v);
-                    ok[k] &= ~listed;
-                    *bits = static_cast<uint16_t>(listed << 8 | ok[k]);
-                }
-            }
-            if (t.v >= 0 && t.v + 8 <= a.V) {
-                raw[k][0] = static_cast<const uint4*>(a.logits)[t.g * (HALF ? 1 : 2)];
-                if (!HALF) raw[k][1] = static_cast<const uint4*>(a.logits)[t.g * 2 + 1];
-            } else {
-                uint32_t word[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool in = t.v + j >= 0 && t.v + j < a.V;
-                    word[j] = !in ? 0 : HALF ? static_cast<const uint16_t*>(a.logits)[t.g * 8 + j] : static_cast<const uint32_t*>(a.logits)[t.g * 8 + j];
-                }
-                if (HALF) {
-                    raw[k][0] = make_uint4(word[0] | word[1] << 16, word[2] | word[3] << 16, word[4] | word[5] << 16, word[6] | word[7] << 16);
-                } else {
-                    raw[k][0] = make_uint4(word[0], word[1], word[2], word[3]);
-                    raw[k][1] = make_uint4(word[4], word[5], word[6], word[7]);
-                }
-            }
-        }
+        const int64_t words = static_cast<int64_t>(row) * a.words;
+        allowed = a.allowed + words, marks = a.marks + words, before = a.before + words;
+#pragma unroll 1
+        for (int i = 0; i < kStages - 1; ++i) issue();
     }
-    // -infinity for those that are left out
-    __device__ __forceinline__ void logits(float (&x)[kTpGroups * 8]) const
+    // Where a piece lies: in the first pass, which a thread reads in another order than it is
+    // written, so that neither meets a bank twice.
+    __device__ __forceinline__ static uint32_t slot(uint32_t piece) { return FIRST ? piece ^ ((piece >> 3) & (kPieces - 1)) : piece; }
+    // The i-th piece of 16 bytes that this thread copies: the first pass side by side, the second
+    // what the thread takes out itself.
+    __device__ __forceinline__ uint32_t mine(int i) const { return HALF || FIRST ? lane + 32 * i : 2 * lane + (i & 1) + 32 * (i & ~1); }
+
+    __device__ __forceinline__ void copy_words(uint32_t dst, const uint32_t* words) const
     {
+        const int w = (next.v >> 5) + lane;
+        if (static_cast<uint32_t>(w) < static_cast<uint32_t>(a.words)) copy4(dst + lane * 4, words + w);
+        if (lane == 0 && w + 32 < a.words) copy4(dst + 128, words + w + 32);
+    }
+    __device__ __forceinline__ void issue()
+    {
+        if (left > 0) {
+            const uint32_t to = smem_u32(smem) + fill, to_masks = to + kLogits;
+            if (next.whole(a)) {
+                const uint4* from = static_cast<const uint4*>(a.logits) + next.g * (HALF ? 1 : 2);
 #pragma unroll
-        for (int k = 0; k < kTpGroups; ++k) {
-            const uint32_t h[8] = {raw[k][0].x, raw[k][0].y, raw[k][0].z, raw[k][0].w, raw[k][1].x, raw[k][1].y, raw[k][1].z, raw[k][1].w};
+                for (int i = 0; i < kPieces; ++i) copy16(to + slot(mine(i)) * 16, from + mine(i));
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < kPieces; ++i) {
+                    const int piece = mine(i), group = HALF ? piece : piece / 2, v = next.v + group * 8;
+                    const int64_t at = next.g * (HALF ? 1 : 2) + piece;
+                    if (whole8(a, v)) {
+                        copy16(to + slot(piece) * 16, static_cast<const uint4*>(a.logits) + at);
+                    } else {  // a group that a row shares with its neighbour, or none of it
+                        uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t u = HALF ? (j & 1 ? h[j / 2] & 0xffff0000u : h[j / 2] << 16) : h[j];
-                x[8 * k + j] = ok[k] >> j & 1 ? __uint_as_float(u) : -INFINITY;
+                        for (int j = 0; j < (HALF ? 8 : 4); ++j) {
+                            const int t = v + (HALF ? j : (piece & 1) * 4 + j);
+                            if (t < 0 || t >= a.V) continue;
+                            if (HALF) w[j / 2] |= static_cast<uint32_t>(static_cast<const uint16_t*>(a.logits)[at * 8 + j]) << (j & 1) * 16;
+                            else w[j % 4] = static_cast<const uint32_t*>(a.logits)[at * 4 + j];
+                        }
+                        *reinterpret_cast<uint4*>(smem + fill + slot(piece) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
             }
+            if (FIRST) {
+                if (a.allowed) copy_words(to_masks, allowed);
+                if (a.listed) {
+                    copy_words(to_masks + kTpWords * 4, marks);
+                    copy_words(to_masks + kTpWords * 8, before);
+                }
+            } else if (a.listed) {
+                const int64_t item = next.item;
+                if (lane < kTpChunk / 128) copy16(to_masks + lane * 16, a.bits + item * (kTpChunk / 32) + lane * 4);
+                if (lane < 2) copy4(to_masks + kTpWords * 4 + lane * 4, reinterpret_cast<const uint32_t*>(a.part + item) + lane);
+            } else if (a.allowed) {
+                copy_words(to_masks, allowed);
+            }
+            --left;
+            next.step();
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        fill = fill + kStage == kStages * kStage ? 0 : fill + kStage;
+    }
+    // Waits for the next chunk; its stage, which stays as it is until the next call.
+    __device__ __forceinline__ const uint8_t* take()
+    {
+        __syncwarp();  // (all are done with the chunk before, into whose stage the copies go)
+        issue();
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        __syncwarp();
+        const uint8_t* const stage = smem + use;
+        use = use + kStage == kStages * kStage ? 0 : use + kStage;
+        return stage;
+    }
+    // 32 bits from token `at` on of a mask's words, the first of which has token v >> 5 << 5.
+    __device__ __forceinline__ static uint32_t bits_at(const uint8_t* stage, int mask, int v, int at)
+    {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(stage + kLogits) + mask * kTpWords + (at >> 5) - (v >> 5);
+        return __funnelshift_r(w[0], w[1], at);
     }
 };
 
+// x of eight tokens, -infinity for those without a bit.
 template <bool HALF>
-__global__ void __launch_bounds__(kTpThreads) target_stats_kernel(TpParams a)
+__device__ __forceinline__ void values8(const uint4& lo, const uint4& hi, uint32_t ok, float* x)
 {
-    __shared__ float2 sh[kTpThreads / 32];
-    wait_for_stream();
-    const int row = blockIdx.x, chunk = blockIdx.y;  // (rows first: the tokens that lists name are often neighbours)
-    const float T = a.temperature ? a.temperature[row / a.m1] : 1.f, c = steepness(T);
-    float x[kTpGroups * 8];
-    TpTokens<HALF>(a, row, chunk, std::true_type()).logits(x);
-    float2 pair = pair_of(x, T, c, a.V, [&](int k) { return group_of(a, row, chunk, k / 8).v + k % 8; });
-    pair = join_block<kTpThreads / 32>(pair, T, c, sh);
-    if (threadIdx.x == 0) a.stats[static_cast<int64_t>(row) * a.pairs + chunk] = pair;
-}
-
-template <bool HALF>
-__global__ void __launch_bounds__(kTpThreads) target_write_kernel(TpParams a)
-{
-    __shared__ float2 sh_total;
-    wait_for_stream();
-    const int row = a.B * a.m1 - 1 - blockIdx.x, chunk = a.chunks - 1 - blockIdx.y;  // what was read last comes first
-    const float T = a.temperature ? a.temperature[row / a.m1] : 1.f, c = steepness(T);
-    const TpTokens<HALF> tokens(a, row, chunk, std::false_type());
-    if (threadIdx.x < 32) {
-        float2 pair = nothing(T, a.V);
-        for (int k = threadIdx.x; k < a.pairs; k += 32) pair = join(pair, a.stats[static_cast<int64_t>(row) * a.pairs + k], T, c);
-        pair = join_warp(pair, T, c);
-        if (threadIdx.x == 0) sh_total = pair;
-    }
-    __syncthreads();
-    const float2 total = sh_total;
-    float x[kTpGroups * 8];
-    tokens.logits(x);
+    const uint32_t h[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-    for (int k = 0; k < kTpGroups; ++k) {  // listed tokens, whose adjusted logits lie in p
-        const uint32_t take = tokens.ok[k] >> 8;
-        if (!take) continue;
-        const TpGroup t = group_of(a, row, chunk, k);
-        const float* from = a.p + t.g * 8;
-        if (t.v >= 0 && t.v + 8 <= a.V) {
-            const float4 lo = reinterpret_cast<const float4*>(from)[0], hi = reinterpret_cast<const float4*>(from)[1];
-            const float y[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (take >> j & 1) x[8 * k + j] = y[j];
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (take >> j & 1) x[8 * k + j] = from[j];
-        }
-    }
-    const float mid = total.x == -INFINITY ? 0.f : total.x, sum = total.y;
-    const bool greedy = T == 0.f, poor = sum != sum;  // a NaN is all allowed tokens'
-    const int chosen = __float_as_int(sum);
-    const float scale = sum == 0.f ? 1.f : 1.f / sum;  // (where nothing is left all exponentials are 0)
-    if (greedy) {
-#pragma unroll
-        for (int k = 0; k < kTpGroups * 8; ++k) x[k] = group_of(a, row, chunk, k / 8).v + k % 8 == chosen ? 1.f : 0.f;
-    } else {
-        const uint64_t off = f2_pack(-mid, -mid), by = f2_pack(c, c), to = f2_pack(scale, scale);
-#pragma unroll
-        for (int k = 0; k < kTpGroups * 8; k += 2) {
-            float lo, hi;
-            f2_unpack(f2_mul(f2_add(f2_pack(x[k], x[k + 1]), off), by), lo, hi);
-            f2_unpack(f2_mul(f2_pack(ex2(lo), ex2(hi)), to), x[k], x[k + 1]);
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < kTpGroups; ++k) {
-        const TpGroup t = group_of(a, row, chunk, k);
-        if (!t.in) continue;
-        if (poor) {
-            const uint32_t ok = a.allowed ? bits_of(a.allowed + static_cast<int64_t>(row) * a.words, a.words, t.v) : 0xffu;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[8 * k + j] = ok >> j & 1 ? NAN : 0.f;
-        }
-        float* to = a.p + t.g * 8;
-        if (t.v >= 0 && t.v + 8 <= a.V) {
-            __stcs(reinterpret_cast<float4*>(to), make_float4(x[8 * k], x[8 * k + 1], x[8 * k + 2], x[8 * k + 3]));
-            __stcs(reinterpret_cast<float4*>(to) + 1, make_float4(x[8 * k + 4], x[8 * k + 5], x[8 * k + 6], x[8 * k + 7]));
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (t.v + j >= 0 && t.v + j < a.V) to[j] = x[8 * k + j];
-        }
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t u = HALF ? (j & 1 ? h[j / 2] & 0xffff0000u : h[j / 2] << 16) : h[j];
+        x[j] = ok >> j & 1 ? __uint_as_float(u) : -INFINITY;
     }
 }
 
-int64_t tp_chunks(int V) { return (V / 8 + 2 + kTpChunk - 1) / kTpChunk; }
+// Takes further x of a row into a thread's pair.  token(k): x[k]'s.
+template <int N, typename F>
+__device__ __forceinline__ void add(float2& pair, const float (&x)[N], float T, float c, F token)
+{
+    float top = x[0];
+#pragma unroll
+    for (int k = 1; k < N; k += 2) top = max3f(top, x[k], x[k + 1 < N ? k + 1 : k]);
+    if (T == 0.f) {
+        int best = top > pair.x ? 0x7f7fffff : __float_as_int(pair.y);
+        bool nan = pair.y != pair.y;
+        pair.x = fmaxf(pair.x, top);
+#pragma unroll
+        for (int k = N - 1; k >= 0; --k) {
+            if (x[k] == pair.x && top > -INFINITY) best = min(best, token(k));
+            nan |= x[k] != x[k];
+        }
+        pair.y = nan ? NAN : __int_as_float(best);
+        return;
+    }
+    if (top > pair.x) {
+        pair.y *= ex2((pair.x - top) * c);  // (0 as yet for a first one)
+        pair.x = top;
+    }
+    const float mid = pair.x == -INFINITY ? 0.f : pair.x;
+    if constexpr (N == 1) {
+        pair.y += ex2(__fmul_rn(__fadd_rn(x[0], -mid), c));
+        return;
+    }
+    uint64_t part = f2_pack(0.f, 0.f);
+    const uint64_t off = f2_pack(-mid, -mid), by = f2_pack(c, c);
+    float lo, hi;
+#pragma unroll
+    for (int k = 0; k < N; k += 2) {
+        f2_unpack(f2_mul(f2_add(f2_pack(x[k], x[(k + 1) % N]), off), by), lo, hi);
+        part = f2_add(part, f2_pack(ex2(lo), ex2(hi)));
+    }
+    f2_unpack(part, lo, hi);
+    pair.y += lo + hi;
+}
+
+// A listed token's logit, which is in the stage of the chunk at `at`, adjusted.
+template <bool HALF>
+__device__ __forceinline__ float adjust(const TpParams& a, const TpPlace& at, const uint8_t* stage, uint2 e, float bias, float rep, float freq, float pres)
+{
+    using Ring = TpRing<HALF, true>;
+    const int off = static_cast<int>(e.x) - at.v;
+    const uint8_t* const from = stage + Ring::slot(off / (HALF ? 8 : 4)) * 16;
+    float y = HALF ? __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(from)[off % 8]) << 16)
+                   : reinterpret_cast<const float*>(from)[off % 4];
+    const uint32_t w = e.y, count = w & kTpCount;
+    if (count || w & kTpSeen) y = y > 0.f ? __fdiv_rn(y, rep) : __fmul_rn(y, rep);
+    if (count) y = __fsub_rn(y, __fadd_rn(__fmul_rn(static_cast<float>(count), freq), pres));
+    if (w & kTpBiased) y = __fadd_rn(y, bias);
+    if (a.allowed) {
+        const uint32_t* words = reinterpret_cast<const uint32_t*>(stage + Ring::kLogits) - (at.v >> 5);
+        if (!(words[e.x >> 5] >> (e.x & 31) & 1)) y = -INFINITY;
+    }
+    return y;
+}
+
+template <bool HALF>
+__global__ void __launch_bounds__(kTpThreads, TpRing<HALF, true>::kResident) target_stats_kernel(TpParams a)
+{
+    using Ring = TpRing<HALF, true>;
+    extern __shared__ __align__(16) uint8_t smem_ring[];
+    wait_for_stream();
+    // (rows first: the tokens that lists name are often neighbours, and their chunks take longest)
+    const int lane = threadIdx.x & 31, row = blockIdx.x * kTpWarps + threadIdx.x / 32, chunk0 = blockIdx.y * a.each;
+    if (row >= a.B * a.m1) return;
+    const int b = row / a.m1, chunks = min(a.each, a.chunks - chunk0);
+    TpPlace at(a, row, chunk0);
+    Ring ring(a, smem_ring, row, at, chunks);
+    const float T = a.temperature ? a.temperature[b] : 1.f, c = steepness(T);
+    const float rep = a.penalty ? a.penalty[3 * b] : 1.f, freq = a.penalty ? a.penalty[3 * b + 1] : 0.f,
+                pres = a.penalty ? a.penalty[3 * b + 2] : 0.f;
+    const uint2* const list = a.list + row * a.listed;
+    float2 pair = nothing(T, a.V);  // of this thread's tokens
+#pragma unroll 1
+    for (int i = 0; i < chunks; ++i, at.step()) {
+        const uint8_t* const stage = ring.take();
+        const int v = at.v + 32 * lane;  // this thread's first token
+        uint32_t ok = 0xffffffffu;
+        if (!at.whole(a)) {
+            if (v < 0) ok = 0xffffffffu << -v;
+            if (v + 32 > a.V) ok &= v < a.V ? 0xffffffffu >> (v + 32 - a.V) : 0u;
+        }
+        uint32_t listed = ok, many = 0, first = 0;  // of the row's list, the first that is in the chunk, and how many are
+        uint2 e[kTpTake];
+        if (a.allowed) ok &= Ring::bits_at(stage, 0, at.v, v);
+        if (a.listed) {
+            listed &= Ring::bits_at(stage, 1, at.v, v);
+            ok &= ~listed;
+            const uint32_t* const w = reinterpret_cast<const uint32_t*>(stage + Ring::kLogits) + kTpWords + lane;
+            const uint32_t ahead = v < 0 ? 0 : w[kTpWords] + __popc(w[0] & ((1u << (v & 31)) - 1));
+            a.bits[at.item * (kTpChunk / 32) + lane] = ok;
+            many = __reduce_add_sync(0xffffffffu, __popc(listed)), first = __shfl_sync(0xffffffffu, ahead, 0);
+            if (lane == 0) a.part[at.item] = make_uint2(first, many);
+#pragma unroll
+            for (int j = 0; j < kTpTake; ++j)
+                if (lane + 32 * j < many) e[j] = list[first + lane + 32 * j];
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            float x[16];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t piece = lane * Ring::kPieces + (2 * s + k) * (HALF ? 1 : 2);
+                const uint4 lo = *reinterpret_cast<const uint4*>(stage + Ring::slot(piece) * 16);
+                const uint4 hi = HALF ? lo : *reinterpret_cast<const uint4*>(stage + Ring::slot(piece + 1) * 16);
+                values8<HALF>(lo, hi, ok >> (16 * s + 8 * k), x + 8 * k);
+            }
+            add(pair, x, T, c, [&](int k) { return v + 16 * s + k; });
+        }
+        // the listed tokens, in their order: a thread one of 32
+        float* const adjusted = a.adjusted + row * a.listed + first + lane;
+#pragma unroll 1
+        for (uint32_t i0 = 0; i0 < many; i0 += 32 * kTpTake) {
+            float bias[kTpTake];
+#pragma unroll
+            for (int j = 0; j < kTpTake; ++j) {
+                bias[j] = 0.f;
+                if (i0 + 32 * j + lane < many && e[j].y & kTpBiased) bias[j] = adjusted[i0 + 32 * j];
+            }
+#pragma unroll
+            for (int j = 0; j < kTpTake; ++j) {
+                if (i0 + 32 * j >= many) break;
+                if (i0 + 32 * j + lane < many) {
+                    const float y[1] = {adjust<HALF>(a, at, stage, e[j], bias[j], rep, freq, pres)};
+                    adjusted[i0 + 32 * j] = y[0];
+                    add(pair, y, T, c, [&](int) { return static_cast<int>(e[j].x); });
+                }
+                if (i0 + 32 * (kTpTake + j) + lane < many) e[j] = list[first + i0 + 32 * (kTpTake + j) + lane];
+            }
+        }
+    }
+    pair = join_warp(pair, T, c);
+    if (lane == 0) a.stats[static_cast<int64_t>(row) * a.parts + blockIdx.y] = pair;
+}
+
+template <bool HALF>
+__global__ void __launch_bounds__(kTpThreads, TpRing<HALF, false>::kResident) target_write_kernel(TpParams a)
+{
+    using Ring = TpRing<HALF, false>;
+    extern __shared__ __align__(16) uint8_t smem_ring[];
+    wait_for_stream();
+    // what was read last comes first, but for the first part, as above
+    const int part = blockIdx.y ? a.parts - static_cast<int>(blockIdx.y) : 0;
+    const int lane = threadIdx.x & 31, row = a.B * a.m1 - 1 - static_cast<int>(blockIdx.x * kTpWarps + threadIdx.x / 32), chunk0 = part * a.each;
+    if (row < 0) return;
+    const int chunks = min(a.each, a.chunks - chunk0);
+    TpPlace at(a, row, chunk0);
+    Ring ring(a, smem_ring, row, at, chunks);
+    const float T = a.temperature ? a.temperature[row / a.m1] : 1.f, c = steepness(T);
+    float2 total = nothing(T, a.V);
+    for (int k = lane; k < a.parts; k += 32) total = join(total, a.stats[static_cast<int64_t>(row) * a.parts + k], T, c);
+    total = join_warp(total, T, c);
+    const bool poor = total.y != total.y, special = poor || T == 0.f;  // (a NaN is all allowed tokens')
+    const float scale = total.y == 0.f ? 1.f : 1.f / total.y;          // (where nothing is left all exponentials are 0)
+    const float mid = total.x == -INFINITY ? 0.f : total.x;
+    const uint2* const list = a.list + row * a.listed;
+    const float* const adjusted = a.adjusted + row * a.listed;
+#pragma unroll 1
+    for (int i = 0; i < chunks; ++i, at.step()) {
+        const uint8_t* const stage = ring.take();
+        float* const out = a.p + at.g * 8;
+        const bool all_whole = at.whole(a);
+        // listed tokens of the chunk: their adjusted logits, and what they are
+        uint32_t token = 0, many = 0, first = 0;
+        float logit = 0.f;
+        if (a.listed) {
+            const uint32_t* const part = reinterpret_cast<const uint32_t*>(stage + Ring::kLogits) + kTpWords;
+            first = part[0], many = part[1];
+            if (lane < many) token = list[first + lane].x, logit = adjusted[first + lane];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int v = at.v + 256 * k + 8 * lane;
+            const bool whole = all_whole || whole8(a, v);
+            uint32_t ok;
+            if (a.listed) {
+                ok = (stage + Ring::kLogits + k * 32)[lane];
+            } else {
+                ok = whole ? 0xffu : inside(a.V, v);
+                if (a.allowed) ok &= Ring::bits_at(stage, 0, at.v, v);
+            }
+            const uint4* const from = reinterpret_cast<const uint4*>(stage) + (HALF ? 32 * k + lane : 64 * k + 2 * lane);
+            float x[8];
+            values8<HALF>(from[0], HALF ? from[0] : from[1], ok, x);
+            if (__builtin_expect(special, 0)) {
+                const uint32_t all = !a.allowed || v >= a.V ? 0xffu : bits_of(a.allowed + static_cast<int64_t>(row) * a.words, a.words, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = poor ? (all >> j & 1 ? NAN : 0.f) : v + j == __float_as_int(total.y) ? 1.f : 0.f;
+            } else {
+                const uint64_t off = f2_pack(-mid, -mid), by = f2_pack(c, c), mul = f2_pack(scale, scale);
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    float lo, hi;
+                    f2_unpack(f2_mul(f2_add(f2_pack(x[j], x[j + 1]), off), by), lo, hi);
+                    f2_unpack(f2_mul(f2_pack(ex2(lo), ex2(hi)), mul), x[j], x[j + 1]);
+                }
+            }
+            float* const to = out + 256 * k + 8 * lane;
+            if (whole) {
+                reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
+                reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (v + j >= 0 && v + j < a.V) to[j] = x[j];
+            }
+        }
+        if (many && !special) {  // (a 0 is there now)
+            __syncwarp();
+            float* const to = a.p + static_cast<int64_t>(row) * a.V;
+            const auto prob = [&](float y) { return __fmul_rn(ex2(__fmul_rn(__fadd_rn(y, -mid), c)), scale); };
+            if (lane < many) to[token] = prob(logit);
+#pragma unroll 1
+            for (uint32_t i0 = 32 + lane; i0 < many + lane; i0 += 32 * kTpTake) {  // (where many neighbours are listed)
+                uint32_t t[kTpTake];
+                float y[kTpTake];
+#pragma unroll
+                for (int j = 0; j < kTpTake; ++j) {
+                    const uint32_t i = i0 + 32 * j;
+                    t[j] = i < many ? list[first + i].x : 0;
+                    y[j] = i < many ? adjusted[first + i] : 0.f;
+                }
+#pragma unroll
+                for (int j = 0; j < kTpTake; ++j)
+                    if (i0 + 32 * j < many) to[t[j]] = prob(y[j]);
+            }
+        }
+    }
+}
+
+int64_t tp_chunks(int V) { return (V + 7 + kTpChunk - 1) / kTpChunk; }  // (a row's first may begin 7 tokens early)
 
 // Offsets of the workspace's parts; the last is its size.
 struct TpRoom {
-    size_t marks, bits, far, bytes;
+    size_t marks, before, bits, part, list, adjusted, bytes;
     int64_t listed;
 };
+
+// Chunks of a warp.
+int tp_each(int64_t rows, int V) { return rows * tp_chunks(V) > device_sm_count() * kTpFew ? 2 : 1; }
+
+int64_t tp_parts(int64_t rows, int V) { return (tp_chunks(V) + tp_each(rows, V) - 1) / tp_each(rows, V); }
 
 TpRoom tp_room(int B, int m1, int V, int H, int K)
 {
     const size_t rows = static_cast<size_t>(B) * m1;
     TpRoom r;
     r.listed = std::min<int64_t>(V, static_cast<int64_t>(H) + (m1 - 1) + K);
-    r.marks = round_up(rows * (tp_chunks(V) + 1) * sizeof(float2), 256);
-    r.bits = r.marks + (r.listed ? round_up(rows * ((V + 31) / 32) * 4, 256) : 0);
-    r.far = r.bits + (r.listed ? round_up(rows * tp_chunks(V) * kTpChunk * 2, 256) : 0);
-    r.bytes = r.far + (r.listed > kTpNear ? round_up(rows * r.listed * sizeof(uint2), 256) : 0);
+    r.marks = round_up(rows * tp_parts(rows, V) * sizeof(float2), 256);
+    const size_t words = r.listed ? round_up(rows * ((V + 31) / 32) * 4, 256) : 0;
+    r.before = r.marks + words;
+    r.bits = r.before + words;
+    r.part = r.bits + (r.listed ? round_up(rows * tp_chunks(V) * (kTpChunk / 8), 256) : 0);
+    r.list = r.part + (r.listed ? round_up(rows * tp_chunks(V) * sizeof(uint2), 256) : 0);
+    r.adjusted = r.list + round_up(rows * r.listed * sizeof(uint2), 256);
+    r.bytes = r.adjusted + round_up(rows * r.listed * sizeof(float), 256);
     return r;
 }
 
 int check_probs(int B, int m1, int V, int H, int K)
 {
     if (B < 1 || m1 < 1 || V < 1 || H < 0 || K < 0) return LOGO_ERR_INVALID_ARG;
-    if (V > LOGO_PROBS_MAX_VOCAB || m1 > 1024 || K > 4096 || static_cast<int64_t>(B) * m1 > (1 << 24) ||
+    if (V > LOGO_PROBS_MAX_VOCAB || m1 > 1024 || K > kTpMaxBiases || static_cast<int64_t>(B) * m1 > (1 << 24) ||
         static_cast<int64_t>(B) * H > (1ll << 40))
         return LOGO_ERR_UNSUPPORTED;
     return LOGO_OK;
 }
 
 template <bool HALF>
-int tp_launch(const TpParams& a, cudaStream_t st)
+int tp_launch(TpParams& a, cudaStream_t st)
 {
-    const int lists_smem = (a.words + 3) / 4 * 32 + (a.listed <= kTpNear ? static_cast<int>(a.listed * sizeof(uint2)) : 0);
+    const int lists_smem = (a.words + 3) / 4 * 32 + a.K * 8 + (a.listed <= kTpNear ? static_cast<int>(a.listed * sizeof(uint2)) : 0);
     static OncePerDevice once;
-    if (once([] { return set_smem_limit(target_lists_kernel<HALF>, (LOGO_PROBS_MAX_VOCAB + 127) / 128 * 32 + kTpNear * static_cast<int>(sizeof(uint2))); }) != cudaSuccess)
+    if (once([] {
+            // (the kernels overlap at their ends, and an SM splits its memory anew only when it is idle)
+            const auto all_shared = [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared); };
+            cudaError_t e = all_shared(target_lists_kernel);
+            if (e == cudaSuccess) e = all_shared(target_stats_kernel<HALF>);
+            if (e == cudaSuccess) e = all_shared(target_write_kernel<HALF>);
+            if (e == cudaSuccess) e = set_smem_limit(target_lists_kernel, (LOGO_PROBS_MAX_VOCAB + 127) / 128 * 32 + kTpMaxBiases * 8 + kTpNear * static_cast<int>(sizeof(uint2)));
+            if (e == cudaSuccess) e = set_smem_limit(target_stats_kernel<HALF>, TpRing<HALF, true>::kSmem);
+            return e == cudaSuccess ? set_smem_limit(target_write_kernel<HALF>, TpRing<HALF, false>::kSmem) : e;
+        }) != cudaSuccess)
         return LOGO_ERR_CUDA;
     const unsigned rows = static_cast<unsigned>(a.B) * a.m1;
     cudaLaunchAttribute attr{};
@@ -533,11 +698,12 @@ int tp_launch(const TpParams& a, cudaStream_t st)
         cfg.gridDim = dim3(rows);
         cfg.blockDim = dim3(kTpListThreads);
         cfg.dynamicSmemBytes = lists_smem;
-        if (cudaLaunchKernelEx(&cfg, target_lists_kernel<HALF>, a) != cudaSuccess) return LOGO_ERR_CUDA;
-        cfg.dynamicSmemBytes = 0;
+        if (cudaLaunchKernelEx(&cfg, target_lists_kernel, a) != cudaSuccess) return LOGO_ERR_CUDA;
     }
-    cfg.gridDim = dim3(rows, a.chunks);
+    cfg.gridDim = dim3((rows + kTpWarps - 1) / kTpWarps, static_cast<unsigned>(a.parts));
     cfg.blockDim = dim3(kTpThreads);
+    cfg.dynamicSmemBytes = TpRing<HALF, true>::kSmem;
+    static_assert(TpRing<HALF, true>::kSmem == TpRing<HALF, false>::kSmem, "one size for both passes");
     if (cudaLaunchKernelEx(&cfg, target_stats_kernel<HALF>, a) != cudaSuccess) return LOGO_ERR_CUDA;
     return cudaLaunchKernelEx(&cfg, target_write_kernel<HALF>, a) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }
@@ -575,10 +741,13 @@ extern "C" int logo_target_probs(const void* logits, int logits_bf16, const floa
     a.allowed = reinterpret_cast<const uint32_t*>(allowed), a.p = p;
     a.B = B, a.m1 = m1, a.V = V, a.H = H, a.K = K;
     a.chunks = static_cast<int>(tp_chunks(V)), a.words = (V + 31) / 32;
+    a.each = tp_each(static_cast<int64_t>(B) * m1, V), a.parts = static_cast<int>(tp_parts(static_cast<int64_t>(B) * m1, V));
     a.listed = history || draft || K > 0 ? room.listed : 0;
-    a.pairs = a.chunks + (a.listed > 0);
-    a.stats = reinterpret_cast<float2*>(ws), a.marks = reinterpret_cast<uint32_t*>(ws + room.marks);
-    a.bits = reinterpret_cast<uint16_t*>(ws + room.bits), a.far = reinterpret_cast<uint2*>(ws + room.far);
+    a.stats = reinterpret_cast<float2*>(ws);
+    a.marks = reinterpret_cast<uint32_t*>(ws + room.marks);
+    a.before = reinterpret_cast<uint32_t*>(ws + room.before);
+    a.bits = reinterpret_cast<uint32_t*>(ws + room.bits), a.part = reinterpret_cast<uint2*>(ws + room.part);
+    a.list = reinterpret_cast<uint2*>(ws + room.list), a.adjusted = reinterpret_cast<float*>(ws + room.adjusted);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return logits_bf16 ? tp_launch<true>(a, st) : tp_launch<false>(a, st);
 }
