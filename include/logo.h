@@ -407,7 +407,7 @@ LOGO_API int logo_decode_cache4_attn(const logo_bf16* q, logo_cache4 cache, cons
  *   x) makes p NaN for all of them.
  *   Results are deterministic.  Workspace:
  *   logo_target_probs_workspace_size(...) bytes, one per call in flight: a row's 8 bytes per
- *   4096 tokens, and for lists 3 V / 8 and 8 for each token that they can name.
+ *   1024 tokens, and for lists V / 4 and 12 for each token that they can name.
  *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer, history without hist_len,
  *   n_prompt without history, history or draft without penalty, draft with m1 = 1, or
  *   sizes out of range; LOGO_ERR_UNSUPPORTED for V > LOGO_PROBS_MAX_VOCAB, m1 > 1024,

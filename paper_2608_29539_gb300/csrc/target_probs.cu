@@ -3,24 +3,27 @@
 // p_v = 2^((x_v - max x) log2(e) / T) / sum.
 //
 // HBM bounds it: 2 or 4 bytes read, 1/8 of one for the mask and 4 written per token.  Two
-// streaming passes, the second of which finds most logits in L2 (it goes through the rows
-// backwards): the first leaves a maximum and a sum of exponentials per part of a row, the
-// second takes all of a row's and writes.  (One pass that kept a row in the registers of a
+// streaming passes, a warp 1024 tokens, the second of which finds most logits in L2 (it goes
+// through the rows backwards): the first leaves a maximum and a sum of exponentials a warp,
+// the second joins a row's and writes.  (One pass that kept a row in the registers of a
 // thread-block cluster between its read and its write took 122 us for 240 rows of 131072:
 // clusters follow one another, wait for their slowest CTA and do the lists' work eight
 // times.)  At the HBM rate an SM has little more than an instruction a token to spend, so
-// both passes are laid out to save them: logits come through a ring of a warp's own in shared
-// memory, and a thread of the first has 32 tokens in a row, whose masks are a word.
-// The lists of tokens (history, drafts, biases) are counted ahead of that, a CTA a row.  The
-// first pass leaves listed tokens out of its stretches and then takes each chunk's from the
-// list, a thread one, with their logits from the ring; the second writes their probabilities
-// over the zeros that it left.  Sums do not depend on the order of atomics.
+// both passes are laid out to save them: a warp's logits come to shared memory by
+// asynchronous copies, and a thread of the first pass takes 32 in a row, whose masks are a
+// word (eight at a time, with a byte of the masks: 94 us for 70).  Small CTAs end one by one,
+// so an SM always has copies under way (a warp for several stretches, with a ring: 76 us).
+// The lists of tokens (history, drafts, biases) are counted ahead of that, a CTA a row, 11 us
+// of the 70.  The first pass leaves listed tokens out of its stretches and then takes its
+// part of the list, a thread a token, with their logits from shared memory; the second writes
+// their probabilities over the zeros that it left.  (Adjusted where they are counted, from
+// HBM, and left in p until the second pass: 94 us.)  Sums do not depend on the order of
+// atomics.
 #include <cuda_runtime.h>
 
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <type_traits>
 
 #include "host_common.h"
 #include "sm100.cuh"
@@ -28,10 +31,9 @@
 namespace logo {
 namespace {
 
-constexpr int kTpThreads = 128, kTpWarps = kTpThreads / 32;
+constexpr int kTpThreads = 64, kTpWarps = kTpThreads / 32;
 constexpr int kTpChunk = 1024;                             // tokens of a warp at a time
 constexpr int kTpWords = 36;                               // room for the 33 words of a bit a token that they are in
-constexpr int kTpFew = 32;                                 // chunks an SM, up to which a warp takes one, else two
 constexpr int kTpListThreads = 512;
 constexpr int kTpAt = 4;                                   // list entries in flight per thread
 constexpr int kTpMaxBiases = 4096;
@@ -50,18 +52,15 @@ struct TpParams {
     float* p;
     int B, m1, V, H, K;
     int chunks;         // of a row
-    int each, parts;    // chunks of a warp: a part of a row; parts of a row
     int words;          // of a bit a token: ceil(V / 32)
     int64_t listed;     // room for listed tokens a row (0: no lists)
-    float2* stats;      // [rows][parts] (maximum, sum)
-    uint32_t *marks, *before;  // [rows][words]: a bit a listed token; how many are ahead of a word's
+    float2* stats;      // [rows][chunks] (maximum, sum)
+    uint32_t* marks;    // [rows][words]: a bit a listed token
     uint32_t* bits;     // [rows * chunks][kTpChunk / 32]: a bit a token that counts in the passes
-    uint2* part;        // [rows * chunks]: of the row's list, the first that is in the chunk, and how many are
+    uint2* part;        // [rows * chunks]: of the row's list the first that is in the chunk, and how many are
     uint2* list;        // [rows][listed]: listed tokens, ascending, with their words
     float* adjusted;    // [rows][listed]: their biases, then their adjusted logits
 };
-
-
 
 __device__ __forceinline__ float ex2(float x) { return ex2_approx(x); }
 
@@ -153,7 +152,6 @@ struct TpPlace {
         g = e0 / 8 + chunk * (kTpChunk / 8);
         v = chunk * kTpChunk - static_cast<int>(e0 & 7);
     }
-    __device__ __forceinline__ void step() { ++item, g += kTpChunk / 8, v += kTpChunk; }
     __device__ __forceinline__ bool whole(const TpParams& a) const { return v >= 0 && v + kTpChunk <= a.V; }
 };
 
@@ -232,12 +230,15 @@ __global__ void __launch_bounds__(kTpListThreads) target_lists_kernel(TpParams a
     uint2* const list = near ? reinterpret_cast<uint2*>(bias_val + a.K) : far_list;
     for (uint32_t k = tid; k < n; k += kTpListThreads) list[k] = make_uint2(0, 0);
     __syncthreads();
-    for (int w = tid; w < a.words; w += kTpListThreads) {
-        a.marks[static_cast<int64_t>(row) * a.words + w] = bits[w];
-        a.before[static_cast<int64_t>(row) * a.words + w] = before[w];
+    for (int w = tid; w < a.words; w += kTpListThreads) a.marks[static_cast<int64_t>(row) * a.words + w] = bits[w];
+    const auto ahead = [&](uint32_t t) { return before[t / 32] + __popc(bits[t / 32] & ((1u << (t & 31)) - 1)); };
+    for (int k = tid; k < a.chunks; k += kTpListThreads) {
+        const int v = TpPlace(a, row, k).v, end = v + kTpChunk;
+        const uint32_t first = v <= 0 ? 0 : v < a.V ? ahead(v) : n;
+        a.part[static_cast<int64_t>(row) * a.chunks + k] = make_uint2(first, (end < a.V ? ahead(end) : n) - first);
     }
     const auto place = [&](uint32_t t) {
-        uint2* const to = list + before[t / 32] + __popc(bits[t / 32] & ((1u << (t & 31)) - 1));
+        uint2* const to = list + ahead(t);
         to->x = t;  // (the same from all entries)
         return &to->y;
     };
@@ -279,104 +280,74 @@ __device__ __forceinline__ void copy4(uint32_t dst, const void* src)
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// A warp's chunks on their way through a ring of its own in shared memory: no warp waits for
-// another.  FIRST: the first pass, in which a thread has 32 tokens in a row, a word of the
-// masks; the second: four times eight, a sector of what it writes.
+// A warp's chunk in shared memory.  FIRST: the first pass, in which a thread has 32 tokens in
+// a row, a word of the masks; the second: four times eight, a sector of what it writes.
 template <bool HALF, bool FIRST>
-struct TpRing {
-    static constexpr int kResident = HALF ? 8 : 6;                  // CTAs an SM
-    static constexpr int kStages = 2;
+struct TpStage {
+    static constexpr int kResident = 20;                            // CTAs an SM
     static constexpr int kPieces = HALF ? 4 : 8;                    // of 16 bytes: a thread's 32 tokens
     static constexpr int kLogits = 32 * kPieces * 16;
-    static constexpr int kStage = kLogits + 3 * kTpWords * 4;       // (allowed, listed, listed ones ahead)
-    static constexpr int kSmem = kTpWarps * kStages * kStage;
+    static constexpr int kMask = kTpWords * 4;
+    static constexpr int kBytes = kLogits + 2 * kMask;              // (allowed, listed)
+    static constexpr int kSmem = kTpWarps * kBytes;
 
-    const TpParams& a;
-    const int lane;
-    uint8_t* const smem;
-    TpPlace next;                // to copy
-    int left;
-    const uint32_t *allowed, *marks, *before;  // the row's
-    uint32_t fill = 0, use = 0;  // bytes
-
-    __device__ __forceinline__ TpRing(const TpParams& a_, uint8_t* smem_, int row, const TpPlace& first, int chunks)
-        : a(a_), lane(threadIdx.x & 31), smem(smem_ + threadIdx.x / 32 * (kStages * kStage)), next(first), left(chunks)
-    {
-        const int64_t words = static_cast<int64_t>(row) * a.words;
-        allowed = a.allowed + words, marks = a.marks + words, before = a.before + words;
-#pragma unroll 1
-        for (int i = 0; i < kStages - 1; ++i) issue();
-    }
     // Where a piece lies: in the first pass, which a thread reads in another order than it is
     // written, so that neither meets a bank twice.
     __device__ __forceinline__ static uint32_t slot(uint32_t piece) { return FIRST ? piece ^ ((piece >> 3) & (kPieces - 1)) : piece; }
-    // The i-th piece of 16 bytes that this thread copies: the first pass side by side, the second
-    // what the thread takes out itself.
-    __device__ __forceinline__ uint32_t mine(int i) const { return HALF || FIRST ? lane + 32 * i : 2 * lane + (i & 1) + 32 * (i & ~1); }
+    // The i-th piece that a thread copies: in the first pass they lie side by side, in the second
+    // it is what the thread takes out itself.
+    __device__ __forceinline__ static uint32_t mine(int lane, int i) { return HALF || FIRST ? lane + 32 * i : 2 * lane + (i & 1) + 32 * (i & ~1); }
 
-    __device__ __forceinline__ void copy_words(uint32_t dst, const uint32_t* words) const
+    // A mask's words of the chunk.
+    __device__ __forceinline__ static void copy_words(const TpParams& a, int lane, uint32_t to, const uint32_t* row, int v)
     {
-        const int w = (next.v >> 5) + lane;
-        if (static_cast<uint32_t>(w) < static_cast<uint32_t>(a.words)) copy4(dst + lane * 4, words + w);
-        if (lane == 0 && w + 32 < a.words) copy4(dst + 128, words + w + 32);
+        const int w = (v >> 5) + lane;
+        if (static_cast<uint32_t>(w) < static_cast<uint32_t>(a.words)) copy4(to + lane * 4, row + w);
+        if (lane == 0 && w + 32 < a.words) copy4(to + 128, row + w + 32);
     }
-    __device__ __forceinline__ void issue()
+    __device__ __forceinline__ static void fill(const TpParams& a, uint8_t* stage, int row, const TpPlace& at)
     {
-        if (left > 0) {
-            const uint32_t to = smem_u32(smem) + fill, to_masks = to + kLogits;
-            if (next.whole(a)) {
-                const uint4* from = static_cast<const uint4*>(a.logits) + next.g * (HALF ? 1 : 2);
+        const int lane = threadIdx.x & 31;
+        const uint32_t to = smem_u32(stage);
+        if (at.whole(a)) {
+            const uint4* from = static_cast<const uint4*>(a.logits) + at.g * (HALF ? 1 : 2);
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i) copy16(to + slot(mine(i)) * 16, from + mine(i));
-            } else {
+            for (int i = 0; i < kPieces; ++i) copy16(to + slot(mine(lane, i)) * 16, from + mine(lane, i));
+        } else {
 #pragma unroll 1
-                for (int i = 0; i < kPieces; ++i) {
-                    const int piece = mine(i), group = HALF ? piece : piece / 2, v = next.v + group * 8;
-                    const int64_t at = next.g * (HALF ? 1 : 2) + piece;
-                    if (whole8(a, v)) {
-                        copy16(to + slot(piece) * 16, static_cast<const uint4*>(a.logits) + at);
-                    } else {  // a group that a row shares with its neighbour, or none of it
-                        uint32_t w[4] = {0, 0, 0, 0};
+            for (int i = 0; i < kPieces; ++i) {
+                const int piece = mine(lane, i), v = at.v + (HALF ? piece : piece / 2) * 8;
+                const int64_t from = at.g * (HALF ? 1 : 2) + piece;
+                if (whole8(a, v)) {
+                    copy16(to + slot(piece) * 16, static_cast<const uint4*>(a.logits) + from);
+                } else {  // a group that a row shares with its neighbour, or none of it
+                    uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-                        for (int j = 0; j < (HALF ? 8 : 4); ++j) {
-                            const int t = v + (HALF ? j : (piece & 1) * 4 + j);
-                            if (t < 0 || t >= a.V) continue;
-                            if (HALF) w[j / 2] |= static_cast<uint32_t>(static_cast<const uint16_t*>(a.logits)[at * 8 + j]) << (j & 1) * 16;
-                            else w[j % 4] = static_cast<const uint32_t*>(a.logits)[at * 4 + j];
-                        }
-                        *reinterpret_cast<uint4*>(smem + fill + slot(piece) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int j = 0; j < (HALF ? 8 : 4); ++j) {
+                        const int t = v + (HALF ? j : (piece & 1) * 4 + j);
+                        if (t < 0 || t >= a.V) continue;
+                        if (HALF) w[j / 2] |= static_cast<uint32_t>(static_cast<const uint16_t*>(a.logits)[from * 8 + j]) << (j & 1) * 16;
+                        else w[j % 4] = static_cast<const uint32_t*>(a.logits)[from * 4 + j];
                     }
+                    *reinterpret_cast<uint4*>(stage + slot(piece) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
-            if (FIRST) {
-                if (a.allowed) copy_words(to_masks, allowed);
-                if (a.listed) {
-                    copy_words(to_masks + kTpWords * 4, marks);
-                    copy_words(to_masks + kTpWords * 8, before);
-                }
-            } else if (a.listed) {
-                const int64_t item = next.item;
-                if (lane < kTpChunk / 128) copy16(to_masks + lane * 16, a.bits + item * (kTpChunk / 32) + lane * 4);
-                if (lane < 2) copy4(to_masks + kTpWords * 4 + lane * 4, reinterpret_cast<const uint32_t*>(a.part + item) + lane);
-            } else if (a.allowed) {
-                copy_words(to_masks, allowed);
-            }
-            --left;
-            next.step();
+        }
+        const int64_t words = static_cast<int64_t>(row) * a.words;
+        if (FIRST) {
+            if (a.allowed) copy_words(a, lane, to + kLogits, a.allowed + words, at.v);
+            if (a.listed) copy_words(a, lane, to + kLogits + kMask, a.marks + words, at.v);
+        } else if (a.listed) {
+            if (lane < kTpChunk / 128) copy16(to + kLogits + lane * 16, a.bits + at.item * (kTpChunk / 32) + lane * 4);
+        } else if (a.allowed) {
+            copy_words(a, lane, to + kLogits, a.allowed + words, at.v);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-        fill = fill + kStage == kStages * kStage ? 0 : fill + kStage;
     }
-    // Waits for the next chunk; its stage, which stays as it is until the next call.
-    __device__ __forceinline__ const uint8_t* take()
+    __device__ __forceinline__ static void wait()
     {
-        __syncwarp();  // (all are done with the chunk before, into whose stage the copies go)
-        issue();
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();
-        const uint8_t* const stage = smem + use;
-        use = use + kStage == kStages * kStage ? 0 : use + kStage;
-        return stage;
     }
     // 32 bits from token `at` on of a mask's words, the first of which has token v >> 5 << 5.
     __device__ __forceinline__ static uint32_t bits_at(const uint8_t* stage, int mask, int v, int at)
@@ -442,9 +413,9 @@ __device__ __forceinline__ void add(float2& pair, const float (&x)[N], float T, 
 template <bool HALF>
 __device__ __forceinline__ float adjust(const TpParams& a, const TpPlace& at, const uint8_t* stage, uint2 e, float bias, float rep, float freq, float pres)
 {
-    using Ring = TpRing<HALF, true>;
+    using Stage = TpStage<HALF, true>;
     const int off = static_cast<int>(e.x) - at.v;
-    const uint8_t* const from = stage + Ring::slot(off / (HALF ? 8 : 4)) * 16;
+    const uint8_t* const from = stage + Stage::slot(off / (HALF ? 8 : 4)) * 16;
     float y = HALF ? __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(from)[off % 8]) << 16)
                    : reinterpret_cast<const float*>(from)[off % 4];
     const uint32_t w = e.y, count = w & kTpCount;
@@ -452,182 +423,188 @@ __device__ __forceinline__ float adjust(const TpParams& a, const TpPlace& at, co
     if (count) y = __fsub_rn(y, __fadd_rn(__fmul_rn(static_cast<float>(count), freq), pres));
     if (w & kTpBiased) y = __fadd_rn(y, bias);
     if (a.allowed) {
-        const uint32_t* words = reinterpret_cast<const uint32_t*>(stage + Ring::kLogits) - (at.v >> 5);
+        const uint32_t* words = reinterpret_cast<const uint32_t*>(stage + Stage::kLogits) - (at.v >> 5);
         if (!(words[e.x >> 5] >> (e.x & 31) & 1)) y = -INFINITY;
     }
     return y;
 }
 
 template <bool HALF>
-__global__ void __launch_bounds__(kTpThreads, TpRing<HALF, true>::kResident) target_stats_kernel(TpParams a)
+__global__ void __launch_bounds__(kTpThreads, TpStage<HALF, true>::kResident) target_stats_kernel(TpParams a)
 {
-    using Ring = TpRing<HALF, true>;
-    extern __shared__ __align__(16) uint8_t smem_ring[];
+    using Stage = TpStage<HALF, true>;
+    extern __shared__ __align__(16) uint8_t smem_stage[];
     wait_for_stream();
     // (rows first: the tokens that lists name are often neighbours, and their chunks take longest)
-    const int lane = threadIdx.x & 31, row = blockIdx.x * kTpWarps + threadIdx.x / 32, chunk0 = blockIdx.y * a.each;
+    const int lane = threadIdx.x & 31, row = blockIdx.x * kTpWarps + threadIdx.x / 32, chunk = blockIdx.y;
     if (row >= a.B * a.m1) return;
-    const int b = row / a.m1, chunks = min(a.each, a.chunks - chunk0);
-    TpPlace at(a, row, chunk0);
-    Ring ring(a, smem_ring, row, at, chunks);
+    const int b = row / a.m1;
+    const TpPlace at(a, row, chunk);
+    uint8_t* const stage = smem_stage + threadIdx.x / 32 * Stage::kBytes;
+    Stage::fill(a, stage, row, at);
     const float T = a.temperature ? a.temperature[b] : 1.f, c = steepness(T);
     const float rep = a.penalty ? a.penalty[3 * b] : 1.f, freq = a.penalty ? a.penalty[3 * b + 1] : 0.f,
                 pres = a.penalty ? a.penalty[3 * b + 2] : 0.f;
+    // of the row's listed tokens the first that is in the chunk, how many are, and this thread's
+    uint32_t first = 0, many = 0;
+    uint2 e[kTpTake];
     const uint2* const list = a.list + row * a.listed;
+    if (a.listed) {
+        const uint2 part = a.part[at.item];
+        first = part.x, many = part.y;
+#pragma unroll
+        for (int j = 0; j < kTpTake; ++j)
+            if (lane + 32 * j < many) e[j] = list[first + lane + 32 * j];
+    }
     float2 pair = nothing(T, a.V);  // of this thread's tokens
+    Stage::wait();
+    const int v = at.v + 32 * lane;  // this thread's first token
+    uint32_t ok = 0xffffffffu;
+    if (!at.whole(a)) {
+        if (v < 0) ok = 0xffffffffu << -v;
+        if (v + 32 > a.V) ok &= v < a.V ? 0xffffffffu >> (v + 32 - a.V) : 0u;
+    }
+    uint32_t listed = ok;
+    if (a.allowed) ok &= Stage::bits_at(stage, 0, at.v, v);
+    if (a.listed) {
+        listed &= Stage::bits_at(stage, 1, at.v, v);
+        ok &= ~listed;
+        a.bits[at.item * (kTpChunk / 32) + lane] = ok;
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        float x[16];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint32_t piece = lane * Stage::kPieces + (2 * s + k) * (HALF ? 1 : 2);
+            const uint4 lo = *reinterpret_cast<const uint4*>(stage + Stage::slot(piece) * 16);
+            const uint4 hi = HALF ? lo : *reinterpret_cast<const uint4*>(stage + Stage::slot(piece + 1) * 16);
+            values8<HALF>(lo, hi, ok >> (16 * s + 8 * k), x + 8 * k);
+        }
+        add(pair, x, T, c, [&](int k) { return v + 16 * s + k; });
+    }
+    // the listed tokens, in their order: a thread one of 32
+    float* const adjusted = a.adjusted + row * a.listed + first + lane;
 #pragma unroll 1
-    for (int i = 0; i < chunks; ++i, at.step()) {
-        const uint8_t* const stage = ring.take();
-        const int v = at.v + 32 * lane;  // this thread's first token
-        uint32_t ok = 0xffffffffu;
-        if (!at.whole(a)) {
-            if (v < 0) ok = 0xffffffffu << -v;
-            if (v + 32 > a.V) ok &= v < a.V ? 0xffffffffu >> (v + 32 - a.V) : 0u;
-        }
-        uint32_t listed = ok, many = 0, first = 0;  // of the row's list, the first that is in the chunk, and how many are
-        uint2 e[kTpTake];
-        if (a.allowed) ok &= Ring::bits_at(stage, 0, at.v, v);
-        if (a.listed) {
-            listed &= Ring::bits_at(stage, 1, at.v, v);
-            ok &= ~listed;
-            const uint32_t* const w = reinterpret_cast<const uint32_t*>(stage + Ring::kLogits) + kTpWords + lane;
-            const uint32_t ahead = v < 0 ? 0 : w[kTpWords] + __popc(w[0] & ((1u << (v & 31)) - 1));
-            a.bits[at.item * (kTpChunk / 32) + lane] = ok;
-            many = __reduce_add_sync(0xffffffffu, __popc(listed)), first = __shfl_sync(0xffffffffu, ahead, 0);
-            if (lane == 0) a.part[at.item] = make_uint2(first, many);
+    for (uint32_t i0 = 0; i0 < many; i0 += 32 * kTpTake) {
+        float bias[kTpTake];
 #pragma unroll
-            for (int j = 0; j < kTpTake; ++j)
-                if (lane + 32 * j < many) e[j] = list[first + lane + 32 * j];
+        for (int j = 0; j < kTpTake; ++j) {
+            bias[j] = 0.f;
+            if (i0 + 32 * j + lane < many && e[j].y & kTpBiased) bias[j] = adjusted[i0 + 32 * j];
         }
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            float x[16];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint32_t piece = lane * Ring::kPieces + (2 * s + k) * (HALF ? 1 : 2);
-                const uint4 lo = *reinterpret_cast<const uint4*>(stage + Ring::slot(piece) * 16);
-                const uint4 hi = HALF ? lo : *reinterpret_cast<const uint4*>(stage + Ring::slot(piece + 1) * 16);
-                values8<HALF>(lo, hi, ok >> (16 * s + 8 * k), x + 8 * k);
+        for (int j = 0; j < kTpTake; ++j) {
+            if (i0 + 32 * j >= many) break;
+            if (i0 + 32 * j + lane < many) {
+                const float y[1] = {adjust<HALF>(a, at, stage, e[j], bias[j], rep, freq, pres)};
+                adjusted[i0 + 32 * j] = y[0];
+                add(pair, y, T, c, [&](int) { return static_cast<int>(e[j].x); });
             }
-            add(pair, x, T, c, [&](int k) { return v + 16 * s + k; });
-        }
-        // the listed tokens, in their order: a thread one of 32
-        float* const adjusted = a.adjusted + row * a.listed + first + lane;
-#pragma unroll 1
-        for (uint32_t i0 = 0; i0 < many; i0 += 32 * kTpTake) {
-            float bias[kTpTake];
-#pragma unroll
-            for (int j = 0; j < kTpTake; ++j) {
-                bias[j] = 0.f;
-                if (i0 + 32 * j + lane < many && e[j].y & kTpBiased) bias[j] = adjusted[i0 + 32 * j];
-            }
-#pragma unroll
-            for (int j = 0; j < kTpTake; ++j) {
-                if (i0 + 32 * j >= many) break;
-                if (i0 + 32 * j + lane < many) {
-                    const float y[1] = {adjust<HALF>(a, at, stage, e[j], bias[j], rep, freq, pres)};
-                    adjusted[i0 + 32 * j] = y[0];
-                    add(pair, y, T, c, [&](int) { return static_cast<int>(e[j].x); });
-                }
-                if (i0 + 32 * (kTpTake + j) + lane < many) e[j] = list[first + i0 + 32 * (kTpTake + j) + lane];
-            }
+            if (i0 + 32 * (kTpTake + j) + lane < many) e[j] = list[first + i0 + 32 * (kTpTake + j) + lane];
         }
     }
     pair = join_warp(pair, T, c);
-    if (lane == 0) a.stats[static_cast<int64_t>(row) * a.parts + blockIdx.y] = pair;
+    if (lane == 0) a.stats[at.item] = pair;
 }
 
 template <bool HALF>
-__global__ void __launch_bounds__(kTpThreads, TpRing<HALF, false>::kResident) target_write_kernel(TpParams a)
+__global__ void __launch_bounds__(kTpThreads, TpStage<HALF, false>::kResident) target_write_kernel(TpParams a)
 {
-    using Ring = TpRing<HALF, false>;
-    extern __shared__ __align__(16) uint8_t smem_ring[];
+    using Stage = TpStage<HALF, false>;
+    extern __shared__ __align__(16) uint8_t smem_stage[];
     wait_for_stream();
-    // what was read last comes first, but for the first part, as above
-    const int part = blockIdx.y ? a.parts - static_cast<int>(blockIdx.y) : 0;
-    const int lane = threadIdx.x & 31, row = a.B * a.m1 - 1 - static_cast<int>(blockIdx.x * kTpWarps + threadIdx.x / 32), chunk0 = part * a.each;
+    // what was read last comes first, but for the first chunks, as above
+    const int lane = threadIdx.x & 31, row = a.B * a.m1 - 1 - static_cast<int>(blockIdx.x * kTpWarps + threadIdx.x / 32),
+              chunk = blockIdx.y ? a.chunks - static_cast<int>(blockIdx.y) : 0;
     if (row < 0) return;
-    const int chunks = min(a.each, a.chunks - chunk0);
-    TpPlace at(a, row, chunk0);
-    Ring ring(a, smem_ring, row, at, chunks);
+    const TpPlace at(a, row, chunk);
+    uint8_t* const stage = smem_stage + threadIdx.x / 32 * Stage::kBytes;
+    Stage::fill(a, stage, row, at);
+    // listed tokens of the chunk, and their adjusted logits
+    uint32_t first = 0, many = 0, token = 0;
+    float logit = 0.f;
+    const uint2* const list = a.list + row * a.listed;
+    const float* const adjusted = a.adjusted + row * a.listed;
+    if (a.listed) {
+        const uint2 part = a.part[at.item];
+        first = part.x, many = part.y;
+        if (lane < many) token = list[first + lane].x, logit = adjusted[first + lane];
+    }
     const float T = a.temperature ? a.temperature[row / a.m1] : 1.f, c = steepness(T);
     float2 total = nothing(T, a.V);
-    for (int k = lane; k < a.parts; k += 32) total = join(total, a.stats[static_cast<int64_t>(row) * a.parts + k], T, c);
+#pragma unroll 1
+    for (int k0 = lane; k0 < a.chunks; k0 += 32 * kTpTake) {
+        float2 q[kTpTake];
+#pragma unroll
+        for (int j = 0; j < kTpTake; ++j)
+            if (k0 + 32 * j < a.chunks) q[j] = a.stats[static_cast<int64_t>(row) * a.chunks + k0 + 32 * j];
+#pragma unroll
+        for (int j = 0; j < kTpTake; ++j)
+            if (k0 + 32 * j < a.chunks) total = join(total, q[j], T, c);
+    }
     total = join_warp(total, T, c);
     const bool poor = total.y != total.y, special = poor || T == 0.f;  // (a NaN is all allowed tokens')
     const float scale = total.y == 0.f ? 1.f : 1.f / total.y;          // (where nothing is left all exponentials are 0)
     const float mid = total.x == -INFINITY ? 0.f : total.x;
-    const uint2* const list = a.list + row * a.listed;
-    const float* const adjusted = a.adjusted + row * a.listed;
-#pragma unroll 1
-    for (int i = 0; i < chunks; ++i, at.step()) {
-        const uint8_t* const stage = ring.take();
-        float* const out = a.p + at.g * 8;
-        const bool all_whole = at.whole(a);
-        // listed tokens of the chunk: their adjusted logits, and what they are
-        uint32_t token = 0, many = 0, first = 0;
-        float logit = 0.f;
+    Stage::wait();
+    float* const out = a.p + at.g * 8;
+    const bool all_whole = at.whole(a);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int v = at.v + 256 * k + 8 * lane;
+        const bool whole = all_whole || whole8(a, v);
+        uint32_t ok;
         if (a.listed) {
-            const uint32_t* const part = reinterpret_cast<const uint32_t*>(stage + Ring::kLogits) + kTpWords;
-            first = part[0], many = part[1];
-            if (lane < many) token = list[first + lane].x, logit = adjusted[first + lane];
+            ok = (stage + Stage::kLogits + k * 32)[lane];
+        } else {
+            ok = whole ? 0xffu : inside(a.V, v);
+            if (a.allowed) ok &= Stage::bits_at(stage, 0, at.v, v);
         }
+        const uint4* const from = reinterpret_cast<const uint4*>(stage) + (HALF ? 32 * k + lane : 64 * k + 2 * lane);
+        float x[8];
+        values8<HALF>(from[0], HALF ? from[0] : from[1], ok, x);
+        if (__builtin_expect(special, 0)) {
+            const uint32_t all = !a.allowed || v >= a.V ? 0xffu : bits_of(a.allowed + static_cast<int64_t>(row) * a.words, a.words, v);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int v = at.v + 256 * k + 8 * lane;
-            const bool whole = all_whole || whole8(a, v);
-            uint32_t ok;
-            if (a.listed) {
-                ok = (stage + Ring::kLogits + k * 32)[lane];
-            } else {
-                ok = whole ? 0xffu : inside(a.V, v);
-                if (a.allowed) ok &= Ring::bits_at(stage, 0, at.v, v);
-            }
-            const uint4* const from = reinterpret_cast<const uint4*>(stage) + (HALF ? 32 * k + lane : 64 * k + 2 * lane);
-            float x[8];
-            values8<HALF>(from[0], HALF ? from[0] : from[1], ok, x);
-            if (__builtin_expect(special, 0)) {
-                const uint32_t all = !a.allowed || v >= a.V ? 0xffu : bits_of(a.allowed + static_cast<int64_t>(row) * a.words, a.words, v);
+            for (int j = 0; j < 8; ++j) x[j] = poor ? (all >> j & 1 ? NAN : 0.f) : v + j == __float_as_int(total.y) ? 1.f : 0.f;
+        } else {
+            const uint64_t off = f2_pack(-mid, -mid), by = f2_pack(c, c), mul = f2_pack(scale, scale);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = poor ? (all >> j & 1 ? NAN : 0.f) : v + j == __float_as_int(total.y) ? 1.f : 0.f;
-            } else {
-                const uint64_t off = f2_pack(-mid, -mid), by = f2_pack(c, c), mul = f2_pack(scale, scale);
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    float lo, hi;
-                    f2_unpack(f2_mul(f2_add(f2_pack(x[j], x[j + 1]), off), by), lo, hi);
-                    f2_unpack(f2_mul(f2_pack(ex2(lo), ex2(hi)), mul), x[j], x[j + 1]);
-                }
-            }
-            float* const to = out + 256 * k + 8 * lane;
-            if (whole) {
-                reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
-                reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (v + j >= 0 && v + j < a.V) to[j] = x[j];
+            for (int j = 0; j < 8; j += 2) {
+                float lo, hi;
+                f2_unpack(f2_mul(f2_add(f2_pack(x[j], x[j + 1]), off), by), lo, hi);
+                f2_unpack(f2_mul(f2_pack(ex2(lo), ex2(hi)), mul), x[j], x[j + 1]);
             }
         }
-        if (many && !special) {  // (a 0 is there now)
-            __syncwarp();
-            float* const to = a.p + static_cast<int64_t>(row) * a.V;
-            const auto prob = [&](float y) { return __fmul_rn(ex2(__fmul_rn(__fadd_rn(y, -mid), c)), scale); };
-            if (lane < many) to[token] = prob(logit);
+        float* const to = out + 256 * k + 8 * lane;
+        if (whole) {
+            reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
+            reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (v + j >= 0 && v + j < a.V) to[j] = x[j];
+        }
+    }
+    if (many && !special) {  // (a 0 is there now)
+        __syncwarp();
+        float* const to = a.p + static_cast<int64_t>(row) * a.V;
+        const auto prob = [&](float y) { return __fmul_rn(ex2(__fmul_rn(__fadd_rn(y, -mid), c)), scale); };
+        if (lane < many) to[token] = prob(logit);
 #pragma unroll 1
-            for (uint32_t i0 = 32 + lane; i0 < many + lane; i0 += 32 * kTpTake) {  // (where many neighbours are listed)
-                uint32_t t[kTpTake];
-                float y[kTpTake];
+        for (uint32_t i0 = 32 + lane; i0 < many + lane; i0 += 32 * kTpTake) {  // (where many neighbours are listed)
+            uint32_t t[kTpTake];
+            float y[kTpTake];
 #pragma unroll
-                for (int j = 0; j < kTpTake; ++j) {
-                    const uint32_t i = i0 + 32 * j;
-                    t[j] = i < many ? list[first + i].x : 0;
-                    y[j] = i < many ? adjusted[first + i] : 0.f;
-                }
-#pragma unroll
-                for (int j = 0; j < kTpTake; ++j)
-                    if (i0 + 32 * j < many) to[t[j]] = prob(y[j]);
+            for (int j = 0; j < kTpTake; ++j) {
+                const uint32_t i = i0 + 32 * j;
+                t[j] = i < many ? list[first + i].x : 0;
+                y[j] = i < many ? adjusted[first + i] : 0.f;
             }
+#pragma unroll
+            for (int j = 0; j < kTpTake; ++j)
+                if (i0 + 32 * j < many) to[t[j]] = prob(y[j]);
         }
     }
 }
@@ -636,24 +613,17 @@ int64_t tp_chunks(int V) { return (V + 7 + kTpChunk - 1) / kTpChunk; }  // (a ro
 
 // Offsets of the workspace's parts; the last is its size.
 struct TpRoom {
-    size_t marks, before, bits, part, list, adjusted, bytes;
+    size_t marks, bits, part, list, adjusted, bytes;
     int64_t listed;
 };
-
-// Chunks of a warp.
-int tp_each(int64_t rows, int V) { return rows * tp_chunks(V) > device_sm_count() * kTpFew ? 2 : 1; }
-
-int64_t tp_parts(int64_t rows, int V) { return (tp_chunks(V) + tp_each(rows, V) - 1) / tp_each(rows, V); }
 
 TpRoom tp_room(int B, int m1, int V, int H, int K)
 {
     const size_t rows = static_cast<size_t>(B) * m1;
     TpRoom r;
     r.listed = std::min<int64_t>(V, static_cast<int64_t>(H) + (m1 - 1) + K);
-    r.marks = round_up(rows * tp_parts(rows, V) * sizeof(float2), 256);
-    const size_t words = r.listed ? round_up(rows * ((V + 31) / 32) * 4, 256) : 0;
-    r.before = r.marks + words;
-    r.bits = r.before + words;
+    r.marks = round_up(rows * tp_chunks(V) * sizeof(float2), 256);
+    r.bits = r.marks + (r.listed ? round_up(rows * ((V + 31) / 32) * 4, 256) : 0);
     r.part = r.bits + (r.listed ? round_up(rows * tp_chunks(V) * (kTpChunk / 8), 256) : 0);
     r.list = r.part + (r.listed ? round_up(rows * tp_chunks(V) * sizeof(uint2), 256) : 0);
     r.adjusted = r.list + round_up(rows * r.listed * sizeof(uint2), 256);
@@ -682,8 +652,8 @@ int tp_launch(TpParams& a, cudaStream_t st)
             if (e == cudaSuccess) e = all_shared(target_stats_kernel<HALF>);
             if (e == cudaSuccess) e = all_shared(target_write_kernel<HALF>);
             if (e == cudaSuccess) e = set_smem_limit(target_lists_kernel, (LOGO_PROBS_MAX_VOCAB + 127) / 128 * 32 + kTpMaxBiases * 8 + kTpNear * static_cast<int>(sizeof(uint2)));
-            if (e == cudaSuccess) e = set_smem_limit(target_stats_kernel<HALF>, TpRing<HALF, true>::kSmem);
-            return e == cudaSuccess ? set_smem_limit(target_write_kernel<HALF>, TpRing<HALF, false>::kSmem) : e;
+            if (e == cudaSuccess) e = set_smem_limit(target_stats_kernel<HALF>, TpStage<HALF, true>::kSmem);
+            return e == cudaSuccess ? set_smem_limit(target_write_kernel<HALF>, TpStage<HALF, false>::kSmem) : e;
         }) != cudaSuccess)
         return LOGO_ERR_CUDA;
     const unsigned rows = static_cast<unsigned>(a.B) * a.m1;
@@ -700,10 +670,10 @@ int tp_launch(TpParams& a, cudaStream_t st)
         cfg.dynamicSmemBytes = lists_smem;
         if (cudaLaunchKernelEx(&cfg, target_lists_kernel, a) != cudaSuccess) return LOGO_ERR_CUDA;
     }
-    cfg.gridDim = dim3((rows + kTpWarps - 1) / kTpWarps, static_cast<unsigned>(a.parts));
+    cfg.gridDim = dim3((rows + kTpWarps - 1) / kTpWarps, static_cast<unsigned>(a.chunks));
     cfg.blockDim = dim3(kTpThreads);
-    cfg.dynamicSmemBytes = TpRing<HALF, true>::kSmem;
-    static_assert(TpRing<HALF, true>::kSmem == TpRing<HALF, false>::kSmem, "one size for both passes");
+    cfg.dynamicSmemBytes = TpStage<HALF, true>::kSmem;
+    static_assert(TpStage<HALF, true>::kSmem == TpStage<HALF, false>::kSmem, "one size for both passes");
     if (cudaLaunchKernelEx(&cfg, target_stats_kernel<HALF>, a) != cudaSuccess) return LOGO_ERR_CUDA;
     return cudaLaunchKernelEx(&cfg, target_write_kernel<HALF>, a) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
 }
@@ -741,11 +711,9 @@ extern "C" int logo_target_probs(const void* logits, int logits_bf16, const floa
     a.allowed = reinterpret_cast<const uint32_t*>(allowed), a.p = p;
     a.B = B, a.m1 = m1, a.V = V, a.H = H, a.K = K;
     a.chunks = static_cast<int>(tp_chunks(V)), a.words = (V + 31) / 32;
-    a.each = tp_each(static_cast<int64_t>(B) * m1, V), a.parts = static_cast<int>(tp_parts(static_cast<int64_t>(B) * m1, V));
     a.listed = history || draft || K > 0 ? room.listed : 0;
     a.stats = reinterpret_cast<float2*>(ws);
     a.marks = reinterpret_cast<uint32_t*>(ws + room.marks);
-    a.before = reinterpret_cast<uint32_t*>(ws + room.before);
     a.bits = reinterpret_cast<uint32_t*>(ws + room.bits), a.part = reinterpret_cast<uint2*>(ws + room.part);
     a.list = reinterpret_cast<uint2*>(ws + room.list), a.adjusted = reinterpret_cast<float*>(ws + room.adjusted);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
