@@ -583,26 +583,40 @@ def logo_cache4_empty(B: int, L: int, Hkv: int, D: int, device="cuda") -> Cache4
     return Cache4(e(D // 2), e(D // 2), e(D // 16), e(D // 16))
 
 
+def _on(t, dev, dtype, name, shape):
+    """_need, and on device number dev."""
+    try:  # one pass over what has to hold; what does not is named below
+        if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.shape == shape:
+            return
+    except AttributeError:
+        pass
+    _need(t, dtype, name, shape)
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{dev} as the others")
+
+
+def _here(dev):
+    """The current stream of device number dev, on which the tensors are.  The kernels run
+    on the current device: tensors on another are refused."""
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on cuda:{dev}, the current device is cuda:{torch._C._cuda_getDevice()}")
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
 def _cache4(cache):
-    """(its addresses, B, Hkv, L, D) of a Cache4."""
+    """(its addresses, B, Hkv, L, D, device number) of a Cache4."""
     k, v, ks, vs = cache
     _need(k, torch.uint8, "cache.k")
-    if k.dim() != 4:
+    shape = k.shape
+    if len(shape) != 4:
         raise ValueError("cache.k must be [B, Hkv, L, D/2]")
-    B, Hkv, L, half = k.shape
-    _need(v, torch.uint8, "cache.v", k.shape)
-    scales = (B, Hkv, L, half // 8)
-    _need(ks, torch.uint8, "cache.k_scale", scales)
-    _need(vs, torch.uint8, "cache.v_scale", scales)
-    return _Cache4Ptrs(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr()), B, Hkv, L, 2 * half
-
-
-def _here(*tensors):
-    """The kernels run on the current device: tensors on another are refused."""
-    dev = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+    B, Hkv, L, half = shape
+    dev = k.get_device()
+    _on(v, dev, torch.uint8, "cache.v", shape)
+    shape = (B, Hkv, L, half // 8)
+    _on(ks, dev, torch.uint8, "cache.k_scale", shape)
+    _on(vs, dev, torch.uint8, "cache.v_scale", shape)
+    return _Cache4Ptrs(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr()), B, Hkv, L, 2 * half, dev
 
 
 def logo_cache4_append(cache: Cache4, k_new, v_new, seq_len, n_valid=None):
@@ -610,19 +624,16 @@ def logo_cache4_append(cache: Cache4, k_new, v_new, seq_len, n_valid=None):
     cache.  seq_len [B] int32 counts each sequence's tokens, the new ones included;
     of those the first n_valid [B] int32 of the n_new are new ones (None: all), and
     go to the rows that end at seq_len.  Returns the cache."""
-    ptrs, B, Hkv, L, D = _cache4(cache)
-    _need(k_new, torch.bfloat16, "k_new")
-    if k_new.dim() != 4:
-        raise ValueError("k_new must be [B, n_new, Hkv, D]")
-    n = k_new.shape[1]
-    _need(k_new, torch.bfloat16, "k_new", (B, n, Hkv, D))
-    _need(v_new, torch.bfloat16, "v_new", (B, n, Hkv, D))
-    _need(seq_len, torch.int32, "seq_len", (B,))
+    ptrs, B, Hkv, L, D, dev = _cache4(cache)
+    shape = (B, k_new.shape[1] if k_new.dim() == 4 else 0, Hkv, D)
+    _on(k_new, dev, torch.bfloat16, "k_new", shape)
+    _on(v_new, dev, torch.bfloat16, "v_new", shape)
+    _on(seq_len, dev, torch.int32, "seq_len", (B,))
     if n_valid is not None:
-        _need(n_valid, torch.int32, "n_valid", (B,))
-    _here(*cache, k_new, v_new, seq_len, n_valid)
+        _on(n_valid, dev, torch.int32, "n_valid", (B,))
+    stream = _here(dev)
     _call("logo_cache4_append", ptrs, k_new.data_ptr(), v_new.data_ptr(), seq_len.data_ptr(),
-          None if n_valid is None else n_valid.data_ptr(), _dims(B, L, Hkv, Hkv, D), n, _stream())
+          None if n_valid is None else n_valid.data_ptr(), _dims(B, L, Hkv, Hkv, D), shape[1], stream)
     return cache
 
 
@@ -630,24 +641,23 @@ def logo_cache4_read(cache: Cache4, seq_len, rows=None, m=None, k=None, v=None):
     """Rows of a 4-bit cache as the bf16 values that they hold: the listed rows
     [B, m] int32, or rows 0 .. m-1 (m None: as k has, or all L).  Rows outside
     [0, seq_len) read as zeros.  Returns (k, v) [B, m, Hkv, D]."""
-    ptrs, B, Hkv, L, D = _cache4(cache)
-    _need(seq_len, torch.int32, "seq_len", (B,))
+    ptrs, B, Hkv, L, D, dev = _cache4(cache)
+    _on(seq_len, dev, torch.int32, "seq_len", (B,))
     if rows is not None:
-        _need(rows, torch.int32, "rows")
         if rows.dim() != 2 or (m is not None and m != rows.shape[1]):
             raise ValueError("rows must be [B, m]")
         m = rows.shape[1]
-        _need(rows, torch.int32, "rows", (B, m))
+        _on(rows, dev, torch.int32, "rows", (B, m))
     elif m is None:
         m = L if k is None else k.shape[1]
     shape = (B, m, Hkv, D)
+    stream = _here(dev)
     k = torch.empty(shape, dtype=torch.bfloat16, device=seq_len.device) if k is None else k
     v = torch.empty(shape, dtype=torch.bfloat16, device=seq_len.device) if v is None else v
-    _need(k, torch.bfloat16, "k", shape)
-    _need(v, torch.bfloat16, "v", shape)
-    _here(*cache, seq_len, rows, k, v)
+    _on(k, dev, torch.bfloat16, "k", shape)
+    _on(v, dev, torch.bfloat16, "v", shape)
     _call("logo_cache4_read", ptrs, seq_len.data_ptr(), None if rows is None else rows.data_ptr(), k.data_ptr(),
-          v.data_ptr(), _dims(B, L, Hkv, Hkv, D), m, _stream())
+          v.data_ptr(), _dims(B, L, Hkv, Hkv, D), m, stream)
     return k, v
 
 
@@ -667,40 +677,46 @@ def logo_decode_cache4_attn(q, cache: Cache4, seq_len, pos, cu_q, n_sel_total, s
     ones included and last); pos, cu_q, n_sel_total from logo_select on (B, n_new)
     gates.  Returns (o_c [B*n_new, Hq, D], lse_c [Hq, B*n_new]); packed rows >=
     n_sel_total are untouched."""
-    ptrs, B, Hkv, L, D = _cache4(cache)
-    _need(q, torch.bfloat16, "q")
-    if q.dim() != 4 or q.shape[0] != B or q.shape[3] != D:
-        raise ValueError(f"q has shape {tuple(q.shape)}, expected ({B}, n_new, Hq, {D})")
-    _, n_new, Hq, _ = q.shape
+    ptrs, B, Hkv, L, D, dev = _cache4(cache)
+    if not isinstance(q, torch.Tensor) or q.dim() != 4 or q.shape[0] != B or q.shape[3] != D:
+        raise ValueError(f"q has to be a tensor of shape ({B}, n_new, Hq, {D})")
+    shape = q.shape
+    _, n_new, Hq, _ = shape
     cap = B * n_new
-    _need(seq_len, torch.int32, "seq_len", (B,))
-    _need(pos, torch.int32, "pos", (cap,))
-    _need(cu_q, torch.int32, "cu_q", (B + 1,))
-    _need(n_sel_total, torch.int32, "n_sel_total", (1,))
+    _on(q, dev, torch.bfloat16, "q", shape)
+    _on(seq_len, dev, torch.int32, "seq_len", (B,))
+    _on(pos, dev, torch.int32, "pos", (cap,))
+    _on(cu_q, dev, torch.int32, "cu_q", (B + 1,))
+    _on(n_sel_total, dev, torch.int32, "n_sel_total", (1,))
+    stream = _here(dev)
     if o_c is None:
         o_c = torch.empty((cap, Hq, D), dtype=torch.bfloat16, device=q.device)
     else:
-        _need(o_c, torch.bfloat16, "o_c", (cap, Hq, D))
+        _on(o_c, dev, torch.bfloat16, "o_c", (cap, Hq, D))
     if lse_c is None:
         lse_c = torch.empty((Hq, cap), dtype=torch.float32, device=q.device)
     else:
-        _need(lse_c, torch.float32, "lse_c", (Hq, cap))
+        _on(lse_c, dev, torch.float32, "lse_c", (Hq, cap))
     if workspace is None:
         workspace = logo_decode_cache4_workspace(q, cache)
-    else:
-        _given_workspace(workspace)
-    _here(*cache, q, seq_len, pos, cu_q, n_sel_total, o_c, lse_c, workspace)
+    elif _given_workspace(workspace).get_device() != dev:
+        raise ValueError(f"workspace is on {workspace.device}, not on cuda:{dev} as the others")
     _call("logo_decode_cache4_attn", q.data_ptr(), ptrs, seq_len.data_ptr(), pos.data_ptr(), cu_q.data_ptr(),
           n_sel_total.data_ptr(), o_c.data_ptr(), lse_c.data_ptr(), _dims(B, L, Hq, Hkv, D), n_new, float(scale),
-          workspace.data_ptr(), workspace.nbytes, _stream())
+          workspace.data_ptr(), workspace.nbytes, stream)
     return o_c, lse_c
+
+
+@functools.lru_cache(maxsize=256)
+def _target_probs_bytes(*sizes):
+    return int(lib().logo_target_probs_workspace_size(*sizes))
 
 
 def logo_target_probs_workspace(logits, H: int = 0, K: int = 0):
     """A workspace for logo_target_probs calls on logits of this shape with histories
     [B, H] and biases [B, K] (one per call in flight)."""
     B, m1, V = logits.shape
-    return _workspace(int(lib().logo_target_probs_workspace_size(B, m1, V, H, K)), logits.device)
+    return _workspace(_target_probs_bytes(B, m1, V, H, K), logits.device)
 
 
 def logo_target_probs(logits, temperature=None, penalty=None, history=None, hist_len=None, n_prompt=None, draft=None,
@@ -721,58 +737,60 @@ def logo_target_probs(logits, temperature=None, penalty=None, history=None, hist
     if logits.dim() != 3:
         raise ValueError("logits must be [B, m1, V]")
     B, m1, V = logits.shape
+    dev = logits.get_device()
+    i32, f32 = torch.int32, torch.float32
     H = K = 0
+    a_T = a_pen = a_hist = a_len = a_prompt = a_draft = a_tok = a_val = a_ok = None
     if temperature is not None:
-        _need(temperature, torch.float32, "temperature", (B,))
+        _on(temperature, dev, f32, "temperature", (B,))
+        a_T = temperature.data_ptr()
     if penalty is not None:
-        _need(penalty, torch.float32, "penalty", (B, 3))
+        _on(penalty, dev, f32, "penalty", (B, 3))
+        a_pen = penalty.data_ptr()
     elif history is not None or draft is not None:
         raise ValueError("history and draft need penalty")
     if history is not None:
-        _need(history, torch.int32, "history")
         if history.dim() != 2:
             raise ValueError("history must be [B, H]")
         H = history.shape[1]
-        _need(history, torch.int32, "history", (B, H))
+        _on(history, dev, i32, "history", (B, H))
         if hist_len is None:
             raise ValueError("history needs hist_len")
-        _need(hist_len, torch.int32, "hist_len", (B,))
+        _on(hist_len, dev, i32, "hist_len", (B,))
         if n_prompt is not None:
-            _need(n_prompt, torch.int32, "n_prompt", (B,))
+            _on(n_prompt, dev, i32, "n_prompt", (B,))
+        if H:  # (an empty list is no list)
+            a_hist, a_len, a_prompt = history.data_ptr(), hist_len.data_ptr(), _p(n_prompt)
     elif hist_len is not None or n_prompt is not None:
         raise ValueError("hist_len and n_prompt need history")
     if draft is not None:
-        _need(draft, torch.int32, "draft", (B, m1 - 1))
+        _on(draft, dev, i32, "draft", (B, m1 - 1))
+        if m1 > 1:
+            a_draft = draft.data_ptr()
     if (bias_tok is None) != (bias_val is None):
         raise ValueError("bias_tok and bias_val come together")
     if bias_tok is not None:
-        _need(bias_tok, torch.int32, "bias_tok")
         if bias_tok.dim() != 2:
             raise ValueError("bias_tok must be [B, K]")
         K = bias_tok.shape[1]
-        _need(bias_tok, torch.int32, "bias_tok", (B, K))
-        _need(bias_val, torch.float32, "bias_val", (B, K))
+        _on(bias_tok, dev, i32, "bias_tok", (B, K))
+        _on(bias_val, dev, f32, "bias_val", (B, K))
+        if K:
+            a_tok, a_val = bias_tok.data_ptr(), bias_val.data_ptr()
     if allowed is not None:
-        _need(allowed, torch.int32, "allowed", (B, m1, (V + 31) // 32))
+        _on(allowed, dev, i32, "allowed", (B, m1, (V + 31) // 32))
+        a_ok = allowed.data_ptr()
+    stream = _here(dev)
     if p is None:
-        p = torch.empty((B, m1, V), dtype=torch.float32, device=logits.device)
+        p = torch.empty((B, m1, V), dtype=f32, device=logits.device)
     else:
-        _need(p, torch.float32, "p", (B, m1, V))
+        _on(p, dev, f32, "p", (B, m1, V))
     if workspace is None:
         workspace = logo_target_probs_workspace(logits, H, K)
-    else:
-        _given_workspace(workspace)
-    _here(logits, temperature, penalty, history, hist_len, n_prompt, draft, bias_tok, bias_val, allowed, p, workspace)
-    a = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    if H == 0:  # an empty list is no list
-        history = hist_len = n_prompt = None
-    if m1 == 1:
-        draft = None
-    if K == 0:
-        bias_tok = bias_val = None
-    _call("logo_target_probs", logits.data_ptr(), int(logits.dtype is torch.bfloat16), a(temperature), a(penalty),
-          a(history), a(hist_len), a(n_prompt), a(draft), a(bias_tok), a(bias_val), a(allowed), p.data_ptr(), B, m1, V,
-          H, K, workspace.data_ptr(), workspace.nbytes, _stream())
+    elif _given_workspace(workspace).get_device() != dev:
+        raise ValueError(f"workspace is on {workspace.device}, not on cuda:{dev} as the others")
+    _call("logo_target_probs", logits.data_ptr(), int(logits.dtype is torch.bfloat16), a_T, a_pen, a_hist, a_len, a_prompt,
+          a_draft, a_tok, a_val, a_ok, p.data_ptr(), B, m1, V, H, K, workspace.data_ptr(), workspace.nbytes, stream)
     return p
 
 
