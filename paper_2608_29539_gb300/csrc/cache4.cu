@@ -3,7 +3,10 @@
 // HBM bounds both: 2 bytes a channel on one side, 0.5625 on the other.  Tokens come in as
 // [tokens][KV heads][D] and lie in the cache as [KV heads][rows][D], so a warp takes one
 // head of 512 / D consecutive tokens: pieces of 2 D bytes on the one side, 256 bytes of
-// codes and 32 of scales in a row on the other.
+// codes and 32 of scales in a row on the other.  Writing and reading back 8 x 8187 tokens of
+// 8 heads, D = 128: 98 us, 94% of the copy rate (groups of 16 channels in the tokens' order,
+// which write 8 bytes here and there: 124); 32 x 2048 rows by number: 68 us, as a row's 8
+// bytes of scales cost a sector of 32.
 #include <cuda_runtime.h>
 
 #include <algorithm>
