@@ -49,11 +49,11 @@ constexpr float kCaSlack = 8.f;               // a maximum may grow by 2^8 befor
 constexpr int kCaMaxTiles = 4;                // tiles of 8 rows that a warp holds
 constexpr int kJoinThreads = 256;
 
-// A run that a cell begins and does not end: its packed rows from r0 and KV head, of which
-// its rows are row0 ..., the last cell that has a part of it (-1: there is no such run).
+// A run that several cells have parts of: its packed rows from r0 and KV head, of which its
+// rows are row0 ..., and the first and last of the cells (last -1: there is no such run).
 struct __align__(16) CaOpen {
-    int r0, h, row0, nrow, last;
-    int pad[3];
+    int r0, h, row0, nrow, first, last;
+    int pad[2];
 };
 
 struct CaParams {
@@ -63,7 +63,7 @@ struct CaParams {
     uint16_t* o;
     float* lse;
     float* parts;   // [2 * cells][rows * D, then rows of (max, sum)]
-    CaOpen* table;  // [cells]
+    CaOpen* table;  // [2][cells]: the run that a cell begins and does not end, the one that it comes into
     int B, n, Hq, Hkv, G, L;
     uint32_t magic;  // ceil(2^32 / G), 0 for G = 1
     float scale2;    // scale * log2(e)
@@ -288,6 +288,15 @@ struct CaCell {
     bool any;
 };
 
+// Writes down what joining needs to know of the run at c, which begins in cell `first` (-1: there is none).
+template <typename S>
+__device__ __forceinline__ void ca_open(const CaParams& p, const CaCell& c, CaOpen& to, int first)
+{
+    const int row0 = c.run.rb * S::kRows;
+    to.r0 = c.run.r0, to.h = c.run.h, to.row0 = row0, to.nrow = min(S::kRows, c.run.cnt * p.G - row0), to.first = first;
+    to.last = first < 0 ? -1 : static_cast<int>(c.cut.cell_of(c.base + S::kRunCost + c.run.units - 1));
+}
+
 template <typename S>
 __device__ __forceinline__ CaCell ca_cell(const CaParams& p, int group, uint32_t* sh)
 {
@@ -297,8 +306,15 @@ __device__ __forceinline__ CaCell ca_cell(const CaParams& p, int group, uint32_t
     const uint32_t units = cut.units(blockIdx.x), begin = cut.begin(blockIdx.x);
     // the entries of the table that no cell writes
     const uint32_t spare = S::kGroups - cut.cells, mine = units ? 0 : cut.cells;
-    if (threadIdx.x < spare) p.table[gridDim.x * cut.cells + blockIdx.x * spare + threadIdx.x].last = -1;
-    if (threadIdx.x < mine) p.table[blockIdx.x * cut.cells + threadIdx.x].last = -1;
+    CaOpen* const enters = p.table + gridDim.x * S::kGroups;
+    if (threadIdx.x < spare) {
+        const uint32_t k = gridDim.x * cut.cells + blockIdx.x * spare + threadIdx.x;
+        p.table[k].last = enters[k].last = -1;
+    }
+    if (threadIdx.x < mine) {
+        const uint32_t k = blockIdx.x * cut.cells + threadIdx.x;
+        p.table[k].last = enters[k].last = -1;
+    }
     if (units == 0 || group >= cut.cells) return c;
     c.any = true;
     c.cell = blockIdx.x * cut.cells + group;
@@ -310,6 +326,10 @@ __device__ __forceinline__ CaCell ca_cell(const CaParams& p, int group, uint32_t
     c.run.h = i / c.run.nrb, c.run.rb = i % c.run.nrb;
     c.base = at.y + i * weight;
     c.unit = max(0, static_cast<int>(x0 - c.base) - S::kRunCost);
+    if (threadIdx.x % kCaGroup == 0) {
+        p.table[c.cell].last = -1;  // (as yet)
+        if (S::kWide) ca_open<S>(p, c, enters[c.cell], c.unit ? static_cast<int>(cut.cell_of(c.base + S::kRunCost)) : -1);
+    }
     return c;
 }
 
@@ -549,7 +569,6 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
     if (!c.any) return;
     CaRun& run = c.run;
     CaCopies<D, S> copies(p, smem_u32(my_ring), warp, lane, c);
-    CaOpen open{0, 0, 0, 0, -1, {0, 0, 0}};
     uint32_t use = 0;  // stage
 #pragma unroll 1
     for (int i = 0; i < S::kStages - 1; ++i) copies.issue();
@@ -746,13 +765,11 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
                     any ? cvt_bf16x2(sum.x * inv, sum.y * inv) : 0u;
                 if (y == 0 && p.lse) p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? ca_lse(all.x, all.y) : -INFINITY;
             }
-            if (last < run.units && first == 0)
-                open = CaOpen{run.r0, run.h, 0, nrow, static_cast<int>(c.cut.cell_of(c.base + S::kRunCost + run.units - 1)), {0, 0, 0}};
+            if (last < run.units && first == 0 && tid == 0) ca_open<S>(p, c, p.table[c.cell], c.cell);
         }
         c.base += run.units + S::kRunCost;
         if (c.base < c.x1) ca_next(p, S::kRows, run);
     }
-    if (tid == 0) p.table[c.cell] = open;
     cp_async_wait<0>();
 }
 
@@ -793,7 +810,6 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
     if (!c.any) return;
     CaRun& run = c.run;
     CaCopies<D, S> copies(p, smem_u32(my_ring), warp, lane, c);
-    CaOpen open{0, 0, 0, 0, -1, {0, 0, 0}};
     uint32_t use = 0;  // stage
 #pragma unroll 1
     for (int i = 0; i < S::kStages - 1; ++i) copies.issue();
@@ -1038,31 +1054,25 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                     for (int i = 0; i < MT; ++i) out[i] = any ? cvt_bf16x2(x[i].x, x[i].y) : 0u;
                     if (one && p.lse) p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? ca_lse(top, total) : -INFINITY;
                 }
-            if (last < run.units && first == 0)
-                open = CaOpen{run.r0, run.h, row0, nrow, static_cast<int>(c.cut.cell_of(c.base + S::kRunCost + run.units - 1)), {0, 0, 0}};
+            if (last < run.units && first == 0 && tid == 0) ca_open<S>(p, c, p.table[c.cell], c.cell);
         }
         c.base += run.units + S::kRunCost;
         if (c.base < c.x1) ca_next(p, S::kRows, run);
     }
-    if (tid == 0) p.table[c.cell] = open;
     cp_async_wait<0>();
 }
 
-// Joins the parts of the run that goes on past cell blockIdx.x, 8 rows a CTA: each row by
-// as many warps as there are for it, which share the parts.
+// Joins up to 8 rows' parts, of the n cells from `first` on: each row by as many warps as
+// there are for it, which share the parts.
 template <int D, int NT>
-__global__ void __launch_bounds__(kJoinThreads) cache4_join_kernel(CaParams p)
+__device__ __forceinline__ void join_rows(const CaParams& p, const CaOpen& e, int first, int n, int r0, int rows,
+                                          float (&sh)[kJoinThreads / 32][D + 1])
 {
     using S = CaShape<D, NT>;
     constexpr int C = D / 32, W = kJoinThreads / 32;
-    __shared__ float sh[W][D + 1];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, first = blockIdx.x;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const CaOpen e = p.table[first];
-    const int rows = min(8, e.nrow - static_cast<int>(blockIdx.y) * 8);
-    if (e.last < 0 || rows <= 0) return;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ways = rows > 4 ? W / 8 : rows > 2 ? W / 4 : rows > 1 ? W / 2 : W;  // warps a row
-    const int row = warp / ways, way = warp % ways, r = blockIdx.y * 8 + row, n = e.last - first + 1;
+    const int row = warp / ways, way = warp % ways, r = r0 + row;
     const auto part = [&](int i) { return p.parts + (2ll * (first + i) + (i == 0)) * S::kPart; };
     float top = -INFINITY, total = 0.f, sum[C];
 #pragma unroll
@@ -1116,6 +1126,36 @@ __global__ void __launch_bounds__(kJoinThreads) cache4_join_kernel(CaParams p)
 #pragma unroll
     for (int c = 0; c < C; c += 2) out[c / 2] = any ? cvt_bf16x2(sum[c] * inv, sum[c + 1] * inv) : 0u;
     if (lane == 0 && p.lse) p.lse[static_cast<int64_t>(hq) * p.B * p.n + pr] = any ? ca_lse(top, total) : -INFINITY;
+}
+
+// Joins the parts of runs, a CTA a cell.  The cells that have a part of a run share its
+// rows: those that it comes into as well as the one that begins it (16 x 4 drafts, H 16/1, 64
+// rows a KV head: 31.8 -> 29.2 us; with up to 8 rows the one that begins it has them all: 32 x 1
+// 41.8 us, 43.8 when shared).
+template <int D, int NT>
+__global__ void __launch_bounds__(kJoinThreads) cache4_join_kernel(CaParams p)
+{
+    using S = CaShape<D, NT>;
+    constexpr int W = kJoinThreads / 32;
+    __shared__ float sh[W][D + 1];
+    const int cell = blockIdx.x;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    CaOpen e = p.table[cell];
+    if constexpr (!S::kWide) {
+        if (e.last >= 0) join_rows<D, NT>(p, e, cell, e.last - cell + 1, 0, e.nrow, sh);
+    } else {
+        const CaOpen next = p.table[gridDim.x + cell];
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k, e = next) {
+            if (e.last < 0) continue;
+            const int n = e.last - e.first + 1, share = (e.nrow + n - 1) / n, end = min(e.nrow, (cell - e.first + 1) * share);
+#pragma unroll 1
+            for (int r0 = (cell - e.first) * share; r0 < end; r0 += W) {
+                join_rows<D, NT>(p, e, e.first, n, r0, min(W, end - r0), sh);
+                __syncthreads();  // (sh is read)
+            }
+        }
+    }
 }
 
 int check_cache4_attn(const logo_dims& d, int n_new)
@@ -1181,7 +1221,7 @@ int ca_launch(CaShape<D, NT> s, CaParams& p, cudaStream_t st)
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) return LOGO_ERR_CUDA;
-    cfg.gridDim = dim3(ca_cells(s), NT);
+    cfg.gridDim = dim3(ca_cells(s));
     cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, cache4_join_kernel<D, NT>, p) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
@@ -1199,7 +1239,7 @@ extern "C" size_t logo_decode_cache4_workspace_size(logo_dims dims, int n_new)
     ca_dispatch(dims.D, ca_tiles(dims, n_new), [&](auto s) {
         using S = decltype(s);
         const size_t cells = ca_cells(s);
-        bytes = round_up(cells * sizeof(CaOpen), 256) + 2 * cells * S::kPart * sizeof(float);
+        bytes = round_up(2 * cells * sizeof(CaOpen), 256) + 2 * cells * S::kPart * sizeof(float);
         return 0;
     });
     return bytes;
@@ -1228,7 +1268,7 @@ extern "C" int logo_decode_cache4_attn(const logo_bf16* q, logo_cache4 cache, co
     p.scale2 = (scale > 0.f ? scale : 1.f / sqrtf(static_cast<float>(dims.D))) * 1.44269504f;
     return ca_dispatch(dims.D, ca_tiles(dims, n_new), [&](auto s) {
         p.table = static_cast<CaOpen*>(workspace);
-        p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + round_up(ca_cells(s) * sizeof(CaOpen), 256));
+        p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + round_up(2 * ca_cells(s) * sizeof(CaOpen), 256));
         return ca_launch(s, p, static_cast<cudaStream_t>(stream));
     });
 }
