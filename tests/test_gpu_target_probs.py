@@ -106,9 +106,11 @@ def test_parts_left_out(drop):
     _check(s, None if "allowed" in drop else ok, _run(s))
 
 
-@pytest.mark.parametrize("B,m1,V,H,K,half", [(1, 2, 30011, 12000, 3, False), (2, 1, 9001, 9500, 0, True)])
+@pytest.mark.parametrize("B,m1,V,H,K,half", [(1, 2, 30011, 12000, 3, False), (2, 1, 9001, 9500, 0, True),
+                                             (1, 1, 278528, 4000, 4096, True), (1, 3, 262147, 4000, 4096, False)])
 def test_long_lists(B, m1, V, H, K, half):
-    """More listed tokens than are counted in shared memory, in place where that can be."""
+    """More listed tokens than are counted in shared memory, and as many as are; in place where
+    that can be."""
     s, ok = _random(B, m1, V, H, K, V + H, half=half)
     _check(s, ok, _run(s))
     if not half:
