@@ -13,6 +13,7 @@
 // asynchronous copies, and a thread of the first pass takes 32 in a row, whose masks are a
 // word (eight at a time, with a byte of the masks: 94 us for 70).  Small CTAs end one by one,
 // so an SM always has copies under way (a warp for several stretches, with a ring: 76 us).
+// Short rows are one CTA's, which does both passes.
 // The lists of tokens (history, drafts, biases) are counted ahead of that, a CTA a row, 11 us
 // of the 70.  The first pass leaves listed tokens out of its stretches and then takes its
 // part of the list, a thread a token, with their logits from shared memory; the second writes
@@ -34,6 +35,7 @@ namespace {
 constexpr int kTpThreads = 64, kTpWarps = kTpThreads / 32;
 constexpr int kTpChunk = 1024;                             // tokens of a warp at a time
 constexpr int kTpWords = 36;                               // room for the 33 words of a bit a token that they are in
+constexpr int kTpRowWarps = 16;                            // chunks of a row up to which one CTA has them all
 constexpr int kTpListThreads = 512;
 constexpr int kTpAt = 4;                                   // list entries in flight per thread
 constexpr int kTpMaxBiases = 4096;
@@ -429,37 +431,43 @@ __device__ __forceinline__ float adjust(const TpParams& a, const TpPlace& at, co
     return y;
 }
 
-template <bool HALF>
-__global__ void __launch_bounds__(kTpThreads, TpStage<HALF, true>::kResident) target_stats_kernel(TpParams a)
-{
-    using Stage = TpStage<HALF, true>;
-    extern __shared__ __align__(16) uint8_t smem_stage[];
-    wait_for_stream();
-    // (rows first: the tokens that lists name are often neighbours, and their chunks take longest)
-    const int lane = threadIdx.x & 31, row = blockIdx.x * kTpWarps + threadIdx.x / 32, chunk = blockIdx.y;
-    if (row >= a.B * a.m1) return;
-    const int b = row / a.m1;
-    const TpPlace at(a, row, chunk);
-    uint8_t* const stage = smem_stage + threadIdx.x / 32 * Stage::kBytes;
-    Stage::fill(a, stage, row, at);
-    const float T = a.temperature ? a.temperature[b] : 1.f, c = steepness(T);
-    const float rep = a.penalty ? a.penalty[3 * b] : 1.f, freq = a.penalty ? a.penalty[3 * b + 1] : 0.f,
-                pres = a.penalty ? a.penalty[3 * b + 2] : 0.f;
-    // of the row's listed tokens the first that is in the chunk, how many are, and this thread's
+// What a chunk's sequence asks for.
+struct TpAsked {
+    float T, c, rep, freq, pres;
+
+    __device__ __forceinline__ TpAsked(const TpParams& a, int row)
+    {
+        const int b = row / a.m1;
+        T = a.temperature ? a.temperature[b] : 1.f, c = steepness(T);
+        rep = a.penalty ? a.penalty[3 * b] : 1.f, freq = a.penalty ? a.penalty[3 * b + 1] : 0.f;
+        pres = a.penalty ? a.penalty[3 * b + 2] : 0.f;
+    }
+};
+
+// Of a row's listed tokens the first that is in a chunk, how many are, and this thread's first few.
+struct TpListed {
     uint32_t first = 0, many = 0;
     uint2 e[kTpTake];
-    const uint2* const list = a.list + row * a.listed;
-    if (a.listed) {
+
+    __device__ __forceinline__ TpListed(const TpParams& a, int row, const TpPlace& at)
+    {
+        if (!a.listed) return;
         const uint2 part = a.part[at.item];
         first = part.x, many = part.y;
 #pragma unroll
         for (int j = 0; j < kTpTake; ++j)
-            if (lane + 32 * j < many) e[j] = list[first + lane + 32 * j];
+            if ((threadIdx.x & 31) + 32 * j < many) e[j] = a.list[row * a.listed + first + (threadIdx.x & 31) + 32 * j];
     }
-    float2 pair = nothing(T, a.V);  // of this thread's tokens
-    Stage::wait();
-    const int v = at.v + 32 * lane;  // this thread's first token
-    uint32_t ok = 0xffffffffu;
+};
+
+// The first pass over a chunk: a thread's pair; ok: which of its 32 tokens count but for listed ones.
+template <bool HALF>
+__device__ __forceinline__ float2 first_pass(const TpParams& a, const uint8_t* stage, int row, const TpPlace& at,
+                                             const TpAsked& q, TpListed& l, uint32_t& ok)
+{
+    using Stage = TpStage<HALF, true>;
+    const int lane = threadIdx.x & 31, v = at.v + 32 * lane;  // this thread's first token
+    ok = 0xffffffffu;
     if (!at.whole(a)) {
         if (v < 0) ok = 0xffffffffu << -v;
         if (v + 32 > a.V) ok &= v < a.V ? 0xffffffffu >> (v + 32 - a.V) : 0u;
@@ -469,8 +477,8 @@ __global__ void __launch_bounds__(kTpThreads, TpStage<HALF, true>::kResident) ta
     if (a.listed) {
         listed &= Stage::bits_at(stage, 1, at.v, v);
         ok &= ~listed;
-        a.bits[at.item * (kTpChunk / 32) + lane] = ok;
     }
+    float2 pair = nothing(q.T, a.V);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         float x[16];
@@ -481,30 +489,127 @@ __global__ void __launch_bounds__(kTpThreads, TpStage<HALF, true>::kResident) ta
             const uint4 hi = HALF ? lo : *reinterpret_cast<const uint4*>(stage + Stage::slot(piece + 1) * 16);
             values8<HALF>(lo, hi, ok >> (16 * s + 8 * k), x + 8 * k);
         }
-        add(pair, x, T, c, [&](int k) { return v + 16 * s + k; });
+        add(pair, x, q.T, q.c, [&](int k) { return v + 16 * s + k; });
     }
     // the listed tokens, in their order: a thread one of 32
-    float* const adjusted = a.adjusted + row * a.listed + first + lane;
+    const uint2* const list = a.list + row * a.listed + l.first + lane;
+    float* const adjusted = a.adjusted + row * a.listed + l.first + lane;
 #pragma unroll 1
-    for (uint32_t i0 = 0; i0 < many; i0 += 32 * kTpTake) {
+    for (uint32_t i0 = 0; i0 < l.many; i0 += 32 * kTpTake) {
         float bias[kTpTake];
 #pragma unroll
         for (int j = 0; j < kTpTake; ++j) {
             bias[j] = 0.f;
-            if (i0 + 32 * j + lane < many && e[j].y & kTpBiased) bias[j] = adjusted[i0 + 32 * j];
+            if (i0 + 32 * j + lane < l.many && l.e[j].y & kTpBiased) bias[j] = adjusted[i0 + 32 * j];
         }
 #pragma unroll
         for (int j = 0; j < kTpTake; ++j) {
-            if (i0 + 32 * j >= many) break;
-            if (i0 + 32 * j + lane < many) {
-                const float y[1] = {adjust<HALF>(a, at, stage, e[j], bias[j], rep, freq, pres)};
+            if (i0 + 32 * j >= l.many) break;
+            if (i0 + 32 * j + lane < l.many) {
+                const float y[1] = {adjust<HALF>(a, at, stage, l.e[j], bias[j], q.rep, q.freq, q.pres)};
                 adjusted[i0 + 32 * j] = y[0];
-                add(pair, y, T, c, [&](int) { return static_cast<int>(e[j].x); });
+                add(pair, y, q.T, q.c, [&](int) { return static_cast<int>(l.e[j].x); });
             }
-            if (i0 + 32 * (kTpTake + j) + lane < many) e[j] = list[first + i0 + 32 * (kTpTake + j) + lane];
+            if (i0 + 32 * (kTpTake + j) + lane < l.many) l.e[j] = list[i0 + 32 * (kTpTake + j)];
         }
     }
-    pair = join_warp(pair, T, c);
+    return pair;
+}
+
+// The second: probabilities from a row's pair.  bits: the stage has, where the masks were, the
+// tokens that count but for listed ones; else there are no lists.
+template <bool HALF, bool FIRST>
+__device__ __forceinline__ void second_pass(const TpParams& a, const uint8_t* stage, int row, const TpPlace& at, float T, float c,
+                                            float2 total, bool bits, uint32_t first, uint32_t many, uint32_t token, float logit)
+{
+    using Stage = TpStage<HALF, FIRST>;
+    const int lane = threadIdx.x & 31;
+    const bool poor = total.y != total.y, special = poor || T == 0.f;  // (a NaN is all allowed tokens')
+    const float scale = total.y == 0.f ? 1.f : 1.f / total.y;          // (where nothing is left all exponentials are 0)
+    const float mid = total.x == -INFINITY ? 0.f : total.x;
+    float* const out = a.p + at.g * 8;
+    const bool all_whole = at.whole(a);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int v = at.v + 256 * k + 8 * lane;
+        const bool whole = all_whole || whole8(a, v);
+        uint32_t ok;
+        if (bits) {
+            ok = (stage + Stage::kLogits + k * 32)[lane];
+        } else {
+            ok = whole ? 0xffu : inside(a.V, v);
+            if (a.allowed) ok &= Stage::bits_at(stage, 0, at.v, v);
+        }
+        const uint32_t piece = HALF ? 32 * k + lane : 64 * k + 2 * lane;
+        const uint4 lo = *reinterpret_cast<const uint4*>(stage + Stage::slot(piece) * 16);
+        const uint4 hi = HALF ? lo : *reinterpret_cast<const uint4*>(stage + Stage::slot(piece + 1) * 16);
+        float x[8];
+        values8<HALF>(lo, hi, ok, x);
+        if (__builtin_expect(special, 0)) {
+            const uint32_t all = !a.allowed || v >= a.V ? 0xffu : bits_of(a.allowed + static_cast<int64_t>(row) * a.words, a.words, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = poor ? (all >> j & 1 ? NAN : 0.f) : v + j == __float_as_int(total.y) ? 1.f : 0.f;
+        } else {
+            const uint64_t off = f2_pack(-mid, -mid), by = f2_pack(c, c), mul = f2_pack(scale, scale);
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                float e0, e1;
+                f2_unpack(f2_mul(f2_add(f2_pack(x[j], x[j + 1]), off), by), e0, e1);
+                f2_unpack(f2_mul(f2_pack(ex2(e0), ex2(e1)), mul), x[j], x[j + 1]);
+            }
+        }
+        float* const to = out + 256 * k + 8 * lane;
+        if (whole) {
+            reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
+            reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (v + j >= 0 && v + j < a.V) to[j] = x[j];
+        }
+    }
+    if (many && !special) {  // (a 0 is there now)
+        __syncwarp();
+        const uint2* const list = a.list + row * a.listed + first;
+        const float* const adjusted = a.adjusted + row * a.listed + first;
+        float* const to = a.p + static_cast<int64_t>(row) * a.V;
+        const auto prob = [&](float y) { return __fmul_rn(ex2(__fmul_rn(__fadd_rn(y, -mid), c)), scale); };
+        if (lane < many) to[token] = prob(logit);
+#pragma unroll 1
+        for (uint32_t i0 = 32 + lane; i0 < many + lane; i0 += 32 * kTpTake) {  // (where many neighbours are listed)
+            uint32_t t[kTpTake];
+            float y[kTpTake];
+#pragma unroll
+            for (int j = 0; j < kTpTake; ++j) {
+                const uint32_t i = i0 + 32 * j;
+                t[j] = i < many ? list[i].x : 0;
+                y[j] = i < many ? adjusted[i] : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < kTpTake; ++j)
+                if (i0 + 32 * j < many) to[t[j]] = prob(y[j]);
+        }
+    }
+}
+
+template <bool HALF>
+__global__ void __launch_bounds__(kTpThreads, TpStage<HALF, true>::kResident) target_stats_kernel(TpParams a)
+{
+    using Stage = TpStage<HALF, true>;
+    extern __shared__ __align__(16) uint8_t smem_stage[];
+    wait_for_stream();
+    // (rows first: the tokens that lists name are often neighbours, and their chunks take longest)
+    const int lane = threadIdx.x & 31, row = blockIdx.x * kTpWarps + threadIdx.x / 32, chunk = blockIdx.y;
+    if (row >= a.B * a.m1) return;
+    const TpPlace at(a, row, chunk);
+    uint8_t* const stage = smem_stage + threadIdx.x / 32 * Stage::kBytes;
+    Stage::fill(a, stage, row, at);
+    const TpAsked q(a, row);
+    TpListed l(a, row, at);
+    Stage::wait();
+    uint32_t ok;
+    const float2 pair = join_warp(first_pass<HALF>(a, stage, row, at, q, l, ok), q.T, q.c);
+    if (a.listed) a.bits[at.item * (kTpChunk / 32) + lane] = ok;
     if (lane == 0) a.stats[at.item] = pair;
 }
 
@@ -524,12 +629,10 @@ __global__ void __launch_bounds__(kTpThreads, TpStage<HALF, false>::kResident) t
     // listed tokens of the chunk, and their adjusted logits
     uint32_t first = 0, many = 0, token = 0;
     float logit = 0.f;
-    const uint2* const list = a.list + row * a.listed;
-    const float* const adjusted = a.adjusted + row * a.listed;
     if (a.listed) {
         const uint2 part = a.part[at.item];
         first = part.x, many = part.y;
-        if (lane < many) token = list[first + lane].x, logit = adjusted[first + lane];
+        if (lane < many) token = a.list[row * a.listed + first + lane].x, logit = a.adjusted[row * a.listed + first + lane];
     }
     const float T = a.temperature ? a.temperature[row / a.m1] : 1.f, c = steepness(T);
     float2 total = nothing(T, a.V);
@@ -544,69 +647,39 @@ __global__ void __launch_bounds__(kTpThreads, TpStage<HALF, false>::kResident) t
             if (k0 + 32 * j < a.chunks) total = join(total, q[j], T, c);
     }
     total = join_warp(total, T, c);
-    const bool poor = total.y != total.y, special = poor || T == 0.f;  // (a NaN is all allowed tokens')
-    const float scale = total.y == 0.f ? 1.f : 1.f / total.y;          // (where nothing is left all exponentials are 0)
-    const float mid = total.x == -INFINITY ? 0.f : total.x;
     Stage::wait();
-    float* const out = a.p + at.g * 8;
-    const bool all_whole = at.whole(a);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int v = at.v + 256 * k + 8 * lane;
-        const bool whole = all_whole || whole8(a, v);
-        uint32_t ok;
-        if (a.listed) {
-            ok = (stage + Stage::kLogits + k * 32)[lane];
-        } else {
-            ok = whole ? 0xffu : inside(a.V, v);
-            if (a.allowed) ok &= Stage::bits_at(stage, 0, at.v, v);
-        }
-        const uint4* const from = reinterpret_cast<const uint4*>(stage) + (HALF ? 32 * k + lane : 64 * k + 2 * lane);
-        float x[8];
-        values8<HALF>(from[0], HALF ? from[0] : from[1], ok, x);
-        if (__builtin_expect(special, 0)) {
-            const uint32_t all = !a.allowed || v >= a.V ? 0xffu : bits_of(a.allowed + static_cast<int64_t>(row) * a.words, a.words, v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = poor ? (all >> j & 1 ? NAN : 0.f) : v + j == __float_as_int(total.y) ? 1.f : 0.f;
-        } else {
-            const uint64_t off = f2_pack(-mid, -mid), by = f2_pack(c, c), mul = f2_pack(scale, scale);
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                float lo, hi;
-                f2_unpack(f2_mul(f2_add(f2_pack(x[j], x[j + 1]), off), by), lo, hi);
-                f2_unpack(f2_mul(f2_pack(ex2(lo), ex2(hi)), mul), x[j], x[j + 1]);
-            }
-        }
-        float* const to = out + 256 * k + 8 * lane;
-        if (whole) {
-            reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
-            reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (v + j >= 0 && v + j < a.V) to[j] = x[j];
-        }
-    }
-    if (many && !special) {  // (a 0 is there now)
-        __syncwarp();
-        float* const to = a.p + static_cast<int64_t>(row) * a.V;
-        const auto prob = [&](float y) { return __fmul_rn(ex2(__fmul_rn(__fadd_rn(y, -mid), c)), scale); };
-        if (lane < many) to[token] = prob(logit);
-#pragma unroll 1
-        for (uint32_t i0 = 32 + lane; i0 < many + lane; i0 += 32 * kTpTake) {  // (where many neighbours are listed)
-            uint32_t t[kTpTake];
-            float y[kTpTake];
-#pragma unroll
-            for (int j = 0; j < kTpTake; ++j) {
-                const uint32_t i = i0 + 32 * j;
-                t[j] = i < many ? list[first + i].x : 0;
-                y[j] = i < many ? adjusted[first + i] : 0.f;
-            }
-#pragma unroll
-            for (int j = 0; j < kTpTake; ++j)
-                if (i0 + 32 * j < many) to[t[j]] = prob(y[j]);
-        }
-    }
+    second_pass<HALF, false>(a, stage, row, at, T, c, total, a.listed != 0, first, many, token, logit);
+}
+
+// Both passes over a row of up to 16 chunks by one CTA, a warp a chunk, which stays in shared
+// memory.  It saves a launch and the second read: 400 rows of 8100, float32, histories of 500
+// 15.9 us (two kernels 21.9), one row of 2000 6.9 (9.6); at 16 chunks they are even (one row of
+// 16300 9.57 and 9.61), beyond that an SM is too slow for a row (32000: 13.1 and 9.6).
+template <bool HALF>
+__global__ void __launch_bounds__(kTpRowWarps * 32) target_row_kernel(TpParams a)
+{
+    using Stage = TpStage<HALF, true>;
+    extern __shared__ __align__(16) uint8_t smem_stage[];
+    __shared__ float2 sh[kTpRowWarps];
+    wait_for_stream();
+    const int lane = threadIdx.x & 31, row = blockIdx.x, chunk = threadIdx.x / 32;
+    const TpPlace at(a, row, chunk);
+    uint8_t* const stage = smem_stage + chunk * Stage::kBytes;
+    Stage::fill(a, stage, row, at);
+    const TpAsked q(a, row);
+    TpListed l(a, row, at);
+    Stage::wait();
+    uint32_t ok;
+    const float2 pair = join_warp(first_pass<HALF>(a, stage, row, at, q, l, ok), q.T, q.c);
+    if (lane == 0) sh[chunk] = pair;
+    __syncthreads();
+    reinterpret_cast<uint32_t*>(stage + Stage::kLogits)[lane] = ok;
+    const float2 total = join_warp(lane < a.chunks ? sh[lane] : nothing(q.T, a.V), q.T, q.c);
+    __syncwarp();
+    uint32_t token = 0;
+    float logit = 0.f;
+    if (lane < l.many) token = a.list[row * a.listed + l.first + lane].x, logit = a.adjusted[row * a.listed + l.first + lane];
+    second_pass<HALF, true>(a, stage, row, at, q.T, q.c, total, true, l.first, l.many, token, logit);
 }
 
 int64_t tp_chunks(int V) { return (V + 7 + kTpChunk - 1) / kTpChunk; }  // (a row's first may begin 7 tokens early)
@@ -652,6 +725,8 @@ int tp_launch(TpParams& a, cudaStream_t st)
             if (e == cudaSuccess) e = all_shared(target_stats_kernel<HALF>);
             if (e == cudaSuccess) e = all_shared(target_write_kernel<HALF>);
             if (e == cudaSuccess) e = set_smem_limit(target_lists_kernel, (LOGO_PROBS_MAX_VOCAB + 127) / 128 * 32 + kTpMaxBiases * 8 + kTpNear * static_cast<int>(sizeof(uint2)));
+            if (e == cudaSuccess) e = all_shared(target_row_kernel<HALF>);
+            if (e == cudaSuccess) e = set_smem_limit(target_row_kernel<HALF>, kTpRowWarps * TpStage<HALF, true>::kBytes);
             if (e == cudaSuccess) e = set_smem_limit(target_stats_kernel<HALF>, TpStage<HALF, true>::kSmem);
             return e == cudaSuccess ? set_smem_limit(target_write_kernel<HALF>, TpStage<HALF, false>::kSmem) : e;
         }) != cudaSuccess)
@@ -669,6 +744,12 @@ int tp_launch(TpParams& a, cudaStream_t st)
         cfg.blockDim = dim3(kTpListThreads);
         cfg.dynamicSmemBytes = lists_smem;
         if (cudaLaunchKernelEx(&cfg, target_lists_kernel, a) != cudaSuccess) return LOGO_ERR_CUDA;
+    }
+    if (a.chunks <= kTpRowWarps) {
+        cfg.gridDim = dim3(rows);
+        cfg.blockDim = dim3(32 * a.chunks);
+        cfg.dynamicSmemBytes = a.chunks * TpStage<HALF, true>::kBytes;
+        return cudaLaunchKernelEx(&cfg, target_row_kernel<HALF>, a) == cudaSuccess ? LOGO_OK : LOGO_ERR_CUDA;
     }
     cfg.gridDim = dim3((rows + kTpWarps - 1) / kTpWarps, static_cast<unsigned>(a.chunks));
     cfg.blockDim = dim3(kTpThreads);

@@ -90,7 +90,8 @@ def _check(s, ok, p):
 @pytest.mark.parametrize("B,m1,V,H,K,half", [
     (1, 1, 1, 3, 1, False), (2, 1, 31, 0, 0, False), (1, 2, 33, 5, 3, True), (3, 4, 1000, 40, 7, True),
     (2, 3, 4099, 700, 30, False), (1, 1, 32000, 300, 0, False), (5, 2, 50021, 2000, 200, True), (1, 8, 131072, 64, 5, True),
-    (1, 1, 262143, 100, 300, False), (1, 1, 278528, 10, 2, True), (40, 1, 2053, 9, 1, False), (2, 300, 257, 50, 3, True)])
+    (1, 1, 262143, 100, 300, False), (1, 1, 278528, 10, 2, True), (40, 1, 2053, 9, 1, False), (2, 300, 257, 50, 3, True),
+    (3, 3, 16377, 90, 9, False), (3, 3, 16379, 90, 9, True)])
 def test_against_the_definition(B, m1, V, H, K, half):
     s, ok = _random(B, m1, V, H, K, V + H, half=half)
     _check(s, ok, _run(s))
@@ -132,8 +133,9 @@ def test_offsets_past_32_bits():
         assert ((p[b] * V - 1).abs() < 1e-4).all()
 
 
-def test_in_place():
-    s, ok = _random(2, 3, 40013, 60, 9, 5)
+@pytest.mark.parametrize("V", [40013, 5003])
+def test_in_place(V):
+    s, ok = _random(2, 3, V, 60, 9, 5)
     x = s["logits"].cuda()
     others = {k: v.cuda() for k, v in s.items() if k != "logits"}
     out = _logo().logo_target_probs(x, **others, p=x)
@@ -141,7 +143,7 @@ def test_in_place():
     _check(s, ok, x)
 
 
-@pytest.mark.parametrize("V", [37, 70001])
+@pytest.mark.parametrize("V", [37, 16379, 70001])
 def test_greedy(V):
     """Ties go to the lowest token, also where a penalty or a bias makes them."""
     s, ok = _random(4, 3, V, 30, 5, 6, half=True, T=[0.0, 0.7, 0.0, 0.0])
@@ -176,8 +178,8 @@ def test_counts_and_sums():
             assert abs(float(q[3]) - want[b][i]) < 1e-5
 
 
-def test_values_that_are_not_finite():
-    V = 3000
+@pytest.mark.parametrize("V", [3000, 20011])
+def test_values_that_are_not_finite(V):
     x = torch.randn((8, 1, V), generator=torch.Generator().manual_seed(1))
     ok = torch.rand((8, 1, V), generator=torch.Generator().manual_seed(2)) < 0.5
     ok[:, :, :20] = True
@@ -201,8 +203,9 @@ def test_values_that_are_not_finite():
         assert np.allclose(np.nan_to_num(p[b, 0]), np.nan_to_num(want), rtol=1e-5, atol=1e-30), b
 
 
-def test_the_same_in_a_graph():
-    s, ok = _random(3, 4, 9001, 100, 10, 8, half=True)
+@pytest.mark.parametrize("V", [9001, 33001])
+def test_the_same_in_a_graph(V):
+    s, ok = _random(3, 4, V, 100, 10, 8, half=True)
     d = {k: v.cuda() for k, v in s.items()}
     logo = _logo()
     logo.logo_target_probs(**d)
