@@ -79,8 +79,10 @@ struct CaShape {
     static constexpr int kRows = 8 * NT;
     // groups an SM and steps of a warp's ring: as many warps as registers allow (one tile of rows:
     // 32 sequences of 16K rows, one token 41.3 us with four groups, 42.5 with three; three tiles, 64
-    // x 5 drafts: 141 with three, 195 with four, which spill, 161 with two)
-    static constexpr int kGroups = kWide ? 3 : 4, kStages = NT == 2 || NT == 3 ? 3 : 2;
+    // x 5 drafts: 141 with three, 195 with four, which spill, 161 with two; four tiles of D = 128,
+    // 32 x 8 drafts over 8K rows: 138 with two, 152 with three, which spill)
+    static constexpr bool kLarge = NT == 4 && D == 128;
+    static constexpr int kGroups = !kWide ? 4 : kLarge ? 2 : 3, kStages = NT == 2 || NT == 3 || kLarge ? 3 : 2;
     static constexpr int kThreads = kGroups * kCaGroup;
     static constexpr int kRunCost = 2;                         // units that beginning a run costs about as much as
     static constexpr int kCodes = kCaKeys * D / 2, kScales = kCaKeys * D / 16;  // bytes a step, K or V
