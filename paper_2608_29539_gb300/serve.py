@@ -190,8 +190,8 @@ class ServeBatch4:
 
     What might not fit the caches is refused, counting rejected drafts too, as their
     number stays on the device (recount() reads it back).  Replays of a captured graph are
-    not seen here: once a call was captured nothing is refused, and a call that finds no
-    room for all its rows overwrites the latest ones."""
+    not seen here: once a call was captured nothing is refused, and where a sequence
+    has no room for all that it brings, its latest rows are overwritten."""
 
     def __init__(self, cfg: Serve4Config, device="cuda"):
         if cfg.B < 1 or cfg.n_new < 1 or cfg.rows < cfg.n_new:
@@ -242,8 +242,11 @@ class ServeBatch4:
         if n_valid is not None:
             L._need(n_valid, torch.int32, "n_valid", (self.cfg.B,))
             n_valid = n_valid.clamp(0, n)
-        # (a replay may come here with full caches)
-        seq_len = self.seq_len.clamp(max=self.cfg.rows - n) + (n if n_valid is None else n_valid)
+        # (a replay may come here with full caches: room is made for what a sequence brings, no more)
+        if n_valid is None:
+            seq_len = self.seq_len.clamp(max=self.cfg.rows - n) + n
+        else:
+            seq_len = torch.minimum(self.seq_len, self.cfg.rows - n_valid) + n_valid
         L.logo_cache4_append(self.cache, k, v, seq_len, n_valid)
         self.seq_len.copy_(seq_len)
         self._rows_used += n

@@ -103,3 +103,19 @@ def test_verification(serve, monkeypatch):
     batch.fill(*_new(1))
     with pytest.raises(ValueError, match="verified"):
         batch.verify(*args)
+
+
+@pytest.mark.parametrize("n_valid,want", [([0, 8], [9, 9]), ([1, 5], [10, 6]), ([4, 8], [10, 9]), (None, [10, 9])])
+def test_what_a_sequence_brings_joins_where_it_fits(serve, n_valid, want):
+    """Once a call was captured nothing is refused: a chunk is as wide as its longest part, and a
+    sequence whose own part fits, or that brings none, keeps all its rows."""
+    batch = _batch(serve)
+    batch.fill(*_new(9, 1.0), torch.tensor([9, 1], dtype=torch.int32))
+    batch._captured = True
+    held = batch.seq_len.tolist()
+    batch.fill(*_new(8, 2.0), None if n_valid is None else torch.tensor(n_valid, dtype=torch.int32))
+    assert batch.seq_len.tolist() == want
+    k = R.values(batch.cache.k, batch.cache.k_scale)[:, 0, :, 0] / R.values(*R.quantise(_new(1)[0]))[0, 0, 0, 0]
+    for b, n in enumerate(n_valid or [8, 8]):
+        kept = min(held[b], batch.cfg.rows - n)
+        assert k[b, :want[b]].tolist() == [1] * kept + [2] * n
