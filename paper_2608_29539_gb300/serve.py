@@ -197,6 +197,8 @@ class ServeBatch4:
         if cfg.B < 1 or cfg.n_new < 1 or cfg.rows < cfg.n_new:
             raise ValueError("need B >= 1, n_new >= 1 and rows >= n_new")
         self.cfg = c = cfg
+        lib = L.lib()
+        attn_bytes = int(lib.logo_decode_cache4_workspace_size(L.Dims(c.B, c.rows, c.Hq, c.Hkv, c.D), c.n_new))
         dev = torch.device(device)
         z = lambda shape, dt: torch.zeros(shape, dtype=dt, device=dev)  # noqa: E731
         self.cache = L.logo_cache4_empty(c.B, c.rows, c.Hkv, c.D, dev)
@@ -209,9 +211,7 @@ class ServeBatch4:
         self.n_sel = z((1,), torch.int32)
         self.o_c = z((cap, c.Hq, c.D), torch.bfloat16)
         self.lse_c = z((c.Hq, cap), torch.float32)
-        lib = L.lib()
-        nbytes = max(int(lib.logo_decode_cache4_workspace_size(L.Dims(c.B, c.rows, c.Hq, c.Hkv, c.D), c.n_new)),
-                     int(lib.logo_select_workspace_size(L.Dims(c.B, c.n_new, 1, 1, 64))))
+        nbytes = max(attn_bytes, int(lib.logo_select_workspace_size(L.Dims(c.B, c.n_new, 1, 1, 64))))
         self.ws = torch.empty((max(nbytes, 256),), dtype=torch.uint8, device=dev)  # the calls are stream-ordered
         self._rows_used = 0       # at most this many rows of any cache hold a token
         self._latest_step = False  # the caches' last rows are the latest step's, and all there
@@ -262,11 +262,15 @@ class ServeBatch4:
         float32.  Returns (o_c [B*n_new, Hq, D] packed, z, row_of): what logo_combine takes
         on (B, n_new); the next step writes to the same buffers."""
         c = self.cfg
-        # what is refused is refused before the caches change
-        L._need(q, torch.bfloat16, "q", (c.B, c.n_new, c.Hq, c.D))
-        L._need(gate_p, torch.float32, "gate_p", (c.B, c.n_new))
-        for name, t in (("k_new", k_new), ("v_new", v_new)):
-            L._need(t, torch.bfloat16, name, (c.B, c.n_new, c.Hkv, c.D))
+        # what one of the calls would refuse is refused before the caches change
+        dev = self.cache.k.get_device()
+        L._on(gate_p, dev, torch.float32, "gate_p", (c.B, c.n_new))
+        for name, t, heads in (("q", q, c.Hq), ("k_new", k_new, c.Hkv), ("v_new", v_new, c.Hkv)):
+            L._on(t, dev, torch.bfloat16, name, (c.B, c.n_new, heads, c.D))
+            if t.data_ptr() % 16:
+                raise ValueError(f"{name} does not begin at a multiple of 16 bytes")
+        if dev >= 0:
+            L._here(dev)
         self._room(c.n_new)
         self.seq_len.clamp_(max=c.rows - c.n_new)  # (a replay may come here with full caches)
         self.seq_len += c.n_new

@@ -119,3 +119,34 @@ def test_what_a_sequence_brings_joins_where_it_fits(serve, n_valid, want):
     for b, n in enumerate(n_valid or [8, 8]):
         kept = min(held[b], batch.cfg.rows - n)
         assert k[b, :want[b]].tolist() == [1] * kept + [2] * n
+
+
+def _off_by_one(t):
+    """The same values at an address that is not a multiple of 16 bytes."""
+    out = torch.zeros(t.numel() + 1, dtype=t.dtype)[1:].view(t.shape)
+    return out.copy_(t)
+
+
+@pytest.mark.parametrize("which", ["q", "k_new", "v_new"])
+def test_what_a_call_of_the_step_refuses_changes_nothing(serve, monkeypatch, which):
+    """Contiguous tensors that begin between 16-byte borders, which the entry points refuse."""
+    def refusing(real):
+        def call(*a, **kw):
+            if any(torch.is_tensor(t) and t.dtype is torch.bfloat16 and t.data_ptr() % 16 for t in a):
+                raise serve.L.LogoError("a call", serve.L.LOGO_ERR_UNSUPPORTED)
+            return real(*a, **kw)
+        return call
+
+    for name in ("logo_cache4_append", "logo_decode_cache4_attn"):
+        monkeypatch.setattr(serve.L, name, refusing(getattr(serve.L, name)))
+    batch = _batch(serve)
+    _step(batch)
+    before = [t.clone() for t in (*batch.cache, batch.seq_len)]
+    x = dict(q=torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16), k_new=_new(3, 8.0)[0], v_new=_new(3)[1], gate_p=torch.ones(2, 3))
+    x[which] = _off_by_one(x[which])
+    with pytest.raises((ValueError, serve.L.LogoError)):
+        batch.step(**x)
+    assert all(torch.equal(a, b) for a, b in zip(before, (*batch.cache, batch.seq_len)))
+    _step(batch)
+    _step(batch)
+    assert batch.seq_len.tolist() == [9, 9]
