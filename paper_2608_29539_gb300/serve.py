@@ -199,6 +199,14 @@ class ServeBatch4:
         self.cfg = c = cfg
         lib = L.lib()
         attn_bytes = int(lib.logo_decode_cache4_workspace_size(L.Dims(c.B, c.rows, c.Hq, c.Hkv, c.D), c.n_new))
+        # what the calls of a step would refuse each time (a size of 0: these sizes)
+        if not attn_bytes:
+            raise ValueError(f"logo_decode_cache4_attn does not take these sizes: {c}")
+        if c.mode not in (L.LOGO_SELECT_THRESHOLD, L.LOGO_SELECT_RATIO) or \
+                (c.mode == L.LOGO_SELECT_RATIO and not 0.0 <= c.ratio <= 1.0):
+            raise ValueError("mode has to be a LOGO_SELECT_* and a ratio in [0, 1]")
+        if not 0.0 <= c.scale <= 3.4e38:
+            raise ValueError("scale has to be 0 or more, and finite in float32")
         dev = torch.device(device)
         z = lambda shape, dt: torch.zeros(shape, dtype=dt, device=dev)  # noqa: E731
         self.cache = L.logo_cache4_empty(c.B, c.rows, c.Hkv, c.D, dev)

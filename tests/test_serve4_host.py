@@ -150,3 +150,11 @@ def test_what_a_call_of_the_step_refuses_changes_nothing(serve, monkeypatch, whi
     _step(batch)
     _step(batch)
     assert batch.seq_len.tolist() == [9, 9]
+
+
+def test_configurations_that_no_step_takes(serve):
+    """What the calls of a step would refuse each time is refused at once."""
+    for kw in (dict(Hq=5), dict(D=96), dict(n_new=5000, rows=5000), dict(mode=7), dict(mode=1, ratio=1.5),
+               dict(scale=-1.0), dict(scale=float("nan")), dict(scale=1e39)):
+        with pytest.raises(ValueError):
+            serve.ServeBatch4(serve.Serve4Config(**(dict(B=2, n_new=3, Hq=4, Hkv=2, D=64, rows=10) | kw)), device="cpu")
