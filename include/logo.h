@@ -365,7 +365,8 @@ LOGO_API int logo_cache4_read(logo_cache4 cache, const int32_t* seq_len, const i
  *   Products in fp16 (the cache's values are exact in it; queries are scaled by a
  *   power of two a row, so they are too but for channels 2^-30 of the row's largest
  *   or less) with fp32 accumulation, softmax in fp32, weights rounded to fp16 for the
- *   product.  Results do not depend on the order in which the GPU runs the blocks.
+ *   product (by 2^-11 of themselves or 2^-35 of the row's largest).  Results do not
+ *   depend on the order in which the GPU runs the blocks.
  *   dims: B, T = L, Hq, Hkv, D in {64, 128}; scale as elsewhere.
  *   Workspace: logo_decode_cache4_workspace_size(dims, n_new) bytes, one per call in
  *   flight.

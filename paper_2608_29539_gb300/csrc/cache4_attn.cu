@@ -16,8 +16,9 @@
 //     4 keys (one 8-byte load a key).  V's pairs along the keys are made by exchanging
 //     nibbles of two keys' words, before the conversion.
 //   - code * scale is exact in fp16.  Queries go through fp16 scaled by a power of two
-//     a row.  P is rounded to fp16; it comes out of S^T's fragments by a transposition
-//     in registers.
+//     a row.  P is rounded to fp16, which keeps three bits more of it than bf16 would, relative
+//     to well below the row's maximum (ca_base); it comes out of S^T's fragments by a
+//     transposition in registers.
 // The batch's (sequence, KV head, rows, 128 keys) units form a line, sequences without a
 // selected row left out.  Each group of four warps takes an equal stretch of it, a cell,
 // its warps 32 keys of a unit each through a ring of their own in shared memory (cp.async;
@@ -45,7 +46,11 @@ constexpr int kCaWarps = 4;                   // of a group
 constexpr int kCaGroup = 32 * kCaWarps;
 constexpr int kCaKeys = 32;                   // keys of a warp's step
 constexpr int kCaUnit = kCaKeys * kCaWarps;   // keys of a unit
-constexpr float kCaSlack = 8.f;               // a maximum may grow by 2^8 before what is summed is rescaled
+// What is subtracted from logits lies 2^10 below a maximum, which may grow by 2^5 before what is
+// summed is rescaled: weights reach 2^15, near fp16's end, so that as little as can be falls
+// below its beginning.  (16 x 4 drafts, H 16/1: 29.5 us; 29.0 with 2^9 and 2^6, 29.8 with 2^11 and
+// 2^4, 31.6 with 2^13 and 2^2; 64 x 5 drafts 140, 140, 140, 146.)
+constexpr float kCaHead = 10.f, kCaSlack = 5.f;
 constexpr int kCaMaxTiles = 4;                // tiles of 8 rows that a warp holds
 constexpr int kJoinThreads = 256;
 
@@ -541,7 +546,25 @@ __device__ __forceinline__ void ca_drop_bad(uint8_t* scales, int step)
         if (scales[j * step] >= 0xf8) scales[j * step] = 0;
 }
 
-__device__ __forceinline__ float ca_lse(float top, float total) { return (top + log2f(total)) * 0.693147181f; }
+// What is subtracted from a row's logits q.k mul (powers of two) whose largest has q.k = top:
+// kCaHead less than it, so that half of fp16's smallest number is 2^-35 of the row's largest weight
+// and not 2^-25: one key often takes nearly all weight, and many others, or the V of others, the
+// rest.  Rounded up, so no weight is above 2^kCaHead.
+__device__ __forceinline__ float ca_base(float top, float mul) { return __fadd_ru(__fmul_ru(top, mul), -kCaHead); }
+
+// The q.k above which that moves: no weight is above 2^(kCaHead + kCaSlack), whatever the
+// quotient's error (a few units of the last place).
+__device__ __forceinline__ float ca_limit(float base, float mul)
+{
+    const float x = __fdividef(__fadd_rd(base, kCaHead + kCaSlack), mul);
+    return __fmaf_rd(fabsf(x), -0x1p-20f, x);
+}
+
+// (the sum is taken back to the maximum, near which its logarithm is exact to more places)
+__device__ __forceinline__ float ca_lse(float base, float total)
+{
+    return (base + kCaHead + log2f(total * (1.f / (1 << static_cast<int>(kCaHead))))) * 0.693147181f;
+}
 
 template <int D>
 __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel(CaParams p)
@@ -581,7 +604,7 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
         if (first < last) {
             ca_queries<D, S>(p, run, 0, nrow, group, tid, merge, q_frag, row_vis, row_mul);
             float mul[2], l[2], o[NS][4];
-            float m[2], lim[2];  // the maximum that is subtracted (0 before there is one) and q.k above which it moves
+            float m[2], lim[2];  // what is subtracted (0 before there is a maximum) and q.k above which it moves
             int vis[2], vis_min = run.len;
             uint32_t poison = 0;  // bit j: row 2t + j sees a value that is not finite in this thread's group
             uint2 q1[NS];
@@ -630,7 +653,7 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
                         for (int d = 4; d < 32; d <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], d));
                         const bool none = lim[j] == -INFINITY;  // nothing seen so far: all sums are 0 (or NaN)
                         if (top[j] == -INFINITY) continue;
-                        const float now = none ? top[j] * mul[j] : fmaxf(m[j], top[j] * mul[j]);
+                        const float base = ca_base(top[j], mul[j]), now = none ? base : fmaxf(m[j], base);
                         const float keep = none ? 1.f : ex2_approx(m[j] - now);
                         l[j] *= keep;
 #pragma unroll
@@ -639,7 +662,7 @@ __global__ void __launch_bounds__(CaShape<D, 1>::kThreads, 1) cache4_attn_kernel
                             o[i][j + 2] *= keep;
                         }
                         m[j] = now;
-                        lim[j] = __fdividef(now + kCaSlack, mul[j]);
+                        lim[j] = ca_limit(now, mul[j]);
                     }
                 }
                 uint32_t pb[2][2];
@@ -796,7 +819,7 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
     float* const wtop = reinterpret_cast<float*>(smem + S::kRing + S::kQ + S::kMerge);  // [warp][row]: maxima, then sums
     int* const row_vis = reinterpret_cast<int*>(wtop + kCaWarps * S::kRows);
     float* const row_mul = reinterpret_cast<float*>(row_vis + S::kRows);
-    float* const row_m = row_mul + S::kRows;    // the maximum that is subtracted (0 before there is one)
+    float* const row_m = row_mul + S::kRows;    // what is subtracted (0 before there is a maximum)
     float* const row_lim = row_m + S::kRows;    // q.k above which it moves
     const int my_key = (g >> 1) + 4 * (g & 1);
     const uint32_t k_at = piece<D>(my_key, t * (D / 8)), k_sc = 2 * S::kCodes + my_key * (D / 16) + t * (D / 64);
@@ -919,7 +942,8 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                             for (int w = 1; w < kCaWarps; ++w) top = fmaxf(top, wtop[w * S::kRows + r]);
                             const float was = row_m[r];
                             const bool none = row_lim[r] == -INFINITY;  // nothing seen so far: all sums are 0 (or NaN)
-                            now[nt][j] = top == -INFINITY ? was : none ? top * row_mul[r] : fmaxf(was, top * row_mul[r]);
+                            const float base = ca_base(top, row_mul[r]);
+                            now[nt][j] = top == -INFINITY ? was : none ? base : fmaxf(was, base);
                             const float keep = none ? 1.f : ex2_approx(was - now[nt][j]);
                             l[nt][j] *= keep;
 #pragma unroll
@@ -938,7 +962,7 @@ __global__ void __launch_bounds__(CaShape<D, NT>::kThreads, 1) cache4_wide_kerne
                                 const int r = nt * 8 + 2 * t + j;
                                 if (now[nt][j] == -INFINITY) continue;
                                 row_m[r] = now[nt][j];
-                                row_lim[r] = __fdividef(now[nt][j] + kCaSlack, row_mul[r]);
+                                row_lim[r] = ca_limit(now[nt][j], row_mul[r]);
                             }
                     }
                     group_sync(group);

@@ -299,3 +299,56 @@ def test_refusals():
         logo.logo_decode_cache4_attn(**(good | dict(q=bf(2, 1, 5, 64))))
     with pytest.raises(logo.LogoError, match="WORKSPACE"):
         logo.logo_decode_cache4_attn(**good, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("D,G,n", [(128, 4, 1), (64, 2, 3), (128, 4, 5), (64, 8, 4)])
+@pytest.mark.parametrize("far", [15.0, 17.0, 18.0, 20.0])
+def test_the_tail_beside_one_key_that_takes_nearly_all_weight(D, G, n, far):
+    """One key with V = 0, `far` above all others, whose V is what comes out.  As many
+    sequences as there are groups of warps, so that each has a run of its own.  Weights go
+    through fp16 relative to 2^-10 of the largest: off by 2^-11 of themselves or by 2^-25 2^-10
+    of the largest weight, at most.  Each group adds its 16 units of 128 keys in
+    steps of 16 and joins a few sums: fewer than 100 additions, an ulp each."""
+    L, B, Hkv = 2048, 640, 1
+    g = torch.Generator().manual_seed(int(far))
+    kc, ks = R.quantise(torch.cat([torch.full((1, 1, 1, D), 6.0), torch.zeros(1, 1, L - 1, D)], 2).to(torch.bfloat16))
+    v = torch.rand((1, 1, L, D), generator=g) + 0.5
+    v[:, :, 0] = 0
+    vc, vs = R.quantise(v.to(torch.bfloat16))
+    q = torch.ones((1, n, G * Hkv, D), dtype=torch.bfloat16)
+    scale = far / (6 * D)
+    ref = R.attn(q, R.values(kc, ks), R.values(vc, vs), [L], [(0, i) for i in range(n)], scale)
+    pos, cu, ns, _ = _pack(torch.ones((B, n), dtype=torch.bool))
+    many = lambda t: t.expand(B, *t.shape[1:])  # noqa: E731
+    o, lse = _call(*(many(t) for t in (q, kc, vc, ks, vs)), [L] * B, pos, cu, ns, scale)
+    x = (D + 8) * 2.0 ** -24 * ref["big"] + 2.0 ** -20
+    rel = 2.0 ** -11 + 2 * x + 100 * 2.0 ** -23
+    want = np.tile(ref["o"], (B, 1, 1))
+    bound = 2.0 ** -8 * want + np.tile(ref["absv"] * rel + ref["sumv"] * 2.0 ** -35, (B, 1, 1))
+    err = np.abs(o - want)
+    assert (err <= 1.01 * bound).all(), float((err / want).max())
+    assert (np.abs(lse - np.tile(ref["lse"], (1, B))) <= x + 100 * 2.0 ** -23 + 2.0 ** -23 * far).all()
+
+
+@pytest.mark.parametrize("D,G,n", [(128, 4, 1), (64, 8, 4)])
+@pytest.mark.parametrize("size", [1e3, 1e6, 3e7])
+def test_large_logits(D, G, n, size):
+    """Logits up to `size`, in no order: whatever their rounding, weights stay finite and what
+    comes out is a mean of V, all of which is between 0.5 and 1.5."""
+    L, B = 1024, 640
+    g = torch.Generator().manual_seed(D)
+    kc, ks = R.quantise(torch.randn((1, 1, L, D), generator=g).to(torch.bfloat16))
+    vc, vs = R.quantise((torch.rand((1, 1, L, D), generator=g) + 0.5).to(torch.bfloat16))
+    low, high = float(R.values(vc, vs).min()), float(R.values(vc, vs).max())
+    q = torch.randn((1, n, G, D), generator=g).to(torch.bfloat16)
+    pos, cu, ns, _ = _pack(torch.ones((B, n), dtype=torch.bool))
+    many = lambda t: t.expand(B, *t.shape[1:])  # noqa: E731
+    raw = torch.einsum("nhd,ld->nhl", q[0].double(), R.values(kc, ks)[0, 0])
+    scale = size / float(raw.abs().max())
+    o, lse = _call(*(many(t) for t in (q, kc, vc, ks, vs)), [L] * B, pos, cu, ns, scale)
+    slack = 1 + 2.0 ** -8 + 2.0 ** -11 + 2.0 ** -16  # o's rounding, a weight's, the sums'
+    assert (o >= low / slack).all() and (o <= high * slack).all()
+    for i in range(n):
+        want = torch.logsumexp(scale * raw[i, :, :L - n + i + 1], 1).numpy()
+        x = (D + 8) * 2.0 ** -24 * scale * float(torch.einsum("hd,ld->hl", q[0, i].double().abs(), R.values(kc, ks)[0, 0].abs()).max())
+        assert (np.abs(lse[:, i::n] - want[:, None]) <= x + 2.0 ** -16 + 2.0 ** -23 * np.abs(want[:, None])).all()
