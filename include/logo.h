@@ -398,14 +398,15 @@ LOGO_API int logo_decode_cache4_attn(const logo_bf16* q, logo_cache4 cache, cons
  *     for a token that a grammar rules out; bits past V are not read as tokens.
  *   temperature [B] float32 (NULL: 1): T > 0: p = softmax over the allowed tokens of
  *     x / T, as 2^((x - max x) log2(e) / T) over their sum; T = 0: 1 for the largest x,
- *     the lowest v among equals, 0 for the others; a T below 0 or NaN makes them NaN.
+ *     the lowest v among equals, 0 for the others.
  *   Each operation named up to x is one float32 operation, exponentials and sum are
  *   float32.
  *   Token numbers outside [0, V) in a list count for nothing (padding).
  * Out: p [B, m1, V] float32; may be logits themselves if those are float32.  0 for
- *   every token that is not allowed; a row that allows none, or only tokens of x =
- *   -infinity, is all 0.  A NaN among a row's allowed tokens (or for T > 0 an infinite
- *   x) makes p NaN for all of them.
+ *   every token that is not allowed, or whose x is -infinity; so a row that allows none,
+ *   or only tokens of x = -infinity, is all 0.  A NaN among the x of a row's allowed
+ *   tokens, or for T > 0 one of +infinity, makes p NaN for all of them, those of x =
+ *   -infinity too, as does a T below 0 or NaN, whatever the x.
  *   Results are deterministic.  Workspace:
  *   logo_target_probs_workspace_size(...) bytes, one per call in flight: a row's 8 bytes per
  *   1024 tokens, and for lists V / 4 and 12 for each token that they can name.

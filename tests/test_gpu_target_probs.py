@@ -254,3 +254,73 @@ def test_refusals():
     want = logo.logo_target_probs(x)
     assert torch.equal(want, logo.logo_target_probs(x, penalty=pen + 1, history=i32(2, 0), hist_len=i32(2),
                                                     bias_tok=i32(2, 0), bias_val=f(2, 0)))
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("V", [3000, 20011])
+def test_lists_with_values_that_are_not_finite(V, half):
+    """NaN and infinities at tokens that a history or a bias names, allowed and masked, for one
+    CTA a row and for two passes; and ones that the penalties and biases make."""
+    B, H, K = 14, 40, 6
+    nan, inf = float("nan"), float("inf")
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn((B, 1, V), generator=g) * 2
+    hist = torch.randint(0, V, (B, H), generator=g).int()
+    hist[:, :8] = torch.arange(8) * (V // 8)
+    tok = torch.full((B, K), -1, dtype=torch.int32)
+    tok[:, 0] = 11
+    val = torch.randn((B, K), generator=g)
+    penalty = torch.tensor([1.3, 0.25, 0.5]).repeat(B, 1)
+    ok = torch.rand((B, 1, V), generator=g) < 0.5
+    ok.scatter_(2, hist.long()[:, None], True)
+    ok[:, :, 11:13] = True
+    T = torch.ones(B)
+    h3 = V // 8 * 3                            # a listed token
+    x[0, 0, h3] = nan                          # allowed: shows
+    x[1, 0, h3], ok[1, 0, h3] = nan, False     # masked: does not
+    x[2, 0, h3], ok[2, 0, h3] = inf, False
+    x[3, 0, h3] = inf
+    x[4] = -inf                                # nothing left, listed tokens among it
+    x[5] = -inf
+    x[5, 0, hist[5].long()] = 0.5              # listed ones alone are left
+    T[6], x[6, 0, h3] = 0.0, inf               # greedy: the largest
+    T[7], x[7, 0, h3] = 0.0, nan
+    val[8, 0] = inf
+    val[9, 0] = -inf
+    tok[10, :2], val[10, 0], val[10, 1] = 12, inf, -inf
+    penalty[11, 1] = 3e38                      # taken twice it is infinite
+    hist[11, 8:10] = hist[11, 0]
+    T[12], x[12] = 0.0, -inf
+    T[13], x[13, 0, h3], ok[13, 0, h3] = 0.0, nan, False
+    s = dict(logits=x.to(torch.bfloat16) if half else x, temperature=T, penalty=penalty, history=hist,
+             hist_len=torch.full((B,), H, dtype=torch.int32), n_prompt=torch.zeros(B, dtype=torch.int32), bias_tok=tok,
+             bias_val=val, allowed=_words(ok))
+    p = _run(s).double().cpu().numpy()
+    for b in range(B):
+        with np.errstate(invalid="ignore", over="ignore"):
+            row = _row(s, ok, b, 0, np.float32)
+            want = R.probs(row, float(T[b]), ok[b, 0].numpy())
+        assert np.array_equal(np.isnan(p[b, 0]), np.isnan(want)), b
+        assert np.isnan(want).any() == (b in (0, 3, 7, 8, 10)) and (want == 0).all() == (b in (4, 12)), b
+        if T[b] == 0:
+            assert np.array_equal(p[b, 0], want, equal_nan=True), b
+            continue
+        # x is rounded as the definition has it; a probability's error is that of its own x and of the
+        # largest, so of tokens that have one (an x of -3e38 has none: its bound is the 2^-126)
+        rel = 2.0 ** -24 * (3 * 2 * np.abs(row[want > 0]).max(initial=0.0) + V / 256 + 96)
+        there = ~np.isnan(want)
+        assert (np.abs(p[b, 0] - want)[there] <= rel * want[there] + 2.0 ** -126).all(), b
+
+
+@pytest.mark.parametrize("lists", [False, True])
+@pytest.mark.parametrize("V", [3000, 20011])
+def test_temperatures_that_are_none(V, lists):
+    """Below 0 or NaN: NaN for all allowed tokens, whatever the logits, 0 for the others."""
+    s, ok = _random(4, 2, V, 30 if lists else 0, 5 if lists else 0, 3, T=[-1.0, float("nan"), -float("inf"), 0.7])
+    s["logits"][0, 1] = -float("inf")
+    ok[1, 0] = False
+    s["allowed"] = _words(ok)
+    p = _run(s).cpu()
+    assert torch.equal(torch.isnan(p[:3]), ok[:3]) and (p[:3][~ok[:3]] == 0).all()
+    only = {k: v[3:] for k, v in s.items()}
+    _check(only, ok[3:], p[3:])
