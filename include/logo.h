@@ -361,7 +361,8 @@ LOGO_API int logo_cache4_read(logo_cache4 cache, const int32_t* seq_len, const i
  *   does not enter its results, NaN included; what it does see shows in them: a query
  *   with a NaN or an infinity has NaN in o and lse.
  * Out: o_c [B*n_new, Hq, D] bf16 packed, lse_c [Hq, B*n_new] float32 packed (may be
- *   NULL); rows >= n_sel_total are left untouched.
+ *   NULL); rows >= n_sel_total are left untouched.  o_c is not q's memory, as rows are
+ *   packed while others' queries are read.
  *   Products in fp16 (the cache's values are exact in it; queries are scaled by a
  *   power of two a row, so they are too but for channels 2^-30 of the row's largest
  *   or less) with fp32 accumulation, softmax in fp32, weights rounded to fp16 for the
@@ -370,8 +371,8 @@ LOGO_API int logo_cache4_read(logo_cache4 cache, const int32_t* seq_len, const i
  *   dims: B, T = L, Hq, Hkv, D in {64, 128}; scale as elsewhere.
  *   Workspace: logo_decode_cache4_workspace_size(dims, n_new) bytes, one per call in
  *   flight.
- *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer or a size out of range;
- *   LOGO_ERR_UNSUPPORTED for D, Hq % Hkv, 16-byte alignment, B * n_new > 2^24,
+ *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer, a size out of range or o_c
+ *   over q; LOGO_ERR_UNSUPPORTED for D, Hq % Hkv, 16-byte alignment, B * n_new > 2^24,
  *   n_new * Hq / Hkv > 8192, Hkv > 2^16, B * n_new * Hq > 2^30, 2^31 pieces of 128 cache
  *   rows and 32 query rows or more ((ceil(L / 128) + 4) * B * Hkv * ceil(n_new * Hq /
  *   Hkv / 32)); LOGO_ERR_WORKSPACE. */

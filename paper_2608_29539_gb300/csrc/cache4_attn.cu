@@ -1286,6 +1286,9 @@ extern "C" int logo_decode_cache4_attn(const logo_bf16* q, logo_cache4 cache, co
         return LOGO_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < logo_decode_cache4_workspace_size(dims, n_new) || !aligned16(workspace))
         return LOGO_ERR_WORKSPACE;
+    // (packed rows are written while queries of other tokens are still to be read)
+    const size_t bytes = static_cast<size_t>(dims.B) * n_new * dims.Hq * dims.D * sizeof(logo_bf16);
+    if (overlap(q, bytes, o_c, bytes)) return LOGO_ERR_INVALID_ARG;
     CaParams p{};
     p.q = q, p.k = cache.k, p.v = cache.v, p.ks = cache.k_scale, p.vs = cache.v_scale;
     p.len = seq_len, p.pos = pos, p.cu_q = cu_q, p.n_sel = n_sel_total, p.o = o_c, p.lse = lse_c;

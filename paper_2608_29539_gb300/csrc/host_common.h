@@ -16,6 +16,13 @@ namespace logo {
 int check_dims(const logo_dims& d);
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Have two stretches of memory a byte in common?
+inline bool overlap(const void* a, size_t na, const void* b, size_t nb)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + nb && y < x + na;
+}
+
 // Number of SMs of the current device (cached per device).
 int device_sm_count();
 

@@ -1,0 +1,31 @@
+"""Outputs of the 4-bit cache's and the probabilities' calls that lie over what is still to
+be read, or over each other (CPU: refused before anything is launched)."""
+import ctypes
+
+import pytest
+
+from paper_2608_29539_gb300 import build
+
+at = lambda x: ctypes.c_void_p(x)  # noqa: E731  (aligned, never dereferenced: refused before use)
+far = at(1 << 30)
+
+
+@pytest.fixture(scope="module")
+def logo():
+    build.build()
+    from paper_2608_29539_gb300 import logo
+    logo.lib()
+    return logo
+
+
+def _cache(logo):
+    return logo._Cache4Ptrs(*(at((i + 8) << 26) for i in range(4)))
+
+
+@pytest.mark.parametrize("shift", [0, 16, 4 * 2 * 8 * 128 * 2 - 16, -16])
+def test_attention_does_not_write_over_its_queries(logo, shift):
+    d = logo.Dims(4, 256, 8, 2, 128)
+    ws = logo.lib().logo_decode_cache4_workspace_size(d, 2)
+    q = 1 << 20
+    assert logo.lib().logo_decode_cache4_attn(at(q), _cache(logo), far, far, far, far, at(q + shift), None, d, 2, 0.0,
+                                              at(1 << 29), ws, None) == logo.LOGO_ERR_INVALID_ARG
