@@ -346,7 +346,8 @@ LOGO_API int logo_cache4_append(logo_cache4 cache, const logo_bf16* k_new, const
  *   rows [B, m] int32: the row numbers wanted of each sequence, in any order, with
  *   repetitions (NULL: rows 0 .. m-1).  Out: k, v [B, m, Hkv, D] bf16, the layout of
  *   the bf16 entry points; zeros where the row number is outside [0, min(seq_len[b],
- *   L)).  dims, limits (m for n_new) and errors as logo_cache4_append. */
+ *   L)).  dims, limits (m for n_new) and errors as logo_cache4_append, and
+ *   LOGO_ERR_INVALID_ARG for k and v that overlap. */
 LOGO_API int logo_cache4_read(logo_cache4 cache, const int32_t* seq_len, const int32_t* rows, logo_bf16* k,
                 logo_bf16* v, logo_dims dims, int m, void* stream);
 

@@ -196,6 +196,8 @@ extern "C" int logo_cache4_read(logo_cache4 cache, const int32_t* seq_len, const
     if (rc != LOGO_OK) return rc;
     if (!k || !v || !seq_len) return LOGO_ERR_INVALID_ARG;
     if (!aligned16(k) || !aligned16(v)) return LOGO_ERR_UNSUPPORTED;
+    const size_t bytes = static_cast<size_t>(dims.B) * m * dims.Hkv * dims.D * sizeof(logo_bf16);
+    if (overlap(k, bytes, v, bytes)) return LOGO_ERR_INVALID_ARG;
     C4Params p{};
     p.k_out = k, p.v_out = v, p.k = cache.k, p.v = cache.v, p.ks = cache.k_scale, p.vs = cache.v_scale;
     p.len = seq_len, p.rows = rows, p.B = dims.B, p.n = m, p.H = dims.Hkv, p.L = dims.T;

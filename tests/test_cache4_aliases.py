@@ -29,3 +29,10 @@ def test_attention_does_not_write_over_its_queries(logo, shift):
     q = 1 << 20
     assert logo.lib().logo_decode_cache4_attn(at(q), _cache(logo), far, far, far, far, at(q + shift), None, d, 2, 0.0,
                                               at(1 << 29), ws, None) == logo.LOGO_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("shift", [0, 16, 4 * 3 * 2 * 64 * 2 - 16, -16])
+def test_rows_are_read_into_two_buffers(logo, shift):
+    k = 1 << 20
+    assert logo.lib().logo_cache4_read(_cache(logo), far, None, at(k), at(k + shift), logo.Dims(4, 256, 2, 2, 64), 3,
+                                       None) == logo.LOGO_ERR_INVALID_ARG
