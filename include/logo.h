@@ -404,17 +404,17 @@ LOGO_API int logo_decode_cache4_attn(const logo_bf16* q, logo_cache4 cache, cons
  *   Each operation named up to x is one float32 operation, exponentials and sum are
  *   float32.
  *   Token numbers outside [0, V) in a list count for nothing (padding).
- * Out: p [B, m1, V] float32; may be logits themselves if those are float32.  0 for
- *   every token that is not allowed, or whose x is -infinity; so a row that allows none,
- *   or only tokens of x = -infinity, is all 0.  A NaN among the x of a row's allowed
- *   tokens, or for T > 0 one of +infinity, makes p NaN for all of them, those of x =
- *   -infinity too, as does a T below 0 or NaN, whatever the x.
+ * Out: p [B, m1, V] float32; may be logits themselves if those are float32, and
+ *   else does not overlap them.  0 for every token that is not allowed, or whose x is
+ *   -infinity; so a row that allows none, or only tokens of x = -infinity, is all 0.  A
+ *   NaN among the x of a row's allowed tokens, or for T > 0 one of +infinity, makes p NaN
+ *   for all of them, those of x = -infinity too, as does a T below 0 or NaN, whatever the x.
  *   Results are deterministic.  Workspace:
  *   logo_target_probs_workspace_size(...) bytes, one per call in flight: a row's 8 bytes per
  *   1024 tokens, and for lists V / 4 and 12 for each token that they can name.
  *   Errors: LOGO_ERR_INVALID_ARG for a missing pointer, history without hist_len,
- *   n_prompt without history, history or draft without penalty, draft with m1 = 1, or
- *   sizes out of range; LOGO_ERR_UNSUPPORTED for V > LOGO_PROBS_MAX_VOCAB, m1 > 1024,
+ *   n_prompt without history, history or draft without penalty, draft with m1 = 1, p
+ *   over a part of the logits, or sizes out of range; LOGO_ERR_UNSUPPORTED for V > LOGO_PROBS_MAX_VOCAB, m1 > 1024,
  *   K > 4096, B * m1 > 2^24, B * H > 2^40, 16-byte alignment of logits or p, bf16 logits in p;
  *   LOGO_ERR_WORKSPACE. */
 #define LOGO_PROBS_MAX_COUNTED 16384

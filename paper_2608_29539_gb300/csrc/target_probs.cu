@@ -785,6 +785,9 @@ extern "C" int logo_target_probs(const void* logits, int logits_bf16, const floa
     if (!aligned16(logits) || !aligned16(p) || (logits_bf16 && logits == p)) return LOGO_ERR_UNSUPPORTED;
     const TpRoom room = tp_room(B, m1, V, H, K);
     if (!workspace || workspace_bytes < room.bytes || !aligned16(workspace)) return LOGO_ERR_WORKSPACE;
+    // (in place each stretch of a row is read before it is written; elsewhere over the logits it is another's)
+    const size_t tokens = static_cast<size_t>(B) * m1 * V;
+    if (logits != p && overlap(logits, tokens * (logits_bf16 ? 2 : 4), p, tokens * 4)) return LOGO_ERR_INVALID_ARG;
     uint8_t* const ws = static_cast<uint8_t*>(workspace);
     TpParams a{};
     a.logits = logits, a.temperature = temperature, a.penalty = penalty, a.history = history, a.hist_len = hist_len;

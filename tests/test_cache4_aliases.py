@@ -36,3 +36,13 @@ def test_rows_are_read_into_two_buffers(logo, shift):
     k = 1 << 20
     assert logo.lib().logo_cache4_read(_cache(logo), far, None, at(k), at(k + shift), logo.Dims(4, 256, 2, 2, 64), 3,
                                        None) == logo.LOGO_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("half", [0, 1])
+@pytest.mark.parametrize("where", ["ahead", "behind", "middle"])
+def test_probabilities_go_over_all_of_the_logits_or_none(logo, half, where):
+    B, m1, V = 2, 3, 1000
+    x, size = 1 << 20, B * m1 * V * 4
+    p = x + {"ahead": 16 - size, "behind": size // (1 + half) - 16, "middle": 4000}[where]
+    assert logo.lib().logo_target_probs(at(x), half, *[None] * 9, at(p), B, m1, V, 0, 0, at(1 << 29), 1 << 20,
+                                        None) == logo.LOGO_ERR_INVALID_ARG
