@@ -128,3 +128,73 @@ def test_replays_of_a_captured_step(n_new):
     for a, b in zip(plain.cache, captured.cache):
         for s, n in enumerate(plain.seq_len.tolist()):
             assert torch.equal(a[s, :, :n], b[s, :, :n])
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(128, 8, 2), (64, 4, 4)])
+def test_a_second_chunk_attends_the_context(D, Hq, Hkv):
+    """A prompt's second chunk, ragged, through the global branch's dense form on what
+    `context` gives: the rows of both chunks as the cache holds them.  The output's rounding to
+    bf16 is 2^-8, a weight's for the product too; logits and sums in fp32 stay below 2^-10."""
+    from paper_2608_29539_gb300 import logo as Lg
+    from paper_2608_29539_gb300.serve import Serve4Config, ServeBatch4
+    B, rows, G = 3, 400, Hq // Hkv
+    g = torch.Generator().manual_seed(D)
+    batch = ServeBatch4(Serve4Config(B, 1, Hq, Hkv, D, rows))
+    bf = lambda *s: torch.randn(s, generator=g).to(torch.bfloat16)  # noqa: E731
+    first, second = [200, 1, 77], [150, 130, 0]
+    held = [[[] for _ in range(B)] for _ in range(2)]
+    for valid in (first, second):
+        n = max(valid)
+        k, v = bf(B, n, Hkv, D), bf(B, n, Hkv, D)
+        batch.fill(k.cuda(), v.cuda(), torch.tensor(valid, dtype=torch.int32, device="cuda"))
+        for x, rows_of in zip((k, v), held):
+            y = C.values(*C.quantise(x))
+            for b in range(B):
+                rows_of[b] += list(y[b, :valid[b]])
+    m = max(a + b for a, b in zip(first, second))
+    k, v = batch.context(m)
+    q, gate = bf(B, m, Hq, D), torch.zeros(B, m)
+    for b in range(B):
+        gate[b, first[b]:first[b] + second[b]] = 1.0
+    _, pos, cu, row_of, n_sel = Lg.logo_select(gate.cuda(), Lg.LOGO_SELECT_THRESHOLD, 0.5)
+    o, lse = Lg.logo_global_sparse_attn_fwd(q.cuda(), k, v, pos, cu, n_sel)
+    torch.cuda.synchronize()
+    assert Lg.logo_get_device_status() == 0 and int(n_sel) == sum(second)
+    for r, (b, t) in enumerate((b, t) for b in range(B) for t in range(first[b], first[b] + second[b])):
+        kk, vv = (torch.stack(h[b][:t + 1]) for h in held)
+        for h in range(Hkv):
+            hs = slice(h * G, (h + 1) * G)
+            x = q[b, t, hs].double() @ kk[:, h].T / D ** 0.5
+            w = torch.softmax(x, 1)
+            want, absv = w @ vv[:, h], w @ vv[:, h].abs()
+            got = o[r, hs].double().cpu()
+            assert ((got - want).abs() <= 1.01 * (2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -10) * absv)).all()
+            assert ((lse[hs, r].double().cpu() - torch.logsumexp(x, 1)).abs() <= 2.0 ** -10).all()
+
+
+def test_filling_after_a_capture():
+    """Captured steps, then a chunk for one sequence: the others keep their rows, however
+    wide the chunk is, and the next replay goes on from there."""
+    from paper_2608_29539_gb300.serve import Serve4Config, ServeBatch4
+    B, n_new, Hq, Hkv, D, rows = 2, 1, 4, 2, 64, 100
+    g = torch.Generator().manual_seed(0)
+    bf = lambda *s: torch.randn(s, generator=g).to(torch.bfloat16).cuda()  # noqa: E731
+    batch = ServeBatch4(Serve4Config(B, n_new, Hq, Hkv, D, rows))
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    batch.fill(bf(B, 93, Hkv, D), bf(B, 93, Hkv, D), i32(93, 8))
+    x = (bf(B, n_new, Hq, D), bf(B, n_new, Hkv, D), bf(B, n_new, Hkv, D), torch.ones(B, n_new, device="cuda"))
+    batch.step(*x)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, _, _ = batch.step(*x)
+    graph.replay()
+    assert batch.seq_len.tolist() == [95, 10]
+    before = [t[0].clone() for t in batch.context()]
+    k, v = bf(B, 40, Hkv, D), bf(B, 40, Hkv, D)
+    batch.fill(k, v, i32(0, 40))
+    assert batch.seq_len.tolist() == [95, 50]
+    assert all(torch.equal(a, b[0]) for a, b in zip(before, batch.context()))
+    want = C.values(*C.quantise(k[1].cpu()))
+    assert torch.equal(batch.context()[0][1, 10:50].double().cpu(), want)
+    graph.replay()
+    assert batch.seq_len.tolist() == [96, 51] and bool(torch.isfinite(o).all())
