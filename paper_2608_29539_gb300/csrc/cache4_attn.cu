@@ -26,8 +26,8 @@
 // their own the hardware favoured the first ones, and the last finished a quarter later.
 // A run (sequence, KV head, rows) that spans several cells is joined from their parts, in
 // order, by a second launch.  H 32/8, D = 128: 32 sequences of up to 16K rows, half of them
-// selected, one token: 41 us for 183 MB (4.4 TB/s, 67% of the copy rate); one of 262139 rows:
-// 60 us for 302 MB; 64 x 5 drafts over up to 8K rows: 141 us for 377 MB.
+// selected, one token: 41.8 us for 183 MB (4.4 TB/s, 66% of the copy rate); one of 262139 rows:
+// 61.1 us for 302 MB; 64 x 5 drafts over up to 8K rows: 140 us for 377 MB.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -82,12 +82,16 @@ template <int D, int NT>
 struct CaShape {
     static constexpr bool kWide = NT > 1;
     static constexpr int kRows = 8 * NT;
-    // groups an SM and steps of a warp's ring: as many warps as registers allow (one tile of rows:
-    // 32 sequences of 16K rows, one token 41.3 us with four groups, 42.5 with three; three tiles, 64
-    // x 5 drafts: 141 with three, 195 with four, which spill, 161 with two; four tiles of D = 128,
-    // 32 x 8 drafts over 8K rows: 138 with two, 152 with three, which spill)
+    // groups an SM and steps of a warp's ring: as many warps as registers allow, but for one tile of
+    // rows of D = 128, where three groups find all the bytes' latency to work in and leave fewer
+    // parts to join (us, three and four groups: 32 sequences of up to 16K rows, one token 41.7 and
+    // 42.0, one of 262139 rows 61.0 and 61.9, 100 of 300 rows 17.2 and 18.4, 64 x 2 drafts of 8K rows
+    // 58.7 and 58.5; D = 64: 16 sequences of 32K rows 48.6 and 45.7, 128 of 4K rows 48.7 and 45.4, but
+    // one of 100000 33.6 and 40.9).  Three tiles, 64 x 5 drafts: 140 with three, 192 with four, which
+    // spill, 159 with two; four tiles of D = 128, 32 x 8 drafts over 8K rows: 138 with two, 151 with
+    // three, which spill; of D = 64: 88 with two, 74 with three, which spill 8 bytes.
     static constexpr bool kLarge = NT == 4 && D == 128;
-    static constexpr int kGroups = !kWide ? 4 : kLarge ? 2 : 3, kStages = NT == 2 || NT == 3 || kLarge ? 3 : 2;
+    static constexpr int kGroups = !kWide ? (D == 128 ? 3 : 4) : kLarge ? 2 : 3, kStages = NT == 2 || NT == 3 || kLarge ? 3 : 2;
     static constexpr int kThreads = kGroups * kCaGroup;
     static constexpr int kRunCost = 2;                         // units that beginning a run costs about as much as
     static constexpr int kCodes = kCaKeys * D / 2, kScales = kCaKeys * D / 16;  // bytes a step, K or V
@@ -1156,7 +1160,7 @@ __device__ __forceinline__ void join_rows(const CaParams& p, const CaOpen& e, in
 
 // Joins the parts of runs, a CTA a cell.  The cells that have a part of a run share its
 // rows: those that it comes into as well as the one that begins it (16 x 4 drafts, H 16/1, 64
-// rows a KV head: 31.8 -> 29.2 us; with up to 8 rows the one that begins it has them all: 32 x 1
+// rows a KV head: 31.8 -> 29.3 us; with up to 8 rows the one that begins it has them all: 32 x 1
 // 41.8 us, 43.8 when shared).
 template <int D, int NT>
 __global__ void __launch_bounds__(kJoinThreads) cache4_join_kernel(CaParams p)

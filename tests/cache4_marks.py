@@ -39,7 +39,7 @@ def caches(B, n, Hq, Hkv, D, L, lens, seed):
 def chain(lens, counts, G, Hkv, n, sms):
     """How many additions a sum passes through at most.  counts: selected tokens a sequence."""
     tiles = min(4, (n * G + 7) // 8)
-    groups = 4 if tiles == 1 else 2
+    groups = 3 if tiles == 1 else 2  # of warps an SM, at least
     units = [max(1, (m + 127) // 128) for m in lens]
     line = sum((u + 2) * ((c * G + 8 * tiles - 1) // (8 * tiles)) * Hkv for u, c in zip(units, counts) if c)
     stretch = line // (sms * groups) + 2
