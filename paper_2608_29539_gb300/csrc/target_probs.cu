@@ -653,8 +653,8 @@ __global__ void __launch_bounds__(kTpThreads, TpStage<HALF, false>::kResident) t
 
 // Both passes over a row of up to 16 chunks by one CTA, a warp a chunk, which stays in shared
 // memory.  It saves a launch and the second read: 400 rows of 8100, float32, histories of 500
-// 15.9 us (two kernels 21.9), one row of 2000 6.9 (9.6); at 16 chunks they are even (one row of
-// 16300 9.57 and 9.61), beyond that an SM is too slow for a row (32000: 13.1 and 9.6).
+// 15.8 us (two kernels 22.0), one row of 2000 7.3 (9.3); at 16 chunks they are even (one row of
+// 16300 9.6 and 9.6, 400 of them, bf16, histories of 1000 26.9 and 26.6), beyond that an SM is too slow for a row (32000: 13.1 and 9.6).
 template <bool HALF>
 __global__ void __launch_bounds__(kTpRowWarps * 32) target_row_kernel(TpParams a)
 {
